@@ -77,7 +77,7 @@ def draw(rng):
         return dict(kind=kind, B=_log(rng, 1, 32), P=_log(rng, 2, 1024), J=8 * _log(rng, 8, 256), C=8 * _log(rng, 8, 256), dtype=dtype)
     most = 4 * 1024 * 2048 * 65521 // (16 if dtype == "f32" else 1)
     H = length(64, 4096)
-    V = _log(rng, 10, 131072)
+    V = _log(rng, 10, min(131072, 2048 * 65521 // (H * (2 if dtype == "f32" else 1))))
     P = rng.choice([1, _log(rng, 2, 1024)])
     B = _log(rng, 1, max(1, min(128 if P == 1 else 16, most // (P * H * V), 6 * 10 ** 8 // (H * V))))
     return dict(kind=kind, B=B, P=min(P, max(1, most // (B * H * V))), H=H, V=V, dtype=dtype)
