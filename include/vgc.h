@@ -393,6 +393,75 @@ int vgc_unpack_apply(const uint32_t* const* words, const uint64_t* n_words,
                      const vgc_optimizer* opt, float* param, float* state1, float* state2,
                      uint64_t n, void* stream);
 
+/* ---- activations kept in 8 bits ----------------------------------------------------------------
+ * What the statistic multiplies besides D are a layer's inputs, which a training step has to keep from the forward to
+ * the backward pass.  Kept here in 8 bits and a byte for 32 of them: a row of C elements is cut into ceil(C / 32) blocks
+ * of 32 consecutive ones (the last may be short), and
+ *     value = code * 2^(exp - 127),   code = round(x / 2^(exp - 127)), ties to even, -127 .. 127
+ * with one exp a block: the smallest, in 1 .. 248, for which the block's largest magnitude is below 127.5 units, so that every
+ * value is within half a unit of x, 1/128 of that magnitude at most (2^-127 where that is more).  Magnitudes above 127 * 2^121
+ * count as that, so that every value is finite.  The value is a bfloat16 exactly.  A block of zeros gets exp = 120; one that holds an infinity or a NaN gets exp = 255 and decodes to NaN throughout.
+ *
+ * x, out: DEVICE, R rows of C elements, dtype VGC_F32 or VGC_BF16; codes: DEVICE int8 [R, C]; exps: DEVICE uint8
+ * [R, ceil(C / 32)].  Aligned to their elements.  C at most 2^31 - 1.  Errors: NULL, SIZE, DTYPE, ALIGN.
+ *
+ * vgc_sqgrad_act8 is vgc_sqgrad with X given in this form (codes [B, P, J], exps [B, P, ceil(J / 32)]) and D in dtype: the sums are
+ * those of the decoded values.  Both factors of the FC form are multiplied as floats, squares included, in either dtype.
+ * workspace (required): DEVICE, 16-byte aligned, vgc_sqgrad_act8_workspace_bytes() bytes.  J at most 4194240. */
+int vgc_act8_encode(int dtype, const void* x, uint64_t R, uint32_t C, int8_t* codes, uint8_t* exps, void* stream);
+int vgc_act8_decode(int dtype, const int8_t* codes, const uint8_t* exps, uint64_t R, uint32_t C, void* out, void* stream);
+size_t vgc_sqgrad_act8_workspace_bytes(int kind, int dtype, uint32_t B, uint32_t P, uint32_t J, uint32_t C);
+int vgc_sqgrad_act8(int kind, int dtype, const int8_t* codes, const uint8_t* exps, const void* D, uint32_t B, uint32_t P, uint32_t J,
+                    uint32_t C, float c, float* g_out, float* s_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- layer norm ----------------------------------------------------------------------------------
+ * Rows of C channels:  mean = sum x / C,  rstd = 1 / sqrt(sum (x - mean)^2 / C + eps),  xhat = (x - mean) rstd,
+ *                      y = gamma xhat + beta
+ * x, y: DEVICE [R, C], dtype VGC_F32 or VGC_BF16; gamma, beta: DEVICE float [C]; mean, rstd: DEVICE float [R].
+ * codes, exps: both NULL, or DEVICE places (as for vgc_act8_encode) that also receive xhat in 8 bits.  R at most 2^31 - 1.
+ *
+ * Backward, rows being P positions of B samples, from the output's gradient dy [B, P, C] (of each sample's own loss):
+ *     d = dy gamma,   dx = rstd (d - sum d / C - xhat sum (d xhat) / C)
+ *     G_z = sum_p dy[z, p] xhat[z, p],  H_z = sum_p dy[z, p]:  the gradients of gamma and beta by sample z;
+ *     g_gamma = c sum_z G_z,  s_gamma = c^2 sum_z G_z . G_z,  g_beta and s_beta likewise from H_z   (Alg. 1; c as for vgc_sqgrad)
+ * xhat is formed from x and mean (codes and exps NULL), or decoded from codes and exps (x and mean NULL).
+ * dx: DEVICE [B, P, C] in dtype, overlapping no input; s_gamma, s_beta: DEVICE float [C]; g_gamma, g_beta: the same, or NULL.
+ * workspace: DEVICE, 16-byte aligned, vgc_layer_norm_backward_workspace_bytes() bytes (the result does not depend on scheduling).
+ * Pointers are aligned to their elements.  All sums are float32.  Errors: NULL, SIZE, DTYPE, ALIGN, PARAM (eps negative or not
+ * finite, c not finite).  A row that holds an infinity or a NaN gives NaN in that row and in the sums, nowhere else. */
+int vgc_layer_norm(int dtype, const void* x, uint64_t R, uint32_t C, const float* gamma, const float* beta, float eps, void* y,
+                   float* mean, float* rstd, int8_t* codes, uint8_t* exps, void* stream);
+size_t vgc_layer_norm_backward_workspace_bytes(uint32_t B, uint32_t P, uint32_t C);
+int vgc_layer_norm_backward(int dtype, const void* dy, const void* x, const float* mean, const int8_t* codes, const uint8_t* exps,
+                            const float* rstd, const float* gamma, uint32_t B, uint32_t P, uint32_t C, float c, void* dx,
+                            float* g_gamma, float* s_gamma, float* g_beta, float* s_beta, void* workspace, size_t workspace_bytes,
+                            void* stream);
+
+/* ---- softmax cross entropy of a linear layer ------------------------------------------------------
+ * z = X W^T for X [N, H] and W [V, H] (a class a row) is formed in pieces of V and never kept:
+ *     lse[n] = log sum_v exp z[n, v],    loss[n] = lse[n] - z[n, target[n]]
+ * A negative target marks a row that is not asked for: its loss is 0.  One of V or more is a mistake: its loss is NaN.
+ *
+ * Backward, rows being P positions of B samples and sample z's own loss  sum_p weight[z, p] loss[z, p]:
+ *     D = weight (exp(z - lse) - [v = target]),  0 in rows that are not asked for, NaN in rows whose target is V or more
+ *     dX = D W,   G_z = sum_p D[z, p]^T X[z, p]  [V, H],   g = c sum_z G_z,  s = c^2 sum_z G_z . G_z   (as vgc_sqgrad with X and D
+ *     in each other's places; what rows that are not asked for hold in X does not matter)
+ * X, W: DEVICE, dtype VGC_F32 or VGC_BF16, 16-byte aligned; target: DEVICE int64 [N]; loss, lse: DEVICE float [N]; weight: DEVICE
+ * float [N], or NULL for 1; dX: DEVICE [N, H] in dtype, 16-byte aligned, or NULL; s_out: DEVICE float [V, H], 16-byte aligned, or
+ * NULL; g_out: the same, or NULL (NULL if s_out is).  lse is what the forward call wrote for the same X and W.
+ * workspace: DEVICE, 16-byte aligned, of the bytes that the function beside it gives; the backward pass's is bounded by X and by a
+ * piece of the classes: half a GiB, and 256 classes at least.
+ * Sums are float32.  VGC_BF16: D is rounded to bfloat16 for dX and kept in 16 significant bits for g and s.  VGC_F32: products of
+ * the operands' 8-bit pieces as in vgc_sqgrad's conv form.  Errors: NULL, SIZE (a zero dimension, N = B P (P rounded up to 32 if it
+ * is not 1) or H beyond 2^20, V beyond 2^24), DTYPE, ALIGN, PARAM. */
+size_t vgc_softmax_loss_workspace_bytes(int dtype, uint32_t N, uint32_t H, uint32_t V);
+int vgc_softmax_loss(int dtype, const void* X, const void* W, const int64_t* target, uint32_t N, uint32_t H, uint32_t V, float* loss,
+                     float* lse, void* workspace, size_t workspace_bytes, void* stream);
+size_t vgc_softmax_loss_backward_workspace_bytes(int dtype, uint32_t B, uint32_t P, uint32_t H, uint32_t V);
+int vgc_softmax_loss_backward(int dtype, const void* X, const void* W, const int64_t* target, const float* lse, const float* weight,
+                              uint32_t B, uint32_t P, uint32_t H, uint32_t V, float c, void* dX, float* g_out, float* s_out,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -720,4 +720,162 @@ int vgc_unpack_apply(const uint32_t* const* words, const uint64_t* n_words, cons
     return vgc_tiles_unpack_apply(words, n_words, hdrs, p, groups, n_groups, plan, scale, opt, param, state1, state2, n, stream, 0);
 }
 
+// ---- activations in 8 bits, layer norm, softmax loss ------------------------------------------------------------------------
+static size_t element_bytes(int dtype) { return dtype == VGC_F32 ? 4 : 2; }
+
+static int act8_check(const char* what, int dtype, const void* x, uint64_t R, uint32_t C, const void* codes, const void* exps) {
+    if (dtype != VGC_F32 && dtype != VGC_BF16) { set_error("%s: unknown dtype %d", what, dtype); return VGC_ERR_DTYPE; }
+    if (!x || !codes || !exps) { set_error("%s: the values, codes and exps are required", what); return VGC_ERR_NULL; }
+    if (R == 0 || C == 0) { set_error("%s: zero dimension", what); return VGC_ERR_SIZE; }
+    if (C > 0x7FFFFFFFu) { set_error("%s: rows of %u elements", what, C); return VGC_ERR_SIZE; }
+    if (!aligned(x, element_bytes(dtype))) { set_error("%s: the values must be aligned to their elements", what); return VGC_ERR_ALIGN; }
+    return VGC_OK;
+}
+
+int vgc_act8_encode(int dtype, const void* x, uint64_t R, uint32_t C, int8_t* codes, uint8_t* exps, void* stream) {
+    const int rc = act8_check("vgc_act8_encode", dtype, x, R, C, codes, exps);
+    return rc != VGC_OK ? rc : launch_act8_encode(dtype, x, R, C, codes, exps, static_cast<hipStream_t>(stream));
+}
+
+int vgc_act8_decode(int dtype, const int8_t* codes, const uint8_t* exps, uint64_t R, uint32_t C, void* out, void* stream) {
+    const int rc = act8_check("vgc_act8_decode", dtype, out, R, C, codes, exps);
+    return rc != VGC_OK ? rc : launch_act8_decode(dtype, codes, exps, R, C, out, static_cast<hipStream_t>(stream));
+}
+
+static int sqgrad_act8_shape(int kind, int dtype, uint32_t B, uint32_t P, uint32_t J, uint32_t C) {
+    if (kind != VGC_FC && kind != VGC_CONV) { set_error("vgc_sqgrad_act8: unknown kind %d", kind); return VGC_ERR_DTYPE; }
+    if (dtype != VGC_F32 && dtype != VGC_BF16) { set_error("vgc_sqgrad_act8: unknown dtype %d", dtype); return VGC_ERR_DTYPE; }
+    if (B == 0 || P == 0 || J == 0 || C == 0) { set_error("vgc_sqgrad_act8: zero dimension"); return VGC_ERR_SIZE; }
+    if (kind == VGC_FC && P != 1) { set_error("vgc_sqgrad_act8: the FC form has P = 1"); return VGC_ERR_SIZE; }
+    if (J > 65535u * 64u) { set_error("vgc_sqgrad_act8: J = %u exceeds the launch limit", J); return VGC_ERR_SIZE; }
+    if ((uint64_t)B * P * C > (1ull << 42)) { set_error("vgc_sqgrad_act8: D has too many elements"); return VGC_ERR_SIZE; }
+    return VGC_OK;
+}
+
+size_t vgc_sqgrad_act8_workspace_bytes(int kind, int dtype, uint32_t B, uint32_t P, uint32_t J, uint32_t C) {
+    return sqgrad_act8_shape(kind, dtype, B, P, J, C) == VGC_OK ? sqgrad_act8_workspace_bytes(kind, dtype, B, P, J, C) : 0;
+}
+
+static int workspace_check(const char* what, const void* workspace, size_t workspace_bytes, size_t need) {
+    if (!workspace && need) { set_error("%s: the workspace is required", what); return VGC_ERR_NULL; }
+    if (workspace_bytes < need) { set_error("%s: workspace of %zu bytes, %zu needed", what, workspace_bytes, need); return VGC_ERR_SIZE; }
+    if (!aligned(workspace, 16)) { set_error("%s: workspace must be 16-byte aligned", what); return VGC_ERR_ALIGN; }
+    return VGC_OK;
+}
+
+int vgc_sqgrad_act8(int kind, int dtype, const int8_t* codes, const uint8_t* exps, const void* D, uint32_t B, uint32_t P, uint32_t J,
+                    uint32_t C, float c, float* g_out, float* s_out, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!codes || !exps || !D || !s_out) { set_error("vgc_sqgrad_act8: codes, exps, D and s_out are required"); return VGC_ERR_NULL; }
+    int rc = sqgrad_act8_shape(kind, dtype, B, P, J, C);
+    if (rc != VGC_OK) return rc;
+    if (!aligned(D, 16) || !aligned(s_out, 16) || (g_out && !aligned(g_out, 16))) {
+        set_error("vgc_sqgrad_act8: D, s_out and g_out must be 16-byte aligned");
+        return VGC_ERR_ALIGN;
+    }
+    if (!std::isfinite(c)) { set_error("vgc_sqgrad_act8: c is not finite"); return VGC_ERR_PARAM; }
+    if ((rc = workspace_check("vgc_sqgrad_act8", workspace, workspace_bytes, sqgrad_act8_workspace_bytes(kind, dtype, B, P, J, C))) != VGC_OK) return rc;
+    return launch_sqgrad_act8(kind, dtype, codes, exps, D, B, P, J, C, c, g_out, s_out, workspace, static_cast<hipStream_t>(stream));
+}
+
+int vgc_layer_norm(int dtype, const void* x, uint64_t R, uint32_t C, const float* gamma, const float* beta, float eps, void* y,
+                   float* mean, float* rstd, int8_t* codes, uint8_t* exps, void* stream) {
+    if (dtype != VGC_F32 && dtype != VGC_BF16) { set_error("vgc_layer_norm: unknown dtype %d", dtype); return VGC_ERR_DTYPE; }
+    if (!x || !gamma || !beta || !y || !mean || !rstd) { set_error("vgc_layer_norm: x, gamma, beta, y, mean and rstd are required"); return VGC_ERR_NULL; }
+    if (!codes != !exps) { set_error("vgc_layer_norm: codes and exps go together"); return VGC_ERR_NULL; }
+    if (R == 0 || C == 0) { set_error("vgc_layer_norm: zero dimension"); return VGC_ERR_SIZE; }
+    if (R > 0x7FFFFFFFu || C > 0x7FFFFFFFu) { set_error("vgc_layer_norm: %llu rows of %u elements", (unsigned long long)R, C); return VGC_ERR_SIZE; }
+    const size_t e = element_bytes(dtype);
+    if (!aligned(x, e) || !aligned(y, e) || !aligned(gamma, 4) || !aligned(beta, 4) || !aligned(mean, 4) || !aligned(rstd, 4)) {
+        set_error("vgc_layer_norm: pointers must be aligned to their elements");
+        return VGC_ERR_ALIGN;
+    }
+    if (!std::isfinite(eps) || eps < 0.0f) { set_error("vgc_layer_norm: eps must be finite and not negative (got %g)", eps); return VGC_ERR_PARAM; }
+    return launch_layer_norm(dtype, x, R, C, gamma, beta, eps, y, mean, rstd, codes, exps, static_cast<hipStream_t>(stream));
+}
+
+static int layer_norm_backward_shape(uint32_t B, uint32_t P, uint32_t C) {
+    if (B == 0 || P == 0 || C == 0) { set_error("vgc_layer_norm_backward: zero dimension"); return VGC_ERR_SIZE; }
+    if ((uint64_t)B * P > 0x7FFFFFFFull || C > 0x7FFFFFFFu) { set_error("vgc_layer_norm_backward: %u x %u rows of %u elements", B, P, C); return VGC_ERR_SIZE; }
+    return VGC_OK;
+}
+
+size_t vgc_layer_norm_backward_workspace_bytes(uint32_t B, uint32_t P, uint32_t C) {
+    return layer_norm_backward_shape(B, P, C) == VGC_OK ? layer_norm_backward_workspace_bytes(B, P, C) : 0;
+}
+
+int vgc_layer_norm_backward(int dtype, const void* dy, const void* x, const float* mean, const int8_t* codes, const uint8_t* exps,
+                            const float* rstd, const float* gamma, uint32_t B, uint32_t P, uint32_t C, float c, void* dx,
+                            float* g_gamma, float* s_gamma, float* g_beta, float* s_beta, void* workspace, size_t workspace_bytes,
+                            void* stream) {
+    if (dtype != VGC_F32 && dtype != VGC_BF16) { set_error("vgc_layer_norm_backward: unknown dtype %d", dtype); return VGC_ERR_DTYPE; }
+    if (!dy || !rstd || !gamma || !dx || !s_gamma || !s_beta) {
+        set_error("vgc_layer_norm_backward: dy, rstd, gamma, dx, s_gamma and s_beta are required");
+        return VGC_ERR_NULL;
+    }
+    if (!x != !mean || !codes != !exps || !x == !codes) {
+        set_error("vgc_layer_norm_backward: the rows come as x and mean or as codes and exps");
+        return VGC_ERR_NULL;
+    }
+    int rc = layer_norm_backward_shape(B, P, C);
+    if (rc != VGC_OK) return rc;
+    const size_t e = element_bytes(dtype);
+    if (!aligned(dy, e) || !aligned(x, e) || !aligned(dx, e) || !aligned(mean, 4) || !aligned(rstd, 4) || !aligned(gamma, 4) ||
+        !aligned(g_gamma, 4) || !aligned(s_gamma, 4) || !aligned(g_beta, 4) || !aligned(s_beta, 4)) {
+        set_error("vgc_layer_norm_backward: pointers must be aligned to their elements");
+        return VGC_ERR_ALIGN;
+    }
+    if (!std::isfinite(c)) { set_error("vgc_layer_norm_backward: c is not finite"); return VGC_ERR_PARAM; }
+    if ((rc = workspace_check("vgc_layer_norm_backward", workspace, workspace_bytes, layer_norm_backward_workspace_bytes(B, P, C))) != VGC_OK) return rc;
+    return launch_layer_norm_backward(dtype, dy, x, mean, codes, exps, rstd, gamma, B, P, C, c, dx, g_gamma, s_gamma, g_beta, s_beta, workspace,
+                                      static_cast<hipStream_t>(stream));
+}
+
+static int softmax_loss_shape(const char* what, int dtype, uint32_t B, uint32_t P, uint32_t H, uint32_t V) {
+    if (dtype != VGC_F32 && dtype != VGC_BF16) { set_error("%s: unknown dtype %d", what, dtype); return VGC_ERR_DTYPE; }
+    if (B == 0 || P == 0 || H == 0 || V == 0) { set_error("%s: zero dimension", what); return VGC_ERR_SIZE; }
+    // (padded to whole steps and cut into six pieces, a tile's 256 rows of any operand stay below 2^32 bytes)
+    if ((uint64_t)B * ((P + 31ull) / 32u * 32u) > (1u << 20) && P > 1) { set_error("%s: %u x %u positions exceed 2^20", what, B, P); return VGC_ERR_SIZE; }
+    if ((uint64_t)B * P > (1u << 20) || H > (1u << 20)) { set_error("%s: %u x %u rows of %u elements exceed 2^20", what, B, P, H); return VGC_ERR_SIZE; }
+    if (V > (1u << 24)) { set_error("%s: %u classes exceed 2^24", what, V); return VGC_ERR_SIZE; }
+    return VGC_OK;
+}
+
+size_t vgc_softmax_loss_workspace_bytes(int dtype, uint32_t N, uint32_t H, uint32_t V) {
+    return softmax_loss_shape("vgc_softmax_loss", dtype, N, 1, H, V) == VGC_OK ? softmax_loss_workspace_bytes(dtype, N, H, V) : 0;
+}
+
+int vgc_softmax_loss(int dtype, const void* X, const void* W, const int64_t* target, uint32_t N, uint32_t H, uint32_t V, float* loss,
+                     float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!X || !W || !target || !loss || !lse) { set_error("vgc_softmax_loss: X, W, target, loss and lse are required"); return VGC_ERR_NULL; }
+    int rc = softmax_loss_shape("vgc_softmax_loss", dtype, N, 1, H, V);
+    if (rc != VGC_OK) return rc;
+    if (!aligned(X, 16) || !aligned(W, 16) || !aligned(target, 8) || !aligned(loss, 4) || !aligned(lse, 4)) {
+        set_error("vgc_softmax_loss: X and W must be 16-byte aligned, the others to their elements");
+        return VGC_ERR_ALIGN;
+    }
+    if ((rc = workspace_check("vgc_softmax_loss", workspace, workspace_bytes, softmax_loss_workspace_bytes(dtype, N, H, V))) != VGC_OK) return rc;
+    return launch_softmax_loss(dtype, X, W, target, N, H, V, loss, lse, workspace, static_cast<hipStream_t>(stream));
+}
+
+size_t vgc_softmax_loss_backward_workspace_bytes(int dtype, uint32_t B, uint32_t P, uint32_t H, uint32_t V) {
+    return softmax_loss_shape("vgc_softmax_loss_backward", dtype, B, P, H, V) == VGC_OK ? softmax_loss_backward_workspace_bytes(dtype, B, P, H, V) : 0;
+}
+
+int vgc_softmax_loss_backward(int dtype, const void* X, const void* W, const int64_t* target, const float* lse, const float* weight,
+                              uint32_t B, uint32_t P, uint32_t H, uint32_t V, float c, void* dX, float* g_out, float* s_out,
+                              void* workspace, size_t workspace_bytes, void* stream) {
+    if (!X || !W || !target || !lse) { set_error("vgc_softmax_loss_backward: X, W, target and lse are required"); return VGC_ERR_NULL; }
+    if ((!dX && !s_out) || (g_out && !s_out)) { set_error("vgc_softmax_loss_backward: dX or s_out is required, and s_out with g_out"); return VGC_ERR_NULL; }
+    int rc = softmax_loss_shape("vgc_softmax_loss_backward", dtype, B, P, H, V);
+    if (rc != VGC_OK) return rc;
+    if (!aligned(X, 16) || !aligned(W, 16) || !aligned(dX, 16) || !aligned(g_out, 16) || !aligned(s_out, 16) || !aligned(target, 8) ||
+        !aligned(lse, 4) || !aligned(weight, 4)) {
+        set_error("vgc_softmax_loss_backward: X, W, dX, g_out and s_out must be 16-byte aligned, the others to their elements");
+        return VGC_ERR_ALIGN;
+    }
+    if (!std::isfinite(c)) { set_error("vgc_softmax_loss_backward: c is not finite"); return VGC_ERR_PARAM; }
+    if ((rc = workspace_check("vgc_softmax_loss_backward", workspace, workspace_bytes, softmax_loss_backward_workspace_bytes(dtype, B, P, H, V))) != VGC_OK) return rc;
+    return launch_softmax_loss_backward(dtype, X, W, target, lse, weight, B, P, H, V, c, dX, g_out, s_out, workspace, static_cast<hipStream_t>(stream));
+}
+
 }  // extern "C"

@@ -308,5 +308,28 @@ int launch_conv2d(int dtype, const void* act, const void* D, uint32_t B, uint32_
 int launch_conv_tiled(int dtype, const void* X, const void* D, uint32_t B, uint32_t P, uint32_t J, uint32_t C,
                       float c, float* g_out, float* s_out, void* workspace, size_t workspace_bytes, hipStream_t stream);
 
+// Activations in 8 bits (vgc_act8.hip)
+int launch_act8_encode(int dtype, const void* x, uint64_t R, uint32_t C, int8_t* codes, uint8_t* exps, hipStream_t stream);
+int launch_act8_decode(int dtype, const int8_t* codes, const uint8_t* exps, uint64_t R, uint32_t C, void* out, hipStream_t stream);
+size_t sqgrad_act8_workspace_bytes(int kind, int dtype, uint32_t B, uint32_t P, uint32_t J, uint32_t C);
+int launch_sqgrad_act8(int kind, int dtype, const int8_t* codes, const uint8_t* exps, const void* D, uint32_t B, uint32_t P, uint32_t J,
+                       uint32_t C, float c, float* g_out, float* s_out, void* workspace, hipStream_t stream);
+
+// Layer norm (vgc_norm.hip)
+int launch_layer_norm(int dtype, const void* x, uint64_t R, uint32_t C, const float* gamma, const float* beta, float eps, void* y, float* mean,
+                      float* rstd, int8_t* codes, uint8_t* exps, hipStream_t stream);
+size_t layer_norm_backward_workspace_bytes(uint32_t B, uint32_t P, uint32_t C);
+int launch_layer_norm_backward(int dtype, const void* dy, const void* x, const float* mean, const int8_t* codes, const uint8_t* exps,
+                               const float* rstd, const float* gamma, uint32_t B, uint32_t P, uint32_t C, float c, void* dx, float* g_gamma,
+                               float* s_gamma, float* g_beta, float* s_beta, void* workspace, hipStream_t stream);
+
+// Softmax cross entropy of a linear layer (vgc_softmax_loss.hip)
+size_t softmax_loss_workspace_bytes(int dtype, uint32_t N, uint32_t H, uint32_t V);
+int launch_softmax_loss(int dtype, const void* X, const void* W, const int64_t* target, uint32_t N, uint32_t H, uint32_t V, float* loss, float* lse,
+                        void* workspace, hipStream_t stream);
+size_t softmax_loss_backward_workspace_bytes(int dtype, uint32_t B, uint32_t P, uint32_t H, uint32_t V);
+int launch_softmax_loss_backward(int dtype, const void* X, const void* W, const int64_t* target, const float* lse, const float* weight, uint32_t B,
+                                 uint32_t P, uint32_t H, uint32_t V, float c, void* dX, float* g_out, float* s_out, void* workspace, hipStream_t stream);
+
 }  // namespace vgc
 #endif

@@ -102,6 +102,21 @@ EXPORTS = {
     "vgc_unpack_apply": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint32, C.c_void_p, C.c_uint32,
                                    C.c_void_p, C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint64,
                                    C.c_void_p]),
+    "vgc_act8_encode": (C.c_int, [C.c_int, C.c_void_p, C.c_uint64, C.c_uint32, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "vgc_act8_decode": (C.c_int, [C.c_int, C.c_void_p, C.c_void_p, C.c_uint64, C.c_uint32, C.c_void_p, C.c_void_p]),
+    "vgc_sqgrad_act8_workspace_bytes": (C.c_size_t, [C.c_int, C.c_int] + [C.c_uint32] * 4),
+    "vgc_sqgrad_act8": (C.c_int, [C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p] + [C.c_uint32] * 4 +
+                        [C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "vgc_layer_norm": (C.c_int, [C.c_int, C.c_void_p, C.c_uint64, C.c_uint32, C.c_void_p, C.c_void_p, C.c_float] + [C.c_void_p] * 6),
+    "vgc_layer_norm_backward_workspace_bytes": (C.c_size_t, [C.c_uint32] * 3),
+    "vgc_layer_norm_backward": (C.c_int, [C.c_int] + [C.c_void_p] * 7 + [C.c_uint32] * 3 + [C.c_float] + [C.c_void_p] * 6 +
+                                [C.c_size_t, C.c_void_p]),
+    "vgc_softmax_loss_workspace_bytes": (C.c_size_t, [C.c_int] + [C.c_uint32] * 3),
+    "vgc_softmax_loss": (C.c_int, [C.c_int, C.c_void_p, C.c_void_p, C.c_void_p] + [C.c_uint32] * 3 + [C.c_void_p] * 3 +
+                         [C.c_size_t, C.c_void_p]),
+    "vgc_softmax_loss_backward_workspace_bytes": (C.c_size_t, [C.c_int] + [C.c_uint32] * 4),
+    "vgc_softmax_loss_backward": (C.c_int, [C.c_int] + [C.c_void_p] * 5 + [C.c_uint32] * 4 + [C.c_float] + [C.c_void_p] * 4 +
+                                  [C.c_size_t, C.c_void_p]),
 }
 
 _lib = None
@@ -547,3 +562,166 @@ def unpack_compact_add_batch(streams, stream_bytes, tile_bytes, run_offsets, hdr
     _check(load().vgc_unpack_compact_add_batch(arr(streams), nb, arr(tile_bytes), arr(run_offsets), arr(hdrs), p, plan.c_groups,
                                                plan.n_groups, _ptr(plan.plan), float(scale), 1 if overwrite else 0, _ptr(dense),
                                                plan.n, _stream()))
+
+
+def _rows(t, what):
+    """(rows, elements a row, dtype code) of a contiguous float32 or bfloat16 tensor [..., C]."""
+    dtype = _DTYPES.get(t.dtype)
+    if dtype is None:
+        raise VgcError(f"{what}: unsupported dtype {t.dtype}")
+    if t.dim() == 0 or not t.is_contiguous():
+        raise VgcError(f"{what}: need a contiguous tensor of rows, got {tuple(t.shape)} (contiguous: {t.is_contiguous()})")
+    Cc = t.shape[-1]
+    return (t.numel() // Cc if Cc else 0), Cc, dtype
+
+
+def _need_act8(a, codes, exps, R, Cc):
+    a.need(codes, R * Cc, torch.int8, "codes")
+    a.need(exps, R * ((Cc + 31) // 32), torch.uint8, "exps")
+
+
+def _workspace(a, workspace, nbytes):
+    if workspace is None and nbytes:
+        raise VgcError(f"workspace: need a uint8 tensor of at least {nbytes} bytes")
+    a.need(workspace, nbytes, torch.uint8, "workspace")
+    return _ptr(workspace), 0 if workspace is None else workspace.numel()
+
+
+def act8_encode(x, codes, exps):
+    """vgc_act8_encode: the rows of x [..., C] (float32 or bfloat16) into codes int8 [..., C] and exps uint8 [..., ceil(C / 32)]."""
+    R, Cc, dtype = _rows(x, "x")
+    a = _Args()
+    a.on_device(x, "x")
+    _need_act8(a, codes, exps, R, Cc)
+    a.launchable()
+    _check(load().vgc_act8_encode(dtype, _ptr(x), R, Cc, _ptr(codes), _ptr(exps), _stream()))
+
+
+def act8_decode(codes, exps, out):
+    """vgc_act8_decode: the kept values into out [..., C] (float32 or bfloat16)."""
+    R, Cc, dtype = _rows(out, "out")
+    a = _Args()
+    a.on_device(out, "out")
+    _need_act8(a, codes, exps, R, Cc)
+    a.launchable()
+    _check(load().vgc_act8_decode(dtype, _ptr(codes), _ptr(exps), R, Cc, _ptr(out), _stream()))
+
+
+def sqgrad_act8_workspace_bytes(kind, dtype, B, P, J, Cc):
+    return int(load().vgc_sqgrad_act8_workspace_bytes(kind, dtype, B, P, J, Cc))
+
+
+def sqgrad_act8(kind, codes, exps, D, c, s_out, g_out=None, workspace=None):
+    """vgc_sqgrad_act8: sqgrad with X kept in 8 bits (codes [B, J] or [B, P, J] and their exps) and D float32 or bfloat16.
+    workspace: uint8 tensor of sqgrad_act8_workspace_bytes() bytes."""
+    dtype = _DTYPES.get(D.dtype)
+    if dtype is None:
+        raise VgcError(f"unsupported dtype {D.dtype}")
+    if codes.dim() != (2 if kind == FC else 3) or D.dim() != codes.dim() or tuple(D.shape[:-1]) != tuple(codes.shape[:-1]) or not D.is_contiguous():
+        raise VgcError(f"codes {tuple(codes.shape)} and D {tuple(D.shape)} do not belong together (or are not contiguous)")
+    B, J, Cc = codes.shape[0], codes.shape[-1], D.shape[-1]
+    P = 1 if kind == FC else codes.shape[1]
+    a = _Args()
+    a.on_device(D, "D")
+    _need_act8(a, codes, exps, B * P, J)
+    a.need(s_out, J * Cc, torch.float32, "s_out")
+    a.need(g_out, J * Cc, torch.float32, "g_out")
+    ws, nbytes = _workspace(a, workspace, sqgrad_act8_workspace_bytes(kind, dtype, B, P, J, Cc))
+    a.launchable()
+    _check(load().vgc_sqgrad_act8(kind, dtype, _ptr(codes), _ptr(exps), _ptr(D), B, P, J, Cc, float(c), _ptr(g_out), _ptr(s_out), ws, nbytes,
+                                  _stream()))
+
+
+def layer_norm(x, gamma, beta, eps, y, mean, rstd, act8=None):
+    """vgc_layer_norm on the rows of x [..., C]; gamma, beta float32 [C]; y like x; mean, rstd float32, one a row.
+    act8: optional (codes, exps) that also receive the normalised rows in 8 bits."""
+    R, Cc, dtype = _rows(x, "x")
+    codes, exps = act8 or (None, None)
+    a = _Args()
+    a.on_device(x, "x")
+    a.need(gamma, Cc, torch.float32, "gamma")
+    a.need(beta, Cc, torch.float32, "beta")
+    a.need(y, R * Cc, x.dtype, "y")
+    a.need(mean, R, torch.float32, "mean")
+    a.need(rstd, R, torch.float32, "rstd")
+    _need_act8(a, codes, exps, R, Cc)
+    a.launchable()
+    _check(load().vgc_layer_norm(dtype, _ptr(x), R, Cc, _ptr(gamma), _ptr(beta), float(eps), _ptr(y), _ptr(mean), _ptr(rstd), _ptr(codes),
+                                 _ptr(exps), _stream()))
+
+
+def layer_norm_backward_workspace_bytes(B, P, Cc):
+    return int(load().vgc_layer_norm_backward_workspace_bytes(B, P, Cc))
+
+
+def layer_norm_backward(dy, x, mean, rstd, gamma, c, dx, s_gamma, s_beta, g_gamma=None, g_beta=None, workspace=None, act8=None):
+    """vgc_layer_norm_backward for dy [B, P, C]: dx, and the two sums over the samples for gamma and beta.  The normalised rows
+    come from x [B, P, C] and mean, or (x and mean None) from act8 = (codes, exps).
+    workspace: uint8 tensor of layer_norm_backward_workspace_bytes() bytes."""
+    if dy.dim() != 3:
+        raise VgcError(f"dy: need [B, P, C], got {tuple(dy.shape)}")
+    R, Cc, dtype = _rows(dy, "dy")
+    B, P = dy.shape[0], dy.shape[1]
+    codes, exps = act8 or (None, None)
+    a = _Args()
+    a.on_device(dy, "dy")
+    a.need(x, R * Cc, dy.dtype, "x")
+    a.need(mean, R, torch.float32, "mean")
+    _need_act8(a, codes, exps, R, Cc)
+    a.need(rstd, R, torch.float32, "rstd")
+    a.need(dx, R * Cc, dy.dtype, "dx")
+    for t, what in ((gamma, "gamma"), (s_gamma, "s_gamma"), (s_beta, "s_beta"), (g_gamma, "g_gamma"), (g_beta, "g_beta")):
+        a.need(t, Cc, torch.float32, what)
+    ws, nbytes = _workspace(a, workspace, layer_norm_backward_workspace_bytes(B, P, Cc))
+    a.launchable()
+    _check(load().vgc_layer_norm_backward(dtype, _ptr(dy), _ptr(x), _ptr(mean), _ptr(codes), _ptr(exps), _ptr(rstd), _ptr(gamma), B, P, Cc,
+                                          float(c), _ptr(dx), _ptr(g_gamma), _ptr(s_gamma), _ptr(g_beta), _ptr(s_beta), ws, nbytes,
+                                          _stream()))
+
+
+def _loss_args(X, W, target):
+    R, H, dtype = _rows(X, "X")
+    if W.dim() != 2 or W.dtype != X.dtype or W.shape[1] != H or not W.is_contiguous():
+        raise VgcError(f"W {tuple(W.shape)} {W.dtype} is not a contiguous [V, {H}] in the type of X, {X.dtype}")
+    a = _Args()
+    a.on_device(X, "X"); a.on_device(W, "W")
+    a.need(target, R, torch.int64, "target")
+    return a, R, H, W.shape[0], dtype
+
+
+def softmax_loss_workspace_bytes(dtype, N, H, V):
+    return int(load().vgc_softmax_loss_workspace_bytes(dtype, N, H, V))
+
+
+def softmax_loss(X, W, target, loss, lse, workspace):
+    """vgc_softmax_loss of the rows of X [..., H] over the classes W [V, H]: target int64 (negative: not asked for), loss and lse
+    float32, one a row.  workspace: uint8 tensor of softmax_loss_workspace_bytes() bytes."""
+    a, R, H, V, dtype = _loss_args(X, W, target)
+    a.need(loss, R, torch.float32, "loss")
+    a.need(lse, R, torch.float32, "lse")
+    ws, nbytes = _workspace(a, workspace, softmax_loss_workspace_bytes(dtype, R, H, V))
+    a.launchable()
+    _check(load().vgc_softmax_loss(dtype, _ptr(X), _ptr(W), _ptr(target), R, H, V, _ptr(loss), _ptr(lse), ws, nbytes, _stream()))
+
+
+def softmax_loss_backward_workspace_bytes(dtype, B, P, H, V):
+    return int(load().vgc_softmax_loss_backward_workspace_bytes(dtype, B, P, H, V))
+
+
+def softmax_loss_backward(X, W, target, lse, weight, c, dX, s_out, g_out=None, workspace=None):
+    """vgc_softmax_loss_backward for X [B, P, H]: dX like X, and the two sums over the samples for W, s_out and g_out float32 [V, H]
+    (dX or the sums may be None).  weight: float32, one a row, or None.
+    workspace: uint8 tensor of softmax_loss_backward_workspace_bytes() bytes."""
+    if X.dim() != 3:
+        raise VgcError(f"X: need [B, P, H], got {tuple(X.shape)}")
+    a, R, H, V, dtype = _loss_args(X, W, target)
+    B, P = X.shape[0], X.shape[1]
+    a.need(lse, R, torch.float32, "lse")
+    a.need(weight, R, torch.float32, "weight")
+    a.need(dX, R * H, X.dtype, "dX")
+    a.need(s_out, V * H, torch.float32, "s_out")
+    a.need(g_out, V * H, torch.float32, "g_out")
+    ws, nbytes = _workspace(a, workspace, softmax_loss_backward_workspace_bytes(dtype, B, P, H, V))
+    a.launchable()
+    _check(load().vgc_softmax_loss_backward(dtype, _ptr(X), _ptr(W), _ptr(target), _ptr(lse), _ptr(weight), B, P, H, V, float(c), _ptr(dX),
+                                            _ptr(g_out), _ptr(s_out), ws, nbytes, _stream()))

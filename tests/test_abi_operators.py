@@ -1,0 +1,69 @@
+"""Argument checks of the 8-bit activations, layer norm and softmax loss entry points: refused on the host, before anything touches
+a GPU (the pointers here are never dereferenced)."""
+import pytest
+
+from paper_1802_06058_amd import vgc
+
+OK, NULL, SIZE, DTYPE, ALIGN, PARAM = 0, -1, -2, -4, -5, -6
+P = 1 << 20                                          # an aligned address
+
+
+def _codes(good, changes, call):
+    for change, want in changes:
+        args = dict(good, **change)
+        assert call(*args.values()) == want, change
+        assert vgc.load().vgc_last_error()
+
+
+def test_act8():
+    lib = vgc.load()
+    good = dict(dtype=0, x=P, R=4, C=40, codes=P, exps=P, stream=None)
+    _codes(good, [(dict(dtype=2), DTYPE), (dict(x=None), NULL), (dict(codes=None), NULL), (dict(exps=None), NULL), (dict(R=0), SIZE), (dict(C=0), SIZE),
+                  (dict(C=1 << 31), SIZE), (dict(x=P + 2), ALIGN), (dict(R=1 << 41), SIZE), (dict(R=1 << 39, C=64), SIZE)], lib.vgc_act8_encode)
+    good = dict(dtype=1, codes=P, exps=P, R=4, C=40, out=P, stream=None)
+    _codes(good, [(dict(dtype=-1), DTYPE), (dict(out=None), NULL), (dict(codes=None), NULL), (dict(R=0), SIZE), (dict(out=P + 1), ALIGN)], lib.vgc_act8_decode)
+    need = vgc.sqgrad_act8_workspace_bytes(vgc.CONV, vgc.BF16, 2, 5, 64, 32)
+    assert need >= 2 * 5 * 64 * 2
+    assert vgc.sqgrad_act8_workspace_bytes(vgc.FC, vgc.BF16, 2, 1, 64, 32) >= 4 * 2 * (64 + 32)
+    for bad in [(2, 0, 2, 5, 64, 32), (1, 2, 2, 5, 64, 32), (0, 0, 2, 5, 64, 32), (1, 0, 0, 5, 64, 32), (1, 0, 2, 5, 1 << 23, 32)]:
+        assert vgc.sqgrad_act8_workspace_bytes(*bad) == 0
+    good = dict(kind=1, dtype=1, codes=P, exps=P, D=P, B=2, P=5, J=64, C=32, c=1.0, g=None, s=P, ws=P, nb=need, stream=None)
+    _codes(good, [(dict(kind=3), DTYPE), (dict(codes=None), NULL), (dict(s=None), NULL), (dict(D=None), NULL), (dict(kind=0), SIZE), (dict(J=0), SIZE), (dict(D=P + 8), ALIGN),
+                  (dict(g=P + 4), ALIGN), (dict(s=P + 4), ALIGN), (dict(c=float("inf")), PARAM), (dict(ws=None), NULL), (dict(nb=need - 1), SIZE), (dict(ws=P + 8), ALIGN)],
+           lib.vgc_sqgrad_act8)
+
+
+def test_layer_norm():
+    lib = vgc.load()
+    good = dict(dtype=0, x=P, R=4, C=40, gamma=P, beta=P, eps=1e-5, y=P, mean=P, rstd=P, codes=None, exps=None, stream=None)
+    _codes(good, [(dict(dtype=2), DTYPE), *[(dict([(k, None)]), NULL) for k in ("x", "gamma", "beta", "y", "mean", "rstd")], (dict(codes=P), NULL), (dict(exps=P), NULL),
+                  (dict(R=0), SIZE), (dict(C=0), SIZE), (dict(R=1 << 31), SIZE), (dict(C=1 << 31), SIZE), (dict(y=P + 2), ALIGN), (dict(gamma=P + 1), ALIGN),
+                  (dict(eps=-1e-9), PARAM), (dict(eps=float("nan")), PARAM)], lib.vgc_layer_norm)
+    need = vgc.layer_norm_backward_workspace_bytes(4, 10, 40)
+    assert need > 0 and vgc.layer_norm_backward_workspace_bytes(0, 10, 40) == 0 and vgc.layer_norm_backward_workspace_bytes(1 << 20, 1 << 20, 40) == 0
+    good = dict(dtype=1, dy=P, x=P, mean=P, codes=None, exps=None, rstd=P, gamma=P, B=4, P=10, C=40, c=0.5, dx=P, gg=None, sg=P, gb=None, sb=P, ws=P, nb=need, stream=None)
+    _codes(good, [(dict(dtype=5), DTYPE), *[(dict([(k, None)]), NULL) for k in ("dy", "rstd", "gamma", "dx", "sg", "sb", "x", "mean")], (dict(codes=P, exps=P), NULL),
+                  (dict(x=None, mean=None), NULL), (dict(x=None, mean=None, codes=P), NULL), (dict(B=0), SIZE), (dict(B=1 << 30, P=4), SIZE), (dict(dy=P + 1), ALIGN), (dict(gg=P + 2), ALIGN),
+                  (dict(c=float("nan")), PARAM), (dict(ws=None), NULL), (dict(nb=need - 1), SIZE), (dict(ws=P + 4), ALIGN)], lib.vgc_layer_norm_backward)
+
+
+def test_softmax_loss():
+    lib = vgc.load()
+    need = vgc.softmax_loss_workspace_bytes(vgc.F32, 6, 40, 30)
+    good = dict(dtype=0, X=P, W=P, target=P, N=6, H=40, V=30, loss=P, lse=P, ws=P, nb=need, stream=None)
+    _codes(good, [(dict(dtype=2), DTYPE), *[(dict([(k, None)]), NULL) for k in ("X", "W", "target", "loss", "lse", "ws")], *[(dict([(k, 0)]), SIZE) for k in ("N", "H", "V")],
+                  (dict(N=(1 << 20) + 1), SIZE), (dict(H=(1 << 20) + 1), SIZE), (dict(V=(1 << 24) + 1), SIZE), (dict(X=P + 8), ALIGN), (dict(W=P + 4), ALIGN), (dict(target=P + 4), ALIGN),
+                  (dict(lse=P + 2), ALIGN), (dict(nb=need - 1), SIZE), (dict(ws=P + 8), ALIGN)], lib.vgc_softmax_loss)
+    need = vgc.softmax_loss_backward_workspace_bytes(vgc.BF16, 2, 3, 40, 30)
+    good = dict(dtype=1, X=P, W=P, target=P, lse=P, weight=None, B=2, P=3, H=40, V=30, c=0.5, dX=P, g=P, s=P, ws=P, nb=need, stream=None)
+    _codes(good, [(dict(dtype=2), DTYPE), *[(dict([(k, None)]), NULL) for k in ("X", "W", "target", "lse", "s", "ws")], (dict(dX=None, g=None, s=None), NULL), (dict(P=0), SIZE),
+                  (dict(B=1 << 16, P=17), SIZE), (dict(dX=P + 8), ALIGN), (dict(s=P + 4), ALIGN), (dict(weight=P + 2), ALIGN), (dict(c=float("-inf")), PARAM), (dict(nb=need - 1), SIZE)],
+           lib.vgc_softmax_loss_backward)
+
+
+@pytest.mark.parametrize("dtype", [vgc.F32, vgc.BF16])
+def test_the_backward_pass_is_bounded_by_a_piece_of_the_classes(dtype):
+    """Twice and four times the vocabulary do not take twice the memory once it is cut into pieces."""
+    a, b, c = (vgc.softmax_loss_backward_workspace_bytes(dtype, 4, 1024, 1024, v) for v in (1 << 17, 1 << 18, 1 << 20))
+    logits = 4 * 1024 * (1 << 20) * 2
+    assert c < 1.1 * a and b < 1.1 * a and c < logits / 4

@@ -1,0 +1,137 @@
+"""Activations in 8 bits: codes and exponents equal the oracle's, decoding is exact, and the statistic is that of the kept values."""
+import numpy as np
+import pytest
+
+from oracle import operators as O
+from oracle import vgc_oracle as V
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def dev():
+    import torch
+    from paper_1802_06058_amd import vgc
+    assert torch.cuda.is_available()
+    vgc.load()
+    return torch.device("cuda:0")
+
+
+def _rows(seed, R, C):
+    rng = np.random.default_rng(seed)
+    x = rng.standard_normal((R, C)) * np.exp2(rng.integers(-130, 120, (R, 1)).astype(float))
+    x *= np.exp2(rng.integers(-12, 1, (R, C)).astype(float))
+    x[rng.random((R, C)) < 0.1] = 0
+    x[:: 7] = 0                                      # whole blocks of zeros
+    x[1::11, 0] = np.exp2(3.0) * 127.5 / 64          # on the edge between two units
+    x[2::11] = np.rint(x[2::11] * 0) + 0.5           # ties
+    x = x.astype(np.float32)
+    if R > 40:
+        x[5, C // 2], x[17, 0], x[23, C - 1], x[29, :] = np.inf, np.nan, -np.inf, np.nan
+        x[31, :] = 1e-42                             # subnormal
+        x[37, 0] = np.finfo(np.float32).max
+    return x
+
+
+SHAPES = [(1, 1), (1, 3), (50, 7), (300, 8), (41, 9), (64, 31), (50, 32), (50, 33), (128, 784), (9, 1000), (5, 1023), (700, 64), (3, 25088), (2000, 5)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("R,C", SHAPES)
+def test_codes_and_values(dev, R, C, dtype):
+    import torch
+    from paper_1802_06058_amd import vgc
+    x = torch.from_numpy(_rows(R * 131 + C, R, C))
+    if dtype == "bf16":
+        x = x.to(torch.bfloat16)
+    nb = (C + 31) // 32
+    codes = torch.full((R * C + 64,), 77, dtype=torch.int8, device=dev)
+    exps = torch.full((R * nb + 64,), 77, dtype=torch.uint8, device=dev)
+    vgc.act8_encode(x.to(dev), codes, exps)
+    q, e = O.act8_encode(x.float().numpy())
+    assert np.array_equal(codes[:R * C].cpu().numpy().reshape(R, C), q)
+    assert np.array_equal(exps[:R * nb].cpu().numpy().reshape(R, nb), e)
+    assert (codes[R * C:] == 77).all() and (exps[R * nb:] == 77).all()        # nothing past the rows
+    want = O.act8_decode(q, e)
+    for out_type in (torch.float32, torch.bfloat16):
+        out = torch.full((R * C + 64,), 5.0, dtype=out_type, device=dev)
+        vgc.act8_decode(codes, exps, out[:R * C].view(R, C))
+        assert np.array_equal(out[:R * C].view(R, C).double().cpu().numpy(), want, equal_nan=True)
+        assert (out[R * C:] == 5).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_that_begin_anywhere(dev, dtype):
+    import torch
+    from paper_1802_06058_amd import vgc
+    R, C = 37, 131
+    x = torch.from_numpy(_rows(9, R, C))
+    buf = torch.empty(R * C + 1, dtype=torch.float32 if dtype == "f32" else torch.bfloat16, device=dev)
+    view = buf[1:].view(R, C)
+    view.copy_(x)
+    codes = torch.empty(R * C + 3, dtype=torch.int8, device=dev)[3:].view(R, C)
+    exps = torch.empty(R * 5 + 1, dtype=torch.uint8, device=dev)[1:].view(R, 5)
+    vgc.act8_encode(view, codes, exps)
+    q, e = O.act8_encode(view.float().cpu().numpy())
+    assert np.array_equal(codes.cpu().numpy(), q) and np.array_equal(exps.cpu().numpy(), e)
+    buf.fill_(3)
+    vgc.act8_decode(codes, exps, view)
+    assert np.array_equal(view.double().cpu().numpy(), O.act8_decode(q, e), equal_nan=True) and float(buf[0]) == 3
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("form,B,P,J,C", [("fc", 1, 1, 5, 3), ("fc", 64, 1, 300, 200), ("fc", 33, 1, 1001, 77), ("conv", 3, 49, 64, 96), ("conv", 1, 1, 40, 8),
+                                          ("conv", 5, 130, 256, 136), ("conv", 2, 33, 37, 21), ("conv", 40, 2, 128, 128)])
+def test_statistic_of_kept_rows(dev, form, B, P, J, C, dtype):
+    """Against the library's own statistic on the decoded values (the same kernel: the same bits), and against 64 bits within
+    float32 sums of exact products: P + B + 8 roundings and as many truncations of 2^-23 of the magnitudes summed (a third more
+    for the samples' squares), which 1e-5 of them covers at these sizes.  Products of float32 pairs are within 2^-22.4."""
+    import torch
+    from paper_1802_06058_amd import vgc
+    kind = vgc.FC if form == "fc" else vgc.CONV
+    rng = np.random.default_rng(B * 7 + J)
+    x = np.maximum(rng.standard_normal((B * P, J)), 0).astype(np.float32)
+    D = torch.from_numpy(rng.standard_normal((B * P, C)).astype(np.float32) * 1e-3)
+    if dtype == "bf16":
+        D = D.to(torch.bfloat16)
+    q, e = O.act8_encode(x)
+    lead = (B,) if kind == vgc.FC else (B, P)
+    codes, exps = torch.from_numpy(q).to(dev).view(*lead, J), torch.from_numpy(e).to(dev)
+    Dd = D.to(dev).view(*lead, C)
+    code = vgc.F32 if dtype == "f32" else vgc.BF16
+    nb = vgc.sqgrad_act8_workspace_bytes(kind, code, B, P, J, C)
+    ws = torch.full((nb,), 0xFF, dtype=torch.uint8, device=dev)
+    s, g = torch.full((J, C), np.nan, device=dev), torch.full((J, C), np.nan, device=dev)
+    vgc.sqgrad_act8(kind, codes, exps, Dd, 1.0 / B, s, g, ws)
+    kept = torch.from_numpy(O.act8_decode(q, e)).to(torch.float32).to(dev).view(*lead, J)
+    wide = kind == vgc.FC or dtype == "f32"
+    s2, g2 = torch.empty_like(s), torch.empty_like(g)
+    nb2 = vgc.sqgrad_workspace_bytes(kind, vgc.F32 if wide else vgc.BF16, B, P, J, C)
+    vgc.sqgrad(kind, kept if wide else kept.to(torch.bfloat16), Dd.float() if wide else Dd, 1.0 / B, s2, g2,
+               torch.empty(nb2, dtype=torch.uint8, device=dev) if nb2 else None)
+    assert torch.equal(s, s2) and torch.equal(g, g2)
+    x64, D64 = O.act8_decode(q, e).reshape(B, P, J), D.double().numpy().reshape(B, P, C)
+    g64, s64 = V.sqgrad_conv(x64, D64, 1.0 / B)
+    ga, sa = V.sqgrad_conv(np.abs(x64), np.abs(D64), 1.0 / B)
+    assert (np.abs(g.double().cpu().numpy() - g64) <= 1e-5 * ga).all()
+    assert (np.abs(s.double().cpu().numpy() - s64) <= 1e-5 * sa).all()
+
+
+def test_refusals(dev):
+    import torch
+    from paper_1802_06058_amd import vgc
+    x = torch.zeros(4, 40, device=dev)
+    codes, exps = torch.zeros(4, 40, dtype=torch.int8, device=dev), torch.zeros(4, 2, dtype=torch.uint8, device=dev)
+    for bad in [(x.half(), codes, exps), (x.t(), codes, exps), (x, codes[:3], exps), (x, codes.float(), exps), (x, codes, exps[:, :1].contiguous()),
+                (x.cpu(), codes, exps), (x, codes, exps.cpu()), (torch.zeros(0, 40, device=dev), codes, exps), (torch.zeros(4, 0, device=dev), codes, exps)]:
+        with pytest.raises(vgc.VgcError):
+            vgc.act8_encode(*bad)
+        with pytest.raises(vgc.VgcError):
+            vgc.act8_decode(bad[1], bad[2], bad[0])
+    D, s = torch.zeros(4, 8, device=dev), torch.zeros(40, 8, device=dev)
+    ws = torch.empty(vgc.sqgrad_act8_workspace_bytes(vgc.FC, vgc.F32, 4, 1, 40, 8), dtype=torch.uint8, device=dev)
+    for call in [lambda: vgc.sqgrad_act8(vgc.FC, codes, exps, D, 1.0, s), lambda: vgc.sqgrad_act8(vgc.FC, codes, exps, D, 1.0, s, None, ws[:-1]),
+                 lambda: vgc.sqgrad_act8(vgc.FC, codes, exps, D[:3], 1.0, s, None, ws), lambda: vgc.sqgrad_act8(vgc.CONV, codes, exps, D, 1.0, s, None, ws),
+                 lambda: vgc.sqgrad_act8(vgc.FC, codes, exps, D, float("nan"), s, None, ws), lambda: vgc.sqgrad_act8(vgc.FC, codes, exps, D, 1.0, s[:39], None, ws)]:
+        with pytest.raises(vgc.VgcError):
+            call()
