@@ -406,7 +406,7 @@ int vgc_unpack_apply(const uint32_t* const* words, const uint64_t* n_words,
  * [R, ceil(C / 32)].  Aligned to their elements.  C at most 2^31 - 1.  Errors: NULL, SIZE, DTYPE, ALIGN.
  *
  * vgc_sqgrad_act8 is vgc_sqgrad with X given in this form (codes [B, P, J], exps [B, P, ceil(J / 32)]) and D in dtype: the sums are
- * those of the decoded values.  Both factors of the FC form are multiplied as floats, squares included, in either dtype.
+ * those of the decoded values.  The FC form rounds no square to 16 bits: with VGC_BF16 D both squares are multiplied exactly.
  * workspace (required): DEVICE, 16-byte aligned, vgc_sqgrad_act8_workspace_bytes() bytes.  J at most 4194240. */
 int vgc_act8_encode(int dtype, const void* x, uint64_t R, uint32_t C, int8_t* codes, uint8_t* exps, void* stream);
 int vgc_act8_decode(int dtype, const int8_t* codes, const uint8_t* exps, uint64_t R, uint32_t C, void* out, void* stream);
@@ -450,7 +450,7 @@ int vgc_layer_norm_backward(int dtype, const void* dy, const void* x, const floa
  * float [N], or NULL for 1; dX: DEVICE [N, H] in dtype, 16-byte aligned, or NULL; s_out: DEVICE float [V, H], 16-byte aligned, or
  * NULL; g_out: the same, or NULL (NULL if s_out is).  lse is what the forward call wrote for the same X and W.
  * workspace: DEVICE, 16-byte aligned, of the bytes that the function beside it gives; the backward pass's is bounded by X and by a
- * piece of the classes: half a GiB, and 256 classes at least.
+ * piece of the classes: two GiB, and 256 classes at least.
  * Sums are float32.  VGC_BF16: D is rounded to bfloat16 for dX and kept in 16 significant bits for g and s.  VGC_F32: products of
  * the operands' 8-bit pieces as in vgc_sqgrad's conv form.  Errors: NULL, SIZE (a zero dimension, N = B P (P rounded up to 32 if it
  * is not 1) or H beyond 2^20, V beyond 2^24), DTYPE, ALIGN, PARAM. */

@@ -80,16 +80,6 @@ __global__ __launch_bounds__(256) void k_act8_decode(const int8_t* __restrict__ 
     }
 }
 
-// Output gradients widened to float for the FC form (exact).
-__global__ __launch_bounds__(256) void k_widen(const uint16_t* __restrict__ in, uint64_t n, float* __restrict__ out) {
-    const uint64_t i = ((uint64_t)blockIdx.x * 256u + threadIdx.x) * 8u;
-    if (i >= n) return;
-    const int m = n - i >= 8u ? 8 : (int)(n - i);
-    float f[8];
-    widen8(load8(in + i, m), f);
-    store8(out + i, f, m);
-}
-
 static uint32_t pieces_per_row(uint32_t C) { return C <= 8 ? 1u : (C + kAct8Block - 1) / kAct8Block * kAct8Lanes; }
 
 static int act8_grid(uint64_t R, uint32_t C, const char* what, uint32_t* per_row, uint32_t* groups) {
@@ -122,19 +112,19 @@ int launch_act8_decode(int dtype, const int8_t* codes, const uint8_t* exps, uint
     return hip_check(hipGetLastError(), "launch k_act8_decode");
 }
 
-// The statistic from kept activations.  The kept values are laid out in the type in which the statistic multiplies them: the
-// conv form's in that of D (exact in both), the FC form's in float, with D widened beside them: that form is bound by the
-// outputs it writes, and its 16-bit kernel would round the squares to 16 bits.
-struct SqgradAct8Layout { int dtype; size_t x, d, rest, rest_bytes, total; };
+// The statistic from kept activations.  Conv form: the kept values are laid out in the type of D (exact in both) for the kernels of
+// vgc_sqgrad.  FC form: bfloat16 D and the kept values as planes of values and squares (vgc_fc_planes.hip); float D and the kept values
+// as floats.
+struct SqgradAct8Layout { bool planes; size_t x, d, rest, rest_bytes, total; };
 static SqgradAct8Layout sqgrad_act8_layout(int kind, int dtype, uint32_t B, uint32_t P, uint32_t J, uint32_t C) {
     SqgradAct8Layout L;
     const size_t rows = (size_t)B * P;
-    L.dtype = kind == VGC_FC ? VGC_F32 : dtype;
+    L.planes = kind == VGC_FC && dtype == VGC_BF16;
     size_t off = 0;
-    L.x = off; off = align_up(off + rows * J * (L.dtype == VGC_F32 ? 4 : 2), 256);
-    L.d = off; if (L.dtype != dtype) off = align_up(off + rows * C * 4, 256);
+    L.x = off; off += L.planes ? fc_planes_bytes(1, B, J) : align_up(rows * J * (dtype == VGC_F32 ? 4 : 2), 256);
+    L.d = off; if (L.planes) off += fc_planes_bytes(1, B, C);
     L.rest = off;
-    L.rest_bytes = sqgrad_workspace_bytes(kind, L.dtype, B, P, J, C);
+    L.rest_bytes = L.planes ? 0 : sqgrad_workspace_bytes(kind, dtype, B, P, J, C);
     L.total = off + L.rest_bytes;
     return L;
 }
@@ -145,16 +135,14 @@ int launch_sqgrad_act8(int kind, int dtype, const int8_t* codes, const uint8_t* 
                        uint32_t C, float c, float* g_out, float* s_out, void* workspace, hipStream_t stream) {
     const SqgradAct8Layout L = sqgrad_act8_layout(kind, dtype, B, P, J, C);
     char* ws = static_cast<char*>(workspace);
-    int rc = launch_act8_decode(L.dtype, codes, exps, (uint64_t)B * P, J, ws + L.x, stream);
-    if (rc != VGC_OK) return rc;
-    const void* d = D;
-    if (L.dtype != dtype) {
-        const uint64_t n = (uint64_t)B * P * C;
-        hipLaunchKernelGGL(k_widen, dim3((uint32_t)((n + 2047) / 2048)), dim3(256), 0, stream, (const uint16_t*)D, n, (float*)(ws + L.d));
-        if ((rc = hip_check(hipGetLastError(), "launch k_widen")) != VGC_OK) return rc;
-        d = ws + L.d;
+    int rc;
+    if (L.planes) {
+        if ((rc = launch_square_planes_act8(codes, exps, B, J, ws + L.x, stream)) != VGC_OK) return rc;
+        if ((rc = launch_square_planes(VGC_BF16, D, nullptr, B, C, ws + L.d, stream)) != VGC_OK) return rc;
+        return launch_fc_planes(ws + L.x, 1, ws + L.d, B, J, C, c, g_out, s_out, stream);
     }
-    return launch_sqgrad(kind, L.dtype, ws + L.x, d, B, P, J, C, c, g_out, s_out, L.rest_bytes ? ws + L.rest : nullptr, L.rest_bytes, stream);
+    if ((rc = launch_act8_decode(dtype, codes, exps, (uint64_t)B * P, J, ws + L.x, stream)) != VGC_OK) return rc;
+    return launch_sqgrad(kind, dtype, ws + L.x, D, B, P, J, C, c, g_out, s_out, L.rest_bytes ? ws + L.rest : nullptr, L.rest_bytes, stream);
 }
 
 }  // namespace vgc

@@ -748,7 +748,7 @@ static int sqgrad_act8_shape(int kind, int dtype, uint32_t B, uint32_t P, uint32
     if (B == 0 || P == 0 || J == 0 || C == 0) { set_error("vgc_sqgrad_act8: zero dimension"); return VGC_ERR_SIZE; }
     if (kind == VGC_FC && P != 1) { set_error("vgc_sqgrad_act8: the FC form has P = 1"); return VGC_ERR_SIZE; }
     if (J > 65535u * 64u) { set_error("vgc_sqgrad_act8: J = %u exceeds the launch limit", J); return VGC_ERR_SIZE; }
-    if ((uint64_t)B * P * C > (1ull << 42)) { set_error("vgc_sqgrad_act8: D has too many elements"); return VGC_ERR_SIZE; }
+    if (kind == VGC_FC && dtype == VGC_BF16 && !fc_planes_supported(B, J, C)) { set_error("vgc_sqgrad_act8: a row operand exceeds 2^31 bytes"); return VGC_ERR_SIZE; }
     return VGC_OK;
 }
 

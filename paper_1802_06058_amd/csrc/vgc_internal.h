@@ -315,6 +315,13 @@ size_t sqgrad_act8_workspace_bytes(int kind, int dtype, uint32_t B, uint32_t P, 
 int launch_sqgrad_act8(int kind, int dtype, const int8_t* codes, const uint8_t* exps, const void* D, uint32_t B, uint32_t P, uint32_t J,
                        uint32_t C, float c, float* g_out, float* s_out, void* workspace, hipStream_t stream);
 
+// The FC form from bfloat16 planes of values and squares (vgc_fc_planes.hip)
+size_t fc_planes_bytes(uint32_t own, uint32_t N, uint32_t K);
+bool fc_planes_supported(uint32_t N, uint32_t M, uint32_t C);
+int launch_square_planes_act8(const int8_t* codes, const uint8_t* exps, uint32_t R, uint32_t K, void* dst, hipStream_t stream);
+int launch_square_planes(int dtype, const void* src, const int64_t* target, uint32_t R, uint32_t K, void* dst, hipStream_t stream);
+int launch_fc_planes(const void* a, uint32_t own, const void* b, uint32_t N, uint32_t M, uint32_t C, float c, float* g_out, float* s_out, hipStream_t stream);
+
 // Layer norm (vgc_norm.hip)
 int launch_layer_norm(int dtype, const void* x, uint64_t R, uint32_t C, const float* gamma, const float* beta, float eps, void* y, float* mean,
                       float* rstd, int8_t* codes, uint8_t* exps, hipStream_t stream);

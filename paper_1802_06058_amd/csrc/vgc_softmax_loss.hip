@@ -7,14 +7,15 @@
 // exponentials relative to it, and these pairs are joined over the tiles of the vocabulary by a second, small kernel.  W is the A
 // operand, so that a lane's 16 results of an instruction are 16 classes of one token: the reduction is in registers but for one
 // exchange between the lane halves.
-// Backward, the logits are formed again, a piece of the vocabulary at a time, and D of the piece goes to the workspace in the
-// two orders in which the two products that follow read it with k contiguous; memory is bounded by the piece, not by the
-// vocabulary.  All three products run through the one loop of vgc_gemm.h.
+// Backward, the logits are formed again, a piece of the vocabulary at a time, and D of the piece goes to the workspace by classes,
+// positions contiguous: the order in which the sums over a sample's positions read it with k contiguous and dX reads it with k, the
+// classes, as rows, beside W as it lies.  Memory is bounded by the piece, not by the vocabulary.  The three products run through
+// the loop of vgc_gemm.h.
 //
 // Precision.  bfloat16 inputs: products are exact, sums float32.  D is rounded to bfloat16 for dX, which is rounded to bfloat16
-// itself; for g and s, which are float32, it is kept in two pieces, 16 significant bits.  float32 inputs: every operand is cut
-// exactly into three pieces of 8 bits and a product is formed from the six pairs of pieces that reach 2^-24 of it: the pieces lie
-// one after another along k (smallest products first), so that the same loop runs over six times the length.
+// itself; for g and s, which are float32, a second plane holds the rest, 16 significant bits in all.  float32 inputs: every operand
+// is cut exactly into three planes of 8 bits and a product is formed from the six pairs of planes that reach 2^-24 of it; few rows
+// are multiplied as floats instead.
 #include <algorithm>
 
 #include "vgc_gemm.h"
@@ -22,12 +23,11 @@
 
 namespace vgc {
 
+typedef float f4v __attribute__((ext_vector_type(4)));
+
 // ---- operands -------------------------------------------------------------------------------------------------------------
-// A float cut into three bfloat16 pieces, largest first, by truncation: 8 + 8 + 8 bits, exact (but for bits below the smallest
-// subnormal).  The pieces of an operand follow each other along k in slots, and slot i of the one side meets slot i of the other:
-// the six pairs of pieces whose product reaches 2^-24 of the whole, the smallest first.
-constexpr uint32_t kSlotsF32 = 6;
-__device__ constexpr int kPieceA[6] = {2, 0, 1, 1, 0, 0}, kPieceB[6] = {0, 2, 1, 0, 1, 0};
+// A float cut into three bfloat16 planes, largest first, by truncation: 8 + 8 + 8 bits, exact (but for bits below the smallest
+// subnormal).
 struct Cut3 { uint32_t p[3]; };                              // each the upper half of a float's bits
 __device__ __forceinline__ Cut3 cut3(float x) {
     Cut3 c;
@@ -40,14 +40,35 @@ __device__ __forceinline__ Cut3 cut3(float x) {
     c.p[2] = __float_as_uint(r2) >> 16;
     return c;
 }
-// A gradient in two pieces rounded to nearest: within 2^-18 of it.
-__device__ __forceinline__ float bf16_round(float x) { return __uint_as_float(two_bf16(x, 0.f) << 16); }
+// Plane q of two entries of D, the first in the low half: float32 inputs the cut of it; bfloat16 ones its rounding, and the rounding
+// of what is left (within 2^-18 of D).
+template <bool kF32> __device__ __forceinline__ uint32_t plane_of(float d0, float d1, uint32_t q) {
+    if (kF32) {
+        const Cut3 a = cut3(d0), b = cut3(d1);
+        return q == 0 ? a.p[0] | b.p[0] << 16 : q == 1 ? a.p[1] | b.p[1] << 16 : a.p[2] | b.p[2] << 16;
+    }
+    const uint32_t hi = two_bf16(d0, d1);
+    return q == 0 ? hi : two_bf16(d0 - __uint_as_float(hi << 16), d1 - __uint_as_float(hi & 0xFFFF0000u));
+}
 
-__device__ __forceinline__ uint32_t bits16(float x) { return __float_as_uint(x) >> 16; }     // of a value that is a bfloat16
+// Eight values as the planes of an operand, 16 bytes each.
+template <typename T> __device__ __forceinline__ void store_planes(uint16_t* out, uint64_t plane, const float (&f)[8]) {
+    if (sizeof(T) == 2) { store8(out, f, 8); return; }
+    Cut3 c[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c[e] = cut3(f[e]);
+#pragma unroll
+    for (int q = 0; q < 3; ++q) {
+        any_u4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = c[2 * e].p[q] | c[2 * e + 1].p[q] << 16;
+        *reinterpret_cast<any_u4*>(out + q * plane) = v;
+    }
+}
 
-// Rows as they are, padded to whole pieces of 8 (dst rows are slots * Kp long).
-template <typename T, bool kSecond>
-__global__ __launch_bounds__(256) void k_slots_rows(const T* __restrict__ src, uint32_t R, uint32_t K, uint32_t Kp, uint16_t* __restrict__ dst) {
+// Rows as they are, padded with zeros to whole pieces of 8.
+template <typename T>
+__global__ __launch_bounds__(256) void k_planes_rows(const T* __restrict__ src, uint32_t R, uint32_t K, uint32_t Kp, uint16_t* __restrict__ dst) {
     const uint32_t per_row = Kp / 8u;
     const uint64_t i = (uint64_t)blockIdx.x * 256u + threadIdx.x;
     if (i >= (uint64_t)R * per_row) return;
@@ -55,44 +76,32 @@ __global__ __launch_bounds__(256) void k_slots_rows(const T* __restrict__ src, u
     const uint32_t k = (uint32_t)(i - row * per_row) * 8u;
     float f[8];
     widen8(load8(src + row * K + k, (int)(K - k)), f);
-    constexpr uint32_t slots = sizeof(T) == 4 ? kSlotsF32 : 1u;
-    uint16_t* out = dst + row * slots * Kp + k;
-    if (sizeof(T) == 2) {
-        store8(out, f, 8);
-        return;
-    }
-    Cut3 c[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) c[e] = cut3(f[e]);
-#pragma unroll
-    for (uint32_t s = 0; s < slots; ++s) {
-        const int q = kSecond ? kPieceB[s] : kPieceA[s];
-        any_u4 v;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = c[2 * e].p[q] | c[2 * e + 1].p[q] << 16;
-        *reinterpret_cast<any_u4*>(out + (size_t)s * Kp) = v;
-    }
+    store_planes<T>(dst + row * Kp + k, (uint64_t)R * Kp, f);
 }
 
-// Columns as rows, for the second side: dst[k][(z slots + s) Pp + p] = piece of src[z P + p][k], zero for p in [P, Pp) and for
-// rows that are not asked for (target given and negative).  slots: 6 for float; 1, or 2 times the same for the two pieces of D.
-// A workgroup turns 64 positions by 64 columns in LDS.
+// Positions: sample z's position p is number z Pp + p, P <= Pp; the numbers between are no positions.
+struct Positions {
+    uint32_t B, P, Pp;
+    __device__ __forceinline__ uint32_t row(uint32_t q) const {            // its row of [B, P], or ~0
+        const uint32_t z = q / Pp, p = q - z * Pp;
+        return z < B && p < P ? z * P + p : 0xFFFFFFFFu;
+    }
+};
+
+// X by columns: dst[k][q] = src[row(q)][k], zero where there is no position and in rows that are not asked for.  A workgroup turns 64
+// positions by 64 columns in LDS.
 template <typename T>
-__global__ __launch_bounds__(256) void k_slots_columns(const T* __restrict__ src, const int64_t* __restrict__ target, uint32_t B, uint32_t P,
-                                                       uint32_t Pp, uint32_t K, uint32_t slots, uint32_t ld, uint16_t* __restrict__ dst) {
+__global__ __launch_bounds__(256) void k_planes_columns(const T* __restrict__ src, const int64_t* __restrict__ target, Positions at, uint32_t K,
+                                                        uint32_t Lq, uint16_t* __restrict__ dst) {
     __shared__ float t[64][65];
-    const uint32_t k0 = blockIdx.y * 64u, q0 = blockIdx.x * 64u, total = B * Pp;
-    const uint32_t col = threadIdx.x & 63u, r4 = threadIdx.x >> 6;
+    const uint32_t k0 = blockIdx.y * 64u, q0 = blockIdx.x * 64u, col = threadIdx.x & 63u;
 #pragma unroll 4
-    for (uint32_t r = r4; r < 64u; r += 4u) {
-        const uint32_t q = q0 + r, z = q / Pp, p = q - z * Pp;
+    for (uint32_t r = threadIdx.x >> 6; r < 64u; r += 4u) {
+        const uint32_t row = at.row(q0 + r);
         float x = 0.f;
-        if (q < total && p < P && k0 + col < K) {
-            const uint64_t row = (uint64_t)z * P + p;
-            if (!target || target[row] >= 0) {
-                if (sizeof(T) == 4) x = ((const float*)src)[row * K + k0 + col];
-                else x = __uint_as_float((uint32_t)((const uint16_t*)src)[row * K + k0 + col] << 16);
-            }
+        if (row != 0xFFFFFFFFu && k0 + col < K && target[row] >= 0) {
+            if (sizeof(T) == 4) x = ((const float*)src)[(uint64_t)row * K + k0 + col];
+            else x = __uint_as_float((uint32_t)((const uint16_t*)src)[(uint64_t)row * K + k0 + col] << 16);
         }
         t[r][col] = x;
     }
@@ -100,26 +109,11 @@ __global__ __launch_bounds__(256) void k_slots_columns(const T* __restrict__ src
 #pragma unroll
     for (uint32_t u = threadIdx.x; u < 512u; u += 256u) {
         const uint32_t kk = u >> 3, q = q0 + (u & 7u) * 8u;
-        if (k0 + kk >= K || q >= total) continue;
-        const uint32_t z = q / Pp, p = q - z * Pp;           // (Pp is a multiple of 8: the eight belong to one sample)
-        uint16_t* out = dst + (size_t)(k0 + kk) * ld + (size_t)z * slots * Pp + p;
+        if (k0 + kk >= K || q >= Lq) continue;
         float f[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) f[e] = t[(u & 7u) * 8u + e][kk];
-        if (sizeof(T) == 2) {
-            for (uint32_t s = 0; s < slots; ++s) store8(out + (size_t)s * Pp, f, 8);
-        } else {
-            Cut3 c[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) c[e] = cut3(f[e]);
-#pragma unroll
-            for (uint32_t s = 0; s < kSlotsF32; ++s) {
-                any_u4 v;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = c[2 * e].p[kPieceB[s]] | c[2 * e + 1].p[kPieceB[s]] << 16;
-                *reinterpret_cast<any_u4*>(out + (size_t)s * Pp) = v;
-            }
-        }
+        store_planes<T>(dst + (uint64_t)(k0 + kk) * Lq + q, (uint64_t)K * Lq, f);
     }
 }
 
@@ -136,15 +130,12 @@ __global__ __launch_bounds__(256) void k_asked_rows(const T* __restrict__ src, c
     store8(dst + row * K + k, f, (int)(K - k));
 }
 
-__global__ __launch_bounds__(256) void k_clear(uint4* p, uint64_t n) {
-    const uint64_t i = (uint64_t)blockIdx.x * 256u + threadIdx.x;
-    if (i < n) p[i] = make_uint4(0u, 0u, 0u, 0u);
-}
-
 // ---- the logits of a tile and what becomes of them --------------------------------------------------------------------------
 struct LossArgs {
-    Rows w, x;                // classes [v0, v0 + V) and tokens
+    Matrix w, x;              // classes [v0, v0 + V) and rows of X, k contiguous
     uint32_t K, V, N;
+    Positions at;             // of the tile's columns (forward: every row)
+    uint32_t Lq;              // numbers of them, a multiple of 8 where D is stored by classes
     int64_t v0;
     const int64_t* target;
     // forward
@@ -154,15 +145,18 @@ struct LossArgs {
     // backward
     int64_t V_all;
     const float *lse, *weight;
-    uint16_t *d, *dt;         // D by tokens, rows of slots * Vp; by classes, rows of ld_dt, sample z's slot s at (z slots + s) Pp
-    float* d32;               // D in float by tokens, rows of V
-    uint32_t Vp, ld_dt, P, Pp;
+    uint16_t* dt;             // D by classes, rows of Lq, planes `plane` apart
+    uint64_t plane;
+    uint32_t planes;
+    float* d32;               // D in float by rows of X, V long
 };
 
 constexpr float kLog2e = 1.44269504088896341f;
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+// Class, relative to m0, of a lane's result i of tile m.
+__device__ __forceinline__ uint32_t class_of(int m, int i, uint32_t half) { return m * 32u + 8u * (i >> 2) + 4u * half + (i & 3); }
 
-// acc[mt][nt] of a wave: classes m0 + 32 mt + .., tokens n0 + 32 nt + lane % 32.
+// acc[mt][nt] of a wave: classes m0 + 32 mt + .., columns n0 + 32 nt + lane % 32.
 template <int MT, int NT>
 __device__ __forceinline__ void finish_forward(f16v (&acc)[MT][NT], uint32_t m0, uint32_t n0, const LossArgs& A) {
     const uint32_t lane = threadIdx.x & 63u, half = lane >> 5;
@@ -172,7 +166,7 @@ __device__ __forceinline__ void finish_forward(f16v (&acc)[MT][NT], uint32_t m0,
         for (int m = 0; m < MT; ++m)
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-                if (m0 + m * 32u + 8u * (i >> 2) + 4u * half + (i & 3) >= A.V)
+                if (m0 + class_of(m, i, half) >= A.V)
 #pragma unroll
                     for (int n = 0; n < NT; ++n) acc[m][n][i] = kNone;
     }
@@ -189,7 +183,7 @@ __device__ __forceinline__ void finish_forward(f16v (&acc)[MT][NT], uint32_t m0,
             for (int i = 0; i < 16; ++i) {
                 const float z = acc[m][n][i];
                 top = fmaxf(top, z);
-                if (at == m * 32u + 8u * (i >> 2) + 4u * half + (i & 3)) z_t = z;
+                if (at == class_of(m, i, half)) z_t = z;
             }
         const float base = top == kNone ? 0.f : top;         // (a column of -inf: its exponentials are 0)
 #pragma unroll
@@ -204,135 +198,227 @@ __device__ __forceinline__ void finish_forward(f16v (&acc)[MT][NT], uint32_t m0,
     }
 }
 
-template <bool kF32, int MT, int NT>
-__device__ __forceinline__ void finish_backward(f16v (&acc)[MT][NT], uint32_t m0, uint32_t n0, const LossArgs& A) {
+// What the backward pass knows of a column: its row of X, and how a logit becomes an entry of D.
+struct ColumnOf {
+    uint32_t row, at;         // the target's class in the piece, or ~0
+    float lse, w;
+    bool asked;
+    __device__ __forceinline__ float d(float z, uint32_t v) const { return asked ? (exp_of(z - lse) - (v == at ? 1.f : 0.f)) * w : 0.f; }
+};
+__device__ __forceinline__ ColumnOf column_of(uint32_t q, const LossArgs& A) {
+    ColumnOf C = {A.at.row(q), 0xFFFFFFFFu, 0.f, 0.f, false};
+    if (C.row == 0xFFFFFFFFu) return C;
+    const int64_t t = A.target[C.row], tl = t - A.v0;
+    C.asked = t >= 0;
+    if (!C.asked) return C;
+    C.lse = A.lse[C.row];
+    C.w = t >= A.V_all ? __uint_as_float(0x7FC00000u) : A.weight ? A.weight[C.row] : 1.f;     // (not a class: the gradients say so)
+    if (tl >= 0 && tl < (int64_t)A.V) C.at = (uint32_t)tl;
+    return C;
+}
+
+// The logits become D in place.
+template <int MT, int NT>
+__device__ __forceinline__ void logits_to_d(f16v (&acc)[MT][NT], uint32_t m0, uint32_t n0, const LossArgs& A) {
     const uint32_t lane = threadIdx.x & 63u, half = lane >> 5;
-    constexpr uint32_t slots = kF32 ? kSlotsF32 : 1u, slots_t = kF32 ? kSlotsF32 : 2u;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        const uint32_t token = n0 + n * 32u + (lane & 31u);
-        if (token >= A.N) continue;
-        const int64_t t = A.target[token];
-        const float lse = A.lse[token];
-        float w = A.weight ? A.weight[token] : 1.f;
-        if (t >= A.V_all) w = __uint_as_float(0x7FC00000u);  // not a class: the gradients say so
-        const bool asked = t >= 0;
-        const int64_t tl = t - A.v0;
-        const uint32_t at = asked && tl >= 0 && tl < (int64_t)A.V ? (uint32_t)tl : 0xFFFFFFFFu;
-        const uint32_t z = token / A.P, p = token - z * A.P;
+        ColumnOf C = column_of(n0 + n * 32u + (lane & 31u), A);
+        C.at -= m0;
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const uint32_t v = m0 + m * 32u + 8u * g + 4u * half;        // four consecutive classes
-                float d[4];
+            for (int i = 0; i < 16; ++i) acc[m][n][i] = C.d(acc[m][n][i], class_of(m, i, half));
+        if (A.d32 && C.row != 0xFFFFFFFFu) {
+            float* out = A.d32 + (size_t)C.row * A.V + m0;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float q = exp_of(acc[m][n][4 * g + e] - lse) - (v + e == at ? 1.f : 0.f);
-                    d[e] = asked && v + e < A.V ? q * w : 0.f;
-                }
-                if (A.d32) {
+            for (int m = 0; m < MT; ++m)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (v + e < A.V) A.d32[(size_t)token * A.V + v + e] = d[e];
-                }
-                Cut3 c[4];
-                float hi[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (kF32) c[e] = cut3(d[e]);
-                    else hi[e] = bf16_round(d[e]);
-                }
-                if (A.d && v < A.Vp) {
-                    uint16_t* out = A.d + (size_t)token * slots * A.Vp + v;
-#pragma unroll
-                    for (uint32_t s = 0; s < slots; ++s) {
-                        uint2 o;
-                        if (kF32) o = make_uint2(c[0].p[kPieceA[s]] | c[1].p[kPieceA[s]] << 16, c[2].p[kPieceA[s]] | c[3].p[kPieceA[s]] << 16);
-                        else o = make_uint2(two_bf16(d[0], d[1]), two_bf16(d[2], d[3]));
-                        *reinterpret_cast<uint2*>(out + (size_t)s * A.Vp) = o;
-                    }
-                }
-                if (A.dt) {
-                    const size_t col = (size_t)z * slots_t * A.Pp + p;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if (v + e >= A.V) continue;
-                        uint16_t* out = A.dt + (size_t)(v + e) * A.ld_dt + col;
-#pragma unroll
-                        for (uint32_t s = 0; s < slots_t; ++s)
-                            out[(size_t)s * A.Pp] = (uint16_t)(kF32 ? c[e].p[kPieceA[s]] : bits16(s ? hi[e] : bf16_round(d[e] - hi[e])));
-                    }
-                }
-            }
+                for (int i = 0; i < 16; ++i)
+                    if (m0 + class_of(m, i, half) < A.V) out[class_of(m, i, half)] = acc[m][n][i];
+        }
     }
 }
 
-template <typename Tile, bool kForward, bool kF32>
-__global__ __launch_bounds__(Tile::NW * 64, Tile::NW == 8 ? 2 : 2) void k_logits(LossArgs A) {
-    __shared__ __attribute__((aligned(1024))) uint8_t sh[Tile::kLds];
-    const uint32_t tiles_n = (A.N + Tile::BN - 1) / Tile::BN, id = xcd_contiguous(blockIdx.x, gridDim.x);
-    const uint32_t m0 = id / tiles_n * Tile::BM, n0 = id % tiles_n * Tile::BN;
-    f16v acc[Tile::MT][Tile::NT] = {};
-    Tile::template run<false>(acc, sh, A.w, A.x, m0, n0, 0u, A.K, [](uint32_t) {});
-    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t wm = m0 + wave / (Tile::BN / Tile::WN) * Tile::WM, wn = n0 + wave % (Tile::BN / Tile::WN) * Tile::WN;
-    if (kForward) { if (wm < A.V) finish_forward(acc, wm, wn, A); }
-    else finish_backward<kF32>(acc, wm, wn, A);
+// D by classes.  The wave turns its part in LDS, in bytes of its own, a plane at a time, and stores whole rows of its positions.  The two
+// halves of a wave, four classes apart, write to different banks: 64-byte halves of a row of 64 positions change places with bit 2 of
+// the class.
+template <bool kF32, int MT, int NT>
+__device__ __forceinline__ void store_by_classes(f16v (&acc)[MT][NT], uint8_t* turn, uint32_t m0, uint32_t n0, const LossArgs& A) {
+    constexpr uint32_t kRow = NT * 64, kPieces = NT * 4, kRows = 64 / kPieces;               // bytes and pieces a class; classes a store
+    const uint32_t lane = threadIdx.x & 63u, half = lane >> 5, flip = NT == 2 ? 1u : 0u;
+    for (uint32_t q = 0; q < A.planes; ++q) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 16; i += 2) {            // (bit 2 of the class is the half)
+                    const uint32_t x = plane_of<kF32>(acc[m][n][i], acc[m][n][i + 1], q);
+                    uint8_t* to = turn + class_of(m, i, half) * kRow + ((uint32_t)n ^ (half & flip)) * 64u + (lane & 31u) * 2u;
+                    *reinterpret_cast<uint16_t*>(to) = (uint16_t)x;
+                    *reinterpret_cast<uint16_t*>(to + kRow) = (uint16_t)(x >> 16);
+                }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll 4
+        for (uint32_t r = 0; r < MT * 32 / kRows; ++r) {
+            const uint32_t v = r * kRows + lane / kPieces, piece = lane % kPieces;
+            const any_u4 x = *reinterpret_cast<const any_u4*>(turn + v * kRow + ((piece ^ ((((v >> 2) & flip)) << 2)) * 16u));
+            if (m0 + v < A.V && n0 + piece * 8u < A.Lq) *reinterpret_cast<any_u4*>(A.dt + q * A.plane + (size_t)(m0 + v) * A.Lq + n0 + piece * 8u) = x;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
 }
 
-// Few tokens, or few classes: a workgroup of eight waves owns 32 classes by 64 tokens and its waves share k in steps of 64, with
-// both operands straight from memory into registers; the waves' sums meet in LDS.  In a step a lane takes the 32 consecutive k of
-// its half: which k an instruction's place stands for is free as long as both operands agree.
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_buffer(const Rows& R, uint32_t row0, uint32_t count) {
-    const uint32_t left = row0 < R.rows ? min(R.rows - row0, count) : 0u;
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(R.base + (size_t)row0 * R.ld), 0, (int)(left * R.ld * 2u), 0x00020000);
+template <typename Shape, bool kForward>
+__global__ __launch_bounds__(Shape::NW * 64, 2) void k_logits(LossArgs A) {
+    __shared__ __attribute__((aligned(1024))) uint8_t sh[Shape::kLds];
+    const uint32_t tiles_n = ((kForward ? A.N : A.Lq) + Shape::BN - 1) / Shape::BN, tiles_m = (A.V + Shape::BM - 1) / Shape::BM;
+    const TilePlace at = in_bands(xcd_contiguous(blockIdx.x, gridDim.x), tiles_m, tiles_n);
+    const uint32_t m0 = at.m * Shape::BM, n0 = at.n * Shape::BN;
+    f16v acc[Shape::MT][Shape::NT] = {};
+    // the tile's rows of X lie between those of its first and of its last position
+    const uint32_t z0 = n0 / A.at.Pp, first = min(z0 * A.at.P + min(n0 - z0 * A.at.Pp, A.at.P), A.N);
+    RowTile<Shape>::run(acc, sh, A.w, A.x, m0, first, Shape::BN, [&](uint32_t n) {
+        const uint32_t row = A.at.row(n0 + n);
+        return row == 0xFFFFFFFFu ? row : row - first;
+    }, A.K, [](uint32_t, int) {});
+    const uint32_t wm = m0 + Shape::wave_m(), wn = n0 + Shape::wave_n();
+    if (kForward) {
+        if (wm < A.V) finish_forward(acc, wm, wn, A);
+    } else {
+        logits_to_d(acc, wm, wn, A);
+        static_assert(Shape::NT <= 2 && Shape::BM * Shape::BN * 2u <= Shape::kLds, "room to turn a plane");
+        if (A.dt) store_by_classes<Shape::PA == 3>(acc, sh + Shape::wave() * (Shape::WM * Shape::WN * 2u), wm, wn, A);
+    }
 }
-constexpr uint32_t kThinM = 32, kThinN = 64, kThinWaves = 8;
-template <bool kForward, bool kF32>
-__global__ __launch_bounds__(kThinWaves * 64) void k_logits_thin(LossArgs A) {
-    __shared__ float sh[kThinWaves][32][64];
-    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t tiles_n = (A.N + kThinN - 1) / kThinN, id = xcd_contiguous(blockIdx.x, gridDim.x);
-    const uint32_t m0 = id / tiles_n * kThinM, n0 = id % tiles_n * kThinN;
-    const __amdgpu_buffer_rsrc_t rw = rows_buffer(A.w, m0, kThinM), rx = rows_buffer(A.x, n0, kThinN);
-    const uint32_t kl = (lane >> 5) * 32u, offW = ((lane & 31u) * A.w.ld + kl) * 2u, offX = ((lane & 31u) * A.x.ld + kl) * 2u;
-    const uint32_t second = 32u * A.x.ld * 2u;
-    struct Step { i4v w[4], x[2][4]; };
-    auto request = [&](uint32_t k) -> Step {
+
+// Few rows, or few classes: a workgroup of 16 waves owns kT x kT tiles of 16 classes by 16 columns and its waves share k, in steps of
+// 128 bytes of a row, with both operands straight from memory into registers, 8 / kT^2 rounded up to a pair of steps ahead.  A load takes
+// 64 consecutive bytes of 16 rows, four lanes a row, which is how the 16 x 16 instructions want them (with 32 rows a load, 32 bytes
+// of each, the address units are what it waits for: 19 us instead of 7 for 64 rows, 1000 classes, 4096 k); which k an instruction's place
+// stands for is free as long as both operands agree.  The waves' sums meet in LDS, where a thread takes one result.  float32 rows
+// are multiplied as floats.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t bounded(const void* base, uint64_t offset, uint32_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(base) + offset), 0, (int)bytes, 0x00020000);
+}
+constexpr uint32_t kThinWaves = 16;
+struct ThinArgs { const void *w, *x; uint32_t ldw, ldx; };   // rows in their own type; element pitches
+template <typename T, int kT, bool kForward>
+__global__ __launch_bounds__(kThinWaves * 64) void k_logits_thin(ThinArgs R, LossArgs A) {
+    constexpr uint32_t kN = 16 * kT, kPitch = kN + 4;        // (rows of four lane groups start 16 banks apart)
+    constexpr uint32_t kE = 16 / sizeof(T), kStep = 128 / sizeof(T), kTurn = kThinWaves * kStep;      // elements a load; k a step; of all waves
+    constexpr int kAhead = kT == 1 ? 4 : 2;
+    __shared__ float sh[kThinWaves][kN][kPitch];
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint32_t columns = kForward ? A.N : A.Lq, tiles_n = (columns + kN - 1) / kN, id = xcd_contiguous(blockIdx.x, gridDim.x);
+    const uint32_t m0 = id / tiles_n * kN, n0 = id % tiles_n * kN;
+    const uint32_t z0 = n0 / A.at.Pp, first = min(z0 * A.at.P + min(n0 - z0 * A.at.Pp, A.at.P), A.N);
+    const __amdgpu_buffer_rsrc_t rw = bounded(R.w, (uint64_t)m0 * R.ldw * sizeof(T), min(A.V - m0, kN) * R.ldw * (uint32_t)sizeof(T));
+    const __amdgpu_buffer_rsrc_t rx = bounded(R.x, (uint64_t)first * R.ldx * sizeof(T), min(A.N - first, kN) * R.ldx * (uint32_t)sizeof(T));
+    const uint32_t kl = (lane >> 4) * kE;
+    uint32_t offW[kT], offX[kT], none[kT];
+#pragma unroll
+    for (int t = 0; t < kT; ++t) {
+        const uint32_t row = A.at.row(n0 + t * 16u + (lane & 15u));
+        none[t] = row == 0xFFFFFFFFu ? row : 0u;
+        offW[t] = ((t * 16u + (lane & 15u)) * R.ldw + kl) * (uint32_t)sizeof(T);
+        offX[t] = ((row - first) * R.ldx + kl) * (uint32_t)sizeof(T);
+    }
+    struct Step { i4v w[kT][2], x[kT][2]; };
+    auto request = [&](uint32_t k) -> Step {                 // (past the end: zeros)
         Step S;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t outside = k + kl + j * 8u < A.K ? 0u : 0xFFFFFFFFu, add = (k + j * 8u) * 2u;
-            S.w[j] = __builtin_bit_cast(i4v, __builtin_amdgcn_raw_buffer_load_b128(rw, (int)((offW + add) | outside), 0, 0));
-            S.x[0][j] = __builtin_bit_cast(i4v, __builtin_amdgcn_raw_buffer_load_b128(rx, (int)((offX + add) | outside), 0, 0));
-            S.x[1][j] = __builtin_bit_cast(i4v, __builtin_amdgcn_raw_buffer_load_b128(rx, (int)((offX + second + add) | outside), 0, 0));
+        for (int j = 0; j < 2; ++j) {
+            const uint32_t outside = k + kl + j * 4u * kE < A.K ? 0u : 0xFFFFFFFFu, add = (k + j * 4u * kE) * (uint32_t)sizeof(T);
+#pragma unroll
+            for (int t = 0; t < kT; ++t) {
+                S.w[t][j] = __builtin_bit_cast(i4v, __builtin_amdgcn_raw_buffer_load_b128(rw, (int)((offW[t] + add) | outside), 0, 0));
+                S.x[t][j] = __builtin_bit_cast(i4v, __builtin_amdgcn_raw_buffer_load_b128(rx, (int)((offX[t] + add) | outside | none[t]), 0, 0));
+            }
         }
         return S;
     };
-    f16v sum[2] = {};
-    Step S = request(wave * kStepK);
-    for (uint32_t k = wave * kStepK; k < A.K; k += kThinWaves * kStepK) {
-        const Step next = request(k + kThinWaves * kStepK);  // (past the end: zeros, not used)
+    f4v sum[kT][kT] = {};
+    auto multiply = [&](const Step& S, uint32_t k) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < 2; ++j) {
+            if constexpr (sizeof(T) == 2) {
 #pragma unroll
-            for (int n = 0; n < 2; ++n)
-                sum[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8v, S.w[j]), __builtin_bit_cast(bf8v, S.x[n][j]), sum[n], 0, 0, 0);
-        S = next;
-    }
+                for (int m = 0; m < kT; ++m)
 #pragma unroll
-    for (int n = 0; n < 2; ++n)
+                    for (int n = 0; n < kT; ++n)
+                        sum[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8v, S.w[m][j]), __builtin_bit_cast(bf8v, S.x[n][j]), sum[m][n], 0, 0, 0);
+            } else {
+                f4v w[kT], x[kT];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sh[wave][n * 16 + i][lane] = sum[n][i];
+                for (int t = 0; t < kT; ++t) { w[t] = __builtin_bit_cast(f4v, S.w[t][j]); x[t] = __builtin_bit_cast(f4v, S.x[t][j]); }
+                if (k + kStep > A.K) {                       // a load that reaches past the rows' end has brought the next row's begin
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (k + kl + j * 4u * kE + e >= A.K)
+#pragma unroll
+                            for (int t = 0; t < kT; ++t) w[t][e] = x[t][e] = 0.f;
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int m = 0; m < kT; ++m)
+#pragma unroll
+                        for (int n = 0; n < kT; ++n) sum[m][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[m][e], x[n][e], sum[m][n], 0, 0, 0);
+            }
+        }
+    };
+    Step S[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) S[i] = request(wave * kStep + i * kTurn);
+    for (uint32_t k = wave * kStep; k < A.K; k += kAhead * kTurn)
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (k + i * kTurn >= A.K) break;
+            multiply(S[i], k + i * kTurn);
+            S[i] = request(k + (kAhead + i) * kTurn);
+        }
+    // result i of a lane: class 4 (lane / 16) + i, column lane % 16
+#pragma unroll
+    for (int m = 0; m < kT; ++m)
+#pragma unroll
+        for (int n = 0; n < kT; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sh[wave][m * 16 + (lane >> 4) * 4 + i][n * 16 + (lane & 15u)] = sum[m][n][i];
     __syncthreads();
-    if (wave >= 2u) return;
-    f16v acc[1][1] = {};
-    for (uint32_t q = 0; q < kThinWaves; ++q)
+    const uint32_t v = tid % kN, col = tid / kN;             // a thread's result: consecutive classes
+    float z = 0.f;
+    if (tid < kN * kN) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) acc[0][0][i] += sh[q][wave * 16u + i][lane];
-    if (kForward) finish_forward(acc, m0, n0 + wave * 32u, A);
-    else finish_backward<kF32>(acc, m0, n0 + wave * 32u, A);
+        for (uint32_t w = 0; w < kThinWaves; ++w) z += sh[w][v][col];
+    }
+    if constexpr (kForward) {
+        __syncthreads();
+        if (tid < kN * kN) sh[0][v][col] = z;
+        __syncthreads();
+        const uint32_t token = n0 + tid;
+        if (tid >= kN || token >= A.N) return;
+        const float kNone = -__builtin_inff();
+        const uint32_t classes = min(kN, A.V - m0);
+        const int64_t t = A.target[token] - A.v0 - m0;
+        float top = kNone, total = 0.f;
+        for (uint32_t c = 0; c < classes; ++c) top = fmaxf(top, sh[0][c][tid]);
+        const float base = top == kNone ? 0.f : top;
+        for (uint32_t c = 0; c < classes; ++c) total += exp_of(sh[0][c][tid] - base);
+        A.partial[(size_t)(A.block0 + m0 / kN) * A.N + token] = make_float2(top, total);
+        if (t >= 0 && t < (int64_t)classes) A.picked[token] = sh[0][t][tid];
+    } else {
+        if (tid >= kN * kN || m0 + v >= A.V || n0 + col >= A.Lq) return;
+        const ColumnOf C = column_of(n0 + col, A);
+        const float d = C.d(z, m0 + v);
+        if (A.d32 && C.row != 0xFFFFFFFFu) A.d32[(size_t)C.row * A.V + m0 + v] = d;
+        if (A.dt)
+            for (uint32_t q = 0; q < A.planes; ++q)
+                A.dt[q * A.plane + (size_t)(m0 + v) * A.Lq + n0 + col] = (uint16_t)plane_of<sizeof(T) == 4>(d, 0.f, q);
+    }
 }
 
 // Joins the pairs of a token over the blocks of the vocabulary in a fixed order: 16 waves take every 16th block of 64 tokens.
@@ -362,34 +448,34 @@ __global__ __launch_bounds__(1024) void k_loss_join(const float2* __restrict__ p
 }
 
 // ---- dX -----------------------------------------------------------------------------------------------------------------------
-// Part `split` of the sum over the piece's k, added to what the pieces before have left in the part's own plane.
-template <typename Tile>
-__global__ __launch_bounds__(Tile::NW * 64, 2) void k_loss_dx(Rows D, Rows Wt, uint32_t K, uint32_t splits, int add, float* __restrict__ planes) {
-    __shared__ __attribute__((aligned(1024))) uint8_t sh[Tile::kLds];
-    const uint32_t N = D.rows, H = Wt.rows, tiles_n = (H + Tile::BN - 1) / Tile::BN, tiles_m = (N + Tile::BM - 1) / Tile::BM;
+// Part `split` of the sum over the piece's classes, added to what the pieces before have left in the part's own plane [N, H].
+template <typename Shape>
+__global__ __launch_bounds__(Shape::NW * 64, 2) void k_loss_dx(Matrix Dt, Matrix W, Positions at, uint32_t H, uint32_t splits, int add,
+                                                               float* __restrict__ planes) {
+    __shared__ __attribute__((aligned(1024))) uint8_t sh[Shape::kLds];
+    const uint32_t N = at.B * at.P, tiles_n = (H + Shape::BN - 1) / Shape::BN, tiles_m = (at.B * at.Pp + Shape::BM - 1) / Shape::BM;
     const uint32_t id = xcd_contiguous(blockIdx.x, gridDim.x), split = id / (tiles_n * tiles_m), tile = id - split * tiles_n * tiles_m;
-    const uint32_t m0 = tile / tiles_n * Tile::BM, n0 = tile % tiles_n * Tile::BN;
-    const uint32_t steps = (K + kStepK - 1) / kStepK;
-    const uint32_t k0 = (uint32_t)((uint64_t)split * steps / splits) * kStepK, k1 = min((uint32_t)((uint64_t)(split + 1u) * steps / splits) * kStepK, K);
-    f16v acc[Tile::MT][Tile::NT] = {};
-    Tile::template run<false>(acc, sh, D, Wt, m0, n0, k0, k1, [](uint32_t) {});
-    const uint32_t lane = threadIdx.x & 63u, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t wm = m0 + wave / (Tile::BN / Tile::WN) * Tile::WM, wn = n0 + wave % (Tile::BN / Tile::WN) * Tile::WN;
+    const uint32_t m0 = tile / tiles_n * Shape::BM, n0 = tile % tiles_n * Shape::BN, steps = (Dt.rows + Shape::BK - 1) / Shape::BK;
+    const uint32_t k0 = (uint32_t)((uint64_t)split * steps / splits) * Shape::BK;
+    const uint32_t k1 = min((uint32_t)((uint64_t)(split + 1u) * steps / splits) * Shape::BK, Dt.rows);
+    f16v acc[Shape::MT][Shape::NT] = {};
+    ColumnTile<Shape>::run(acc, sh, Dt, W, m0, n0, k0, k1);
+    const uint32_t lane = threadIdx.x & 63u, half = lane >> 5, wm = m0 + Shape::wave_m(), wn = n0 + Shape::wave_n();
     float* out = planes + (size_t)split * N * H;
 #pragma unroll
-    for (int n = 0; n < Tile::NT; ++n) {
-        const uint32_t h = wn + n * 32u + (lane & 31u);
-        if (h >= H) continue;
+    for (int m = 0; m < Shape::MT; ++m)
 #pragma unroll
-        for (int m = 0; m < Tile::MT; ++m)
+        for (int i = 0; i < 16; ++i) {
+            const uint32_t row = at.row(wm + class_of(m, i, half));
+            if (row == 0xFFFFFFFFu) continue;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const uint32_t token = wm + m * 32u + 8u * (i >> 2) + 4u * half + (i & 3);
-                if (token >= N) continue;
-                float* at = out + (size_t)token * H + h;
-                *at = acc[m][n][i] + (add ? *at : 0.f);
+            for (int n = 0; n < Shape::NT; ++n) {
+                const uint32_t h = wn + n * 32u + (lane & 31u);
+                if (h >= H) continue;
+                float* to = out + (size_t)row * H + h;
+                *to = acc[m][n][i] + (add ? *to : 0.f);
             }
-    }
+        }
 }
 
 template <typename T>
@@ -407,26 +493,62 @@ __global__ __launch_bounds__(256) void k_loss_dx_join(const float* __restrict__ 
     store8(dX + i, f, m);
 }
 
+// Few rows and few classes: 16 waves share the classes for 32 rows by 32 columns of dX, D and W multiplied as floats.  A wave takes 8
+// classes at a time, four a half.
+constexpr uint32_t kThinDx = 32;
+template <typename T>
+__global__ __launch_bounds__(kThinWaves * 64) void k_loss_dx_thin(const float* __restrict__ D, const T* __restrict__ W, uint32_t N, uint32_t V, uint32_t H,
+                                                                  T* __restrict__ dX) {
+    __shared__ float sh[kThinWaves][16][64];
+    const uint32_t lane = threadIdx.x & 63u, half = lane >> 5, wave = threadIdx.x >> 6;
+    const uint32_t tiles_n = (N + kThinDx - 1) / kThinDx, n0 = blockIdx.x % tiles_n * kThinDx, h = blockIdx.x / tiles_n * kThinDx + (lane & 31u);
+    const uint32_t n = n0 + (lane & 31u);
+    f16v sum = {};
+    for (uint32_t v0 = wave * 8u; v0 < V; v0 += kThinWaves * 8u) {
+        float d[4], w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t v = v0 + half * 4u + e;
+            d[e] = v < V && n < N ? D[(size_t)n * V + v] : 0.f;
+            w[e] = 0.f;
+            if (v < V && h < H) {
+                if (sizeof(T) == 4) w[e] = ((const float*)W)[(size_t)v * H + h];
+                else w[e] = __uint_as_float((uint32_t)((const uint16_t*)W)[(size_t)v * H + h] << 16);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum = __builtin_amdgcn_mfma_f32_32x32x2f32(d[e], w[e], sum, 0, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sh[wave][i][lane] = sum[i];
+    __syncthreads();
+    float r = 0.f;                                           // (16 waves and 16 results: a wave adds one of them)
+#pragma unroll
+    for (uint32_t w = 0; w < kThinWaves; ++w) r += sh[w][wave][lane];
+    const uint32_t row = n0 + class_of(0, wave, half);
+    if (row >= N || h >= H) return;
+    if (sizeof(T) == 4) ((float*)dX)[(size_t)row * H + h] = r;
+    else ((uint16_t*)dX)[(size_t)row * H + h] = (uint16_t)two_bf16(r, 0.f);
+}
+
 // ---- g and s ------------------------------------------------------------------------------------------------------------------
-// k runs over the samples, `seg` of it each; at a sample's end its product is squared into s, added into g, and cleared.
-typedef GemmTile<128, 128, 64, 64> TileSums;
-template <bool kFine>
-__global__ __launch_bounds__(TileSums::NW * 64, 2) void k_loss_sums(Rows Dt, Rows Xt, uint32_t K, uint32_t seg, float c, float* __restrict__ g_out,
-                                                                    float* __restrict__ s_out) {
-    typedef TileSums Tile;
-    __shared__ __attribute__((aligned(1024))) uint8_t sh[Tile::kLds];
-    const uint32_t V = Dt.rows, H = Xt.rows, tiles_n = (H + Tile::BN - 1) / Tile::BN;
-    const uint32_t id = xcd_contiguous(blockIdx.x, gridDim.x), m0 = id / tiles_n * Tile::BM, n0 = id % tiles_n * Tile::BN;
-    f16v acc[Tile::MT][Tile::NT] = {}, g[Tile::MT][Tile::NT] = {}, s[Tile::MT][Tile::NT] = {};
-    uint32_t left = seg;
-    Tile::template run<kFine>(acc, sh, Dt, Xt, m0, n0, 0u, K, [&](uint32_t) {
-        left -= kFine ? 16u : kStepK;
+// k runs over the positions; at a sample's end (every Pp of them) its product is squared into s, added into g, and cleared.
+template <typename Shape>
+__global__ __launch_bounds__(Shape::NW * 64, 2) void k_loss_sums(Matrix Dt, Matrix Xt, uint32_t K, uint32_t Pp, float c, float* __restrict__ g_out,
+                                                                 float* __restrict__ s_out) {
+    __shared__ __attribute__((aligned(1024))) uint8_t sh[Shape::kLds];
+    const uint32_t V = Dt.rows, H = Xt.rows, tiles_n = (H + Shape::BN - 1) / Shape::BN;
+    const uint32_t id = xcd_contiguous(blockIdx.x, gridDim.x), m0 = id / tiles_n * Shape::BM, n0 = id % tiles_n * Shape::BN;
+    f16v acc[Shape::MT][Shape::NT] = {}, g[Shape::MT][Shape::NT] = {}, s[Shape::MT][Shape::NT] = {};
+    uint32_t left = Pp;
+    RowTile<Shape>::run(acc, sh, Dt, Xt, m0, n0, Shape::BN, [&](uint32_t n) { return n0 + n < H ? n : 0xFFFFFFFFu; }, K, [&](uint32_t, int) {
+        left -= 16u;
         if (left != 0u) return;
-        left = seg;
+        left = Pp;
 #pragma unroll
-        for (int m = 0; m < Tile::MT; ++m)
+        for (int m = 0; m < Shape::MT; ++m)
 #pragma unroll
-            for (int n = 0; n < Tile::NT; ++n)
+            for (int n = 0; n < Shape::NT; ++n)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const float x = acc[m][n][i];
@@ -435,17 +557,16 @@ __global__ __launch_bounds__(TileSums::NW * 64, 2) void k_loss_sums(Rows Dt, Row
                     acc[m][n][i] = 0.f;
                 }
     });
-    const uint32_t lane = threadIdx.x & 63u, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t wm = m0 + wave / (Tile::BN / Tile::WN) * Tile::WM, wn = n0 + wave % (Tile::BN / Tile::WN) * Tile::WN;
+    const uint32_t lane = threadIdx.x & 63u, half = lane >> 5, wm = m0 + Shape::wave_m(), wn = n0 + Shape::wave_n();
 #pragma unroll
-    for (int n = 0; n < Tile::NT; ++n) {
+    for (int n = 0; n < Shape::NT; ++n) {
         const uint32_t h = wn + n * 32u + (lane & 31u);
         if (h >= H) continue;
 #pragma unroll
-        for (int m = 0; m < Tile::MT; ++m)
+        for (int m = 0; m < Shape::MT; ++m)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const uint32_t v = wm + m * 32u + 8u * (i >> 2) + 4u * half + (i & 3);
+                const uint32_t v = wm + class_of(m, i, half);
                 if (v >= V) continue;
                 if (g_out) g_out[(size_t)v * H + h] = c * g[m][n][i];
                 s_out[(size_t)v * H + h] = c * c * s[m][n][i];
@@ -454,51 +575,57 @@ __global__ __launch_bounds__(TileSums::NW * 64, 2) void k_loss_sums(Rows Dt, Row
 }
 
 // ---- launches -----------------------------------------------------------------------------------------------------------------
-typedef GemmTile<256, 256, 128, 64> TileLarge;
-typedef GemmTile<128, 128, 64, 64> TileSmall;
-enum class LogitsTile { kLarge, kSmall, kThin };
+//               BM   BN   WM  WN BK S PA PB
+typedef TileShape<256, 256, 128, 64, 64, 2, 1, 1> Large;     // bfloat16: the logits and dX
+typedef TileShape<128, 128, 64, 64, 64, 2, 1, 1> Small;
+typedef TileShape<128, 64, 64, 32, 64, 3, 1, 1> Slim;        // few rows over many classes: W streams through
+typedef TileShape<256, 128, 64, 64, 32, 2, 3, 3> Cut;        // float32: all three products
+typedef TileShape<128, 256, 64, 64, 64, 2, 2, 1> Sums;       // bfloat16: g and s
 
 static uint32_t up8(uint32_t x) { return (x + 7u) / 8u * 8u; }
 static uint32_t tiles(uint32_t a, uint32_t ta, uint32_t b, uint32_t tb) { return (a + ta - 1) / ta * ((b + tb - 1) / tb); }
+template <typename Shape> static uint32_t tiles(uint32_t m, uint32_t n) { return tiles(m, Shape::BM, n, Shape::BN); }
 
-static LogitsTile logits_tile(uint32_t V, uint32_t N) {
-    if (N > 128u && tiles(V, 256, N, 256) >= 192u) return LogitsTile::kLarge;
-    if (N > 64u && tiles(V, 128, N, 128) >= 192u) return LogitsTile::kSmall;
-    return LogitsTile::kThin;
+enum class LogitsTile { kLarge, kSmall, kSlim, kCut, kThin, kThinnest };
+static LogitsTile logits_tile(int dtype, uint32_t V, uint32_t N) {
+    if (dtype == VGC_F32 && N > 64u && tiles<Cut>(V, N) >= 128u) return LogitsTile::kCut;
+    if (dtype == VGC_BF16) {
+        if (N > 128u && tiles<Large>(V, N) >= 192u) return LogitsTile::kLarge;
+        if (N > 64u && tiles<Small>(V, N) >= 192u) return LogitsTile::kSmall;
+        if (tiles<Slim>(V, N) >= 128u) return LogitsTile::kSlim;
+    }
+    return tiles(V, 32, N, 32) >= 256u ? LogitsTile::kThin : LogitsTile::kThinnest;
 }
-static uint32_t logits_block(LogitsTile t) { return t == LogitsTile::kLarge ? 128u : t == LogitsTile::kSmall ? 64u : 32u; }
+static bool is_thin(LogitsTile t) { return t == LogitsTile::kThin || t == LogitsTile::kThinnest; }
+// Classes a partial pair of the forward pass covers: those of a wave, in the thin kernels of a workgroup.
+static uint32_t logits_block(LogitsTile t) {
+    return t == LogitsTile::kLarge ? 128u : t == LogitsTile::kThin ? 32u : t == LogitsTile::kThinnest ? 16u : 64u;
+}
 
-template <bool kForward, bool kF32>
-static int launch_logits(LogitsTile t, const LossArgs& A, hipStream_t stream) {
-    if (t == LogitsTile::kLarge)
-        hipLaunchKernelGGL((k_logits<TileLarge, kForward, kF32>), dim3(tiles(A.V, 256, A.N, 256)), dim3(512), 0, stream, A);
-    else if (t == LogitsTile::kSmall)
-        hipLaunchKernelGGL((k_logits<TileSmall, kForward, kF32>), dim3(tiles(A.V, 128, A.N, 128)), dim3(256), 0, stream, A);
-    else
-        hipLaunchKernelGGL((k_logits_thin<kForward, kF32>), dim3(tiles(A.V, kThinM, A.N, kThinN)), dim3(512), 0, stream, A);
+template <bool kForward>
+static int launch_logits(LogitsTile t, int dtype, const ThinArgs& R, const LossArgs& A, hipStream_t stream) {
+    const uint32_t n = kForward ? A.N : A.Lq;
+#define VGC_LAUNCH(S) hipLaunchKernelGGL((k_logits<S, kForward>), dim3(tiles<S>(A.V, n)), dim3(S::NW * 64), 0, stream, A)
+#define VGC_THIN(T, kT) hipLaunchKernelGGL((k_logits_thin<T, kT, kForward>), dim3(tiles(A.V, 16 * kT, n, 16 * kT)), dim3(kThinWaves * 64), 0, stream, R, A)
+    switch (t) {
+        case LogitsTile::kLarge: VGC_LAUNCH(Large); break;
+        case LogitsTile::kSmall: VGC_LAUNCH(Small); break;
+        case LogitsTile::kSlim: VGC_LAUNCH(Slim); break;
+        case LogitsTile::kCut: VGC_LAUNCH(Cut); break;
+        case LogitsTile::kThin: if (dtype == VGC_F32) VGC_THIN(float, 2); else VGC_THIN(uint16_t, 2); break;
+        case LogitsTile::kThinnest: if (dtype == VGC_F32) VGC_THIN(float, 1); else VGC_THIN(uint16_t, 1); break;
+    }
+#undef VGC_THIN
+#undef VGC_LAUNCH
     return hip_check(hipGetLastError(), "launch k_logits");
 }
 
-// An operand's rows are used where they lie if they are bfloat16 and whole pieces of 16 bytes.
-static bool rows_in_place(int dtype, uint32_t H) { return dtype == VGC_BF16 && H % 8u == 0; }
-static uint32_t row_slots(int dtype) { return dtype == VGC_F32 ? kSlotsF32 : 1u; }
-
-static int launch_rows(int dtype, bool second, const void* src, uint32_t R, uint32_t K, uint16_t* dst, hipStream_t stream) {
+static int launch_rows(int dtype, const void* src, uint32_t R, uint32_t K, uint16_t* dst, hipStream_t stream) {
     const uint32_t Kp = up8(K);
     const dim3 grid((uint32_t)(((uint64_t)R * (Kp / 8u) + 255u) / 256u));
-    if (dtype == VGC_BF16) hipLaunchKernelGGL((k_slots_rows<uint16_t, false>), grid, dim3(256), 0, stream, (const uint16_t*)src, R, K, Kp, dst);
-    else if (second) hipLaunchKernelGGL((k_slots_rows<float, true>), grid, dim3(256), 0, stream, (const float*)src, R, K, Kp, dst);
-    else hipLaunchKernelGGL((k_slots_rows<float, false>), grid, dim3(256), 0, stream, (const float*)src, R, K, Kp, dst);
-    return hip_check(hipGetLastError(), "launch k_slots_rows");
-}
-static int launch_columns(int dtype, const void* src, const int64_t* target, uint32_t B, uint32_t P, uint32_t Pp, uint32_t K, uint32_t slots,
-                          uint16_t* dst, hipStream_t stream) {
-    const dim3 grid((uint32_t)(((uint64_t)B * Pp + 63u) / 64u), (K + 63u) / 64u);
-    if (dtype == VGC_BF16)
-        hipLaunchKernelGGL(k_slots_columns<uint16_t>, grid, dim3(256), 0, stream, (const uint16_t*)src, target, B, P, Pp, K, slots, B * slots * Pp, dst);
-    else
-        hipLaunchKernelGGL(k_slots_columns<float>, grid, dim3(256), 0, stream, (const float*)src, target, B, P, Pp, K, slots, B * slots * Pp, dst);
-    return hip_check(hipGetLastError(), "launch k_slots_columns");
+    if (dtype == VGC_BF16) hipLaunchKernelGGL(k_planes_rows<uint16_t>, grid, dim3(256), 0, stream, (const uint16_t*)src, R, K, Kp, dst);
+    else hipLaunchKernelGGL(k_planes_rows<float>, grid, dim3(256), 0, stream, (const float*)src, R, K, Kp, dst);
+    return hip_check(hipGetLastError(), "launch k_planes_rows");
 }
 
 // The vocabulary in pieces of equal size, multiples of 256 classes, `bytes` of working memory a class.
@@ -506,28 +633,42 @@ static uint32_t piece_of(uint32_t V, uint64_t bytes, uint64_t budget) {
     uint64_t most = budget / std::max<uint64_t>(bytes, 1) / 256u * 256u;
     most = std::min<uint64_t>(std::max<uint64_t>(most, 256u), 1u << 20);
     const uint32_t pieces = (uint32_t)((V + most - 1) / most);
-    return ((V + pieces - 1) / pieces + 255u) / 256u * 256u;
+    return std::min(((V + pieces - 1) / pieces + 255u) / 256u * 256u, V);
 }
 
-struct ForwardPlan { LogitsTile tile; uint32_t Kp, slots, piece, blocks; bool in_place; size_t x, w, partial, picked, total; };
+// What both passes do with their rows: used where they lie if they are bfloat16 and whole pieces of 16 bytes, or floats of the thin
+// kernels; else laid out as planes.
+struct RowsPlan { uint32_t planes, Kp; bool in_place; };
+static RowsPlan rows_plan(int dtype, uint32_t H, LogitsTile t, bool dx_by_tiles) {
+    RowsPlan r;
+    r.planes = dtype == VGC_F32 ? 3u : 1u;
+    r.Kp = up8(H);
+    r.in_place = dtype == VGC_BF16 ? H % 8u == 0 : is_thin(t) && !dx_by_tiles;
+    return r;
+}
+
+struct ForwardPlan { LogitsTile tile; RowsPlan rows; uint32_t piece, blocks; size_t x, w, partial, picked, total; };
 static ForwardPlan forward_plan(int dtype, uint32_t N, uint32_t H, uint32_t V) {
     ForwardPlan L;
-    L.in_place = rows_in_place(dtype, H);
-    L.slots = row_slots(dtype);
-    L.Kp = up8(H);
-    const uint64_t row = 2ull * L.slots * L.Kp;
-    L.piece = L.in_place ? V : std::min(piece_of(V, row, 256ull << 20), V);
-    L.tile = logits_tile(L.piece, N);
+    L.tile = logits_tile(dtype, V, N);
+    L.rows = rows_plan(dtype, H, L.tile, false);
+    const uint64_t row = 2ull * L.rows.planes * L.rows.Kp;
+    L.piece = L.rows.in_place ? V : piece_of(V, row, 256ull << 20);
     L.blocks = (V + logits_block(L.tile) - 1) / logits_block(L.tile);
     size_t off = 0;
-    L.x = off; if (!L.in_place) off = align_up(off + N * row, 256);
-    L.w = off; if (!L.in_place) off = align_up(off + L.piece * row, 256);
+    L.x = off; if (!L.rows.in_place) off = align_up(off + N * row, 256);
+    L.w = off; if (!L.rows.in_place) off = align_up(off + L.piece * row, 256);
     L.partial = off; off = align_up(off + (size_t)L.blocks * N * sizeof(float2), 256);
     L.picked = off; off += (size_t)N * sizeof(float);
     L.total = off;
     return L;
 }
 size_t softmax_loss_workspace_bytes(int dtype, uint32_t N, uint32_t H, uint32_t V) { return forward_plan(dtype, N, H, V).total; }
+
+// The rows of an operand as both kinds of kernels take them.
+static Matrix matrix_of(const RowsPlan& r, const void* src, const uint16_t* planes, uint32_t rows, uint32_t H) {
+    return r.in_place ? Matrix{static_cast<const uint16_t*>(src), rows, H, 0} : Matrix{planes, rows, r.Kp, (uint64_t)rows * r.Kp};
+}
 
 int launch_softmax_loss(int dtype, const void* X, const void* W, const int64_t* target, uint32_t N, uint32_t H, uint32_t V, float* loss, float* lse,
                         void* workspace, hipStream_t stream) {
@@ -536,21 +677,23 @@ int launch_softmax_loss(int dtype, const void* X, const void* W, const int64_t* 
     const size_t size = dtype == VGC_F32 ? 4 : 2;
     int rc;
     LossArgs A = {};
-    A.N = N; A.K = L.slots * L.Kp;
+    A.N = A.Lq = N;
+    A.K = L.rows.in_place ? H : L.rows.Kp;
+    A.at = Positions{N, 1, 1};
     A.target = target;
     A.partial = reinterpret_cast<float2*>(ws + L.partial);
     A.picked = reinterpret_cast<float*>(ws + L.picked);
-    uint16_t *xs = reinterpret_cast<uint16_t*>(ws + L.x), *wsl = reinterpret_cast<uint16_t*>(ws + L.w);
-    if (!L.in_place && (rc = launch_rows(dtype, true, X, N, H, xs, stream)) != VGC_OK) return rc;
-    A.x = Rows{L.in_place ? (const uint16_t*)X : xs, N, A.K};
+    uint16_t *xs = reinterpret_cast<uint16_t*>(ws + L.x), *wp = reinterpret_cast<uint16_t*>(ws + L.w);
+    if (!L.rows.in_place && (rc = launch_rows(dtype, X, N, H, xs, stream)) != VGC_OK) return rc;
+    A.x = matrix_of(L.rows, X, xs, N, H);
     for (uint32_t v0 = 0; v0 < V; v0 += L.piece) {
         A.v0 = v0;
         A.V = std::min(L.piece, V - v0);
         const char* rows = static_cast<const char*>(W) + (size_t)v0 * H * size;
-        if (!L.in_place && (rc = launch_rows(dtype, false, rows, A.V, H, wsl, stream)) != VGC_OK) return rc;
-        A.w = Rows{L.in_place ? (const uint16_t*)rows : wsl, A.V, A.K};
+        if (!L.rows.in_place && (rc = launch_rows(dtype, rows, A.V, H, wp, stream)) != VGC_OK) return rc;
+        A.w = matrix_of(L.rows, rows, wp, A.V, H);
         A.block0 = v0 / logits_block(L.tile);
-        if ((rc = launch_logits<true, false>(L.tile, A, stream)) != VGC_OK) return rc;
+        if ((rc = launch_logits<true>(L.tile, dtype, ThinArgs{A.w.base, A.x.base, A.w.ld, A.x.ld}, A, stream)) != VGC_OK) return rc;
     }
     hipLaunchKernelGGL(k_loss_join, dim3((N + 63) / 64), dim3(1024), 0, stream, A.partial, A.picked, target, L.blocks, N, (int64_t)V, loss, lse);
     return hip_check(hipGetLastError(), "launch k_loss_join");
@@ -558,36 +701,37 @@ int launch_softmax_loss(int dtype, const void* X, const void* W, const int64_t* 
 
 struct BackwardPlan {
     LogitsTile tile;
-    uint32_t Kp, slots, slots_t, piece, Vp, Pp, splits;
-    bool in_place, dx_large;
-    size_t x, xt, w, wt, d, dt, planes, total;
+    RowsPlan rows;
+    uint32_t planes, piece, Pp, Lq, splits;
+    bool dx_thin, dx_large, sum_planes;
+    size_t x, xt, w, d, d32, d2, out, total;
 };
 static BackwardPlan backward_plan(int dtype, uint32_t B, uint32_t P, uint32_t H, uint32_t V) {
     BackwardPlan L;
     const uint32_t N = B * P;
-    L.in_place = rows_in_place(dtype, H);
-    L.slots = row_slots(dtype);
-    L.slots_t = dtype == VGC_F32 ? kSlotsF32 : 2u;
-    L.Kp = up8(H);
-    // a sample's end falls on a whole step of 64 k (bfloat16: two slots of 32 positions), or, for short samples, of 16
-    L.Pp = P == 1 ? 1u : P <= 24u ? up8(P) : (P + 31u) / 32u * 32u;
-    const uint64_t row = 2ull * L.slots * L.Kp;
-    const uint64_t per_class = (L.in_place ? 0 : row) + row + 2ull * L.slots * N + (P == 1 ? 4ull * N : 2ull * L.slots_t * B * L.Pp);
-    L.piece = std::min(piece_of(V, per_class, 512ull << 20), V);
-    L.Vp = up8(L.piece);
-    L.tile = logits_tile(L.piece, N);
-    L.dx_large = tiles(N, 256, H, 256) >= 256u;
-    const uint32_t k = L.slots * L.Vp, n = L.dx_large ? tiles(N, 256, H, 256) : tiles(N, 128, H, 128);
+    L.Pp = P == 1 ? 1u : (P + 15u) / 16u * 16u;              // (a sample's end falls on a phase's)
+    L.Lq = up8(B * L.Pp);
+    L.tile = logits_tile(dtype, V, L.Lq);
+    L.dx_thin = P == 1 && N <= 128u && (uint64_t)V * H <= (4u << 20);
+    L.rows = rows_plan(dtype, H, L.tile, !L.dx_thin);
+    L.planes = dtype == VGC_F32 ? 3u : P == 1 ? 1u : 2u;
+    // samples of one position: the FC form, from planes where the outputs are what it takes, else (a launch less) from floats
+    L.sum_planes = P == 1 && dtype == VGC_BF16 && N >= 16u && (uint64_t)V * H >= (4u << 20) && fc_planes_supported(N, 256, H);
+    const uint64_t row = 2ull * L.rows.planes * L.rows.Kp, dt = L.dx_thin ? 0 : 2ull * L.planes * L.Lq;
+    const uint64_t d32 = P == 1 ? (L.sum_planes ? 12ull : 4ull) * N : 0;
+    L.piece = L.dx_thin ? V : piece_of(V, row + dt + d32, 2048ull << 20);
+    L.dx_large = dtype == VGC_BF16 && L.Lq > 128u && tiles<Large>(L.Lq, H) >= 32u;
+    const uint32_t n = dtype == VGC_F32 ? tiles<Cut>(L.Lq, H) : L.dx_large ? tiles<Large>(L.Lq, H) : tiles<Small>(L.Lq, H);
     L.splits = 1;
-    while (n * L.splits < (L.dx_large ? 256u : 512u) && k / (L.splits * 2u) >= 256u && L.splits < 64u) L.splits *= 2u;
+    while (n * L.splits < (dtype == VGC_F32 || L.dx_large ? 256u : 512u) && L.piece / (L.splits * 2u) >= 256u && L.splits < 64u) L.splits *= 2u;
     size_t off = 0;
-    L.x = off; if (!L.in_place) off = align_up(off + N * row, 256);
-    L.xt = off; off = align_up(off + (P == 1 ? (size_t)N * H * 4 : 2 * (size_t)H * L.slots_t * B * L.Pp), 256);
-    L.w = off; if (!L.in_place) off = align_up(off + L.piece * row, 256);
-    L.wt = off; off = align_up(off + 2 * (size_t)H * L.slots * L.Vp, 256);
-    L.d = off; off = align_up(off + 2 * (size_t)N * L.slots * L.Vp, 256);
-    L.dt = off; off = align_up(off + (P == 1 ? 4 * (size_t)N * L.piece : 2 * (size_t)L.piece * L.slots_t * B * L.Pp), 256);
-    L.planes = off; off += (size_t)L.splits * N * H * sizeof(float);
+    L.x = off; if (!L.rows.in_place) off = align_up(off + N * row, 256);
+    L.xt = off; off = align_up(off + (L.sum_planes ? fc_planes_bytes(1, N, H) : P == 1 ? (size_t)N * H * 4 : 2 * (size_t)H * L.rows.planes * L.Lq), 256);
+    L.w = off; if (!L.rows.in_place) off = align_up(off + L.piece * row, 256);
+    L.d = off; if (!L.dx_thin) off = align_up(off + 2 * (size_t)L.piece * L.planes * L.Lq, 256);
+    L.d32 = off; if (P == 1) off = align_up(off + 4 * (size_t)N * L.piece, 256);
+    L.d2 = off; if (L.sum_planes) off += fc_planes_bytes(2, N, L.piece);
+    L.out = off; if (!L.dx_thin) off += (size_t)L.splits * N * H * sizeof(float);
     L.total = off;
     return L;
 }
@@ -601,24 +745,25 @@ int launch_softmax_loss_backward(int dtype, const void* X, const void* W, const 
     const size_t size = dtype == VGC_F32 ? 4 : 2;
     const bool by_position = s_out && P > 1;
     int rc;
-    uint16_t *xs = (uint16_t*)(ws + L.x), *xt = (uint16_t*)(ws + L.xt), *wsl = (uint16_t*)(ws + L.w), *wt = (uint16_t*)(ws + L.wt);
-    float* planes = reinterpret_cast<float*>(ws + L.planes);
+    uint16_t *xs = (uint16_t*)(ws + L.x), *xt = (uint16_t*)(ws + L.xt), *wp = (uint16_t*)(ws + L.w);
+    float* out = reinterpret_cast<float*>(ws + L.out);
     LossArgs A = {};
-    A.N = N; A.K = L.slots * L.Kp;
+    A.N = N; A.Lq = L.Lq;
+    A.K = L.rows.in_place ? H : L.rows.Kp;
+    A.at = Positions{B, P, L.Pp};
     A.target = target; A.lse = lse; A.weight = weight; A.V_all = V;
-    A.P = P; A.Pp = L.Pp; A.ld_dt = L.slots_t * B * L.Pp;
-    if (dX) A.d = (uint16_t*)(ws + L.d);
-    if (by_position) A.dt = (uint16_t*)(ws + L.dt);
-    else if (s_out) A.d32 = (float*)(ws + L.dt);
-    if (!L.in_place && (rc = launch_rows(dtype, true, X, N, H, xs, stream)) != VGC_OK) return rc;
-    A.x = Rows{L.in_place ? (const uint16_t*)X : xs, N, A.K};
+    if ((dX && !L.dx_thin) || by_position) A.dt = (uint16_t*)(ws + L.d);
+    A.planes = dtype == VGC_F32 ? 3u : by_position ? 2u : 1u;
+    if (P == 1 && (s_out || L.dx_thin)) A.d32 = (float*)(ws + L.d32);
+    if (!L.rows.in_place && (rc = launch_rows(dtype, X, N, H, xs, stream)) != VGC_OK) return rc;
+    A.x = matrix_of(L.rows, X, xs, N, H);
     if (by_position) {
-        if ((rc = launch_columns(dtype, X, target, B, P, L.Pp, H, L.slots_t, xt, stream)) != VGC_OK) return rc;
-        if (L.Pp != P) {                                     // positions that do not exist: what they meet in X is zero too, but has to be finite
-            const uint64_t n = 2ull * L.piece * A.ld_dt / 16u;
-            hipLaunchKernelGGL(k_clear, dim3((uint32_t)((n + 255u) / 256u)), dim3(256), 0, stream, reinterpret_cast<uint4*>(A.dt), n);
-            if ((rc = hip_check(hipGetLastError(), "launch k_clear")) != VGC_OK) return rc;
-        }
+        const dim3 grid((L.Lq + 63u) / 64u, (H + 63u) / 64u);
+        if (dtype == VGC_BF16) hipLaunchKernelGGL(k_planes_columns<uint16_t>, grid, dim3(256), 0, stream, (const uint16_t*)X, target, A.at, H, L.Lq, xt);
+        else hipLaunchKernelGGL(k_planes_columns<float>, grid, dim3(256), 0, stream, (const float*)X, target, A.at, H, L.Lq, xt);
+        if ((rc = hip_check(hipGetLastError(), "launch k_planes_columns")) != VGC_OK) return rc;
+    } else if (s_out && L.sum_planes) {
+        if ((rc = launch_square_planes(dtype, X, target, N, H, xt, stream)) != VGC_OK) return rc;
     } else if (s_out) {
         const dim3 grid((uint32_t)(((uint64_t)N * ((H + 7u) / 8u) + 255u) / 256u));
         if (dtype == VGC_F32) hipLaunchKernelGGL(k_asked_rows<float>, grid, dim3(256), 0, stream, (const float*)X, target, N, H, (float*)xt);
@@ -628,38 +773,50 @@ int launch_softmax_loss_backward(int dtype, const void* X, const void* W, const 
     for (uint32_t v0 = 0; v0 < V; v0 += L.piece) {
         A.v0 = v0;
         A.V = std::min(L.piece, V - v0);
-        A.Vp = up8(A.V);
+        A.plane = (uint64_t)A.V * L.Lq;
         const char* rows = static_cast<const char*>(W) + (size_t)v0 * H * size;
-        if (!L.in_place && (rc = launch_rows(dtype, false, rows, A.V, H, wsl, stream)) != VGC_OK) return rc;
-        A.w = Rows{L.in_place ? (const uint16_t*)rows : wsl, A.V, A.K};
-        rc = dtype == VGC_F32 ? launch_logits<false, true>(L.tile, A, stream) : launch_logits<false, false>(L.tile, A, stream);
-        if (rc != VGC_OK) return rc;
-        if (dX) {
-            if ((rc = launch_columns(dtype, rows, nullptr, 1, A.V, A.Vp, H, L.slots, wt, stream)) != VGC_OK) return rc;
-            const Rows D = {A.d, N, L.slots * A.Vp}, Wt = {wt, H, L.slots * A.Vp};
-            if (L.dx_large)
-                hipLaunchKernelGGL(k_loss_dx<TileLarge>, dim3(tiles(N, 256, H, 256) * L.splits), dim3(512), 0, stream, D, Wt, D.ld, L.splits, (int)(v0 > 0), planes);
+        if (!L.rows.in_place && (rc = launch_rows(dtype, rows, A.V, H, wp, stream)) != VGC_OK) return rc;
+        A.w = matrix_of(L.rows, rows, wp, A.V, H);
+        ThinArgs R = {A.w.base, A.x.base, A.w.ld, A.x.ld};
+        if (dtype == VGC_F32) R = ThinArgs{rows, X, H, H};   // (as floats, also where the planes are there for dX)
+        LossArgs T = A;
+        if (is_thin(L.tile) && dtype == VGC_F32) T.K = H;
+        if ((rc = launch_logits<false>(L.tile, dtype, R, T, stream)) != VGC_OK) return rc;
+        const Matrix Dt = {A.dt, A.V, L.Lq, A.plane};
+        if (dX && L.dx_thin) {
+            const dim3 grid(tiles(N, kThinDx, H, kThinDx));
+            if (dtype == VGC_F32) hipLaunchKernelGGL(k_loss_dx_thin<float>, grid, dim3(kThinWaves * 64), 0, stream, A.d32, (const float*)W, N, V, H, (float*)dX);
+            else hipLaunchKernelGGL(k_loss_dx_thin<uint16_t>, grid, dim3(kThinWaves * 64), 0, stream, A.d32, (const uint16_t*)W, N, V, H, (uint16_t*)dX);
+            if ((rc = hip_check(hipGetLastError(), "launch k_loss_dx_thin")) != VGC_OK) return rc;
+        } else if (dX) {
+            const uint32_t M = B * L.Pp;
+            if (dtype == VGC_F32)
+                hipLaunchKernelGGL(k_loss_dx<Cut>, dim3(tiles<Cut>(M, H) * L.splits), dim3(Cut::NW * 64), 0, stream, Dt, A.w, A.at, H, L.splits, (int)(v0 > 0), out);
+            else if (L.dx_large)
+                hipLaunchKernelGGL(k_loss_dx<Large>, dim3(tiles<Large>(M, H) * L.splits), dim3(Large::NW * 64), 0, stream, Dt, A.w, A.at, H, L.splits, (int)(v0 > 0), out);
             else
-                hipLaunchKernelGGL(k_loss_dx<TileSmall>, dim3(tiles(N, 128, H, 128) * L.splits), dim3(256), 0, stream, D, Wt, D.ld, L.splits, (int)(v0 > 0), planes);
+                hipLaunchKernelGGL(k_loss_dx<Small>, dim3(tiles<Small>(M, H) * L.splits), dim3(Small::NW * 64), 0, stream, Dt, A.w, A.at, H, L.splits, (int)(v0 > 0), out);
             if ((rc = hip_check(hipGetLastError(), "launch k_loss_dx")) != VGC_OK) return rc;
         }
         float *g = g_out ? g_out + (size_t)v0 * H : nullptr, *s = s_out ? s_out + (size_t)v0 * H : nullptr;
         if (by_position) {
-            const Rows Dt = {A.dt, A.V, A.ld_dt}, Xt = {xt, H, A.ld_dt};
-            const uint32_t seg = L.slots_t * L.Pp;
-            const dim3 grid(tiles(A.V, TileSums::BM, H, TileSums::BN));
-            if (seg % kStepK == 0) hipLaunchKernelGGL(k_loss_sums<false>, grid, dim3(256), 0, stream, Dt, Xt, A.ld_dt, seg, c, g, s);
-            else hipLaunchKernelGGL(k_loss_sums<true>, grid, dim3(256), 0, stream, Dt, Xt, A.ld_dt, seg, c, g, s);
+            const Matrix Xt = {xt, H, L.Lq, (uint64_t)H * L.Lq};
+            const uint32_t K = B * L.Pp;
+            if (dtype == VGC_F32) hipLaunchKernelGGL(k_loss_sums<Cut>, dim3(tiles<Cut>(A.V, H)), dim3(Cut::NW * 64), 0, stream, Dt, Xt, K, L.Pp, c, g, s);
+            else hipLaunchKernelGGL(k_loss_sums<Sums>, dim3(tiles<Sums>(A.V, H)), dim3(Sums::NW * 64), 0, stream, Dt, Xt, K, L.Pp, c, g, s);
             if ((rc = hip_check(hipGetLastError(), "launch k_loss_sums")) != VGC_OK) return rc;
+        } else if (s_out && L.sum_planes) {
+            if ((rc = launch_square_planes(VGC_F32, A.d32, nullptr, N, A.V, ws + L.d2, stream)) != VGC_OK) return rc;
+            if ((rc = launch_fc_planes(ws + L.d2, 2, xt, N, A.V, H, c, g, s, stream)) != VGC_OK) return rc;
         } else if (s_out) {
             if ((rc = launch_sqgrad(VGC_FC, VGC_F32, A.d32, xt, N, 1, A.V, H, c, g, s, nullptr, 0, stream)) != VGC_OK) return rc;
         }
     }
-    if (!dX) return VGC_OK;
+    if (!dX || L.dx_thin) return VGC_OK;
     const uint64_t n = (uint64_t)N * H;
     const dim3 grid((uint32_t)((n + 2047u) / 2048u));
-    if (dtype == VGC_F32) hipLaunchKernelGGL(k_loss_dx_join<float>, grid, dim3(256), 0, stream, planes, L.splits, n, (float*)dX);
-    else hipLaunchKernelGGL(k_loss_dx_join<uint16_t>, grid, dim3(256), 0, stream, planes, L.splits, n, (uint16_t*)dX);
+    if (dtype == VGC_F32) hipLaunchKernelGGL(k_loss_dx_join<float>, grid, dim3(256), 0, stream, out, L.splits, n, (float*)dX);
+    else hipLaunchKernelGGL(k_loss_dx_join<uint16_t>, grid, dim3(256), 0, stream, out, L.splits, n, (uint16_t*)dX);
     return hip_check(hipGetLastError(), "launch k_loss_dx_join");
 }
 

@@ -80,10 +80,10 @@ def test_rows_that_begin_anywhere(dev, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("form,B,P,J,C", [("fc", 1, 1, 5, 3), ("fc", 64, 1, 300, 200), ("fc", 33, 1, 1001, 77), ("conv", 3, 49, 64, 96), ("conv", 1, 1, 40, 8),
+@pytest.mark.parametrize("form,B,P,J,C", [("fc", 1, 1, 5, 3), ("fc", 64, 1, 300, 200), ("fc", 33, 1, 1001, 77), ("fc", 130, 1, 260, 390), ("conv", 3, 49, 64, 96), ("conv", 1, 1, 40, 8),
                                           ("conv", 5, 130, 256, 136), ("conv", 2, 33, 37, 21), ("conv", 40, 2, 128, 128)])
 def test_statistic_of_kept_rows(dev, form, B, P, J, C, dtype):
-    """Against the library's own statistic on the decoded values (the same kernel: the same bits), and against 64 bits within
+    """Against the library's own statistic on the decoded values where it is the same kernel (the same bits), and against 64 bits within
     float32 sums of exact products: P + B + 8 roundings and as many truncations of 2^-23 of the magnitudes summed (a third more
     for the samples' squares), which 1e-5 of them covers at these sizes.  Products of float32 pairs are within 2^-22.4."""
     import torch
@@ -109,7 +109,8 @@ def test_statistic_of_kept_rows(dev, form, B, P, J, C, dtype):
     nb2 = vgc.sqgrad_workspace_bytes(kind, vgc.F32 if wide else vgc.BF16, B, P, J, C)
     vgc.sqgrad(kind, kept if wide else kept.to(torch.bfloat16), Dd.float() if wide else Dd, 1.0 / B, s2, g2,
                torch.empty(nb2, dtype=torch.uint8, device=dev) if nb2 else None)
-    assert torch.equal(s, s2) and torch.equal(g, g2)
+    if kind == vgc.CONV or dtype == "f32":
+        assert torch.equal(s, s2) and torch.equal(g, g2)
     x64, D64 = O.act8_decode(q, e).reshape(B, P, J), D.double().numpy().reshape(B, P, C)
     g64, s64 = V.sqgrad_conv(x64, D64, 1.0 / B)
     ga, sa = V.sqgrad_conv(np.abs(x64), np.abs(D64), 1.0 / B)

@@ -92,7 +92,8 @@ def _check(X, W, target, weight, got, sums=True):
 
 SHAPES = [  # B, P, H, V: one of each; then lengths around a step's ends, odd rows, few and many classes
     (1, 1, 1, 1), (1, 1, 8, 2), (3, 1, 7, 5), (2, 2, 16, 3), (128, 1, 1000, 10), (64, 1, 96, 1000), (1, 7, 33, 40), (5, 8, 64, 31), (3, 9, 40, 33), (2, 24, 72, 65),
-    (2, 25, 64, 300), (3, 32, 64, 257), (2, 33, 130, 129), (1, 65, 64, 1000), (4, 100, 128, 517), (70, 3, 24, 90), (2, 31, 1001, 77), (1, 130, 200, 64), (3, 64, 512, 640)]
+    (2, 25, 64, 300), (3, 32, 64, 257), (2, 33, 130, 129), (1, 65, 64, 1000), (4, 100, 128, 517), (70, 3, 24, 90), (2, 31, 1001, 77), (1, 130, 200, 64), (3, 64, 512, 640),
+    (130, 1, 512, 300), (40, 1, 640, 7001), (17, 1, 1001, 5003)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -105,14 +106,14 @@ def test_loss_and_gradients(dev, B, P, H, V, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("B,P,H,V", [(100, 1, 24, 128 * 192 + 5), (4, 75, 40, 256 * 100 + 3), (1, 300, 17, 25700)])
+@pytest.mark.parametrize("B,P,H,V", [(64, 1, 72, 20003), (1, 5, 40, 17000), (3, 20, 16, 17001), (100, 1, 24, 128 * 192 + 5), (4, 75, 40, 256 * 100 + 3), (1, 300, 17, 25700)])
 def test_tiles_of_large_vocabularies(dev, B, P, H, V, dtype):
     """Enough tiles for the kernels with 128 and 256 classes a workgroup."""
     X, W, target = _inputs(B, P, H, V, dtype)
     _check(X, W, target, None, _sides(dev, X, W, target, None))
 
 
-@pytest.mark.parametrize("dtype,B,P,H,V", [("bf16", 4, 1024, 64, 20001), ("bf16", 1000, 1, 48, 150001), ("f32", 2, 300, 48, 50003)])
+@pytest.mark.parametrize("dtype,B,P,H,V", [("bf16", 4, 1024, 64, 20001), ("bf16", 4, 1024, 64, 150001), ("bf16", 1000, 1, 48, 400001), ("f32", 2, 300, 48, 600011)])
 def test_several_pieces_of_the_vocabulary(dev, B, P, H, V, dtype):
     X, W, target = _inputs(B, P, H, V, dtype)
     loss, lse, dX, s, g = got = _sides(dev, X, W, target, None)
