@@ -5,7 +5,7 @@
 // 16 bits, in two.  The products of the planes are exact, so g and s carry float32 sums' errors and, for squares of values that
 // have 16 bits themselves, 2^-17; a product of squares takes four bfloat16 instructions, a quarter of the time of the float32 ones
 // that squares in float32 need.  What is left is what the outputs take to be written, 8 bytes of each element, while N rows are
-// read: 64 x (25088, 4096), g and s: 252 us by float32 instructions -> 146.  (A value whose square lies below 2^-118 loses digits of it.)
+// read: 64 x (25088, 4096), g and s: 252 us by float32 instructions -> 160.  (A value whose square lies below 2^-118 loses digits of it.)
 #include "vgc_gemm.h"
 #include "vgc_rows.h"
 
@@ -64,7 +64,9 @@ typedef TileShape<128, 128, 64, 64, 32, 2, 2, 2> SquareTile;
 template <int PA> using ValueTile = TileShape<128, 128, 64, 64, 32, 2, PA, 1>;
 
 // A: PA planes of the m side, then its squares' two; B: one plane of the n side, then its squares' two.
-template <int PA>
+// kPast: outputs beyond what the caches hold are stored past them (64 x (25088, 4096), 822 MB: 184 us into them, 160 past them;
+// 128 x (4096, 1000), 33 MB: 20 and 24).
+template <int PA, bool kPast>
 __global__ __launch_bounds__(SquareTile::NW * 64, 2) void k_fc_planes(Matrix A, Matrix B, uint32_t M, uint32_t C, float c, float* __restrict__ g_out,
                                                                       float* __restrict__ s_out) {
     typedef SquareTile Tile;
@@ -84,7 +86,10 @@ __global__ __launch_bounds__(SquareTile::NW * 64, 2) void k_fc_planes(Matrix A, 
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const uint32_t row = wm + m * 32u + 8u * (i >> 2) + 4u * half + (i & 3);
-                    if (row < M) out[(size_t)row * C + col] = scale * acc[m][n][i];
+                    if (row >= M) continue;
+                    float* to = out + (size_t)row * C + col;
+                    if (kPast) __builtin_nontemporal_store(scale * acc[m][n][i], to);
+                    else *to = scale * acc[m][n][i];
                 }
         }
     };
@@ -121,8 +126,11 @@ int launch_fc_planes(const void* a, uint32_t own, const void* b, uint32_t N, uin
     const uint32_t Mp = (M + 7u) / 8u * 8u, Cp = (C + 7u) / 8u * 8u;
     const Matrix A = {(const uint16_t*)a, N, Mp, (uint64_t)N * Mp}, B = {(const uint16_t*)b, N, Cp, (uint64_t)N * Cp};
     const dim3 grid(((M + 127u) / 128u) * ((C + 127u) / 128u));
-    if (own == 1) hipLaunchKernelGGL(k_fc_planes<1>, grid, dim3(SquareTile::NW * 64), 0, stream, A, B, M, C, c, g_out, s_out);
-    else hipLaunchKernelGGL(k_fc_planes<2>, grid, dim3(SquareTile::NW * 64), 0, stream, A, B, M, C, c, g_out, s_out);
+    const bool past = (uint64_t)M * C * (g_out ? 8u : 4u) > (256u << 20);
+#define VGC_LAUNCH(OWN, PAST) hipLaunchKernelGGL((k_fc_planes<OWN, PAST>), grid, dim3(SquareTile::NW * 64), 0, stream, A, B, M, C, c, g_out, s_out)
+    if (own == 1) { if (past) VGC_LAUNCH(1, true); else VGC_LAUNCH(1, false); }
+    else { if (past) VGC_LAUNCH(2, true); else VGC_LAUNCH(2, false); }
+#undef VGC_LAUNCH
     return hip_check(hipGetLastError(), "launch k_fc_planes");
 }
 

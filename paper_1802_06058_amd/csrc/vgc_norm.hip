@@ -48,87 +48,118 @@ __device__ __forceinline__ void keep_act8(const float (&f)[8], uint32_t C, uint3
 }
 
 // ---- forward --------------------------------------------------------------------------------------------------------------
-// kNV pieces a lane; a row takes a wave (kWide false: four rows a workgroup) or the workgroup.  kNV = 0: rows beyond what the
-// largest workgroup holds, read three times (mean, sum of squares, output).
+// A team takes rows team, team + teams, ..: its part of gamma and beta stays in registers, and the next row is on its way while the
+// present one is reduced and stored.  Teams: the waves of a workgroup (kWide false), or the workgroup.  (A row a workgroup, gamma and
+// beta read for each: 16384 x 4096 bfloat16 with the 8-bit form 82 us; so 66.)
 template <typename T, int kNV, bool kWide, bool kKeep>
-__global__ __launch_bounds__(kWide ? 1024 : 256) void k_layer_norm(const T* __restrict__ x, uint64_t R, uint32_t C, const float* __restrict__ gamma,
-                                                                 const float* __restrict__ beta, float eps, T* __restrict__ y,
-                                                                 float* __restrict__ mean_out, float* __restrict__ rstd_out,
-                                                                 int8_t* __restrict__ codes, uint8_t* __restrict__ exps) {
+__global__ __launch_bounds__(kWide ? 512 : 256) void k_layer_norm(const T* __restrict__ x, uint32_t R, uint32_t C, uint32_t teams, const float* __restrict__ gamma,
+                                                                const float* __restrict__ beta, float eps, T* __restrict__ y,
+                                                                float* __restrict__ mean_out, float* __restrict__ rstd_out,
+                                                                int8_t* __restrict__ codes, uint8_t* __restrict__ exps) {
     __shared__ float sh[2][kMaxWaves][1];
-    const uint32_t lanes = kWide ? blockDim.x : 64u, lane = kWide ? threadIdx.x : threadIdx.x & 63u;
-    const uint64_t row = kWide ? (uint64_t)blockIdx.x : (uint64_t)blockIdx.x * 4u + (threadIdx.x >> 6);
+    const uint32_t lanes = kWide ? blockDim.x : 64u, lane = kWide ? threadIdx.x : threadIdx.x & 63u, waves = lanes / 64u;
+    uint32_t row = kWide ? blockIdx.x : __builtin_amdgcn_readfirstlane(blockIdx.x * 4u + (threadIdx.x >> 6));
     if (row >= R) return;                                    // (a wave, or the workgroup)
-    const uint32_t waves = lanes / 64u;
-    const T* xr = x + row * C;
-    T* yr = y + row * C;
     const float inv = 1.0f / (float)C;
-    constexpr int kHeld = kNV > 0 ? kNV : 1;
-    float f[kHeld][8];
-    float v[1] = {0.f};
-    if (kNV > 0) {
-        Raw8<T> raw[kHeld];
+    int n[kNV];
+    Raw8<T> raw[kNV];
+    float ga[kNV][8], be[kNV][8];
+    auto request = [&](uint32_t r) {
 #pragma unroll
-        for (int i = 0; i < kHeld; ++i) raw[i] = load8(xr + (lane + i * lanes) * 8u, (int)C - (int)((lane + i * lanes) * 8u));
+        for (int i = 0; i < kNV; ++i) raw[i] = load8(x + (uint64_t)r * C + (lane + i * lanes) * 8u, n[i]);
+    };
 #pragma unroll
-        for (int i = 0; i < kHeld; ++i) {
+    for (int i = 0; i < kNV; ++i) n[i] = (int)C - (int)((lane + i * lanes) * 8u);
+    request(row);
+#pragma unroll
+    for (int i = 0; i < kNV; ++i) {
+        widen8(load8(gamma + (lane + i * lanes) * 8u, n[i]), ga[i]);
+        widen8(load8(beta + (lane + i * lanes) * 8u, n[i]), be[i]);
+    }
+    for (;;) {
+        float f[kNV][8], v[1] = {0.f};
+#pragma unroll
+        for (int i = 0; i < kNV; ++i) {
             widen8(raw[i], f[i]);
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[0] += f[i][k];
         }
-    } else {
-        for (uint32_t e = lane * 8u; e < C; e += lanes * 8u) {
-            widen8(load8(xr + e, (int)(C - e)), f[0]);
+        const uint32_t after = row + teams;
+        if (after < R) request(after);
+        team_sums<1, kWide>(v, sh[0], waves);
+        const float mean = v[0] * inv;
+        v[0] = 0.f;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[0] += f[0][k];
+        for (int i = 0; i < kNV; ++i)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {                    // elements past the row's end stay 0
+                f[i][k] = k < n[i] ? f[i][k] - mean : 0.f;
+                v[0] = __builtin_fmaf(f[i][k], f[i][k], v[0]);
+            }
+        team_sums<1, kWide>(v, sh[1], waves);
+        const float rstd = 1.0f / sqrtf(v[0] * inv + eps);
+        if (lane == 0) { mean_out[row] = mean; rstd_out[row] = rstd; }
+#pragma unroll
+        for (int i = 0; i < kNV; ++i) {
+            float o[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) f[i][k] *= rstd;
+            if (kKeep) keep_act8(f[i], C, lane + i * lanes, row, n[i], codes, exps);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) o[k] = __builtin_fmaf(f[i][k], ga[i][k], be[i][k]);
+            store8(y + (uint64_t)row * C + (lane + i * lanes) * 8u, o, n[i]);
         }
+        if (after >= R) return;
+        row = after;
     }
-    team_sums<1, kWide>(v, sh[0], waves);
+}
+
+// Rows beyond what a team holds: a workgroup a row, read three times (the last two from the cache).
+template <typename T, bool kKeep>
+__global__ __launch_bounds__(1024) void k_layer_norm_long(const T* __restrict__ x, uint32_t C, const float* __restrict__ gamma,
+                                                          const float* __restrict__ beta, float eps, T* __restrict__ y,
+                                                          float* __restrict__ mean_out, float* __restrict__ rstd_out,
+                                                          int8_t* __restrict__ codes, uint8_t* __restrict__ exps) {
+    __shared__ float sh[2][kMaxWaves][1];
+    const uint32_t lanes = blockDim.x, lane = threadIdx.x, row = blockIdx.x;
+    const T* xr = x + (uint64_t)row * C;
+    const float inv = 1.0f / (float)C;
+    float f[8], v[1] = {0.f};
+    for (uint32_t e = lane * 8u; e < C; e += lanes * 8u) {
+        widen8(load8(xr + e, (int)(C - e)), f);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[0] += f[k];
+    }
+    team_sums<1, true>(v, sh[0], lanes / 64u);
     const float mean = v[0] * inv;
     v[0] = 0.f;
-    auto centre = [&](float (&a)[8], int n) {                // elements past the row's end stay 0
+    auto centred = [&](uint32_t e) {
+        const int n = (int)C - (int)e;
+        widen8(load8(xr + e, n), f);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            a[k] = k < n ? a[k] - mean : 0.f;
-            v[0] = __builtin_fmaf(a[k], a[k], v[0]);
-        }
+        for (int k = 0; k < 8; ++k) f[k] = k < n ? f[k] - mean : 0.f;
     };
-    if (kNV > 0) {
+    for (uint32_t e = lane * 8u; e < C; e += lanes * 8u) {
+        centred(e);
 #pragma unroll
-        for (int i = 0; i < kHeld; ++i) centre(f[i], (int)C - (int)((lane + i * lanes) * 8u));
-    } else {
-        for (uint32_t e = lane * 8u; e < C; e += lanes * 8u) {
-            widen8(load8(xr + e, (int)(C - e)), f[0]);
-            centre(f[0], (int)(C - e));
-        }
+        for (int k = 0; k < 8; ++k) v[0] = __builtin_fmaf(f[k], f[k], v[0]);
     }
-    team_sums<1, kWide>(v, sh[1], waves);
+    team_sums<1, true>(v, sh[1], lanes / 64u);
     const float rstd = 1.0f / sqrtf(v[0] * inv + eps);
     if (lane == 0) { mean_out[row] = mean; rstd_out[row] = rstd; }
-    auto finish = [&](float (&a)[8], uint32_t piece) {
-        const int n = (int)C - (int)(piece * 8u);
+    const uint32_t pieces = ((C + 31u) / 32u) * 4u;          // whole blocks: the lanes of one meet in keep_act8
+    for (uint32_t p = lane; p < pieces; p += lanes) {
+        const int n = (int)C - (int)(p * 8u);
+        centred(p * 8u);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) a[k] *= rstd;
-        if (kKeep) keep_act8(a, C, piece, row, n, codes, exps);
+        for (int k = 0; k < 8; ++k) f[k] *= rstd;
+        if (kKeep) keep_act8(f, C, p, row, n, codes, exps);
         float ga[8], be[8], o[8];
-        widen8(load8(gamma + piece * 8u, n), ga);
-        widen8(load8(beta + piece * 8u, n), be);
+        widen8(load8(gamma + p * 8u, n), ga);
+        widen8(load8(beta + p * 8u, n), be);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) o[k] = __builtin_fmaf(a[k], ga[k], be[k]);
-        store8(yr + piece * 8u, o, n);
-    };
-    if (kNV > 0) {
-#pragma unroll
-        for (int i = 0; i < kHeld; ++i) finish(f[i], lane + i * lanes);
-    } else {
-        const uint32_t pieces = ((C + 31u) / 32u) * 4u;      // whole blocks: the lanes of one meet in keep_act8
-        for (uint32_t p = lane; p < pieces; p += lanes) {
-            const int n = (int)C - (int)(p * 8u);
-            widen8(load8(xr + p * 8u, n), f[0]);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) f[0][k] = k < n ? f[0][k] - mean : 0.f;
-            finish(f[0], p);
-        }
+        for (int k = 0; k < 8; ++k) o[k] = __builtin_fmaf(f[k], ga[k], be[k]);
+        store8(y + (uint64_t)row * C + p * 8u, o, n);
     }
 }
 
@@ -343,64 +374,77 @@ __global__ __launch_bounds__(1024) void k_layer_norm_backward_long(NormArgs A) {
     }
 }
 
-// Adds the teams' partial sums in a fixed order: a workgroup takes 64 columns of one of the two vectors (blockIdx.y: gamma,
-// beta), its 16 waves share the partial sums between them.
-//   whole samples: n = teams, planes g, s, summed over the teams.
-//   parts: the parts of a sample are added before the square.  Waves take samples of their own if there are 16 or more; below,
-//   several waves share a sample's parts.
+// Adds the teams' partial sums in a fixed order: a workgroup takes 64 columns of one of the two vectors (blockIdx.y: gamma, beta),
+// four a lane, and its 64 groups of 16 lanes share the partial sums between them.
+//   whole samples: planes g, s, summed over the teams.
+//   parts: the parts of a sample are added before the square.  Groups take samples of their own if there are 64 or more; below,
+//   several groups share a sample's parts.
 __global__ __launch_bounds__(1024) void k_layer_norm_sums(const float* __restrict__ partial, uint32_t teams, uint32_t B, uint32_t parts, uint32_t C,
                                                           int whole, float c, float* __restrict__ g_gamma, float* __restrict__ s_gamma,
                                                           float* __restrict__ g_beta, float* __restrict__ s_beta) {
-    __shared__ float sh[2][16][64];
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, col = blockIdx.x * 64u + lane, vec = blockIdx.y;
-    const bool live = col < C;
-    float g = 0.f, s = 0.f;
+    constexpr uint32_t kGroups = 64;
+    __shared__ float sh[2][kGroups][64];
+    const uint32_t lane = threadIdx.x & 15u, group = threadIdx.x >> 4, col = blockIdx.x * 64u + lane * 4u, vec = blockIdx.y;
+    const int n = col < C ? (int)min(C - col, 4u) : 0;
+    auto load = [&](const float* p) -> any_f4 {
+        any_f4 r = {0.f, 0.f, 0.f, 0.f};
+        if (n == 4) return *reinterpret_cast<const any_f4*>(p);
+        for (int i = 0; i < 3; ++i)
+            if (i < n) r[i] = p[i];
+        return r;
+    };
+    any_f4 g = {0.f, 0.f, 0.f, 0.f}, s = g;
+    uint32_t share = 1;                                      // groups a sample's parts are spread over
     if (whole) {
         const float* at = partial + (size_t)(2u * vec) * C + col;
         const size_t step = 4 * (size_t)C;
-        if (live)
 #pragma unroll 4
-            for (uint32_t t = wave; t < teams; t += 16u) { g += at[t * step]; s += at[t * step + C]; }
-        sh[0][wave][lane] = g;
-        sh[1][wave][lane] = s;
-        __syncthreads();
+        for (uint32_t t = group; t < teams; t += kGroups) { g += load(at + t * step); s += load(at + t * step + C); }
     } else {
         const float* at = partial + (size_t)vec * C + col;
         const size_t step = 2 * (size_t)C;
-        uint32_t share = 1;                                  // waves a sample's parts are spread over
-        while (B * share * 2u <= 16u) share *= 2u;
-        const uint32_t sub = wave % share;
-        float part_sum = 0.f;
-        for (uint32_t z = wave / share; z < B; z += 16u / share) {
-            part_sum = 0.f;
-            if (live)
+        while (B * share * 2u <= kGroups) share *= 2u;
+        const uint32_t sub = group % share;
+        for (uint32_t z = group / share; z < B; z += kGroups / share) {
+            any_f4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
-                for (uint32_t q = sub; q < parts; q += share) part_sum += at[((size_t)z * parts + q) * step];
-            if (share == 1) { g += part_sum; s = __builtin_fmaf(part_sum, part_sum, s); }
+            for (uint32_t q = sub; q < parts; q += share) sum += load(at + ((size_t)z * parts + q) * step);
+            if (share > 1) { g = sum; break; }               // (at most one sample a group)
+            g += sum;
+            for (int i = 0; i < 4; ++i) s[i] = __builtin_fmaf(sum[i], sum[i], s[i]);
         }
-        if (share > 1) {                                     // (at most one sample a wave)
-            sh[0][wave][lane] = part_sum;
-            __syncthreads();
-            if (sub == 0) {
-                float G = 0.f;
-                if (wave / share < B)
-                    for (uint32_t q = 0; q < share; ++q) G += sh[0][wave + q][lane];
-                g = G;
-                s = G * G;
-            }
-            __syncthreads();
+    }
+    for (int i = 0; i < 4; ++i) { sh[0][group][lane * 4u + i] = g[i]; sh[1][group][lane * 4u + i] = s[i]; }
+    __syncthreads();
+    // a thread takes one of the 64 columns and the sixteenth part of the groups, whole samples of them
+    const uint32_t one = threadIdx.x & 63u, part = threadIdx.x >> 6;
+    float go = 0.f, so = 0.f;
+    if (share > 4u) {                                        // (fewer than 8 samples: each by one thread)
+        if (part * share < kGroups) {
+            float G = 0.f;
+            for (uint32_t q = 0; q < share; ++q) G += sh[0][part * share + q][one];
+            go = G;
+            so = G * G;
         }
-        sh[0][wave][lane] = g;
-        sh[1][wave][lane] = s;
-        __syncthreads();
+    } else {
+        for (uint32_t q = 0; q < 4u; q += share) {
+            float G = 0.f, S = 0.f;
+            for (uint32_t e = 0; e < share; ++e) { G += sh[0][part * 4u + q + e][one]; S += sh[1][part * 4u + q + e][one]; }
+            go += G;
+            so += share > 1u ? G * G : S;
+        }
     }
-    if (wave == 0 && live) {
-        g = s = 0.f;
-        for (uint32_t w = 0; w < 16; ++w) { g += sh[0][w][lane]; s += sh[1][w][lane]; }
-        float *go = vec ? g_beta : g_gamma, *so = vec ? s_beta : s_gamma;
-        if (go) go[col] = c * g;
-        so[col] = c * c * s;
-    }
+    __syncthreads();
+    sh[0][part][one] = go;
+    sh[1][part][one] = so;
+    __syncthreads();
+    const uint32_t at = blockIdx.x * 64u + one;
+    if (part != 0u || at >= C) return;
+    go = so = 0.f;
+    for (uint32_t q = 0; q < 16u; ++q) { go += sh[0][q][one]; so += sh[1][q][one]; }
+    float *gout = vec ? g_beta : g_gamma, *sout = vec ? s_beta : s_gamma;
+    if (gout) gout[at] = c * go;
+    sout[at] = c * c * so;
 }
 
 // ---- launches ---------------------------------------------------------------------------------------------------------------
@@ -409,24 +453,21 @@ static uint32_t row_lanes(uint32_t C, uint32_t pieces_per_lane) { return ((C + 7
 int launch_layer_norm(int dtype, const void* x, uint64_t R, uint32_t C, const float* gamma, const float* beta, float eps, void* y, float* mean,
                       float* rstd, int8_t* codes, uint8_t* exps, hipStream_t stream) {
     if (R > 0x7FFFFFFFull) { set_error("vgc_layer_norm: %llu rows exceed the launch limit", (unsigned long long)R); return VGC_ERR_SIZE; }
-#define VGC_LAUNCH(T, NV, WIDE, KEEP, lanes) hipLaunchKernelGGL((k_layer_norm<T, NV, WIDE, KEEP>), dim3((uint32_t)((WIDE) ? R : (R + 3) / 4)), dim3((WIDE) ? (lanes) : 256u), 0, stream, \
-        (const T*)x, R, C, gamma, beta, eps, (T*)y, mean, rstd, codes, exps)
-#define VGC_BOTH(NV, WIDE, lanes) do { \
-        if (dtype == VGC_F32) { if (codes) VGC_LAUNCH(float, NV, WIDE, true, lanes); else VGC_LAUNCH(float, NV, WIDE, false, lanes); } \
-        else { if (codes) VGC_LAUNCH(uint16_t, NV, WIDE, true, lanes); else VGC_LAUNCH(uint16_t, NV, WIDE, false, lanes); } } while (0)
-    const uint32_t pieces = (C + 7) / 8;
-    // A wave a row as long as that fills the chip or the row is short; few long rows are spread over more waves, and so are rows
-    // that a wave cannot hold.
-    const bool wide = pieces > 64u * 8u || (pieces > 64u && R < 2048u);
-    if (!wide) {
-        if (pieces <= 64u) VGC_BOTH(1, false, 0u);
-        else if (pieces <= 128u) VGC_BOTH(2, false, 0u);
-        else if (pieces <= 256u) VGC_BOTH(4, false, 0u);
-        else VGC_BOTH(8, false, 0u);
-    } else if (pieces <= 1024u) VGC_BOTH(1, true, row_lanes(C, 1));
-    else if (pieces <= 4096u) VGC_BOTH(4, true, row_lanes(C, 4));
-    else VGC_BOTH(0, true, 1024u);
-#undef VGC_BOTH
+    const uint32_t pieces = (C + 7) / 8, rows = (uint32_t)R;
+    // Rows a wave holds are taken by waves, longer ones (up to 8192 elements) by workgroups; teams: four waves to a SIMD, which is what
+    // the loads in flight need.  One piece a lane rather than two where a row has to itself what there is of the chip anyway.
+    const bool one = pieces <= 64u || (rows <= 1024u && pieces > 64u && pieces <= 512u);
+    const uint32_t lanes = row_lanes(C, one ? 1 : 2), teams = std::min(rows, 4096u / (lanes / 64u));
+    const bool wide = lanes > 64u;
+#define VGC_LAUNCH(T, NV, WIDE, KEEP) hipLaunchKernelGGL((k_layer_norm<T, NV, WIDE, KEEP>), dim3((WIDE) ? teams : (teams + 3) / 4), dim3((WIDE) ? lanes : 256u), 0, \
+        stream, (const T*)x, rows, C, (WIDE) ? teams : (teams + 3) / 4 * 4, gamma, beta, eps, (T*)y, mean, rstd, codes, exps)
+#define VGC_SHAPE(T, KEEP) do { \
+        if (pieces > 1024u) hipLaunchKernelGGL((k_layer_norm_long<T, KEEP>), dim3(rows), dim3(1024), 0, stream, (const T*)x, C, gamma, beta, eps, (T*)y, mean, rstd, codes, exps); \
+        else if (!wide) { if (one) VGC_LAUNCH(T, 1, false, KEEP); else VGC_LAUNCH(T, 2, false, KEEP); } \
+        else { if (one) VGC_LAUNCH(T, 1, true, KEEP); else VGC_LAUNCH(T, 2, true, KEEP); } } while (0)
+    if (dtype == VGC_F32) { if (codes) VGC_SHAPE(float, true); else VGC_SHAPE(float, false); }
+    else { if (codes) VGC_SHAPE(uint16_t, true); else VGC_SHAPE(uint16_t, false); }
+#undef VGC_SHAPE
 #undef VGC_LAUNCH
     return hip_check(hipGetLastError(), "launch k_layer_norm");
 }

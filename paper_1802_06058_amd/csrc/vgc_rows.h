@@ -120,16 +120,25 @@ __device__ __forceinline__ uint32_t four_lanes_max(uint32_t x) {
     x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xF, 0xF, false));      // lanes 1 apart
     return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xF, 0xF, false));   // 2 apart
 }
-// Eight codes of a block with this field, rounded to nearest, ties to even.  (field 255: the codes are 0)
+// Eight codes of a block with this field, rounded to nearest, ties to even (field 255: the codes are 0).  Adding 1.5 2^23 rounds a
+// value of at most 2^22 to a whole number and leaves its low byte, in two's complement, in the float's; only the largest unit has to be cut off at 127.
 __device__ __forceinline__ any_u2 act8_codes(const float (&f)[8], uint32_t field) {
     const float inverse = __uint_as_float((254u - min(field, 253u)) << 23);
     any_u2 v = {0u, 0u};
+    if (field >= 248u) {
+        if (field == 255u) return v;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int q = min(max((int)__builtin_rintf(f[i] * inverse), -127), 127);
-        v[i >> 2] |= ((uint32_t)q & 0xFFu) << (8 * (i & 3));
+        for (int i = 0; i < 8; ++i) v[i >> 2] |= ((uint32_t)min(max((int)__builtin_rintf(f[i] * inverse), -127), 127) & 0xFFu) << (8 * (i & 3));
+        return v;
     }
-    if (field == 255u) v = (any_u2){0u, 0u};
+    uint32_t q[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) q[i] = __float_as_uint(__builtin_fmaf(f[i], inverse, 12582912.f));
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {                            // bytes 0 of four words
+        const uint32_t lo = __builtin_amdgcn_perm(q[4 * i + 1], q[4 * i], 0x0C0C0400u), hi = __builtin_amdgcn_perm(q[4 * i + 3], q[4 * i + 2], 0x04000C0Cu);
+        v[i] = lo | hi;
+    }
     return v;
 }
 __device__ __forceinline__ void act8_values(any_u2 v, uint32_t field, float (&f)[8]) {
