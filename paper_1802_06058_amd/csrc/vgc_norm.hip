@@ -7,23 +7,23 @@
 // registers by then, so that a large mean costs no digits.
 //
 // Both are bound by memory: x, y once forward; dy, x (or its 8-bit form) and dx once backward.  A row belongs to a team of
-// lanes that hold it in registers, eight consecutive elements a lane and piece.  Backward, a team keeps its columns from row to
-// row, so that the column sums stay in registers too and leave once per team, as float32 partial sums that a second, small
-// kernel adds in a fixed order and, where a sample was spread over several teams, squares.  No atomics: results do not depend
-// on scheduling.
+// 8, 16, 32 or 64 lanes, or to a workgroup, as it needs to hold it in registers, eight consecutive elements a lane and piece.
+// Backward, a team keeps its columns from row to row, so that the column sums stay in registers too; they leave once per workgroup, as
+// float32 partial sums that a second, small kernel adds in a fixed order and, where a sample was spread over several workgroups,
+// squares.  No atomics: results do not depend on scheduling.
 #include <algorithm>
 
 #include "vgc_rows.h"
 
 namespace vgc {
 
-// Sums of `kN` values over the lanes of a team, the same in all of them.  A team is a wave, or the whole workgroup; then `sh`
-// holds a value per wave, and one barrier separates its writers from its readers (the caller alternates between two arrays).
-template <int kN, bool kWide>
+// Sums of `kN` values over the lanes of a team, the same in all of them: kL lanes, or (kL = 0) the workgroup.  Then `sh` holds a value
+// per wave, and one barrier separates its writers from its readers (the caller alternates between two arrays).
+template <int kN, int kL>
 __device__ __forceinline__ void team_sums(float (&v)[kN], float (*sh)[kN], uint32_t waves) {
 #pragma unroll
-    for (int i = 0; i < kN; ++i) v[i] = wave_sum(v[i]);
-    if (kWide) {
+    for (int i = 0; i < kN; ++i) v[i] = lanes_sum<kL == 0 ? 64 : kL>(v[i]);
+    if (kL == 0) {
         const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63u;
         if (lane == 0)
 #pragma unroll
@@ -49,17 +49,17 @@ __device__ __forceinline__ void keep_act8(const float (&f)[8], uint32_t C, uint3
 
 // ---- forward --------------------------------------------------------------------------------------------------------------
 // A team takes rows team, team + teams, ..: its part of gamma and beta stays in registers, and the next row is on its way while the
-// present one is reduced and stored.  Teams: the waves of a workgroup (kWide false), or the workgroup.  (A row a workgroup, gamma and
-// beta read for each: 16384 x 4096 bfloat16 with the 8-bit form 82 us; so 66.)
-template <typename T, int kNV, bool kWide, bool kKeep>
-__global__ __launch_bounds__(kWide ? 512 : 256) void k_layer_norm(const T* __restrict__ x, uint32_t R, uint32_t C, uint32_t teams, const float* __restrict__ gamma,
+// present one is reduced and stored.  Teams: kL lanes each, or (kL = 0) the workgroup.  (A row a workgroup, gamma and beta read for each:
+// 16384 x 4096 bfloat16 67 us; so 53.)
+template <typename T, int kNV, int kL, bool kKeep>
+__global__ __launch_bounds__(kL == 0 ? 512 : 256) void k_layer_norm(const T* __restrict__ x, uint32_t R, uint32_t C, uint32_t teams, const float* __restrict__ gamma,
                                                                 const float* __restrict__ beta, float eps, T* __restrict__ y,
                                                                 float* __restrict__ mean_out, float* __restrict__ rstd_out,
                                                                 int8_t* __restrict__ codes, uint8_t* __restrict__ exps) {
     __shared__ float sh[2][kMaxWaves][1];
-    const uint32_t lanes = kWide ? blockDim.x : 64u, lane = kWide ? threadIdx.x : threadIdx.x & 63u, waves = lanes / 64u;
-    uint32_t row = kWide ? blockIdx.x : __builtin_amdgcn_readfirstlane(blockIdx.x * 4u + (threadIdx.x >> 6));
-    if (row >= R) return;                                    // (a wave, or the workgroup)
+    const uint32_t lanes = kL == 0 ? blockDim.x : (uint32_t)kL, lane = kL == 0 ? threadIdx.x : threadIdx.x % lanes, waves = lanes / 64u;
+    uint32_t row = kL == 0 ? blockIdx.x : blockIdx.x * (256u / lanes) + threadIdx.x / lanes;
+    if (row >= R) return;                                    // (a team)
     const float inv = 1.0f / (float)C;
     int n[kNV];
     Raw8<T> raw[kNV];
@@ -86,7 +86,7 @@ __global__ __launch_bounds__(kWide ? 512 : 256) void k_layer_norm(const T* __res
         }
         const uint32_t after = row + teams;
         if (after < R) request(after);
-        team_sums<1, kWide>(v, sh[0], waves);
+        team_sums<1, kL>(v, sh[0], waves);
         const float mean = v[0] * inv;
         v[0] = 0.f;
 #pragma unroll
@@ -96,7 +96,7 @@ __global__ __launch_bounds__(kWide ? 512 : 256) void k_layer_norm(const T* __res
                 f[i][k] = k < n[i] ? f[i][k] - mean : 0.f;
                 v[0] = __builtin_fmaf(f[i][k], f[i][k], v[0]);
             }
-        team_sums<1, kWide>(v, sh[1], waves);
+        team_sums<1, kL>(v, sh[1], waves);
         const float rstd = 1.0f / sqrtf(v[0] * inv + eps);
         if (lane == 0) { mean_out[row] = mean; rstd_out[row] = rstd; }
 #pragma unroll
@@ -130,7 +130,7 @@ __global__ __launch_bounds__(1024) void k_layer_norm_long(const T* __restrict__ 
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[0] += f[k];
     }
-    team_sums<1, true>(v, sh[0], lanes / 64u);
+    team_sums<1, 0>(v, sh[0], lanes / 64u);
     const float mean = v[0] * inv;
     v[0] = 0.f;
     auto centred = [&](uint32_t e) {
@@ -144,7 +144,7 @@ __global__ __launch_bounds__(1024) void k_layer_norm_long(const T* __restrict__ 
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[0] = __builtin_fmaf(f[k], f[k], v[0]);
     }
-    team_sums<1, true>(v, sh[1], lanes / 64u);
+    team_sums<1, 0>(v, sh[1], lanes / 64u);
     const float rstd = 1.0f / sqrtf(v[0] * inv + eps);
     if (lane == 0) { mean_out[row] = mean; rstd_out[row] = rstd; }
     const uint32_t pieces = ((C + 31u) / 32u) * 4u;          // whole blocks: the lanes of one meet in keep_act8
@@ -175,9 +175,9 @@ struct NormArgs {
     const int8_t* codes;
     const uint8_t* exps;
     void* dx;
-    float* partial;           // of team t: planes of C floats, see below
-    uint32_t B, P, C, parts;  // teams a sample is spread over (1: a team takes whole samples)
-    uint32_t teams;
+    float* partial;           // of every workgroup: planes of C floats, see below
+    uint32_t B, P, C, parts;  // workgroups a sample is spread over
+    uint32_t groups;
 };
 
 template <typename T, bool kKept>
@@ -202,26 +202,29 @@ __device__ __forceinline__ void row_xhat(const RowIn<T, kKept>& r, float mean, f
     }
 }
 
-// Teams: the waves of a workgroup (kWide false), or the workgroup.  kRows rows are in flight at a time, the next ones' loads
-// issued before the present ones are reduced.  kWhole: the team takes samples [t B / teams, (t + 1) B / teams) whole, keeps
-// g and s of its columns, and leaves four planes (g and s of gamma, of beta); else it takes part t % parts of sample
-// t / parts and leaves its two column sums.
-template <typename T, bool kKept, int kNV, int kRows, bool kWide, bool kWhole>
-__global__ __launch_bounds__(kWide ? 512 : 256) void k_layer_norm_backward(NormArgs A) {
+// Teams: kL lanes each, or (kL = 0) the workgroup.  kRows rows are in flight at a time, the next ones' loads issued before the
+// present ones are reduced.  kWhole: a team takes samples whole, number t of n teams those of [t B / n, (t + 1) B / n), and keeps g
+// and s of its columns; the workgroup leaves four planes (g and s of gamma, of beta), its teams' added.  Else a workgroup takes part
+// w % parts of sample w / parts, its teams rows in turn, and leaves its two column sums.
+template <typename T, bool kKept, int kNV, int kRows, int kL, bool kWhole>
+__global__ __launch_bounds__(kL == 0 ? 512 : 256) void k_layer_norm_backward(NormArgs A) {
+    constexpr uint32_t kTeams = kL == 0 ? 1u : 256u / (kL == 0 ? 1 : kL);
     __shared__ float sh[2][kMaxWaves][2 * kRows];
-    const uint32_t lanes = kWide ? blockDim.x : 64u, lane = kWide ? threadIdx.x : threadIdx.x & 63u, waves = lanes / 64u;
-    const uint32_t team = kWide ? blockIdx.x : __builtin_amdgcn_readfirstlane(blockIdx.x * 4u + (threadIdx.x >> 6));
-    if (team >= A.teams) return;                             // (a wave, or the workgroup)
-    const uint32_t C = A.C, P = A.P;
+    __shared__ float add[kL == 0 ? 1 : 256 * kNV * 8];
+    const uint32_t lanes = kL == 0 ? blockDim.x : (uint32_t)kL, lane = kL == 0 ? threadIdx.x : threadIdx.x % lanes, waves = lanes / 64u;
+    const uint32_t team = kL == 0 ? 0u : threadIdx.x / lanes, C = A.C, P = A.P;
     const float inv = 1.0f / (float)C;
-    uint32_t row, end;                                       // the team's rows
+    uint32_t row, end, step;                                 // the team's rows
     if (kWhole) {
-        row = (uint32_t)((uint64_t)team * A.B / A.teams) * P;
-        end = (uint32_t)((uint64_t)(team + 1u) * A.B / A.teams) * P;
+        const uint64_t t = (uint64_t)blockIdx.x * kTeams + team, n = (uint64_t)A.groups * kTeams;
+        row = (uint32_t)(t * A.B / n) * P;
+        end = (uint32_t)((t + 1u) * A.B / n) * P;
+        step = 1u;
     } else {
-        const uint32_t z = team / A.parts, part = team - z * A.parts;
-        row = z * P + (uint32_t)((uint64_t)part * P / A.parts);
+        const uint32_t z = blockIdx.x / A.parts, part = blockIdx.x - z * A.parts;
+        row = z * P + (uint32_t)((uint64_t)part * P / A.parts) + team;
         end = z * P + (uint32_t)((uint64_t)(part + 1u) * P / A.parts);
+        step = kTeams;
     }
     float ga[kNV][8];
     int n[kNV];
@@ -231,7 +234,7 @@ __global__ __launch_bounds__(kWide ? 512 : 256) void k_layer_norm_backward(NormA
         widen8(load8(A.gamma + (lane + i * lanes) * 8u, n[i]), ga[i]);
     }
     constexpr int kS = kWhole ? kNV : 1;
-    float cg[kNV][8] = {}, cb[kNV][8] = {};                  // column sums of the sample (or of its part)
+    float cg[kNV][8] = {}, cb[kNV][8] = {};                  // column sums of the sample (or of the team's rows of it)
     float gg[kS][8] = {}, gs[kS][8] = {}, bg[kS][8] = {}, bs[kS][8] = {};
     Raw8<T> dy[kRows][kNV];
     RowIn<T, kKept> in[kRows][kNV];
@@ -239,7 +242,7 @@ __global__ __launch_bounds__(kWide ? 512 : 256) void k_layer_norm_backward(NormA
     auto request = [&](uint32_t at) {
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
-            const uint64_t q = min(at + (uint32_t)r, end - 1u);          // (rows past the end are the last one again, and not used)
+            const uint64_t q = at + r * step < end ? at + r * step : at;   // (rows past the end are the first one again, and not used)
 #pragma unroll
             for (int i = 0; i < kNV; ++i) {
                 dy[r][i] = load8(static_cast<const T*>(A.dy) + q * C + (lane + i * lanes) * 8u, n[i]);
@@ -251,18 +254,18 @@ __global__ __launch_bounds__(kWide ? 512 : 256) void k_layer_norm_backward(NormA
     };
     uint32_t turn = 0, left = P;                             // rows until the sample is complete
     if (row < end) request(row);
-    for (; row < end; row += kRows) {
+    for (; row < end; row += kRows * step) {
         float d[kRows][kNV][8], h[kRows][kNV][8], rs[kRows], v[2 * kRows];
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
             rs[r] = rstd[r];
             float a = 0.f, b = 0.f;
-            const float live = row + (uint32_t)r < end ? 1.f : 0.f;
+            const bool live = row + r * step < end;
 #pragma unroll
             for (int i = 0; i < kNV; ++i) {
                 widen8(dy[r][i], d[r][i]);
                 row_xhat<T, kKept>(in[r][i], mean[r], rstd[r], n[i], h[r][i]);
-                if (live != 0.f) {                           // (uniform)
+                if (live) {                                  // (the same in a team)
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
                         cb[i][k] += d[r][i][k];
@@ -278,7 +281,7 @@ __global__ __launch_bounds__(kWide ? 512 : 256) void k_layer_norm_backward(NormA
             }
             v[2 * r] = a;
             v[2 * r + 1] = b;
-            if (kWhole && live != 0.f && --left == 0) {      // square the sample's sums into s, add them into g, clear
+            if (kWhole && live && --left == 0) {             // square the sample's sums into s, add them into g, clear
                 left = P;
 #pragma unroll
                 for (int i = 0; i < kS; ++i)
@@ -292,14 +295,14 @@ __global__ __launch_bounds__(kWide ? 512 : 256) void k_layer_norm_backward(NormA
                     }
             }
         }
-        if (row + kRows < end) request(row + kRows);
-        team_sums<2 * kRows, kWide>(v, sh[turn], waves);
+        if (row + kRows * step < end) request(row + kRows * step);
+        team_sums<2 * kRows, kL>(v, sh[turn], waves);
         turn ^= 1u;
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
-            if (row + (uint32_t)r >= end) break;
+            if (row + r * step >= end) break;
             const float a = v[2 * r] * inv, b = v[2 * r + 1] * inv;
-            T* out = static_cast<T*>(A.dx) + (uint64_t)(row + (uint32_t)r) * C;
+            T* out = static_cast<T*>(A.dx) + (uint64_t)(row + r * step) * C;
 #pragma unroll
             for (int i = 0; i < kNV; ++i) {
                 float o[8];
@@ -309,19 +312,38 @@ __global__ __launch_bounds__(kWide ? 512 : 256) void k_layer_norm_backward(NormA
             }
         }
     }
-    float* out = A.partial + (size_t)team * (kWhole ? 4u : 2u) * C;
+    float* out = A.partial + (size_t)blockIdx.x * (kWhole ? 4u : 2u) * C;
+    auto leave = [&](const float (&x)[kNV][8], uint32_t plane) {           // the teams' sums in order, by the first team
+        float sum[kNV][8];
 #pragma unroll
-    for (int i = 0; i < kNV; ++i) {
-        const uint32_t e = (lane + i * lanes) * 8u;
-        if (kWhole) {
-            store8(out + e, gg[i < kS ? i : 0], n[i]);
-            store8(out + C + e, gs[i < kS ? i : 0], n[i]);
-            store8(out + 2 * (size_t)C + e, bg[i < kS ? i : 0], n[i]);
-            store8(out + 3 * (size_t)C + e, bs[i < kS ? i : 0], n[i]);
-        } else {
-            store8(out + e, cg[i], n[i]);
-            store8(out + C + e, cb[i], n[i]);
+        for (int i = 0; i < kNV; ++i)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum[i][k] = x[i][k];
+        if (kL != 0) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < kNV; ++i)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) add[(i * 8 + k) * 256u + threadIdx.x] = x[i][k];
+            __syncthreads();
+            if (team != 0u) return;
+            for (uint32_t t = 1; t < kTeams; ++t)
+#pragma unroll
+                for (int i = 0; i < kNV; ++i)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) sum[i][k] += add[(i * 8 + k) * 256u + t * lanes + lane];
         }
+#pragma unroll
+        for (int i = 0; i < kNV; ++i) store8(out + (size_t)plane * C + (lane + i * lanes) * 8u, sum[i], n[i]);
+    };
+    if constexpr (kWhole) {
+        leave(gg, 0);
+        leave(gs, 1);
+        leave(bg, 2);
+        leave(bs, 3);
+    } else {
+        leave(cg, 0);
+        leave(cb, 1);
     }
 }
 
@@ -330,11 +352,11 @@ __global__ __launch_bounds__(kWide ? 512 : 256) void k_layer_norm_backward(NormA
 template <typename T, bool kKept>
 __global__ __launch_bounds__(1024) void k_layer_norm_backward_long(NormArgs A) {
     __shared__ float sh[2][kMaxWaves][2];
-    const uint32_t lanes = blockDim.x, lane = threadIdx.x, team = blockIdx.x, C = A.C;
+    const uint32_t lanes = blockDim.x, lane = threadIdx.x, C = A.C;
     const float inv = 1.0f / (float)C;
-    const uint32_t z = team / A.parts, part = team % A.parts;
+    const uint32_t z = blockIdx.x / A.parts, part = blockIdx.x % A.parts;
     const uint32_t p0 = (uint32_t)((uint64_t)part * A.P / A.parts), p1 = (uint32_t)((uint64_t)(part + 1u) * A.P / A.parts);
-    float *cg = A.partial + (size_t)team * 2u * C, *cb = cg + C;
+    float *cg = A.partial + (size_t)blockIdx.x * 2u * C, *cb = cg + C;
     uint32_t turn = 0;
     for (uint32_t p = p0; p < p1; ++p) {
         const uint64_t row = (uint64_t)z * A.P + p;
@@ -368,7 +390,7 @@ __global__ __launch_bounds__(1024) void k_layer_norm_backward_long(NormArgs A) {
                 store8(cb + e, sb, n);
                 store8(static_cast<T*>(A.dx) + row * C + e, o, n);
             }
-            if (turns == 0) team_sums<2, true>(v, sh[turn], lanes / 64u);
+            if (turns == 0) team_sums<2, 0>(v, sh[turn], lanes / 64u);
         }
         turn ^= 1u;
     }
@@ -376,10 +398,10 @@ __global__ __launch_bounds__(1024) void k_layer_norm_backward_long(NormArgs A) {
 
 // Adds the teams' partial sums in a fixed order: a workgroup takes 64 columns of one of the two vectors (blockIdx.y: gamma, beta),
 // four a lane, and its 64 groups of 16 lanes share the partial sums between them.
-//   whole samples: planes g, s, summed over the teams.
+//   whole samples: planes g, s, summed over the workgroups that left them.
 //   parts: the parts of a sample are added before the square.  Groups take samples of their own if there are 64 or more; below,
 //   several groups share a sample's parts.
-__global__ __launch_bounds__(1024) void k_layer_norm_sums(const float* __restrict__ partial, uint32_t teams, uint32_t B, uint32_t parts, uint32_t C,
+__global__ __launch_bounds__(1024) void k_layer_norm_sums(const float* __restrict__ partial, uint32_t groups, uint32_t B, uint32_t parts, uint32_t C,
                                                           int whole, float c, float* __restrict__ g_gamma, float* __restrict__ s_gamma,
                                                           float* __restrict__ g_beta, float* __restrict__ s_beta) {
     constexpr uint32_t kGroups = 64;
@@ -399,7 +421,7 @@ __global__ __launch_bounds__(1024) void k_layer_norm_sums(const float* __restric
         const float* at = partial + (size_t)(2u * vec) * C + col;
         const size_t step = 4 * (size_t)C;
 #pragma unroll 4
-        for (uint32_t t = group; t < teams; t += kGroups) { g += load(at + t * step); s += load(at + t * step + C); }
+        for (uint32_t t = group; t < groups; t += kGroups) { g += load(at + t * step); s += load(at + t * step + C); }
     } else {
         const float* at = partial + (size_t)vec * C + col;
         const size_t step = 2 * (size_t)C;
@@ -448,23 +470,36 @@ __global__ __launch_bounds__(1024) void k_layer_norm_sums(const float* __restric
 }
 
 // ---- launches ---------------------------------------------------------------------------------------------------------------
-static uint32_t row_lanes(uint32_t C, uint32_t pieces_per_lane) { return ((C + 7) / 8 + pieces_per_lane * 64 - 1) / (pieces_per_lane * 64) * 64; }
+// A team: the fewest lanes (8, 16, 32, 64) that hold a row with a piece each, 64 with two pieces, or a workgroup (`group`) of as many
+// waves as it takes with two pieces a lane (with one: `single`).  held: rows of up to 8192 elements.
+struct Team { uint32_t lanes; bool group, single, held; };
+static Team team_of(uint32_t C, bool single) {
+    const uint32_t pieces = (C + 7) / 8, each = single ? 64u : 128u;
+    Team t = {64u, pieces > each, single, pieces <= 1024u};
+    if (t.group) t.lanes = t.held ? (pieces + each - 1) / each * 64u : 1024u;
+    else if (pieces <= 64u) { t.single = true; t.lanes = pieces <= 8u ? 8u : pieces <= 16u ? 16u : pieces <= 32u ? 32u : 64u; }
+    return t;
+}
 
 int launch_layer_norm(int dtype, const void* x, uint64_t R, uint32_t C, const float* gamma, const float* beta, float eps, void* y, float* mean,
                       float* rstd, int8_t* codes, uint8_t* exps, hipStream_t stream) {
     if (R > 0x7FFFFFFFull) { set_error("vgc_layer_norm: %llu rows exceed the launch limit", (unsigned long long)R); return VGC_ERR_SIZE; }
-    const uint32_t pieces = (C + 7) / 8, rows = (uint32_t)R;
-    // Rows a wave holds are taken by waves, longer ones (up to 8192 elements) by workgroups; teams: four waves to a SIMD, which is what
-    // the loads in flight need.  One piece a lane rather than two where a row has to itself what there is of the chip anyway.
-    const bool one = pieces <= 64u || (rows <= 1024u && pieces > 64u && pieces <= 512u);
-    const uint32_t lanes = row_lanes(C, one ? 1 : 2), teams = std::min(rows, 4096u / (lanes / 64u));
-    const bool wide = lanes > 64u;
-#define VGC_LAUNCH(T, NV, WIDE, KEEP) hipLaunchKernelGGL((k_layer_norm<T, NV, WIDE, KEEP>), dim3((WIDE) ? teams : (teams + 3) / 4), dim3((WIDE) ? lanes : 256u), 0, \
-        stream, (const T*)x, rows, C, (WIDE) ? teams : (teams + 3) / 4 * 4, gamma, beta, eps, (T*)y, mean, rstd, codes, exps)
+    // Teams: four waves' worth to a SIMD, which is what the loads in flight need.  One piece a lane where a row has to itself what there is
+    // of the chip anyway.
+    const uint32_t rows = (uint32_t)R;
+    const Team t = team_of(C, rows <= 1024u && C <= 4096u);
+    const uint32_t each = t.group ? 1u : 256u / t.lanes, want = t.group ? 4096u / (t.lanes / 64u) : 1024u;
+    const uint32_t groups = std::min((rows + each - 1) / each, want);
+#define VGC_LAUNCH(T, NV, L, KEEP) hipLaunchKernelGGL((k_layer_norm<T, NV, L, KEEP>), dim3(groups), dim3(t.group ? t.lanes : 256u), 0, stream, \
+        (const T*)x, rows, C, groups * each, gamma, beta, eps, (T*)y, mean, rstd, codes, exps)
 #define VGC_SHAPE(T, KEEP) do { \
-        if (pieces > 1024u) hipLaunchKernelGGL((k_layer_norm_long<T, KEEP>), dim3(rows), dim3(1024), 0, stream, (const T*)x, C, gamma, beta, eps, (T*)y, mean, rstd, codes, exps); \
-        else if (!wide) { if (one) VGC_LAUNCH(T, 1, false, KEEP); else VGC_LAUNCH(T, 2, false, KEEP); } \
-        else { if (one) VGC_LAUNCH(T, 1, true, KEEP); else VGC_LAUNCH(T, 2, true, KEEP); } } while (0)
+        if (!t.held) hipLaunchKernelGGL((k_layer_norm_long<T, KEEP>), dim3(rows), dim3(1024), 0, stream, (const T*)x, C, gamma, beta, eps, (T*)y, mean, rstd, codes, exps); \
+        else if (t.group) { if (t.single) VGC_LAUNCH(T, 1, 0, KEEP); else VGC_LAUNCH(T, 2, 0, KEEP); } \
+        else if (!t.single) VGC_LAUNCH(T, 2, 64, KEEP); \
+        else if (t.lanes == 64u) VGC_LAUNCH(T, 1, 64, KEEP); \
+        else if (t.lanes == 32u) VGC_LAUNCH(T, 1, 32, KEEP); \
+        else if (t.lanes == 16u) VGC_LAUNCH(T, 1, 16, KEEP); \
+        else VGC_LAUNCH(T, 1, 8, KEEP); } while (0)
     if (dtype == VGC_F32) { if (codes) VGC_SHAPE(float, true); else VGC_SHAPE(float, false); }
     else { if (codes) VGC_SHAPE(uint16_t, true); else VGC_SHAPE(uint16_t, false); }
 #undef VGC_SHAPE
@@ -472,47 +507,52 @@ int launch_layer_norm(int dtype, const void* x, uint64_t R, uint32_t C, const fl
     return hip_check(hipGetLastError(), "launch k_layer_norm");
 }
 
-struct NormTeams { uint32_t lanes, parts, teams; bool wide, whole, held; };
-// About 2048 waves' worth of teams: two to a SIMD, which is what the loads in flight need.  Samples are taken whole when there
-// are enough of them, else cut into parts of at least four rows.
-static NormTeams norm_teams(uint32_t B, uint32_t P, uint32_t C) {
-    NormTeams t;
-    const uint32_t pieces = (C + 7) / 8;
-    t.held = pieces <= 1024u;
-    t.lanes = t.held ? row_lanes(C, pieces <= 64u ? 1 : 2) : 1024u;
-    t.wide = t.lanes > 64u;
-    const uint32_t want = 2048u / (t.lanes / 64u);
-    t.whole = t.held && B >= want;
-    if (t.whole) { t.parts = 1; t.teams = want; return t; }
-    t.parts = std::min((want + B - 1) / B, (P + 3) / 4);
-    t.teams = B * t.parts;
-    return t;
+struct NormPlan { Team team; uint32_t parts, groups; bool whole; };
+// About 2048 waves: two to a SIMD, which is what the loads in flight need.  A sample is cut into parts of at least two rows a team (four
+// for a workgroup); samples are taken whole where a team then has no more rows to go through, one after another.
+static NormPlan norm_plan(uint32_t B, uint32_t P, uint32_t C) {
+    NormPlan L;
+    L.team = team_of(C, false);
+    const uint32_t teams = L.team.group ? 1u : 256u / L.team.lanes, want = L.team.group ? 2048u / (L.team.lanes / 64u) : 512u;
+    const uint32_t rows = L.team.group ? 4u : 2u * teams;    // of a part at least
+    auto up = [](uint64_t a, uint64_t b) { return (a + b - 1) / b; };
+    L.parts = (uint32_t)std::min(up(want, B), up(P, rows));
+    L.whole = L.team.held && P * up(B, (uint64_t)want * teams) <= up(P, (uint64_t)teams * L.parts) * up((uint64_t)B * L.parts, want);
+    if (L.whole) L.parts = 1;
+    L.groups = L.whole ? (uint32_t)std::min<uint64_t>(up(B, teams), want) : B * L.parts;
+    return L;
 }
 size_t layer_norm_backward_workspace_bytes(uint32_t B, uint32_t P, uint32_t C) {
-    const NormTeams t = norm_teams(B, P, C);
-    return (size_t)t.teams * (t.whole ? 4u : 2u) * C * sizeof(float);
+    const NormPlan L = norm_plan(B, P, C);
+    return (size_t)L.groups * (L.whole ? 4u : 2u) * C * sizeof(float);
 }
 
 int launch_layer_norm_backward(int dtype, const void* dy, const void* x, const float* mean, const int8_t* codes, const uint8_t* exps,
                                const float* rstd, const float* gamma, uint32_t B, uint32_t P, uint32_t C, float c, void* dx, float* g_gamma,
                                float* s_gamma, float* g_beta, float* s_beta, void* workspace, hipStream_t stream) {
-    const NormTeams t = norm_teams(B, P, C);
-    const NormArgs A = {dy, x, mean, rstd, gamma, codes, exps, dx, static_cast<float*>(workspace), B, P, C, t.parts, t.teams};
-    const dim3 grid(t.wide ? t.teams : (t.teams + 3) / 4), block(t.wide ? t.lanes : 256u);
-    const uint32_t pieces = (C + 7) / 8;
-#define VGC_LAUNCH(T, KEPT, NV, ROWS, WIDE, WHOLE) hipLaunchKernelGGL((k_layer_norm_backward<T, KEPT, NV, ROWS, WIDE, WHOLE>), grid, block, 0, stream, A)
+    const NormPlan L = norm_plan(B, P, C);
+    const Team& t = L.team;
+    const NormArgs A = {dy, x, mean, rstd, gamma, codes, exps, dx, static_cast<float*>(workspace), B, P, C, L.parts, L.groups};
+    const dim3 grid(L.groups), block(t.group ? t.lanes : 256u);
+    // (two rows in flight; one where whole samples of two pieces a lane leave no registers for two)
+#define VGC_LAUNCH(T, KEPT, NV, LANES) do { \
+        if (L.whole) hipLaunchKernelGGL((k_layer_norm_backward<T, KEPT, NV, NV == 2 ? 1 : 2, LANES, true>), grid, block, 0, stream, A); \
+        else hipLaunchKernelGGL((k_layer_norm_backward<T, KEPT, NV, 2, LANES, false>), grid, block, 0, stream, A); } while (0)
 #define VGC_SHAPE(T, KEPT) do { \
         if (!t.held) hipLaunchKernelGGL((k_layer_norm_backward_long<T, KEPT>), grid, block, 0, stream, A); \
-        else if (pieces <= 64u) { if (t.whole) VGC_LAUNCH(T, KEPT, 1, 2, false, true); else VGC_LAUNCH(T, KEPT, 1, 2, false, false); } \
-        else if (!t.wide) { if (t.whole) VGC_LAUNCH(T, KEPT, 2, 2, false, true); else VGC_LAUNCH(T, KEPT, 2, 2, false, false); } \
-        else { if (t.whole) VGC_LAUNCH(T, KEPT, 2, 2, true, true); else VGC_LAUNCH(T, KEPT, 2, 2, true, false); } } while (0)
+        else if (t.group) VGC_LAUNCH(T, KEPT, 2, 0); \
+        else if (!t.single) VGC_LAUNCH(T, KEPT, 2, 64); \
+        else if (t.lanes == 64u) VGC_LAUNCH(T, KEPT, 1, 64); \
+        else if (t.lanes == 32u) VGC_LAUNCH(T, KEPT, 1, 32); \
+        else if (t.lanes == 16u) VGC_LAUNCH(T, KEPT, 1, 16); \
+        else VGC_LAUNCH(T, KEPT, 1, 8); } while (0)
     if (dtype == VGC_F32) { if (codes) VGC_SHAPE(float, true); else VGC_SHAPE(float, false); }
     else { if (codes) VGC_SHAPE(uint16_t, true); else VGC_SHAPE(uint16_t, false); }
 #undef VGC_SHAPE
 #undef VGC_LAUNCH
     int rc = hip_check(hipGetLastError(), "launch k_layer_norm_backward");
     if (rc != VGC_OK) return rc;
-    hipLaunchKernelGGL(k_layer_norm_sums, dim3((C + 63) / 64, 2), dim3(1024), 0, stream, (const float*)workspace, t.teams, B, t.parts, C, (int)t.whole,
+    hipLaunchKernelGGL(k_layer_norm_sums, dim3((C + 63) / 64, 2), dim3(1024), 0, stream, (const float*)workspace, L.groups, B, L.parts, C, (int)L.whole,
                        c, g_gamma, s_gamma, g_beta, s_beta);
     return hip_check(hipGetLastError(), "launch k_layer_norm_sums");
 }

@@ -160,5 +160,18 @@ __device__ __forceinline__ float wave_sum(float x) {
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
 }
 
+// The same over groups of kL lanes (8, 16, 32 or 64), in each of them.
+template <int kL> __device__ __forceinline__ float lanes_sum(float x) {
+    if constexpr (kL == 64) return wave_sum(x);
+#define VGC_DPP_ADD(ctrl) x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), ctrl, 0xF, 0xF, false))
+    VGC_DPP_ADD(0xB1);                                       // lanes 1 apart
+    VGC_DPP_ADD(0x4E);                                       // 2 apart
+    VGC_DPP_ADD(0x141);                                      // the other four of eight
+    if constexpr (kL >= 16) VGC_DPP_ADD(0x140);              // the other eight of a row
+#undef VGC_DPP_ADD
+    if constexpr (kL >= 32) x += __shfl_xor(x, 16);
+    return x;
+}
+
 }  // namespace vgc
 #endif

@@ -36,7 +36,7 @@ def _depth(C):
 
 
 FORWARD = [(1, 1), (5, 1), (3, 2), (7, 7), (4, 8), (9, 33), (130, 64), (1, 512), (3, 513), (2050, 520), (128, 1000), (2100, 1000), (2049, 2048), (2048, 4096),
-           (5, 1025), (3, 4097), (2, 8200), (2, 32768), (2, 32776), (3, 40001)]
+           (5, 1025), (3, 4097), (1000, 16), (300, 100), (77, 250), (40000, 24), (5, 4100), (2000, 5000), (2, 8192), (2, 8200), (2, 32768), (2, 32776), (3, 40001)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -105,7 +105,8 @@ def test_constant_rows_large_means_and_rows_that_are_not_finite(dev):
 
 
 BACKWARD = [(1, 1, 1), (1, 1, 7), (2, 3, 8), (1, 300, 33), (3, 1, 100), (5, 49, 64), (2100, 1, 64), (2050, 3, 40), (2060, 2, 520), (1100, 2, 1030), (520, 2, 4096), (300, 1, 8192),
-            (16, 5, 1000), (17, 64, 2048), (1, 1025, 512), (4, 9, 4096), (2, 3, 8192), (2, 5, 8200), (1, 2, 20001)]
+            (16, 5, 1000), (17, 64, 2048), (1, 1025, 512), (4, 9, 4096), (2, 3, 8192), (2, 5, 8200), (1, 2, 20001),
+            (3, 70, 16), (2, 130, 100), (40, 9, 250), (9, 700, 24), (17000, 1, 30), (4200, 1, 200), (600, 8, 128), (70, 33, 300)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
