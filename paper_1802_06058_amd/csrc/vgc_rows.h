@@ -173,5 +173,16 @@ template <int kL> __device__ __forceinline__ float lanes_sum(float x) {
     return x;
 }
 
+// The largest over groups of 16 or 32 lanes, in each of them (a NaN does not count).
+template <int kL> __device__ __forceinline__ void lanes_max(float& x) {
+#define VGC_DPP_MAX(ctrl) x = fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), ctrl, 0xF, 0xF, false)))
+    VGC_DPP_MAX(0xB1);
+    VGC_DPP_MAX(0x4E);
+    VGC_DPP_MAX(0x141);
+    VGC_DPP_MAX(0x140);
+#undef VGC_DPP_MAX
+    if constexpr (kL >= 32) x = fmaxf(x, __shfl_xor(x, 16));
+}
+
 }  // namespace vgc
 #endif

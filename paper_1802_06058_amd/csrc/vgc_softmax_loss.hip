@@ -315,6 +315,13 @@ __global__ __launch_bounds__(kThinWaves * 64) void k_logits_thin(ThinArgs R, Los
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t columns = kForward ? A.N : A.Lq, tiles_n = (columns + kN - 1) / kN, id = xcd_contiguous(blockIdx.x, gridDim.x);
     const uint32_t m0 = id / tiles_n * kN, n0 = id % tiles_n * kN;
+    // a thread's result: consecutive classes; what it takes besides the logit is asked for first
+    const uint32_t v = tid % kN, col = tid / kN;
+    const bool mine = tid < kN * kN && m0 + v < A.V && n0 + col < columns;
+    ColumnOf C;
+    int64_t t = -1;
+    if constexpr (kForward) { if (mine) t = A.target[n0 + col]; }
+    else if (mine) C = column_of(n0 + col, A);
     const uint32_t z0 = n0 / A.at.Pp, first = min(z0 * A.at.P + min(n0 - z0 * A.at.Pp, A.at.P), A.N);
     const __amdgpu_buffer_rsrc_t rw = bounded(R.w, (uint64_t)m0 * R.ldw * sizeof(T), min(A.V - m0, kN) * R.ldw * (uint32_t)sizeof(T));
     const __amdgpu_buffer_rsrc_t rx = bounded(R.x, (uint64_t)first * R.ldx * sizeof(T), min(A.N - first, kN) * R.ldx * (uint32_t)sizeof(T));
@@ -373,13 +380,14 @@ __global__ __launch_bounds__(kThinWaves * 64) void k_logits_thin(ThinArgs R, Los
     };
     Step S[kAhead];
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) S[i] = request(wave * kStep + i * kTurn);
+    for (int i = 0; i < kAhead; ++i)
+        if (wave * kStep + i * kTurn < A.K) S[i] = request(wave * kStep + i * kTurn);
     for (uint32_t k = wave * kStep; k < A.K; k += kAhead * kTurn)
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
             if (k + i * kTurn >= A.K) break;
             multiply(S[i], k + i * kTurn);
-            S[i] = request(k + (kAhead + i) * kTurn);
+            if (k + (kAhead + i) * kTurn < A.K) S[i] = request(k + (kAhead + i) * kTurn);
         }
     // result i of a lane: class 4 (lane / 16) + i, column lane % 16
 #pragma unroll
@@ -389,30 +397,23 @@ __global__ __launch_bounds__(kThinWaves * 64) void k_logits_thin(ThinArgs R, Los
 #pragma unroll
             for (int i = 0; i < 4; ++i) sh[wave][m * 16 + (lane >> 4) * 4 + i][n * 16 + (lane & 15u)] = sum[m][n][i];
     __syncthreads();
-    const uint32_t v = tid % kN, col = tid / kN;             // a thread's result: consecutive classes
     float z = 0.f;
     if (tid < kN * kN) {
 #pragma unroll
         for (uint32_t w = 0; w < kThinWaves; ++w) z += sh[w][v][col];
     }
-    if constexpr (kForward) {
-        __syncthreads();
-        if (tid < kN * kN) sh[0][v][col] = z;
-        __syncthreads();
-        const uint32_t token = n0 + tid;
-        if (tid >= kN || token >= A.N) return;
+    if constexpr (kForward) {                                // 16 kT consecutive lanes hold a token's classes
         const float kNone = -__builtin_inff();
-        const uint32_t classes = min(kN, A.V - m0);
-        const int64_t t = A.target[token] - A.v0 - m0;
-        float top = kNone, total = 0.f;
-        for (uint32_t c = 0; c < classes; ++c) top = fmaxf(top, sh[0][c][tid]);
+        if (!mine) z = kNone;
+        float top = z;
+        lanes_max<kN>(top);
         const float base = top == kNone ? 0.f : top;
-        for (uint32_t c = 0; c < classes; ++c) total += exp_of(sh[0][c][tid] - base);
-        A.partial[(size_t)(A.block0 + m0 / kN) * A.N + token] = make_float2(top, total);
-        if (t >= 0 && t < (int64_t)classes) A.picked[token] = sh[0][t][tid];
+        const float total = lanes_sum<kN>(exp_of(z - base));
+        if (!mine) return;
+        if (v == 0u) A.partial[(size_t)(A.block0 + m0 / kN) * A.N + n0 + col] = make_float2(top, total);
+        if (t == A.v0 + m0 + v) A.picked[n0 + col] = z;
     } else {
-        if (tid >= kN * kN || m0 + v >= A.V || n0 + col >= A.Lq) return;
-        const ColumnOf C = column_of(n0 + col, A);
+        if (!mine) return;
         const float d = C.d(z, m0 + v);
         if (A.d32 && C.row != 0xFFFFFFFFu) A.d32[(size_t)C.row * A.V + m0 + v] = d;
         if (A.dt)
@@ -532,6 +533,43 @@ __global__ __launch_bounds__(kThinWaves * 64) void k_loss_dx_thin(const float* _
 }
 
 // ---- g and s ------------------------------------------------------------------------------------------------------------------
+// Samples of one position, few of them, and few classes: a workgroup takes 64 columns of X by 4 classes, its 16 waves share the samples.
+// Rows that are not asked for count as zeros whatever they hold.
+template <typename T>
+__global__ __launch_bounds__(1024) void k_loss_sums_thin(const float* __restrict__ D, const T* __restrict__ X, const int64_t* __restrict__ target, uint32_t N,
+                                                         uint32_t V, uint32_t H, float c, float* __restrict__ g_out, float* __restrict__ s_out) {
+    __shared__ float sh[2][4][16][64];
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t blocks_v = (V + 3u) / 4u, h = blockIdx.x / blocks_v * 64u + lane, v0 = blockIdx.x % blocks_v * 4u, count = min(4u, V - v0);
+    float g[4] = {}, s[4] = {};
+#pragma unroll 4
+    for (uint32_t n = wave; n < N; n += 16u) {
+        float x = 0.f;
+        if (h < H && target[n] >= 0) {
+            if (sizeof(T) == 4) x = ((const float*)X)[(size_t)n * H + h];
+            else x = __uint_as_float((uint32_t)((const uint16_t*)X)[(size_t)n * H + h] << 16);
+        }
+#pragma unroll
+        for (uint32_t e = 0; e < 4u; ++e) {
+            const float p = x * (e < count ? D[(size_t)n * V + v0 + e] : 0.f);
+            g[e] += p;
+            s[e] = __builtin_fmaf(p, p, s[e]);
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { sh[0][e][wave][lane] = g[e]; sh[1][e][wave][lane] = s[e]; }
+    __syncthreads();
+    if (wave >= 8u) return;                                  // a wave adds one of the eight sums
+    const uint32_t e = wave & 3u, which = wave >> 2;
+    float sum = 0.f;
+#pragma unroll
+    for (uint32_t w = 0; w < 16u; ++w) sum += sh[which][e][w][lane];
+    if (h >= H || e >= count) return;
+    const size_t at = (size_t)(v0 + e) * H + h;
+    if (which) s_out[at] = c * c * sum;
+    else if (g_out) g_out[at] = c * sum;
+}
+
 // k runs over the positions; at a sample's end (every Pp of them) its product is squared into s, added into g, and cleared.
 template <typename Shape>
 __global__ __launch_bounds__(Shape::NW * 64, 2) void k_loss_sums(Matrix Dt, Matrix Xt, uint32_t K, uint32_t Pp, float c, float* __restrict__ g_out,
@@ -703,7 +741,7 @@ struct BackwardPlan {
     LogitsTile tile;
     RowsPlan rows;
     uint32_t planes, piece, Pp, Lq, splits;
-    bool dx_thin, dx_large, sum_planes;
+    bool dx_thin, dx_large, sum_planes, sum_thin;
     size_t x, xt, w, d, d32, d2, out, total;
 };
 static BackwardPlan backward_plan(int dtype, uint32_t B, uint32_t P, uint32_t H, uint32_t V) {
@@ -715,7 +753,8 @@ static BackwardPlan backward_plan(int dtype, uint32_t B, uint32_t P, uint32_t H,
     L.dx_thin = P == 1 && N <= 128u && (uint64_t)V * H <= (4u << 20);
     L.rows = rows_plan(dtype, H, L.tile, !L.dx_thin);
     L.planes = dtype == VGC_F32 ? 3u : P == 1 ? 1u : 2u;
-    // samples of one position: the FC form, from planes where the outputs are what it takes, else (a launch less) from floats
+    // samples of one position: the FC form, from planes where the outputs are what it takes, directly where it is small, else from floats
+    L.sum_thin = P == 1 && N <= 256u && (uint64_t)V * H <= (256u << 10);
     L.sum_planes = P == 1 && dtype == VGC_BF16 && N >= 16u && (uint64_t)V * H >= (4u << 20) && fc_planes_supported(N, 256, H);
     const uint64_t row = 2ull * L.rows.planes * L.rows.Kp, dt = L.dx_thin ? 0 : 2ull * L.planes * L.Lq;
     const uint64_t d32 = P == 1 ? (L.sum_planes ? 12ull : 4ull) * N : 0;
@@ -726,7 +765,7 @@ static BackwardPlan backward_plan(int dtype, uint32_t B, uint32_t P, uint32_t H,
     while (n * L.splits < (dtype == VGC_F32 || L.dx_large ? 256u : 512u) && L.piece / (L.splits * 2u) >= 256u && L.splits < 64u) L.splits *= 2u;
     size_t off = 0;
     L.x = off; if (!L.rows.in_place) off = align_up(off + N * row, 256);
-    L.xt = off; off = align_up(off + (L.sum_planes ? fc_planes_bytes(1, N, H) : P == 1 ? (size_t)N * H * 4 : 2 * (size_t)H * L.rows.planes * L.Lq), 256);
+    L.xt = off; off = align_up(off + (L.sum_planes ? fc_planes_bytes(1, N, H) : L.sum_thin ? 0 : P == 1 ? (size_t)N * H * 4 : 2 * (size_t)H * L.rows.planes * L.Lq), 256);
     L.w = off; if (!L.rows.in_place) off = align_up(off + L.piece * row, 256);
     L.d = off; if (!L.dx_thin) off = align_up(off + 2 * (size_t)L.piece * L.planes * L.Lq, 256);
     L.d32 = off; if (P == 1) off = align_up(off + 4 * (size_t)N * L.piece, 256);
@@ -764,7 +803,7 @@ int launch_softmax_loss_backward(int dtype, const void* X, const void* W, const 
         if ((rc = hip_check(hipGetLastError(), "launch k_planes_columns")) != VGC_OK) return rc;
     } else if (s_out && L.sum_planes) {
         if ((rc = launch_square_planes(dtype, X, target, N, H, xt, stream)) != VGC_OK) return rc;
-    } else if (s_out) {
+    } else if (s_out && !L.sum_thin) {
         const dim3 grid((uint32_t)(((uint64_t)N * ((H + 7u) / 8u) + 255u) / 256u));
         if (dtype == VGC_F32) hipLaunchKernelGGL(k_asked_rows<float>, grid, dim3(256), 0, stream, (const float*)X, target, N, H, (float*)xt);
         else hipLaunchKernelGGL(k_asked_rows<uint16_t>, grid, dim3(256), 0, stream, (const uint16_t*)X, target, N, H, (float*)xt);
@@ -808,6 +847,11 @@ int launch_softmax_loss_backward(int dtype, const void* X, const void* W, const 
         } else if (s_out && L.sum_planes) {
             if ((rc = launch_square_planes(VGC_F32, A.d32, nullptr, N, A.V, ws + L.d2, stream)) != VGC_OK) return rc;
             if ((rc = launch_fc_planes(ws + L.d2, 2, xt, N, A.V, H, c, g, s, stream)) != VGC_OK) return rc;
+        } else if (s_out && L.sum_thin) {
+            const dim3 grid(tiles(H, 64u, A.V, 4u));
+            if (dtype == VGC_F32) hipLaunchKernelGGL(k_loss_sums_thin<float>, grid, dim3(1024), 0, stream, A.d32, (const float*)X, target, N, A.V, H, c, g, s);
+            else hipLaunchKernelGGL(k_loss_sums_thin<uint16_t>, grid, dim3(1024), 0, stream, A.d32, (const uint16_t*)X, target, N, A.V, H, c, g, s);
+            if ((rc = hip_check(hipGetLastError(), "launch k_loss_sums_thin")) != VGC_OK) return rc;
         } else if (s_out) {
             if ((rc = launch_sqgrad(VGC_FC, VGC_F32, A.d32, xt, N, 1, A.V, H, c, g, s, nullptr, 0, stream)) != VGC_OK) return rc;
         }
