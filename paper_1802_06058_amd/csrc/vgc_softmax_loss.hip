@@ -501,25 +501,45 @@ template <typename T>
 __global__ __launch_bounds__(kThinWaves * 64) void k_loss_dx_thin(const float* __restrict__ D, const T* __restrict__ W, uint32_t N, uint32_t V, uint32_t H,
                                                                   T* __restrict__ dX) {
     __shared__ float sh[kThinWaves][16][64];
-    const uint32_t lane = threadIdx.x & 63u, half = lane >> 5, wave = threadIdx.x >> 6;
+    const uint32_t lane = threadIdx.x & 63u, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t tiles_n = (N + kThinDx - 1) / kThinDx, n0 = blockIdx.x % tiles_n * kThinDx, h = blockIdx.x / tiles_n * kThinDx + (lane & 31u);
     const uint32_t n = n0 + (lane & 31u);
     f16v sum = {};
-    for (uint32_t v0 = wave * 8u; v0 < V; v0 += kThinWaves * 8u) {
-        float d[4], w[4];
+    struct Step { float d[4], w[4]; };
+    auto request = [&](uint32_t v0) -> Step {
+        Step S;
+        const uint32_t first = v0 + half * 4u;               // (four of a row's entries at once: one at a time the address units take 20 us)
+        any_f4 d = {0.f, 0.f, 0.f, 0.f};
+        if (n < N && first + 3u < V) d = *reinterpret_cast<const any_f4*>(D + (size_t)n * V + first);
+        else if (n < N)
+            for (uint32_t e = 0; e < 3u; ++e)
+                if (first + e < V) d[e] = D[(size_t)n * V + first + e];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const uint32_t v = v0 + half * 4u + e;
-            d[e] = v < V && n < N ? D[(size_t)n * V + v] : 0.f;
-            w[e] = 0.f;
+            const uint32_t v = first + e;
+            S.d[e] = d[e];
+            S.w[e] = 0.f;
             if (v < V && h < H) {
-                if (sizeof(T) == 4) w[e] = ((const float*)W)[(size_t)v * H + h];
-                else w[e] = __uint_as_float((uint32_t)((const uint16_t*)W)[(size_t)v * H + h] << 16);
+                if (sizeof(T) == 4) S.w[e] = ((const float*)W)[(size_t)v * H + h];
+                else S.w[e] = __uint_as_float((uint32_t)((const uint16_t*)W)[(size_t)v * H + h] << 16);
             }
         }
+        return S;
+    };
+    constexpr uint32_t kTurn = kThinWaves * 8u;
+    constexpr int kAhead = 2;
+    Step S[kAhead];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum = __builtin_amdgcn_mfma_f32_32x32x2f32(d[e], w[e], sum, 0, 0, 0);
-    }
+    for (int i = 0; i < kAhead; ++i)
+        if (wave * 8u + i * kTurn < V) S[i] = request(wave * 8u + i * kTurn);
+    for (uint32_t v0 = wave * 8u; v0 < V; v0 += kAhead * kTurn)
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (v0 + i * kTurn >= V) break;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum = __builtin_amdgcn_mfma_f32_32x32x2f32(S[i].d[e], S[i].w[e], sum, 0, 0, 0);
+            if (v0 + (kAhead + i) * kTurn < V) S[i] = request(v0 + (kAhead + i) * kTurn);
+        }
 #pragma unroll
     for (int i = 0; i < 16; ++i) sh[wave][i][lane] = sum[i];
     __syncthreads();
