@@ -95,8 +95,9 @@ __global__ __launch_bounds__(256) void k_planes_columns(const T* __restrict__ sr
                                                         uint32_t Lq, uint16_t* __restrict__ dst) {
     __shared__ float t[64][65];
     const uint32_t k0 = blockIdx.y * 64u, q0 = blockIdx.x * 64u, col = threadIdx.x & 63u;
-#pragma unroll 4
-    for (uint32_t r = threadIdx.x >> 6; r < 64u; r += 4u) {
+#pragma unroll
+    for (uint32_t i = 0; i < 16u; ++i) {
+        const uint32_t r = i * 4u + (threadIdx.x >> 6);
         const uint32_t row = at.row(q0 + r);
         float x = 0.f;
         if (row != 0xFFFFFFFFu && k0 + col < K && target[row] >= 0) {
@@ -486,6 +487,7 @@ __global__ __launch_bounds__(256) void k_loss_dx_join(const float* __restrict__ 
     const int m = n - i >= 8u ? 8 : (int)(n - i);
     float f[8], g[8];
     widen8(load8(planes + i, m), f);
+#pragma unroll 4
     for (uint32_t s = 1; s < splits; ++s) {
         widen8(load8(planes + s * n + i, m), g);
 #pragma unroll
@@ -644,15 +646,20 @@ static uint32_t up8(uint32_t x) { return (x + 7u) / 8u * 8u; }
 static uint32_t tiles(uint32_t a, uint32_t ta, uint32_t b, uint32_t tb) { return (a + ta - 1) / ta * ((b + tb - 1) / tb); }
 template <typename Shape> static uint32_t tiles(uint32_t m, uint32_t n) { return tiles(m, Shape::BM, n, Shape::BN); }
 
+// The kernel that forms the logits.  Forward times (us, both launches) that the rule goes by:
+//   16 x 16 or 32 x 32 results a workgroup while there are no more workgroups than compute units, so that k is what is shared out: 64
+//     rows, 4096 k, 1000 classes: 13.2, 20.4, slim tiles 24.3; 128 rows: 22.3, 21.2, 25.0; 256 rows, 2000 classes: 70.3, 37.7, 25.6.
+//   slim tiles until there are enough of the others: 16000 classes x 1024 k, 256 rows: slim 18.7, small 20.6, large 28.7; 512 rows: 30.8,
+//     24.8, 30.5; 1024 rows: 50.4, 44.1, 38.9; 64000 classes, 64 rows: 37, 39, 44; 128 rows: 48, 42, 44; 256 rows: 71, 60, 51.
+//   float32: tiles of planes from 2 M logits on, which their laying out has to be paid by: 4000 classes x 1024 k, 512 rows: 73, as floats 86;
+//     16000 x 128: 89 and 89; 4000 x 256: 74 and 47; 64000 x 64: 254 and 204.
 enum class LogitsTile { kLarge, kSmall, kSlim, kCut, kThin, kThinnest };
 static LogitsTile logits_tile(int dtype, uint32_t V, uint32_t N) {
-    if (dtype == VGC_F32 && N > 64u && tiles<Cut>(V, N) >= 128u) return LogitsTile::kCut;
-    if (dtype == VGC_BF16) {
-        if (N > 128u && tiles<Large>(V, N) >= 192u) return LogitsTile::kLarge;
-        if (N > 64u && tiles<Small>(V, N) >= 192u) return LogitsTile::kSmall;
-        if (tiles<Slim>(V, N) >= 128u) return LogitsTile::kSlim;
-    }
-    return tiles(V, 32, N, 32) >= 256u ? LogitsTile::kThin : LogitsTile::kThinnest;
+    if (tiles(V, 16, N, 16) <= 256u) return LogitsTile::kThinnest;
+    if (dtype == VGC_F32) return N > 64u && (uint64_t)V * N >= 2000000u ? LogitsTile::kCut : LogitsTile::kThin;
+    if (tiles(V, 32, N, 32) <= 256u) return LogitsTile::kThin;
+    if (N > 128u && tiles<Large>(V, N) >= 192u) return LogitsTile::kLarge;
+    return N > 64u && tiles<Small>(V, N) >= 320u ? LogitsTile::kSmall : LogitsTile::kSlim;
 }
 static bool is_thin(LogitsTile t) { return t == LogitsTile::kThin || t == LogitsTile::kThinnest; }
 // Classes a partial pair of the forward pass covers: those of a wave, in the thin kernels of a workgroup.
@@ -770,7 +777,11 @@ static BackwardPlan backward_plan(int dtype, uint32_t B, uint32_t P, uint32_t H,
     L.Pp = P == 1 ? 1u : (P + 15u) / 16u * 16u;              // (a sample's end falls on a phase's)
     L.Lq = up8(B * L.Pp);
     L.tile = logits_tile(dtype, V, L.Lq);
-    L.dx_thin = P == 1 && N <= 128u && (uint64_t)V * H <= (4u << 20);
+    // dX of few rows from floats, without planes or partial sums, while that is little work (us with the logits: bfloat16, 1000 classes, 64 x
+    // 4096: 29 and 31 by tiles, 128 x 4096: 47 and 39, 4000 classes, 16 x 512: 48 and 19; float32, 1000 x 128 x 4096: 61 and 90, 4000 x 256 x
+    // 2048: 155 and 143)
+    const uint64_t work = (uint64_t)N * V * H;
+    L.dx_thin = P == 1 && (uint64_t)N * V <= (64u << 20) && (dtype == VGC_F32 ? work <= 2000000000u : V <= 1024u && work <= (256u << 20));
     L.rows = rows_plan(dtype, H, L.tile, !L.dx_thin);
     L.planes = dtype == VGC_F32 ? 3u : P == 1 ? 1u : 2u;
     // samples of one position: the FC form, from planes where the outputs are what it takes, directly where it is small, else from floats
@@ -779,7 +790,9 @@ static BackwardPlan backward_plan(int dtype, uint32_t B, uint32_t P, uint32_t H,
     const uint64_t row = 2ull * L.rows.planes * L.rows.Kp, dt = L.dx_thin ? 0 : 2ull * L.planes * L.Lq;
     const uint64_t d32 = P == 1 ? (L.sum_planes ? 12ull : 4ull) * N : 0;
     L.piece = L.dx_thin ? V : piece_of(V, row + dt + d32, 2048ull << 20);
-    L.dx_large = dtype == VGC_BF16 && L.Lq > 128u && tiles<Large>(L.Lq, H) >= 32u;
+    // large tiles where there is work for them (16000 classes, 2048 x 2048: 265 us and 277 by small ones, 512 x 4096: 160 and 158, 256 x 512:
+    // 51 and 39; 4000 classes, 4096 x 4096: 257 and 287)
+    L.dx_large = dtype == VGC_BF16 && L.Lq > 128u && (uint64_t)L.Lq * H * V >= 50000000000u;
     const uint32_t n = dtype == VGC_F32 ? tiles<Cut>(L.Lq, H) : L.dx_large ? tiles<Large>(L.Lq, H) : tiles<Small>(L.Lq, H);
     L.splits = 1;
     while (n * L.splits < (dtype == VGC_F32 || L.dx_large ? 256u : 512u) && L.piece / (L.splits * 2u) >= 256u && L.splits < 64u) L.splits *= 2u;
