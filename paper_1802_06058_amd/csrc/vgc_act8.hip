@@ -41,11 +41,12 @@ __global__ __launch_bounds__(256) void k_act8_encode(const T* __restrict__ x, ui
     for (int u = 0; u < kUnits; ++u) {
         at[u] = walk.at(u * 256u + threadIdx.x);
         n[u] = at[u].row < R ? (int)C - (int)(at[u].piece * 8u) : 0;     // (0 or less: a lane past the end, whose block's others may not be)
-        raw[u] = load8(x + at[u].row * C + at[u].piece * 8u, n[u]);
+        raw[u] = load8(x + at[u].row * C + at[u].piece * 8u, n[u], rows_at_end(at[u].row, R));
     }
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
         float f[8];
+        clip8(raw[u], n[u]);
         widen8(raw[u], f);
         uint32_t top = act8_top(f);
         if (kLanes == 4) top = four_lanes_max(top);
@@ -69,7 +70,7 @@ __global__ __launch_bounds__(256) void k_act8_decode(const int8_t* __restrict__ 
     for (int u = 0; u < kUnits; ++u) {
         at[u] = walk.at(u * 256u + threadIdx.x);
         n[u] = at[u].row < R ? (int)C - (int)(at[u].piece * 8u) : 0;
-        v[u] = load_codes(codes + at[u].row * C + at[u].piece * 8u, n[u]);
+        v[u] = load_codes(codes + at[u].row * C + at[u].piece * 8u, n[u], rows_at_end(at[u].row, R));   // (what is past n is not stored)
         field[u] = n[u] > 0 ? exps[at[u].row * (per_row / kLanes) + at[u].piece / kLanes] : 0u;
     }
 #pragma unroll

@@ -66,7 +66,7 @@ __global__ __launch_bounds__(kL == 0 ? 512 : 256) void k_layer_norm(const T* __r
     float ga[kNV][8], be[kNV][8];
     auto request = [&](uint32_t r) {
 #pragma unroll
-        for (int i = 0; i < kNV; ++i) raw[i] = load8(x + (uint64_t)r * C + (lane + i * lanes) * 8u, n[i]);
+        for (int i = 0; i < kNV; ++i) raw[i] = load8(x + (uint64_t)r * C + (lane + i * lanes) * 8u, n[i], rows_at_end(r, R));
     };
 #pragma unroll
     for (int i = 0; i < kNV; ++i) n[i] = (int)C - (int)((lane + i * lanes) * 8u);
@@ -80,6 +80,7 @@ __global__ __launch_bounds__(kL == 0 ? 512 : 256) void k_layer_norm(const T* __r
         float f[kNV][8], v[1] = {0.f};
 #pragma unroll
         for (int i = 0; i < kNV; ++i) {
+            if (C % 8u != 0) clip8(raw[i], n[i]);
             widen8(raw[i], f[i]);
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[0] += f[i][k];
@@ -181,19 +182,20 @@ struct NormArgs {
 };
 
 template <typename T, bool kKept>
-__device__ __forceinline__ RowIn<T, kKept> row_load(const NormArgs& A, uint64_t row, uint32_t piece, int n) {
+__device__ __forceinline__ RowIn<T, kKept> row_load(const NormArgs& A, uint64_t row, uint32_t piece, int n, bool at_end) {
     RowIn<T, kKept> r;
     if constexpr (kKept) {
-        r.q = load_codes(A.codes + row * A.C + piece * 8u, n);
+        r.q = load_codes(A.codes + row * A.C + piece * 8u, n, at_end);
         r.field = n > 0 ? A.exps[row * ((A.C + kAct8Block - 1) / kAct8Block) + piece / 4u] : 0u;
     } else {
-        r.x = load8(static_cast<const T*>(A.x) + row * A.C + piece * 8u, n);
+        r.x = load8(static_cast<const T*>(A.x) + row * A.C + piece * 8u, n, at_end);
     }
     return r;
 }
 template <typename T, bool kKept>
-__device__ __forceinline__ void row_xhat(const RowIn<T, kKept>& r, float mean, float rstd, int n, float (&f)[8]) {
+__device__ __forceinline__ void row_xhat(RowIn<T, kKept>& r, float mean, float rstd, int n, bool ragged, float (&f)[8]) {
     if constexpr (kKept) {
+        if (ragged) clip_codes(r.q, n);
         act8_values(r.q, r.field, f);
     } else {
         widen8(r.x, f);
@@ -214,6 +216,8 @@ __global__ __launch_bounds__(kL == 0 ? 512 : 256) void k_layer_norm_backward(Nor
     const uint32_t lanes = kL == 0 ? blockDim.x : (uint32_t)kL, lane = kL == 0 ? threadIdx.x : threadIdx.x % lanes, waves = lanes / 64u;
     const uint32_t team = kL == 0 ? 0u : threadIdx.x / lanes, C = A.C, P = A.P;
     const float inv = 1.0f / (float)C;
+    const uint64_t rows = (uint64_t)A.B * P;
+    const bool ragged = C % 8u != 0;                         // (a row's last piece is short)
     uint32_t row, end, step;                                 // the team's rows
     if (kWhole) {
         const uint64_t t = (uint64_t)blockIdx.x * kTeams + team, n = (uint64_t)A.groups * kTeams;
@@ -245,8 +249,8 @@ __global__ __launch_bounds__(kL == 0 ? 512 : 256) void k_layer_norm_backward(Nor
             const uint64_t q = at + r * step < end ? at + r * step : at;   // (rows past the end are the first one again, and not used)
 #pragma unroll
             for (int i = 0; i < kNV; ++i) {
-                dy[r][i] = load8(static_cast<const T*>(A.dy) + q * C + (lane + i * lanes) * 8u, n[i]);
-                in[r][i] = row_load<T, kKept>(A, q, lane + i * lanes, n[i]);
+                dy[r][i] = load8(static_cast<const T*>(A.dy) + q * C + (lane + i * lanes) * 8u, n[i], rows_at_end(q, rows));
+                in[r][i] = row_load<T, kKept>(A, q, lane + i * lanes, n[i], rows_at_end(q, rows));
             }
             mean[r] = kKept ? 0.f : A.mean[q];
             rstd[r] = A.rstd[q];
@@ -263,8 +267,9 @@ __global__ __launch_bounds__(kL == 0 ? 512 : 256) void k_layer_norm_backward(Nor
             const bool live = row + r * step < end;
 #pragma unroll
             for (int i = 0; i < kNV; ++i) {
+                if (ragged) clip8(dy[r][i], n[i]);
                 widen8(dy[r][i], d[r][i]);
-                row_xhat<T, kKept>(in[r][i], mean[r], rstd[r], n[i], h[r][i]);
+                row_xhat<T, kKept>(in[r][i], mean[r], rstd[r], n[i], ragged, h[r][i]);
                 if (live) {                                  // (the same in a team)
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
@@ -368,7 +373,8 @@ __global__ __launch_bounds__(1024) void k_layer_norm_backward_long(NormArgs A) {
                 const int n = (int)(C - e);
                 float d[8], h[8], ga[8], o[8];
                 widen8(load8(static_cast<const T*>(A.dy) + row * C + e, n), d);
-                row_xhat<T, kKept>(row_load<T, kKept>(A, row, e / 8u, n), mean, rstd, n, h);
+                RowIn<T, kKept> in = row_load<T, kKept>(A, row, e / 8u, n, true);
+                row_xhat<T, kKept>(in, mean, rstd, n, false, h);
                 widen8(load8(A.gamma + e, n), ga);
                 if (turns == 0) {
 #pragma unroll

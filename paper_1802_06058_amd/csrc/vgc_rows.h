@@ -8,8 +8,10 @@
 namespace vgc {
 
 // A lane's eight consecutive elements of a row, widened to float.  Rows begin at any multiple of the element's size (a row of
-// odd length moves the next one), which one load of 16 bytes takes on this target; the last piece of a row may be short and is
-// read and written element by element.  n: elements of the piece that exist (8 or more: all).
+// odd length moves the next one), which one load of 16 bytes takes on this target.  n: elements of the piece that exist (8 or more:
+// all, 0 or less: none).  The last piece of a row may be short.  It is written element by element; reading it so makes the wave wait for
+// what it asked for before (rows of 1023 bfloat16: backward 193 us, of 1024: 102), so where eight elements are there to be read all the
+// same (rows follow: at_end false) they are read, and clipped when they are used.
 typedef uint32_t any_u4 __attribute__((ext_vector_type(4), aligned(2)));
 typedef float any_f4 __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t any_u2 __attribute__((ext_vector_type(2), aligned(1)));
@@ -18,28 +20,40 @@ template <typename T> struct Raw8;                           // as it is in memo
 template <> struct Raw8<uint16_t> { uint32_t w[4]; };
 template <> struct Raw8<float> { float f[8]; };
 
-__device__ __forceinline__ Raw8<uint16_t> load8(const uint16_t* p, int n) {
+__device__ __forceinline__ Raw8<uint16_t> load8(const uint16_t* p, int n, bool at_end = true) {
     Raw8<uint16_t> r = {};
-    if (n >= 8) {
+    if (n >= 8 || (n > 0 && !at_end)) {
         const any_u4 v = *reinterpret_cast<const any_u4*>(p);
         for (int i = 0; i < 4; ++i) r.w[i] = v[i];
-    } else {
+    }
+    if (__builtin_expect(n > 0 && n < 8 && at_end, 0)) {     // (a branch of its own: lanes without a piece do not enter it)
         for (int i = 0; i < 7; ++i)
             if (i < n) r.w[i >> 1] |= (uint32_t)p[i] << (16 * (i & 1));
     }
     return r;
 }
-__device__ __forceinline__ Raw8<float> load8(const float* p, int n) {
+__device__ __forceinline__ Raw8<float> load8(const float* p, int n, bool at_end = true) {
     Raw8<float> r = {};
-    if (n >= 8) {
+    if (n >= 8 || (n > 0 && !at_end)) {
         const any_f4 a = *reinterpret_cast<const any_f4*>(p), b = *reinterpret_cast<const any_f4*>(p + 4);
         for (int i = 0; i < 4; ++i) { r.f[i] = a[i]; r.f[4 + i] = b[i]; }
-    } else {
+    }
+    if (__builtin_expect(n > 0 && n < 8 && at_end, 0)) {
         for (int i = 0; i < 7; ++i)
             if (i < n) r.f[i] = p[i];
     }
     return r;
 }
+__device__ __forceinline__ void clip8(Raw8<uint16_t>& r, int n) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.w[i] &= n >= 2 * i + 2 ? 0xFFFFFFFFu : n == 2 * i + 1 ? 0xFFFFu : 0u;
+}
+__device__ __forceinline__ void clip8(Raw8<float>& r, int n) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r.f[i] = i < n ? r.f[i] : 0.f;
+}
+// Whether eight elements from any place of this row lie inside the rows' array.
+__device__ __forceinline__ bool rows_at_end(uint64_t row, uint64_t R) { return row + 8u >= R; }
 __device__ __forceinline__ void widen8(const Raw8<uint16_t>& r, float (&f)[8]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(r.w[i] << 16); f[2 * i + 1] = __uint_as_float(r.w[i] & 0xFFFF0000u); }
@@ -79,12 +93,18 @@ __device__ __forceinline__ void store8(float* p, const float (&f)[8], int n) {
             if (i < n) p[i] = f[i];
     }
 }
-__device__ __forceinline__ any_u2 load_codes(const int8_t* p, int n) {
+__device__ __forceinline__ any_u2 load_codes(const int8_t* p, int n, bool at_end = true) {
     any_u2 v = {0u, 0u};
-    if (n >= 8) return *reinterpret_cast<const any_u2*>(p);
-    for (int i = 0; i < 7; ++i)
-        if (i < n) v[i >> 2] |= (uint32_t)(uint8_t)p[i] << (8 * (i & 3));
+    if (n >= 8 || (n > 0 && !at_end)) v = *reinterpret_cast<const any_u2*>(p);
+    if (__builtin_expect(n > 0 && n < 8 && at_end, 0)) {
+        for (int i = 0; i < 7; ++i)
+            if (i < n) v[i >> 2] |= (uint32_t)(uint8_t)p[i] << (8 * (i & 3));
+    }
     return v;
+}
+__device__ __forceinline__ void clip_codes(any_u2& v, int n) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) v[i] &= n >= 4 * i + 4 ? 0xFFFFFFFFu : n <= 4 * i ? 0u : (1u << (8 * (n - 4 * i))) - 1u;
 }
 __device__ __forceinline__ void store_codes(int8_t* p, any_u2 v, int n) {
     if (n >= 8) {
