@@ -490,11 +490,11 @@ static Team team_of(uint32_t C, bool single) {
 int launch_layer_norm(int dtype, const void* x, uint64_t R, uint32_t C, const float* gamma, const float* beta, float eps, void* y, float* mean,
                       float* rstd, int8_t* codes, uint8_t* exps, hipStream_t stream) {
     if (R > 0x7FFFFFFFull) { set_error("vgc_layer_norm: %llu rows exceed the launch limit", (unsigned long long)R); return VGC_ERR_SIZE; }
-    // Teams: four waves' worth to a SIMD, which is what the loads in flight need.  One piece a lane where a row has to itself what there is
-    // of the chip anyway.
+    // Sixteen waves a compute unit, which is what the loads in flight need, in whole workgroups a compute unit.  One piece a lane where a row
+    // has to itself what there is of the chip anyway.
     const uint32_t rows = (uint32_t)R;
     const Team t = team_of(C, rows <= 1024u && C <= 4096u);
-    const uint32_t each = t.group ? 1u : 256u / t.lanes, want = t.group ? 4096u / (t.lanes / 64u) : 1024u;
+    const uint32_t each = t.group ? 1u : 256u / t.lanes, want = 256u * (t.group ? std::max(1u, 16u / (t.lanes / 64u)) : 4u);
     const uint32_t groups = std::min((rows + each - 1) / each, want);
 #define VGC_LAUNCH(T, NV, L, KEEP) hipLaunchKernelGGL((k_layer_norm<T, NV, L, KEEP>), dim3(groups), dim3(t.group ? t.lanes : 256u), 0, stream, \
         (const T*)x, rows, C, groups * each, gamma, beta, eps, (T*)y, mean, rstd, codes, exps)
@@ -514,18 +514,28 @@ int launch_layer_norm(int dtype, const void* x, uint64_t R, uint32_t C, const fl
 }
 
 struct NormPlan { Team team; uint32_t parts, groups; bool whole; };
-// About 2048 waves: two to a SIMD, which is what the loads in flight need.  A sample is cut into parts of at least two rows a team (four
-// for a workgroup); samples are taken whole where a team then has no more rows to go through, one after another.
+// Workgroups come in multiples of the 256 compute units, or just below one: a few beyond it take as long as all of the next (48 samples of
+// 1257 x 2500 kept rows: 432 workgroups of five waves 177 us, 624 of them 226).  As many times 256 as are resident, 16 waves a compute unit (8
+// with two pieces a lane, 12 with whole samples; a workgroup's waves counted as a power of two, as they share out the SIMDs), while a
+// team has 48 rows to go through for the partial sums it leaves (whole samples: 96); up to 8 waves a compute unit while it has 8.
+// A sample is cut into parts of at least two rows a team (four for a workgroup); samples are taken whole where a team then has no more
+// rows to go through, one after another.
 static NormPlan norm_plan(uint32_t B, uint32_t P, uint32_t C) {
     NormPlan L;
-    L.team = team_of(C, false);
-    const uint32_t teams = L.team.group ? 1u : 256u / L.team.lanes, want = L.team.group ? 2048u / (L.team.lanes / 64u) : 512u;
-    const uint32_t rows = L.team.group ? 4u : 2u * teams;    // of a part at least
+    L.team = team_of(C, C <= 4096u);                         // (one piece a lane: 60336 rows of 2048 bfloat16 176 -> 166 us, of 4096 367 -> 300)
     auto up = [](uint64_t a, uint64_t b) { return (a + b - 1) / b; };
-    L.parts = (uint32_t)std::min(up(want, B), up(P, rows));
-    L.whole = L.team.held && P * up(B, (uint64_t)want * teams) <= up(P, (uint64_t)teams * L.parts) * up((uint64_t)B * L.parts, want);
+    const uint32_t teams = L.team.group ? 1u : 256u / L.team.lanes, of = L.team.group ? L.team.lanes / 64u : 4u;
+    const uint32_t waves = of <= 1u ? 1u : of == 2u ? 2u : of <= 4u ? 4u : of <= 8u ? 8u : 16u;
+    auto times = [&](uint32_t resident, uint64_t rows) {     // workgroups a compute unit
+        const uint64_t most = resident / waves, some = 8u / waves, each = (uint64_t)B * P / (teams * 256u);
+        return (uint32_t)std::max<uint64_t>(1, std::max(std::min(most, each / rows), std::min(std::min(most, some), each / 8u)));
+    };
+    const uint32_t rows = L.team.group ? 4u : 2u * teams;    // of a part at least
+    const uint32_t want = 256u * times(L.team.single ? 16u : 8u, 48u), want_whole = 256u * times(L.team.single ? 12u : 8u, 96u);
+    L.parts = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(want / B, up(P, rows)));
+    L.whole = L.team.held && P * up(B, (uint64_t)want_whole * teams) <= up(P, (uint64_t)teams * L.parts) * up((uint64_t)B * L.parts, want);
     if (L.whole) L.parts = 1;
-    L.groups = L.whole ? (uint32_t)std::min<uint64_t>(up(B, teams), want) : B * L.parts;
+    L.groups = L.whole ? (uint32_t)std::min<uint64_t>(up(B, teams), want_whole) : B * L.parts;
     return L;
 }
 size_t layer_norm_backward_workspace_bytes(uint32_t B, uint32_t P, uint32_t C) {
@@ -546,6 +556,7 @@ int launch_layer_norm_backward(int dtype, const void* dy, const void* x, const f
         else hipLaunchKernelGGL((k_layer_norm_backward<T, KEPT, NV, 2, LANES, false>), grid, block, 0, stream, A); } while (0)
 #define VGC_SHAPE(T, KEPT) do { \
         if (!t.held) hipLaunchKernelGGL((k_layer_norm_backward_long<T, KEPT>), grid, block, 0, stream, A); \
+        else if (t.group && t.single) VGC_LAUNCH(T, KEPT, 1, 0); \
         else if (t.group) VGC_LAUNCH(T, KEPT, 2, 0); \
         else if (!t.single) VGC_LAUNCH(T, KEPT, 2, 64); \
         else if (t.lanes == 64u) VGC_LAUNCH(T, KEPT, 1, 64); \
