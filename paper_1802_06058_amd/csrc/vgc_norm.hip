@@ -50,7 +50,9 @@ __device__ __forceinline__ void keep_act8(const float (&f)[8], uint32_t C, uint3
 // ---- forward --------------------------------------------------------------------------------------------------------------
 // A team takes rows team, team + teams, ..: its part of gamma and beta stays in registers, and the next row is on its way while the
 // present one is reduced and stored.  Teams: kL lanes each, or (kL = 0) the workgroup.  (A row a workgroup, gamma and beta read for each:
-// 16384 x 4096 bfloat16 67 us; so 53.)
+// 16384 x 4096 bfloat16 68.5 us; so 52.6.)
+// 16384 x 4096 bfloat16: 50 us, 5.4 TB/s of x and y; kept in 8 bits too and decoded again by vgc_act8_decode 107, 4.3 TB/s.  128 x 1000
+// float32: 8 us a call, which is the call's own time.
 template <typename T, int kNV, int kL, bool kKeep>
 __global__ __launch_bounds__(kL == 0 ? 512 : 256) void k_layer_norm(const T* __restrict__ x, uint32_t R, uint32_t C, uint32_t teams, const float* __restrict__ gamma,
                                                                 const float* __restrict__ beta, float eps, T* __restrict__ y,
@@ -207,7 +209,8 @@ __device__ __forceinline__ void row_xhat(RowIn<T, kKept>& r, float mean, float r
 // Teams: kL lanes each, or (kL = 0) the workgroup.  kRows rows are in flight at a time, the next ones' loads issued before the
 // present ones are reduced.  kWhole: a team takes samples whole, number t of n teams those of [t B / n, (t + 1) B / n), and keeps g
 // and s of its columns; the workgroup leaves four planes (g and s of gamma, of beta), its teams' added.  Else a workgroup takes part
-// w % parts of sample w / parts, its teams rows in turn, and leaves its two column sums.
+// w % parts of sample w / parts, its teams rows in turn, and leaves its two column sums.  Bound by memory: 16 samples of 1024 x 4096
+// bfloat16 from the kept rows 72 us with the sums, 4.7 TB/s of dy, codes and dx; 32 of 49 x 2048 float32 from x 15.7, of which 8 are the call's.
 template <typename T, bool kKept, int kNV, int kRows, int kL, bool kWhole>
 __global__ __launch_bounds__(kL == 0 ? 512 : 256) void k_layer_norm_backward(NormArgs A) {
     constexpr uint32_t kTeams = kL == 0 ? 1u : 256u / (kL == 0 ? 1 : kL);
@@ -490,17 +493,19 @@ static Team team_of(uint32_t C, bool single) {
 int launch_layer_norm(int dtype, const void* x, uint64_t R, uint32_t C, const float* gamma, const float* beta, float eps, void* y, float* mean,
                       float* rstd, int8_t* codes, uint8_t* exps, hipStream_t stream) {
     if (R > 0x7FFFFFFFull) { set_error("vgc_layer_norm: %llu rows exceed the launch limit", (unsigned long long)R); return VGC_ERR_SIZE; }
-    // Sixteen waves a compute unit, which is what the loads in flight need, in whole workgroups a compute unit.  One piece a lane where a row
-    // has to itself what there is of the chip anyway.
+    // Sixteen waves a compute unit, which is what the loads in flight need, in whole workgroups a compute unit.  Many rows that are not
+    // kept: one piece a lane (us; bfloat16, two pieces and one: 16384 x 4096 52.6 and 49.9, 60000 x 2048 94.5 and 91.4, but 4096 x 4096 13.5
+    // and 14.9, 16384 x 4096 kept 107.3 and 108.5).
     const uint32_t rows = (uint32_t)R;
-    const Team t = team_of(C, rows <= 1024u && C <= 4096u);
+    const Team t = team_of(C, !codes && rows >= 16384u && C <= 4096u);
     const uint32_t each = t.group ? 1u : 256u / t.lanes, want = 256u * (t.group ? std::max(1u, 16u / (t.lanes / 64u)) : 4u);
     const uint32_t groups = std::min((rows + each - 1) / each, want);
 #define VGC_LAUNCH(T, NV, L, KEEP) hipLaunchKernelGGL((k_layer_norm<T, NV, L, KEEP>), dim3(groups), dim3(t.group ? t.lanes : 256u), 0, stream, \
         (const T*)x, rows, C, groups * each, gamma, beta, eps, (T*)y, mean, rstd, codes, exps)
 #define VGC_SHAPE(T, KEEP) do { \
         if (!t.held) hipLaunchKernelGGL((k_layer_norm_long<T, KEEP>), dim3(rows), dim3(1024), 0, stream, (const T*)x, C, gamma, beta, eps, (T*)y, mean, rstd, codes, exps); \
-        else if (t.group) { if (t.single) VGC_LAUNCH(T, 1, 0, KEEP); else VGC_LAUNCH(T, 2, 0, KEEP); } \
+        else if (t.group && t.single) VGC_LAUNCH(T, 1, 0, false); \
+        else if (t.group) VGC_LAUNCH(T, 2, 0, KEEP); \
         else if (!t.single) VGC_LAUNCH(T, 2, 64, KEEP); \
         else if (t.lanes == 64u) VGC_LAUNCH(T, 1, 64, KEEP); \
         else if (t.lanes == 32u) VGC_LAUNCH(T, 1, 32, KEEP); \
@@ -519,7 +524,7 @@ struct NormPlan { Team team; uint32_t parts, groups; bool whole; };
 // with two pieces a lane, 12 with whole samples; a workgroup's waves counted as a power of two, as they share out the SIMDs), while a
 // team has 48 rows to go through for the partial sums it leaves (whole samples: 96); up to 8 waves a compute unit while it has 8.
 // A sample is cut into parts of at least two rows a team (four for a workgroup); samples are taken whole where a team then has no more
-// rows to go through, one after another.
+// rows to go through, one after another (16384 samples of one row of 2048 bfloat16: whole 53 us, apart 317).
 static NormPlan norm_plan(uint32_t B, uint32_t P, uint32_t C) {
     NormPlan L;
     L.team = team_of(C, C <= 4096u);                         // (one piece a lane: 60336 rows of 2048 bfloat16 176 -> 166 us, of 4096 367 -> 300)
@@ -550,7 +555,8 @@ int launch_layer_norm_backward(int dtype, const void* dy, const void* x, const f
     const Team& t = L.team;
     const NormArgs A = {dy, x, mean, rstd, gamma, codes, exps, dx, static_cast<float*>(workspace), B, P, C, L.parts, L.groups};
     const dim3 grid(L.groups), block(t.group ? t.lanes : 256u);
-    // (two rows in flight; one where whole samples of two pieces a lane leave no registers for two)
+    // (two rows in flight: 16 x 1024 x 4096 bfloat16 kept 72 us, with one 82; one where whole samples of two pieces a lane leave no registers
+    // for two)
 #define VGC_LAUNCH(T, KEPT, NV, LANES) do { \
         if (L.whole) hipLaunchKernelGGL((k_layer_norm_backward<T, KEPT, NV, NV == 2 ? 1 : 2, LANES, true>), grid, block, 0, stream, A); \
         else hipLaunchKernelGGL((k_layer_norm_backward<T, KEPT, NV, 2, LANES, false>), grid, block, 0, stream, A); } while (0)

@@ -576,8 +576,8 @@ def _rows(t, what):
 
 
 def _need_all(wanted):
-    """The checks of _Args on a call's tensors, given as (tensor or None, elements, dtype, name): one loop without calls of its own (five
-    tensors 2.4 us less a call), and only when one of them does not fit, the report."""
+    """The checks of _Args on a call's tensors, given as (tensor or None, elements, dtype, name): one loop without calls of its own (three
+    tensors 0.8 us less a call), and only when one of them does not fit, the report."""
     index = wanted[0][0].get_device()
     for t, numel, dtype, _ in wanted:
         if t is not None and (t.dtype is not dtype or t.numel() < numel or t.get_device() != index or not t.is_contiguous()):
