@@ -225,8 +225,14 @@ template <typename Shape> struct ColumnTile : Shape {
     static_assert(BM >= 128 && BN >= 128, "four units a row");
 
     // acc += a[k, m0 ..] b[k, n0 ..] over rows k in [k0, k1).  Columns past a row's end read its successor's, or zeros.
+    // after(step, ks) as for the loop; steps count from k0.
     static __device__ __forceinline__ void run(f16v (&acc)[Shape::MT][Shape::NT], uint8_t* sh, const Matrix& A, const Matrix& B, uint32_t m0,
                                                uint32_t n0, uint32_t k0, uint32_t k1) {
+        run(acc, sh, A, B, m0, n0, k0, k1, [](uint32_t, int) {});
+    }
+    template <typename After>
+    static __device__ __forceinline__ void run(f16v (&acc)[Shape::MT][Shape::NT], uint8_t* sh, const Matrix& A, const Matrix& B, uint32_t m0,
+                                               uint32_t n0, uint32_t k0, uint32_t k1, After after) {
         const uint32_t lane = threadIdx.x & 63u, wave = Shape::wave();
         const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)sh) + wave * 1024u;
         i4v ra[PA], rb[PB];
@@ -269,7 +275,7 @@ template <typename Shape> struct ColumnTile : Shape {
         };
         auto fa = [&](uint32_t stage, int q, int ks, int t) { return read(sh + stage + q * Shape::kPlaneA + fA[t] + ks * 16 * BM * 2, 4 * BM * 2); };
         auto fb = [&](uint32_t stage, int q, int ks, int t) { return read(sh + stage + q * Shape::kPlaneB + fB[t] + ks * 16 * BN * 2, 4 * BN * 2); };
-        Shape::loop(acc, sh, steps, issue, fa, fb, [](uint32_t, int) {});
+        Shape::loop(acc, sh, steps, issue, fa, fb, after);
     }
 };
 

@@ -193,7 +193,7 @@ template <int kL> __device__ __forceinline__ float lanes_sum(float x) {
     return x;
 }
 
-// The largest over groups of 16 or 32 lanes, in each of them (a NaN does not count).
+// The largest over groups of 16, 32 or 64 lanes, in each of them (a NaN does not count).
 template <int kL> __device__ __forceinline__ void lanes_max(float& x) {
 #define VGC_DPP_MAX(ctrl) x = fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), ctrl, 0xF, 0xF, false)))
     VGC_DPP_MAX(0xB1);
@@ -202,6 +202,7 @@ template <int kL> __device__ __forceinline__ void lanes_max(float& x) {
     VGC_DPP_MAX(0x140);
 #undef VGC_DPP_MAX
     if constexpr (kL >= 32) x = fmaxf(x, __shfl_xor(x, 16));
+    if constexpr (kL >= 64) x = fmaxf(x, __shfl_xor(x, 32));
 }
 
 }  // namespace vgc

@@ -13,7 +13,8 @@
 // the loop of vgc_gemm.h.
 //
 // Precision.  bfloat16 inputs: products are exact, sums float32.  D is rounded to bfloat16 for dX, which is rounded to bfloat16
-// itself; for g and s, which are float32, a second plane holds the rest, 16 significant bits in all.  float32 inputs: every operand
+// itself; for g and s, which are float32, a second plane holds the rest, 16 significant bits in all (both relative to the sample's
+// largest weight).  A third plane for the target's entries alone was tried: its registers are not there, k_loss_sums spilled.  float32 inputs: every operand
 // is cut exactly into three planes of 8 bits and a product is formed from the six pairs of planes that reach 2^-24 of it; few rows
 // are multiplied as floats instead.
 #include <algorithm>
@@ -88,6 +89,31 @@ struct Positions {
     }
 };
 
+// What D of a sample is relative to while it is rounded: with bfloat16 inputs its largest weight, so that the entry of a missed class,
+// which is most of what g, s and dX consist of, is -1 in bfloat16 as it is, and not a weight's rounding that all positions of a
+// sample share (2 x 38 positions, weights 1/38, 44209 classes: s 4.4e-6 off, so 2.1e-6).  of: by sample, or (own: samples of one position)
+// the weights themselves; NULL: 1.
+__device__ __forceinline__ float scale_from(float top) { return top > 0.f && top < __builtin_inff() ? top : 1.f; }
+struct Scales {
+    const float* of;
+    bool own;
+    __device__ __forceinline__ float at(uint32_t z) const { return !of ? 1.f : own ? scale_from(fabsf(of[z])) : of[z]; }
+};
+__global__ __launch_bounds__(1024) void k_loss_scales(const float* __restrict__ weight, const int64_t* __restrict__ target, uint32_t P, float* __restrict__ scales) {
+    __shared__ float sh[16];
+    float top = 0.f;
+    for (uint32_t p = threadIdx.x; p < P; p += 1024u) {
+        const size_t row = (size_t)blockIdx.x * P + p;
+        if (target[row] >= 0) top = fmaxf(top, fabsf(weight[row]));
+    }
+    lanes_max<64>(top);
+    if ((threadIdx.x & 63u) == 0u) sh[threadIdx.x >> 6] = top;
+    __syncthreads();
+    if (threadIdx.x != 0u) return;
+    for (int w = 1; w < 16; ++w) top = fmaxf(top, sh[w]);
+    scales[blockIdx.x] = scale_from(top);
+}
+
 // X by columns: dst[k][q] = src[row(q)][k], zero where there is no position and in rows that are not asked for.  A workgroup turns 64
 // positions by 64 columns in LDS.
 template <typename T>
@@ -146,6 +172,7 @@ struct LossArgs {
     // backward
     int64_t V_all;
     const float *lse, *weight;
+    Scales scales;
     uint16_t* dt;             // D by classes, rows of Lq, planes `plane` apart
     uint64_t plane;
     uint32_t planes;
@@ -202,18 +229,20 @@ __device__ __forceinline__ void finish_forward(f16v (&acc)[MT][NT], uint32_t m0,
 // What the backward pass knows of a column: its row of X, and how a logit becomes an entry of D.
 struct ColumnOf {
     uint32_t row, at;         // the target's class in the piece, or ~0
-    float lse, w;
+    float lse, w, scale;      // w: relative to the sample's scale
     bool asked;
-    __device__ __forceinline__ float d(float z, uint32_t v) const { return asked ? (exp_of(z - lse) - (v == at ? 1.f : 0.f)) * w : 0.f; }
+    __device__ __forceinline__ float d(float z, uint32_t v) const { return of(z - lse, v); }
+    __device__ __forceinline__ float of(float z, uint32_t v) const { return asked ? (exp_of(z) - (v == at ? 1.f : 0.f)) * w : 0.f; }
 };
 __device__ __forceinline__ ColumnOf column_of(uint32_t q, const LossArgs& A) {
-    ColumnOf C = {A.at.row(q), 0xFFFFFFFFu, 0.f, 0.f, false};
+    ColumnOf C = {A.at.row(q), 0xFFFFFFFFu, 0.f, 0.f, 1.f, false};
     if (C.row == 0xFFFFFFFFu) return C;
     const int64_t t = A.target[C.row], tl = t - A.v0;
     C.asked = t >= 0;
     if (!C.asked) return C;
     C.lse = A.lse[C.row];
-    C.w = t >= A.V_all ? __uint_as_float(0x7FC00000u) : A.weight ? A.weight[C.row] : 1.f;     // (not a class: the gradients say so)
+    C.scale = A.scales.at(q / A.at.Pp);
+    C.w = t >= A.V_all ? __uint_as_float(0x7FC00000u) : A.weight ? A.weight[C.row] / C.scale : 1.f;       // (not a class: the gradients say so)
     if (tl >= 0 && tl < (int64_t)A.V) C.at = (uint32_t)tl;
     return C;
 }
@@ -236,7 +265,7 @@ __device__ __forceinline__ void logits_to_d(f16v (&acc)[MT][NT], uint32_t m0, ui
             for (int m = 0; m < MT; ++m)
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    if (m0 + class_of(m, i, half) < A.V) out[class_of(m, i, half)] = acc[m][n][i];
+                    if (m0 + class_of(m, i, half) < A.V) out[class_of(m, i, half)] = acc[m][n][i] * C.scale;
         }
     }
 }
@@ -273,6 +302,30 @@ __device__ __forceinline__ void store_by_classes(f16v (&acc)[MT][NT], uint8_t* t
     }
 }
 
+// Products far below the sum that a matrix instruction adds them to come out too small rather than rounded: with the six products of
+// planes that float32 operands bring for every 16 k, sums shrink as they grow (bfloat16 operands, whose products are of one
+// size, show none of it).  Taken out of the instructions' reach every 128 k, a sum is rounded as float sums are.
+template <typename Shape, bool kOn> struct InParts {
+    __device__ __forceinline__ void after(f16v (&)[Shape::MT][Shape::NT], uint32_t, int) {}
+    __device__ __forceinline__ void end(f16v (&)[Shape::MT][Shape::NT]) {}
+};
+template <typename Shape> struct InParts<Shape, true> {
+    f16v total[Shape::MT][Shape::NT] = {};
+    __device__ __forceinline__ void after(f16v (&acc)[Shape::MT][Shape::NT], uint32_t step, int ks) {
+        if (ks != Shape::KS - 1 || (step + 1u) * Shape::BK % 128u != 0u) return;
+#pragma unroll
+        for (int m = 0; m < Shape::MT; ++m)
+#pragma unroll
+            for (int n = 0; n < Shape::NT; ++n) { total[m][n] += acc[m][n]; acc[m][n] = f16v{}; }
+    }
+    __device__ __forceinline__ void end(f16v (&acc)[Shape::MT][Shape::NT]) {
+#pragma unroll
+        for (int m = 0; m < Shape::MT; ++m)
+#pragma unroll
+            for (int n = 0; n < Shape::NT; ++n) acc[m][n] += total[m][n];
+    }
+};
+
 // 65536 classes x 2048 k, 4096 bfloat16 rows: forward 0.88-1.0 ms, 1.1-1.25 PFLOP/s, by the clock that the card keeps under the load
 // (1.73-1.78 GHz; with zeros for inputs 0.73), LDS free of conflicts; as D, 65521 classes, 1.13-1.27 ms, with two planes, 1.07 GB, to be stored
 // at the end of every tile.
@@ -285,10 +338,13 @@ __global__ __launch_bounds__(Shape::NW * 64, 2) void k_logits(LossArgs A) {
     f16v acc[Shape::MT][Shape::NT] = {};
     // the tile's rows of X lie between those of its first and of its last position
     const uint32_t z0 = n0 / A.at.Pp, first = min(z0 * A.at.P + min(n0 - z0 * A.at.Pp, A.at.P), A.N);
+    // float32: in parts of 128 k (600 rows of 4096 channels, logits of 14: lse 1.2e-4 too small, so 1e-6 off)
+    InParts<Shape, Shape::PA == 3> parts;
     RowTile<Shape>::run(acc, sh, A.w, A.x, m0, first, Shape::BN, [&](uint32_t n) {
         const uint32_t row = A.at.row(n0 + n);
         return row == 0xFFFFFFFFu ? row : row - first;
-    }, A.K, [](uint32_t, int) {});
+    }, A.K, [&](uint32_t step, int ks) { parts.after(acc, step, ks); });
+    parts.end(acc);
     const uint32_t wm = m0 + Shape::wave_m(), wn = n0 + Shape::wave_n();
     if (kForward) {
         if (wm < A.V) finish_forward(acc, wm, wn, A);
@@ -401,14 +457,14 @@ __global__ __launch_bounds__(kThinWaves * 64) void k_logits_thin(ThinArgs R, Los
 #pragma unroll
             for (int i = 0; i < 4; ++i) sh[wave][m * 16 + (lane >> 4) * 4 + i][n * 16 + (lane & 15u)] = sum[m][n][i];
     __syncthreads();
-    float z = 0.f;
+    double whole = 0.;                                       // (the sixteen in float: dX of 3 rows of 3095 float32 2.1e-6 off, so 1.3e-6)
     if (tid < kN * kN) {
 #pragma unroll
-        for (uint32_t w = 0; w < kThinWaves; ++w) z += sh[w][v][col];
+        for (uint32_t w = 0; w < kThinWaves; ++w) whole += (double)sh[w][v][col];
     }
     if constexpr (kForward) {                                // 16 kT consecutive lanes hold a token's classes
         const float kNone = -__builtin_inff();
-        if (!mine) z = kNone;
+        const float z = mine ? (float)whole : kNone;
         float top = z;
         lanes_max<kN>(top);
         const float base = top == kNone ? 0.f : top;
@@ -418,8 +474,8 @@ __global__ __launch_bounds__(kThinWaves * 64) void k_logits_thin(ThinArgs R, Los
         if (t == A.v0 + m0 + v) A.picked[n0 + col] = z;
     } else {
         if (!mine) return;
-        const float d = C.d(z, m0 + v);
-        if (A.d32 && C.row != 0xFFFFFFFFu) A.d32[(size_t)C.row * A.V + m0 + v] = d;
+        const float d = C.of((float)(whole - (double)C.lse), m0 + v);
+        if (A.d32 && C.row != 0xFFFFFFFFu) A.d32[(size_t)C.row * A.V + m0 + v] = d * C.scale;
         if (A.dt)
             for (uint32_t q = 0; q < A.planes; ++q)
                 A.dt[q * A.plane + (size_t)(m0 + v) * A.Lq + n0 + col] = (uint16_t)plane_of<sizeof(T) == 4>(d, 0.f, q);
@@ -456,7 +512,7 @@ __global__ __launch_bounds__(1024) void k_loss_join(const float2* __restrict__ p
 // Part `split` of the sum over the piece's classes, added to what the pieces before have left in the part's own plane [N, H].
 // Bound by the matrix instructions: 4096 x 2048 from 65521 classes of bfloat16 0.87-0.96 ms, 1.15-1.27 PFLOP/s.
 template <typename Shape>
-__global__ __launch_bounds__(Shape::NW * 64, 2) void k_loss_dx(Matrix Dt, Matrix W, Positions at, uint32_t H, uint32_t splits, int add,
+__global__ __launch_bounds__(Shape::NW * 64, 2) void k_loss_dx(Matrix Dt, Matrix W, Positions at, Scales scales, uint32_t H, uint32_t splits, int add,
                                                                float* __restrict__ planes) {
     __shared__ __attribute__((aligned(1024))) uint8_t sh[Shape::kLds];
     const uint32_t N = at.B * at.P, tiles_n = (H + Shape::BN - 1) / Shape::BN, tiles_m = (at.B * at.Pp + Shape::BM - 1) / Shape::BM;
@@ -465,7 +521,9 @@ __global__ __launch_bounds__(Shape::NW * 64, 2) void k_loss_dx(Matrix Dt, Matrix
     const uint32_t k0 = (uint32_t)((uint64_t)split * steps / splits) * Shape::BK;
     const uint32_t k1 = min((uint32_t)((uint64_t)(split + 1u) * steps / splits) * Shape::BK, Dt.rows);
     f16v acc[Shape::MT][Shape::NT] = {};
-    ColumnTile<Shape>::run(acc, sh, Dt, W, m0, n0, k0, k1);
+    InParts<Shape, Shape::PA == 3> parts;
+    ColumnTile<Shape>::run(acc, sh, Dt, W, m0, n0, k0, k1, [&](uint32_t step, int ks) { parts.after(acc, step, ks); });
+    parts.end(acc);
     const uint32_t lane = threadIdx.x & 63u, half = lane >> 5, wm = m0 + Shape::wave_m(), wn = n0 + Shape::wave_n();
     float* out = planes + (size_t)split * N * H;
 #pragma unroll
@@ -474,12 +532,13 @@ __global__ __launch_bounds__(Shape::NW * 64, 2) void k_loss_dx(Matrix Dt, Matrix
         for (int i = 0; i < 16; ++i) {
             const uint32_t row = at.row(wm + class_of(m, i, half));
             if (row == 0xFFFFFFFFu) continue;
+            const float scale = scales.at(row / at.P);
 #pragma unroll
             for (int n = 0; n < Shape::NT; ++n) {
                 const uint32_t h = wn + n * 32u + (lane & 31u);
                 if (h >= H) continue;
                 float* to = out + (size_t)row * H + h;
-                *to = acc[m][n][i] + (add ? *to : 0.f);
+                *to = acc[m][n][i] * scale + (add ? *to : 0.f);
             }
         }
 }
@@ -600,16 +659,21 @@ __global__ __launch_bounds__(1024) void k_loss_sums_thin(const float* __restrict
 // Bound by the matrix instructions, two planes of D by one of X, bfloat16 65521 x 2048 from 4 x 1024 positions: 2.0-2.2 ms, 1.0-1.1 PFLOP/s of
 // them, 1.07 GB of outputs within.
 template <typename Shape>
-__global__ __launch_bounds__(Shape::NW * 64, 2) void k_loss_sums(Matrix Dt, Matrix Xt, uint32_t K, uint32_t Pp, float c, float* __restrict__ g_out,
+__global__ __launch_bounds__(Shape::NW * 64, 2) void k_loss_sums(Matrix Dt, Matrix Xt, uint32_t B, uint32_t Pp, Scales scales, float c, float* __restrict__ g_out,
                                                                  float* __restrict__ s_out) {
     __shared__ __attribute__((aligned(1024))) uint8_t sh[Shape::kLds];
     const uint32_t V = Dt.rows, H = Xt.rows, tiles_n = (H + Shape::BN - 1) / Shape::BN;
     const uint32_t id = xcd_contiguous(blockIdx.x, gridDim.x), m0 = id / tiles_n * Shape::BM, n0 = id % tiles_n * Shape::BN;
     f16v acc[Shape::MT][Shape::NT] = {}, g[Shape::MT][Shape::NT] = {}, s[Shape::MT][Shape::NT] = {};
-    uint32_t left = Pp;
-    RowTile<Shape>::run(acc, sh, Dt, Xt, m0, n0, Shape::BN, [&](uint32_t n) { return n0 + n < H ? n : 0xFFFFFFFFu; }, K, [&](uint32_t, int) {
+    InParts<Shape, Shape::PA == 3> parts;
+    constexpr bool kScaled = Shape::PA == 2;                 // (bfloat16: the others' D is what it is)
+    uint32_t left = Pp, z = 0;
+    float scale = kScaled ? scales.at(0) : 1.f;
+    RowTile<Shape>::run(acc, sh, Dt, Xt, m0, n0, Shape::BN, [&](uint32_t n) { return n0 + n < H ? n : 0xFFFFFFFFu; }, B * Pp, [&](uint32_t step, int ks) {
         left -= 16u;
-        if (left != 0u) return;
+        if (left != 0u) { parts.after(acc, step, ks); return; }
+        parts.end(acc);
+        parts = {};
         left = Pp;
 #pragma unroll
         for (int m = 0; m < Shape::MT; ++m)
@@ -617,11 +681,13 @@ __global__ __launch_bounds__(Shape::NW * 64, 2) void k_loss_sums(Matrix Dt, Matr
             for (int n = 0; n < Shape::NT; ++n)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const float x = acc[m][n][i];
+                    const float x = kScaled ? acc[m][n][i] * scale : acc[m][n][i];
                     g[m][n][i] += x;
                     s[m][n][i] = __builtin_fmaf(x, x, s[m][n][i]);
                     acc[m][n][i] = 0.f;
                 }
+        z = min(z + 1u, B - 1u);                             // (past the last sample there are steps of zeros)
+        if (kScaled) scale = scales.at(z);
     });
     const uint32_t lane = threadIdx.x & 63u, half = lane >> 5, wm = m0 + Shape::wave_m(), wn = n0 + Shape::wave_n();
 #pragma unroll
@@ -645,7 +711,9 @@ __global__ __launch_bounds__(Shape::NW * 64, 2) void k_loss_sums(Matrix Dt, Matr
 typedef TileShape<256, 256, 128, 64, 64, 2, 1, 1> Large;     // bfloat16: the logits and dX
 typedef TileShape<128, 128, 64, 64, 64, 2, 1, 1> Small;
 typedef TileShape<128, 64, 64, 32, 64, 3, 1, 1> Slim;        // few rows over many classes: W streams through
-typedef TileShape<256, 128, 64, 64, 32, 2, 3, 3> Cut;        // float32: all three products
+typedef TileShape<256, 128, 64, 64, 32, 2, 3, 3> Cut;        // float32: the logits and dX
+typedef TileShape<128, 128, 64, 32, 32, 2, 3, 3> CutSums;    // float32: g and s (registers for four accumulators; with 64 x 64 a wave they
+//   spilled: 4 x 512 positions of 1024, 4000 classes, the backward pass 404 us, so 301; 10 x 297 of 3755, 1191 classes, 799 and 727)
 typedef TileShape<128, 256, 64, 64, 64, 2, 2, 1> Sums;       // bfloat16: g and s
 
 static uint32_t up8(uint32_t x) { return (x + 7u) / 8u * 8u; }
@@ -775,7 +843,7 @@ struct BackwardPlan {
     RowsPlan rows;
     uint32_t planes, piece, Pp, Lq, splits;
     bool dx_thin, dx_large, sum_planes, sum_thin;
-    size_t x, xt, w, d, d32, d2, out, total;
+    size_t x, xt, w, d, d32, d2, out, scales, total;
 };
 static BackwardPlan backward_plan(int dtype, uint32_t B, uint32_t P, uint32_t H, uint32_t V) {
     BackwardPlan L;
@@ -811,6 +879,8 @@ static BackwardPlan backward_plan(int dtype, uint32_t B, uint32_t P, uint32_t H,
     L.d32 = off; if (P == 1) off = align_up(off + 4 * (size_t)N * L.piece, 256);
     L.d2 = off; if (L.sum_planes) off += fc_planes_bytes(2, N, L.piece);
     L.out = off; if (!L.dx_thin) off += (size_t)L.splits * N * H * sizeof(float);
+    off = align_up(off, 16);
+    L.scales = off; if (dtype == VGC_BF16 && P > 1) off += (size_t)B * sizeof(float);
     L.total = off;
     return L;
 }
@@ -831,6 +901,14 @@ int launch_softmax_loss_backward(int dtype, const void* X, const void* W, const 
     A.K = L.rows.in_place ? H : L.rows.Kp;
     A.at = Positions{B, P, L.Pp};
     A.target = target; A.lse = lse; A.weight = weight; A.V_all = V;
+    A.scales = Scales{nullptr, P == 1};
+    if (dtype == VGC_BF16 && weight) {
+        A.scales.of = P == 1 ? weight : (const float*)(ws + L.scales);
+        if (P > 1) {
+            hipLaunchKernelGGL(k_loss_scales, dim3(B), dim3(1024), 0, stream, weight, target, P, (float*)(ws + L.scales));
+            if ((rc = hip_check(hipGetLastError(), "launch k_loss_scales")) != VGC_OK) return rc;
+        }
+    }
     if ((dX && !L.dx_thin) || by_position) A.dt = (uint16_t*)(ws + L.d);
     A.planes = dtype == VGC_F32 ? 3u : by_position ? 2u : 1u;
     if (P == 1 && (s_out || L.dx_thin)) A.d32 = (float*)(ws + L.d32);
@@ -870,19 +948,18 @@ int launch_softmax_loss_backward(int dtype, const void* X, const void* W, const 
         } else if (dX) {
             const uint32_t M = B * L.Pp;
             if (dtype == VGC_F32)
-                hipLaunchKernelGGL(k_loss_dx<Cut>, dim3(tiles<Cut>(M, H) * L.splits), dim3(Cut::NW * 64), 0, stream, Dt, A.w, A.at, H, L.splits, (int)(v0 > 0), out);
+                hipLaunchKernelGGL(k_loss_dx<Cut>, dim3(tiles<Cut>(M, H) * L.splits), dim3(Cut::NW * 64), 0, stream, Dt, A.w, A.at, A.scales, H, L.splits, (int)(v0 > 0), out);
             else if (L.dx_large)
-                hipLaunchKernelGGL(k_loss_dx<Large>, dim3(tiles<Large>(M, H) * L.splits), dim3(Large::NW * 64), 0, stream, Dt, A.w, A.at, H, L.splits, (int)(v0 > 0), out);
+                hipLaunchKernelGGL(k_loss_dx<Large>, dim3(tiles<Large>(M, H) * L.splits), dim3(Large::NW * 64), 0, stream, Dt, A.w, A.at, A.scales, H, L.splits, (int)(v0 > 0), out);
             else
-                hipLaunchKernelGGL(k_loss_dx<Small>, dim3(tiles<Small>(M, H) * L.splits), dim3(Small::NW * 64), 0, stream, Dt, A.w, A.at, H, L.splits, (int)(v0 > 0), out);
+                hipLaunchKernelGGL(k_loss_dx<Small>, dim3(tiles<Small>(M, H) * L.splits), dim3(Small::NW * 64), 0, stream, Dt, A.w, A.at, A.scales, H, L.splits, (int)(v0 > 0), out);
             if ((rc = hip_check(hipGetLastError(), "launch k_loss_dx")) != VGC_OK) return rc;
         }
         float *g = g_out ? g_out + (size_t)v0 * H : nullptr, *s = s_out ? s_out + (size_t)v0 * H : nullptr;
         if (by_position) {
             const Matrix Xt = {xt, H, L.Lq, (uint64_t)H * L.Lq};
-            const uint32_t K = B * L.Pp;
-            if (dtype == VGC_F32) hipLaunchKernelGGL(k_loss_sums<Cut>, dim3(tiles<Cut>(A.V, H)), dim3(Cut::NW * 64), 0, stream, Dt, Xt, K, L.Pp, c, g, s);
-            else hipLaunchKernelGGL(k_loss_sums<Sums>, dim3(tiles<Sums>(A.V, H)), dim3(Sums::NW * 64), 0, stream, Dt, Xt, K, L.Pp, c, g, s);
+            if (dtype == VGC_F32) hipLaunchKernelGGL(k_loss_sums<CutSums>, dim3(tiles<CutSums>(A.V, H)), dim3(CutSums::NW * 64), 0, stream, Dt, Xt, B, L.Pp, A.scales, c, g, s);
+            else hipLaunchKernelGGL(k_loss_sums<Sums>, dim3(tiles<Sums>(A.V, H)), dim3(Sums::NW * 64), 0, stream, Dt, Xt, B, L.Pp, A.scales, c, g, s);
             if ((rc = hip_check(hipGetLastError(), "launch k_loss_sums")) != VGC_OK) return rc;
         } else if (s_out && L.sum_planes) {
             if ((rc = launch_square_planes(VGC_F32, A.d32, nullptr, N, A.V, ws + L.d2, stream)) != VGC_OK) return rc;

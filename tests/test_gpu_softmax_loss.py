@@ -264,3 +264,54 @@ def test_refusals(dev):
             vgc.softmax_loss_backward(**{**good, **change})
     vgc.softmax_loss_backward(**good)
     assert vgc.softmax_loss_backward_workspace_bytes(vgc.F32, 1 << 11, 1 << 11, H, V) == 0
+
+
+@pytest.mark.parametrize("P", [38, 57])
+def test_weights_that_all_positions_share(dev, P):
+    """Rows that miss their classes, each weighted 1 / P, which bfloat16 does not hold: what that rounds to must not be what every position brings.
+    Relative to their samples' weight the targets' entries are p - 1 with p about 1 / V, kept to 2^-9 of p in two pieces: 1e-7; a class has a few
+    positions, whose products, sums, squares and factors round a dozen times at 2^-24: 1e-6 bounds s.  dX is rounded once, to 2^-9 of itself
+    at most, besides the sum of the other entries, each rounded by itself."""
+    import torch
+    B, H, V = 2, 64, 20011
+    X, W, target = _inputs(B, P, H, V, "bf16", masked=0)
+    X = torch.from_numpy(np.random.default_rng(3).standard_normal((B, P, H)).astype(np.float32)).to(torch.bfloat16)
+    weight = torch.full((B, P), 1.0 / P)
+    got = _sides(dev, X, W, target, weight)
+    _check(X, W, target, weight, got)
+    _, dXw, _, sw, _ = O.softmax_loss_backward(_np(X), _np(W), target.numpy().reshape(-1), _np(got[1]), weight.numpy(), 1.0 / B)
+    off = lambda a, b: np.linalg.norm(a - b) / np.linalg.norm(b)
+    assert off(_np(got[3]), sw) <= 1e-6 and off(_np(got[2]).reshape(dXw.shape), dXw) <= 2.05e-3
+
+
+@pytest.mark.parametrize("N,V", [(600, 4000), (3, 7000)])
+def test_logits_of_long_float_rows_do_not_shrink(dev, N, V):
+    """One class far above the others, so that lse is its logit, 14, a sum of H terms that all point one way.  Float sums that are rounded, in
+    whatever order, are off by sqrt(H) 2^-24 of it by chance; cut off instead they would all be too small."""
+    import torch
+    from paper_1802_06058_amd import vgc
+    H, gen = 3000, torch.Generator().manual_seed(1)
+    W = torch.randn(V, H, generator=gen) / H ** 0.5
+    target = torch.randint(0, V, (N,), generator=gen)
+    X = (0.02 * torch.randn(N, H, generator=gen) + 14 * W[target] / (W[target] ** 2).sum(1, keepdim=True)).float()
+    want = torch.logsumexp(X.double() @ W.double().t(), 1)
+    loss, lse = torch.empty(N, device=dev), torch.empty(N, device=dev)
+    ws = torch.empty(vgc.softmax_loss_workspace_bytes(vgc.F32, N, H, V), dtype=torch.uint8, device=dev)
+    vgc.softmax_loss(X.to(dev), W.to(dev), target.to(dev), loss, lse, ws)
+    assert float((lse.cpu().double() - want).pow(2).mean().sqrt()) <= H ** 0.5 * 2.0 ** -24 * 14
+
+
+def test_weights_of_every_kind_in_a_sample(dev):
+    """Zero throughout, negative, far apart, and infinite or NaN where the row is not asked for."""
+    import torch
+    B, P, H, V = 5, 20, 40, 300
+    for dtype in ("bf16", "f32"):
+        X, W, target = _inputs(B, P, H, V, dtype)
+        weight = torch.from_numpy(np.random.default_rng(2).standard_normal((B, P)).astype(np.float32))
+        weight[1] = 0
+        weight[2] *= 1e-20
+        weight[3, ::2] *= 1e-10
+        clean = weight.clone()
+        clean[target < 0] = 1
+        weight[target < 0] = torch.where(torch.arange(int((target < 0).sum())) % 2 == 0, float("inf"), float("nan"))
+        _check(X, W, target, clean, _sides(dev, X, W, target, weight))
