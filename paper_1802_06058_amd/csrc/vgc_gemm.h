@@ -7,7 +7,7 @@
 //
 // An operand may consist of several planes that add up to it (an exact cut of a float, or a value in two pieces); a product of
 // operands is the sum over the pairs of planes that matter, smallest first, formed from the same fragments in one pass: three
-// planes a side meet in the six pairs that reach 2^-24, two planes meet one in two.
+// planes a side meet in the six pairs that reach 2^-24, two or three planes meet one in as many.
 //
 // Lane l of the instruction holds, for row m = l % 32, the eight k = 8 (l / 32) .. + 7.  Its 16 results are
 // C[m = 8 (i / 4) + 4 (l / 32) + i % 4][n = l % 32], i = 0..15.
@@ -76,6 +76,7 @@ __device__ __forceinline__ TilePlace in_bands(uint32_t id, uint32_t tiles_m, uin
 template <int PA, int PB> struct Pairs;
 template <> struct Pairs<1, 1> { static constexpr int n = 1, a[1] = {0}, b[1] = {0}; };
 template <> struct Pairs<2, 1> { static constexpr int n = 2, a[2] = {1, 0}, b[2] = {0, 0}; };
+template <> struct Pairs<3, 1> { static constexpr int n = 3, a[3] = {2, 1, 0}, b[3] = {0, 0, 0}; };
 template <> struct Pairs<2, 2> { static constexpr int n = 4, a[4] = {1, 1, 0, 0}, b[4] = {1, 0, 1, 0}; };
 template <> struct Pairs<3, 3> { static constexpr int n = 6, a[6] = {2, 0, 1, 1, 0, 0}, b[6] = {0, 2, 1, 0, 1, 0}; };
 

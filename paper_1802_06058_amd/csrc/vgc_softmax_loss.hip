@@ -13,8 +13,9 @@
 // the loop of vgc_gemm.h.
 //
 // Precision.  bfloat16 inputs: products are exact, sums float32.  D is rounded to bfloat16 for dX, which is rounded to bfloat16
-// itself; for g and s, which are float32, a second plane holds the rest, 16 significant bits in all (both relative to the sample's
-// largest weight).  A third plane for the target's entries alone was tried: its registers are not there, k_loss_sums spilled.  float32 inputs: every operand
+// itself; for g and s, which are float32, a second plane holds the rest, 16 significant bits in all, and of up to 512 positions a third
+// what that leaves (relative to the sample's largest weight).  A third plane for the target's entries alone was tried: k_loss_sums has no
+// registers for it.  float32 inputs: every operand
 // is cut exactly into three planes of 8 bits and a product is formed from the six pairs of planes that reach 2^-24 of it; few rows
 // are multiplied as floats instead.
 #include <algorithm>
@@ -41,15 +42,19 @@ __device__ __forceinline__ Cut3 cut3(float x) {
     c.p[2] = __float_as_uint(r2) >> 16;
     return c;
 }
-// Plane q of two entries of D, the first in the low half: float32 inputs the cut of it; bfloat16 ones its rounding, and the rounding
-// of what is left (within 2^-18 of D).
-template <bool kF32> __device__ __forceinline__ uint32_t plane_of(float d0, float d1, uint32_t q) {
+// The next plane of two entries of D, the first in the low half, taken out of them: float32 inputs the next 8 bits of the cut; bfloat16
+// ones the rounding of what is left (two planes: within 2^-18 of D; three: all of it).
+template <bool kF32> __device__ __forceinline__ uint32_t next_plane(float& d0, float& d1) {
     if (kF32) {
         const Cut3 a = cut3(d0), b = cut3(d1);
-        return q == 0 ? a.p[0] | b.p[0] << 16 : q == 1 ? a.p[1] | b.p[1] << 16 : a.p[2] | b.p[2] << 16;
+        d0 = __uint_as_float(a.p[1] << 16) + __uint_as_float(a.p[2] << 16);
+        d1 = __uint_as_float(b.p[1] << 16) + __uint_as_float(b.p[2] << 16);
+        return a.p[0] | b.p[0] << 16;
     }
-    const uint32_t hi = two_bf16(d0, d1);
-    return q == 0 ? hi : two_bf16(d0 - __uint_as_float(hi << 16), d1 - __uint_as_float(hi & 0xFFFF0000u));
+    const uint32_t x = two_bf16(d0, d1);
+    d0 -= __uint_as_float(x << 16);
+    d1 -= __uint_as_float(x & 0xFFFF0000u);
+    return x;
 }
 
 // Eight values as the planes of an operand, 16 bytes each.
@@ -270,7 +275,7 @@ __device__ __forceinline__ void logits_to_d(f16v (&acc)[MT][NT], uint32_t m0, ui
     }
 }
 
-// D by classes.  The wave turns its part in LDS, in bytes of its own, a plane at a time, and stores whole rows of its positions.  The two
+// D by classes (used up).  The wave turns its part in LDS, in bytes of its own, a plane at a time, and stores whole rows of its positions.  The two
 // halves of a wave, four classes apart, write to different banks: 64-byte halves of a row of 64 positions change places with bit 2 of
 // the class.
 template <bool kF32, int MT, int NT>
@@ -284,7 +289,10 @@ __device__ __forceinline__ void store_by_classes(f16v (&acc)[MT][NT], uint8_t* t
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int i = 0; i < 16; i += 2) {            // (bit 2 of the class is the half)
-                    const uint32_t x = plane_of<kF32>(acc[m][n][i], acc[m][n][i + 1], q);
+                    float d0 = acc[m][n][i], d1 = acc[m][n][i + 1];
+                    const uint32_t x = next_plane<kF32>(d0, d1);
+                    acc[m][n][i] = d0;
+                    acc[m][n][i + 1] = d1;
                     uint8_t* to = turn + class_of(m, i, half) * kRow + ((uint32_t)n ^ (half & flip)) * 64u + (lane & 31u) * 2u;
                     *reinterpret_cast<uint16_t*>(to) = (uint16_t)x;
                     *reinterpret_cast<uint16_t*>(to + kRow) = (uint16_t)(x >> 16);
@@ -339,7 +347,7 @@ __global__ __launch_bounds__(Shape::NW * 64, 2) void k_logits(LossArgs A) {
     // the tile's rows of X lie between those of its first and of its last position
     const uint32_t z0 = n0 / A.at.Pp, first = min(z0 * A.at.P + min(n0 - z0 * A.at.Pp, A.at.P), A.N);
     // float32: in parts of 128 k (600 rows of 4096 channels, logits of 14: lse 1.2e-4 too small, so 1e-6 off)
-    InParts<Shape, Shape::PA == 3> parts;
+    InParts<Shape, Shape::PB == 3> parts;
     RowTile<Shape>::run(acc, sh, A.w, A.x, m0, first, Shape::BN, [&](uint32_t n) {
         const uint32_t row = A.at.row(n0 + n);
         return row == 0xFFFFFFFFu ? row : row - first;
@@ -351,7 +359,7 @@ __global__ __launch_bounds__(Shape::NW * 64, 2) void k_logits(LossArgs A) {
     } else {
         logits_to_d(acc, wm, wn, A);
         static_assert(Shape::NT <= 2 && Shape::BM * Shape::BN * 2u <= Shape::kLds, "room to turn a plane");
-        if (A.dt) store_by_classes<Shape::PA == 3>(acc, sh + Shape::wave() * (Shape::WM * Shape::WN * 2u), wm, wn, A);
+        if (A.dt) store_by_classes<Shape::PB == 3>(acc, sh + Shape::wave() * (Shape::WM * Shape::WN * 2u), wm, wn, A);
     }
 }
 
@@ -474,11 +482,13 @@ __global__ __launch_bounds__(kThinWaves * 64) void k_logits_thin(ThinArgs R, Los
         if (t == A.v0 + m0 + v) A.picked[n0 + col] = z;
     } else {
         if (!mine) return;
-        const float d = C.of((float)(whole - (double)C.lse), m0 + v);
+        float d = C.of((float)(whole - (double)C.lse), m0 + v);
         if (A.d32 && C.row != 0xFFFFFFFFu) A.d32[(size_t)C.row * A.V + m0 + v] = d * C.scale;
         if (A.dt)
-            for (uint32_t q = 0; q < A.planes; ++q)
-                A.dt[q * A.plane + (size_t)(m0 + v) * A.Lq + n0 + col] = (uint16_t)plane_of<sizeof(T) == 4>(d, 0.f, q);
+            for (uint32_t q = 0; q < A.planes; ++q) {
+                float none = 0.f;
+                A.dt[q * A.plane + (size_t)(m0 + v) * A.Lq + n0 + col] = (uint16_t)next_plane<sizeof(T) == 4>(d, none);
+            }
     }
 }
 
@@ -521,7 +531,7 @@ __global__ __launch_bounds__(Shape::NW * 64, 2) void k_loss_dx(Matrix Dt, Matrix
     const uint32_t k0 = (uint32_t)((uint64_t)split * steps / splits) * Shape::BK;
     const uint32_t k1 = min((uint32_t)((uint64_t)(split + 1u) * steps / splits) * Shape::BK, Dt.rows);
     f16v acc[Shape::MT][Shape::NT] = {};
-    InParts<Shape, Shape::PA == 3> parts;
+    InParts<Shape, Shape::PB == 3> parts;
     ColumnTile<Shape>::run(acc, sh, Dt, W, m0, n0, k0, k1, [&](uint32_t step, int ks) { parts.after(acc, step, ks); });
     parts.end(acc);
     const uint32_t lane = threadIdx.x & 63u, half = lane >> 5, wm = m0 + Shape::wave_m(), wn = n0 + Shape::wave_n();
@@ -665,8 +675,8 @@ __global__ __launch_bounds__(Shape::NW * 64, 2) void k_loss_sums(Matrix Dt, Matr
     const uint32_t V = Dt.rows, H = Xt.rows, tiles_n = (H + Shape::BN - 1) / Shape::BN;
     const uint32_t id = xcd_contiguous(blockIdx.x, gridDim.x), m0 = id / tiles_n * Shape::BM, n0 = id % tiles_n * Shape::BN;
     f16v acc[Shape::MT][Shape::NT] = {}, g[Shape::MT][Shape::NT] = {}, s[Shape::MT][Shape::NT] = {};
-    InParts<Shape, Shape::PA == 3> parts;
-    constexpr bool kScaled = Shape::PA == 2;                 // (bfloat16: the others' D is what it is)
+    InParts<Shape, Shape::PB == 3> parts;
+    constexpr bool kScaled = Shape::PB == 1;                 // (bfloat16; float32 planes hold D as it is)
     uint32_t left = Pp, z = 0;
     float scale = kScaled ? scales.at(0) : 1.f;
     RowTile<Shape>::run(acc, sh, Dt, Xt, m0, n0, Shape::BN, [&](uint32_t n) { return n0 + n < H ? n : 0xFFFFFFFFu; }, B * Pp, [&](uint32_t step, int ks) {
@@ -715,6 +725,7 @@ typedef TileShape<256, 128, 64, 64, 32, 2, 3, 3> Cut;        // float32: the log
 typedef TileShape<128, 128, 64, 32, 32, 2, 3, 3> CutSums;    // float32: g and s (registers for four accumulators; with 64 x 64 a wave they
 //   spilled: 4 x 512 positions of 1024, 4000 classes, the backward pass 404 us, so 301; 10 x 297 of 3755, 1191 classes, 799 and 727)
 typedef TileShape<128, 256, 64, 64, 64, 2, 2, 1> Sums;       // bfloat16: g and s
+typedef TileShape<128, 128, 64, 32, 64, 2, 3, 1> SumsOfFew;  // of few positions
 
 static uint32_t up8(uint32_t x) { return (x + 7u) / 8u * 8u; }
 static uint32_t tiles(uint32_t a, uint32_t ta, uint32_t b, uint32_t tb) { return (a + ta - 1) / ta * ((b + tb - 1) / tb); }
@@ -857,7 +868,10 @@ static BackwardPlan backward_plan(int dtype, uint32_t B, uint32_t P, uint32_t H,
     const uint64_t work = (uint64_t)N * V * H;
     L.dx_thin = P == 1 && (uint64_t)N * V <= (64u << 20) && (dtype == VGC_F32 ? work <= 2000000000u : V <= 1024u && work <= (256u << 20));
     L.rows = rows_plan(dtype, H, L.tile, !L.dx_thin);
-    L.planes = dtype == VGC_F32 ? 3u : P == 1 ? 1u : 2u;
+    // bfloat16: D of few positions in three planes, all its bits, as few positions do not average what two leave out: s off by, two and
+    // three, 2 x 34 positions, 34861 classes 3.2e-6 and 3.4e-7, 11 x 36, 85 classes 2.3e-6 and 2.4e-7, (two) 7 x 853, 5181 classes 1.1e-6.
+    // us of the call: 2 x 38 x 776, 44209 classes 221 and 186; 4 x 64 x 1024, 32000 classes 176 and 204; 4 x 128: 224 and 287; 4 x 256: 347 and 478
+    L.planes = dtype == VGC_F32 ? 3u : P == 1 ? 1u : N <= 512u ? 3u : 2u;
     // samples of one position: the FC form, from planes where the outputs are what it takes (us of the whole call by planes and by floats, 4 M
     // outputs: 47.0 and 47.6), directly where it is small (200000 outputs: 19 and by floats 21, 500000: 36 and 30), else from floats
     L.sum_thin = P == 1 && N <= 256u && (uint64_t)V * H <= (256u << 10);
@@ -910,7 +924,7 @@ int launch_softmax_loss_backward(int dtype, const void* X, const void* W, const 
         }
     }
     if ((dX && !L.dx_thin) || by_position) A.dt = (uint16_t*)(ws + L.d);
-    A.planes = dtype == VGC_F32 ? 3u : by_position ? 2u : 1u;
+    A.planes = dtype == VGC_F32 || by_position ? L.planes : 1u;
     if (P == 1 && (s_out || L.dx_thin)) A.d32 = (float*)(ws + L.d32);
     if (!L.rows.in_place && (rc = launch_rows(dtype, X, N, H, xs, stream)) != VGC_OK) return rc;
     A.x = matrix_of(L.rows, X, xs, N, H);
@@ -959,6 +973,7 @@ int launch_softmax_loss_backward(int dtype, const void* X, const void* W, const 
         if (by_position) {
             const Matrix Xt = {xt, H, L.Lq, (uint64_t)H * L.Lq};
             if (dtype == VGC_F32) hipLaunchKernelGGL(k_loss_sums<CutSums>, dim3(tiles<CutSums>(A.V, H)), dim3(CutSums::NW * 64), 0, stream, Dt, Xt, B, L.Pp, A.scales, c, g, s);
+            else if (L.planes == 3u) hipLaunchKernelGGL(k_loss_sums<SumsOfFew>, dim3(tiles<SumsOfFew>(A.V, H)), dim3(SumsOfFew::NW * 64), 0, stream, Dt, Xt, B, L.Pp, A.scales, c, g, s);
             else hipLaunchKernelGGL(k_loss_sums<Sums>, dim3(tiles<Sums>(A.V, H)), dim3(Sums::NW * 64), 0, stream, Dt, Xt, B, L.Pp, A.scales, c, g, s);
             if ((rc = hip_check(hipGetLastError(), "launch k_loss_sums")) != VGC_OK) return rc;
         } else if (s_out && L.sum_planes) {
