@@ -553,20 +553,34 @@ __global__ __launch_bounds__(Shape::NW * 64, 2) void k_loss_dx(Matrix Dt, Matrix
         }
 }
 
-template <typename T>
-__global__ __launch_bounds__(256) void k_loss_dx_join(const float* __restrict__ planes, uint32_t splits, uint64_t n, T* __restrict__ dX) {
-    const uint64_t i = ((uint64_t)blockIdx.x * 256u + threadIdx.x) * 8u;
-    if (i >= n) return;
-    const int m = n - i >= 8u ? 8 : (int)(n - i);
-    float f[8], g[8];
-    widen8(load8(planes + i, m), f);
+// Adds the parts' planes in a fixed order, eight elements a lane; kWaves waves share many planes of few elements (6 x 529 from 64: 15 us
+// by one, 4 by 16).
+template <typename T, uint32_t kWaves>
+__global__ __launch_bounds__(kWaves == 1 ? 256 : kWaves * 64) void k_loss_dx_join(const float* __restrict__ planes, uint32_t splits, uint64_t n, T* __restrict__ dX) {
+    const uint32_t lane = threadIdx.x & 63u, wave = kWaves == 1 ? 0u : threadIdx.x >> 6;
+    const uint64_t i = (kWaves == 1 ? (uint64_t)blockIdx.x * 256u + threadIdx.x : (uint64_t)blockIdx.x * 64u + lane) * 8u;
+    const int m = i >= n ? 0 : n - i >= 8u ? 8 : (int)(n - i);
+    float f[8] = {}, g[8];
+    if (m > 0) {
 #pragma unroll 4
-    for (uint32_t s = 1; s < splits; ++s) {
-        widen8(load8(planes + s * n + i, m), g);
+        for (uint32_t s = wave; s < splits; s += kWaves) {
+            widen8(load8(planes + s * n + i, m), g);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] += g[e];
+            for (int e = 0; e < 8; ++e) f[e] += g[e];
+        }
     }
-    store8(dX + i, f, m);
+    if constexpr (kWaves > 1) {
+        __shared__ float sh[kWaves][8][64];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sh[wave][e][lane] = f[e];
+        __syncthreads();
+        if (wave != 0u) return;
+#pragma unroll
+        for (uint32_t w = 1; w < kWaves; ++w)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] += sh[w][e][lane];
+    }
+    if (m > 0) store8(dX + i, f, m);
 }
 
 // Few rows and few classes: 16 waves share the classes for 32 rows by 32 columns of dX, D and W multiplied as floats.  A wave takes 8
@@ -668,7 +682,8 @@ __global__ __launch_bounds__(1024) void k_loss_sums_thin(const float* __restrict
 // k runs over the positions; at a sample's end (every Pp of them) its product is squared into s, added into g, and cleared.
 // Bound by the matrix instructions, two planes of D by one of X, bfloat16 65521 x 2048 from 4 x 1024 positions: 2.0-2.2 ms, 1.0-1.1 PFLOP/s of
 // them, 1.07 GB of outputs within.
-template <typename Shape>
+// kPast: outputs beyond what the caches hold are stored past them.
+template <typename Shape, bool kPast>
 __global__ __launch_bounds__(Shape::NW * 64, 2) void k_loss_sums(Matrix Dt, Matrix Xt, uint32_t B, uint32_t Pp, Scales scales, float c, float* __restrict__ g_out,
                                                                  float* __restrict__ s_out) {
     __shared__ __attribute__((aligned(1024))) uint8_t sh[Shape::kLds];
@@ -710,8 +725,14 @@ __global__ __launch_bounds__(Shape::NW * 64, 2) void k_loss_sums(Matrix Dt, Matr
             for (int i = 0; i < 16; ++i) {
                 const uint32_t v = wm + class_of(m, i, half);
                 if (v >= V) continue;
-                if (g_out) g_out[(size_t)v * H + h] = c * g[m][n][i];
-                s_out[(size_t)v * H + h] = c * c * s[m][n][i];
+                float *gp = g_out + (size_t)v * H + h, *sp = s_out + (size_t)v * H + h;
+                if (kPast) {
+                    if (g_out) __builtin_nontemporal_store(c * g[m][n][i], gp);
+                    __builtin_nontemporal_store(c * c * s[m][n][i], sp);
+                } else {
+                    if (g_out) *gp = c * g[m][n][i];
+                    *sp = c * c * s[m][n][i];
+                }
             }
     }
 }
@@ -972,9 +993,15 @@ int launch_softmax_loss_backward(int dtype, const void* X, const void* W, const 
         float *g = g_out ? g_out + (size_t)v0 * H : nullptr, *s = s_out ? s_out + (size_t)v0 * H : nullptr;
         if (by_position) {
             const Matrix Xt = {xt, H, L.Lq, (uint64_t)H * L.Lq};
-            if (dtype == VGC_F32) hipLaunchKernelGGL(k_loss_sums<CutSums>, dim3(tiles<CutSums>(A.V, H)), dim3(CutSums::NW * 64), 0, stream, Dt, Xt, B, L.Pp, A.scales, c, g, s);
-            else if (L.planes == 3u) hipLaunchKernelGGL(k_loss_sums<SumsOfFew>, dim3(tiles<SumsOfFew>(A.V, H)), dim3(SumsOfFew::NW * 64), 0, stream, Dt, Xt, B, L.Pp, A.scales, c, g, s);
-            else hipLaunchKernelGGL(k_loss_sums<Sums>, dim3(tiles<Sums>(A.V, H)), dim3(Sums::NW * 64), 0, stream, Dt, Xt, B, L.Pp, A.scales, c, g, s);
+            // (us of the call, into the caches and past them: 33 MB of outputs 83 and 87, 114 MB 163 and 168, 262 MB 214 and 197, 983 MB 415 and 367)
+            const bool past = (uint64_t)V * H * (g ? 8u : 4u) > (192ull << 20);
+#define VGC_SUMS(S) do { \
+                if (past) hipLaunchKernelGGL((k_loss_sums<S, true>), dim3(tiles<S>(A.V, H)), dim3(S::NW * 64), 0, stream, Dt, Xt, B, L.Pp, A.scales, c, g, s); \
+                else hipLaunchKernelGGL((k_loss_sums<S, false>), dim3(tiles<S>(A.V, H)), dim3(S::NW * 64), 0, stream, Dt, Xt, B, L.Pp, A.scales, c, g, s); } while (0)
+            if (dtype == VGC_F32) VGC_SUMS(CutSums);
+            else if (L.planes == 3u) VGC_SUMS(SumsOfFew);
+            else VGC_SUMS(Sums);
+#undef VGC_SUMS
             if ((rc = hip_check(hipGetLastError(), "launch k_loss_sums")) != VGC_OK) return rc;
         } else if (s_out && L.sum_planes) {
             if ((rc = launch_square_planes(VGC_F32, A.d32, nullptr, N, A.V, ws + L.d2, stream)) != VGC_OK) return rc;
@@ -990,9 +1017,11 @@ int launch_softmax_loss_backward(int dtype, const void* X, const void* W, const 
     }
     if (!dX || L.dx_thin) return VGC_OK;
     const uint64_t n = (uint64_t)N * H;
-    const dim3 grid((uint32_t)((n + 2047u) / 2048u));
-    if (dtype == VGC_F32) hipLaunchKernelGGL(k_loss_dx_join<float>, grid, dim3(256), 0, stream, out, L.splits, n, (float*)dX);
-    else hipLaunchKernelGGL(k_loss_dx_join<uint16_t>, grid, dim3(256), 0, stream, out, L.splits, n, (uint16_t*)dX);
+#define VGC_JOIN(T, kWaves, per) hipLaunchKernelGGL((k_loss_dx_join<T, kWaves>), dim3((uint32_t)((n + per - 1u) / per)), dim3(kWaves == 1 ? 256 : kWaves * 64), 0, \
+        stream, out, L.splits, n, (T*)dX)
+    if (dtype == VGC_F32) { if (L.splits >= 16u) VGC_JOIN(float, 16, 512u); else VGC_JOIN(float, 1, 2048u); }
+    else { if (L.splits >= 16u) VGC_JOIN(uint16_t, 16, 512u); else VGC_JOIN(uint16_t, 1, 2048u); }
+#undef VGC_JOIN
     return hip_check(hipGetLastError(), "launch k_loss_dx_join");
 }
 
