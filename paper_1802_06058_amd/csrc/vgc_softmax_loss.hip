@@ -891,7 +891,8 @@ static BackwardPlan backward_plan(int dtype, uint32_t B, uint32_t P, uint32_t H,
     L.rows = rows_plan(dtype, H, L.tile, !L.dx_thin);
     // bfloat16: D of few positions in three planes, all its bits, as few positions do not average what two leave out: s off by, two and
     // three, 2 x 34 positions, 34861 classes 3.2e-6 and 3.4e-7, 11 x 36, 85 classes 2.3e-6 and 2.4e-7, (two) 7 x 853, 5181 classes 1.1e-6.
-    // us of the call: 2 x 38 x 776, 44209 classes 221 and 186; 4 x 64 x 1024, 32000 classes 176 and 204; 4 x 128: 224 and 287; 4 x 256: 347 and 478
+    // us of the call: 2 x 38 x 776, 44209 classes 227 and 160; 40 x 2048, 60000 classes 305 and 368; 4 x 64 x 1024, 32000 classes 171 and 195;
+    // 4 x 128: 229 and 271; 4 x 256: 343 and 462
     L.planes = dtype == VGC_F32 ? 3u : P == 1 ? 1u : N <= 512u ? 3u : 2u;
     // samples of one position: the FC form, from planes where the outputs are what it takes (us of the whole call by planes and by floats, 4 M
     // outputs: 47.0 and 47.6), directly where it is small (200000 outputs: 19 and by floats 21, 500000: 36 and 30), else from floats
