@@ -12,12 +12,11 @@
 // classes, as rows, beside W as it lies.  Memory is bounded by the piece, not by the vocabulary.  The three products run through
 // the loop of vgc_gemm.h.
 //
-// Precision.  bfloat16 inputs: products are exact, sums float32.  D is rounded to bfloat16 for dX, which is rounded to bfloat16
-// itself; for g and s, which are float32, a second plane holds the rest, 16 significant bits in all, and of up to 512 positions a third
-// what that leaves (relative to the sample's largest weight).  A third plane for the target's entries alone was tried: k_loss_sums has no
-// registers for it.  float32 inputs: every operand
-// is cut exactly into three planes of 8 bits and a product is formed from the six pairs of planes that reach 2^-24 of it; few rows
-// are multiplied as floats instead.
+// Precision.  bfloat16 inputs: products are exact, sums float32.  D, relative to its sample's largest weight, is rounded to bfloat16 for
+// dX, which is rounded to bfloat16 itself; for g and s, which are float32, a second plane holds the rest, 16 significant bits in all, and
+// of few positions or small products a third what that leaves.  (A third plane for the target's entries alone was tried: k_loss_sums has no
+// registers for it.)  float32 inputs: every operand is cut exactly into three planes of 8 bits and a product is formed from the six pairs
+// of planes that reach 2^-24 of it; few rows are multiplied as floats instead.
 #include <algorithm>
 
 #include "vgc_gemm.h"
@@ -889,11 +888,12 @@ static BackwardPlan backward_plan(int dtype, uint32_t B, uint32_t P, uint32_t H,
     const uint64_t work = (uint64_t)N * V * H;
     L.dx_thin = P == 1 && (uint64_t)N * V <= (64u << 20) && (dtype == VGC_F32 ? work <= 2000000000u : V <= 1024u && work <= (256u << 20));
     L.rows = rows_plan(dtype, H, L.tile, !L.dx_thin);
-    // bfloat16: D of few positions in three planes, all its bits, as few positions do not average what two leave out: s off by, two and
+    // bfloat16: D of few positions, and of small products, in three planes, all its bits, as few positions do not average what two leave out: s off by, two and
     // three, 2 x 34 positions, 34861 classes 3.2e-6 and 3.4e-7, 11 x 36, 85 classes 2.3e-6 and 2.4e-7, (two) 7 x 853, 5181 classes 1.1e-6.
     // us of the call: 2 x 38 x 776, 44209 classes 227 and 160; 40 x 2048, 60000 classes 305 and 368; 4 x 64 x 1024, 32000 classes 171 and 195;
-    // 4 x 128: 229 and 271; 4 x 256: 343 and 462
-    L.planes = dtype == VGC_F32 ? 3u : P == 1 ? 1u : N <= 512u ? 3u : 2u;
+    // 4 x 128: 229 and 271; 4 x 256: 343 and 462; where the product is small three cost nothing: 15 x 127 x 192, 3958 classes 104 and 97, 4 x 512 x
+    // 1024, 4000 classes 133 and 137, but 2 x 1024 x 1000, 8000 classes 195 and 235, 16 x 128 x 256, 30000 classes 272 and 355
+    L.planes = dtype == VGC_F32 ? 3u : P == 1 ? 1u : N <= 512u || (uint64_t)N * V * H <= 9000000000u ? 3u : 2u;
     // samples of one position: the FC form, from planes where the outputs are what it takes (us of the whole call by planes and by floats, 4 M
     // outputs: 47.0 and 47.6), directly where it is small (200000 outputs: 19 and by floats 21, 500000: 36 and 30), else from floats
     L.sum_thin = P == 1 && N <= 256u && (uint64_t)V * H <= (256u << 10);
