@@ -13,7 +13,8 @@
 // the loop of vgc_gemm.h.
 //
 // Precision.  bfloat16 inputs: products are exact, sums float32.  D, relative to its sample's largest weight, is rounded to bfloat16 for
-// dX, which is rounded to bfloat16 itself; for g and s, which are float32, a second plane holds the rest, 16 significant bits in all, and
+// dX, which is rounded to bfloat16 itself; what that left of the target's entry, which all other classes' entries add up to, is added to dX in float
+// (128 rows of 1024, 8192 classes, without: dX 2.04e-3 off, so 1.66e-3, which its own rounding alone is); for g and s, which are float32, a second plane holds the rest, 16 significant bits in all, and
 // of few positions or small products a third what that leaves.  (A third plane for the target's entries alone was tried: k_loss_sums has no
 // registers for it.)  float32 inputs: every operand is cut exactly into three planes of 8 bits and a product is formed from the six pairs
 // of planes that reach 2^-24 of it; few rows are multiplied as floats instead.
@@ -181,6 +182,7 @@ struct LossArgs {
     uint64_t plane;
     uint32_t planes;
     float* d32;               // D in float by rows of X, V long
+    float* rest;              // by rows of X: what rounding to bfloat16 left of the target's entry (bfloat16, for dX; or NULL)
 };
 
 constexpr float kLog2e = 1.44269504088896341f;
@@ -251,18 +253,30 @@ __device__ __forceinline__ ColumnOf column_of(uint32_t q, const LossArgs& A) {
     return C;
 }
 
+// What rounding to bfloat16 leaves of an entry of D.
+__device__ __forceinline__ float left_of(float d) {
+    float none = 0.f;
+    next_plane<false>(d, none);
+    return d;
+}
+
 // The logits become D in place.
-template <int MT, int NT>
+template <bool kF32, int MT, int NT>
 __device__ __forceinline__ void logits_to_d(f16v (&acc)[MT][NT], uint32_t m0, uint32_t n0, const LossArgs& A) {
     const uint32_t lane = threadIdx.x & 63u, half = lane >> 5;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         ColumnOf C = column_of(n0 + n * 32u + (lane & 31u), A);
         C.at -= m0;
+        float of_target = 0.f;
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) acc[m][n][i] = C.d(acc[m][n][i], class_of(m, i, half));
+            for (int i = 0; i < 16; ++i) {
+                acc[m][n][i] = C.d(acc[m][n][i], class_of(m, i, half));
+                if (!kF32 && class_of(m, i, half) == C.at) of_target = acc[m][n][i];
+            }
+        if (!kF32 && A.rest && C.at < MT * 32u && ((C.at >> 2) & 1u) == half) A.rest[C.row] = left_of(of_target) * C.scale;
         if (A.d32 && C.row != 0xFFFFFFFFu) {
             float* out = A.d32 + (size_t)C.row * A.V + m0;
 #pragma unroll
@@ -356,7 +370,7 @@ __global__ __launch_bounds__(Shape::NW * 64, 2) void k_logits(LossArgs A) {
     if (kForward) {
         if (wm < A.V) finish_forward(acc, wm, wn, A);
     } else {
-        logits_to_d(acc, wm, wn, A);
+        logits_to_d<Shape::PB == 3>(acc, wm, wn, A);
         static_assert(Shape::NT <= 2 && Shape::BM * Shape::BN * 2u <= Shape::kLds, "room to turn a plane");
         if (A.dt) store_by_classes<Shape::PB == 3>(acc, sh + Shape::wave() * (Shape::WM * Shape::WN * 2u), wm, wn, A);
     }
@@ -483,6 +497,7 @@ __global__ __launch_bounds__(kThinWaves * 64) void k_logits_thin(ThinArgs R, Los
         if (!mine) return;
         float d = C.of((float)(whole - (double)C.lse), m0 + v);
         if (A.d32 && C.row != 0xFFFFFFFFu) A.d32[(size_t)C.row * A.V + m0 + v] = d * C.scale;
+        if (sizeof(T) == 2 && A.rest && C.at == m0 + v) A.rest[C.row] = left_of(d) * C.scale;
         if (A.dt)
             for (uint32_t q = 0; q < A.planes; ++q) {
                 float none = 0.f;
@@ -552,10 +567,44 @@ __global__ __launch_bounds__(Shape::NW * 64, 2) void k_loss_dx(Matrix Dt, Matrix
         }
 }
 
+// What the target's entry, the largest of a row that misses its class, lost when it was rounded: added to dX as so much of the class's row.
+struct TargetRest {
+    const float* rest;
+    const int64_t* target;
+    const uint16_t* W;
+    int64_t V;
+    uint32_t H;
+    __device__ __forceinline__ void add(uint64_t i, int m, float (&f)[8]) const {
+        uint64_t row = i / H;
+        uint32_t h = (uint32_t)(i - row * H);
+        for (int e = 0; e < m;) {                            // (eight elements may belong to several rows)
+            const int many = (int)min(H - h, (uint32_t)(m - e));
+            const int64_t t = target[row];
+            if (t >= 0 && t < V) {
+                const float r = rest[row];
+                if (many == 8) {
+                    float w[8];
+                    widen8(load8(W + (uint64_t)t * H + h, 8), w);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) f[k] = __builtin_fmaf(r, w[k], f[k]);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (k >= e && k < e + many) f[k] = __builtin_fmaf(r, __uint_as_float((uint32_t)W[(uint64_t)t * H + h + (k - e)] << 16), f[k]);
+                }
+            }
+            e += many;
+            h = 0;
+            ++row;
+        }
+    }
+};
+
 // Adds the parts' planes in a fixed order, eight elements a lane; kWaves waves share many planes of few elements (6 x 529 from 64: 15 us
 // by one, 4 by 16).
 template <typename T, uint32_t kWaves>
-__global__ __launch_bounds__(kWaves == 1 ? 256 : kWaves * 64) void k_loss_dx_join(const float* __restrict__ planes, uint32_t splits, uint64_t n, T* __restrict__ dX) {
+__global__ __launch_bounds__(kWaves == 1 ? 256 : kWaves * 64) void k_loss_dx_join(const float* __restrict__ planes, uint32_t splits, uint64_t n, TargetRest target,
+                                                                                  T* __restrict__ dX) {
     const uint32_t lane = threadIdx.x & 63u, wave = kWaves == 1 ? 0u : threadIdx.x >> 6;
     const uint64_t i = (kWaves == 1 ? (uint64_t)blockIdx.x * 256u + threadIdx.x : (uint64_t)blockIdx.x * 64u + lane) * 8u;
     const int m = i >= n ? 0 : n - i >= 8u ? 8 : (int)(n - i);
@@ -567,6 +616,7 @@ __global__ __launch_bounds__(kWaves == 1 ? 256 : kWaves * 64) void k_loss_dx_joi
 #pragma unroll
             for (int e = 0; e < 8; ++e) f[e] += g[e];
         }
+        if (sizeof(T) == 2 && wave == 0u) target.add(i, m, f);
     }
     if constexpr (kWaves > 1) {
         __shared__ float sh[kWaves][8][64];
@@ -874,7 +924,7 @@ struct BackwardPlan {
     RowsPlan rows;
     uint32_t planes, piece, Pp, Lq, splits;
     bool dx_thin, dx_large, sum_planes, sum_thin;
-    size_t x, xt, w, d, d32, d2, out, scales, total;
+    size_t x, xt, w, d, d32, d2, out, scales, rest, total;
 };
 static BackwardPlan backward_plan(int dtype, uint32_t B, uint32_t P, uint32_t H, uint32_t V) {
     BackwardPlan L;
@@ -917,6 +967,7 @@ static BackwardPlan backward_plan(int dtype, uint32_t B, uint32_t P, uint32_t H,
     L.out = off; if (!L.dx_thin) off += (size_t)L.splits * N * H * sizeof(float);
     off = align_up(off, 16);
     L.scales = off; if (dtype == VGC_BF16 && P > 1) off += (size_t)B * sizeof(float);
+    L.rest = off; if (dtype == VGC_BF16 && !L.dx_thin) off += (size_t)N * sizeof(float);
     L.total = off;
     return L;
 }
@@ -948,6 +999,7 @@ int launch_softmax_loss_backward(int dtype, const void* X, const void* W, const 
     if ((dX && !L.dx_thin) || by_position) A.dt = (uint16_t*)(ws + L.d);
     A.planes = dtype == VGC_F32 || by_position ? L.planes : 1u;
     if (P == 1 && (s_out || L.dx_thin)) A.d32 = (float*)(ws + L.d32);
+    if (dtype == VGC_BF16 && dX && !L.dx_thin) A.rest = (float*)(ws + L.rest);
     if (!L.rows.in_place && (rc = launch_rows(dtype, X, N, H, xs, stream)) != VGC_OK) return rc;
     A.x = matrix_of(L.rows, X, xs, N, H);
     if (by_position) {
@@ -1018,8 +1070,9 @@ int launch_softmax_loss_backward(int dtype, const void* X, const void* W, const 
     }
     if (!dX || L.dx_thin) return VGC_OK;
     const uint64_t n = (uint64_t)N * H;
+    const TargetRest rest = {A.rest, target, (const uint16_t*)W, V, H};
 #define VGC_JOIN(T, kWaves, per) hipLaunchKernelGGL((k_loss_dx_join<T, kWaves>), dim3((uint32_t)((n + per - 1u) / per)), dim3(kWaves == 1 ? 256 : kWaves * 64), 0, \
-        stream, out, L.splits, n, (T*)dX)
+        stream, out, L.splits, n, rest, (T*)dX)
     if (dtype == VGC_F32) { if (L.splits >= 16u) VGC_JOIN(float, 16, 512u); else VGC_JOIN(float, 1, 2048u); }
     else { if (L.splits >= 16u) VGC_JOIN(uint16_t, 16, 512u); else VGC_JOIN(uint16_t, 1, 2048u); }
 #undef VGC_JOIN

@@ -1,0 +1,80 @@
+"""The softmax loss's kernels that only larger problems reach, entry by entry against 64 bits, and the size rules that lead to them.
+
+Tolerances are those of test_gpu_softmax_loss.py: a logit has H roundings of 2^-23 of the magnitudes summed, an exponential the relative error of
+its argument, D is rounded to 2^-8 for dX and to 2^-17 for g and s, and sums have as many roundings as terms."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+E = 2.0 ** -23
+
+
+@pytest.fixture(scope="module")
+def dev():
+    import torch
+    from paper_1802_06058_amd import vgc
+    assert torch.cuda.is_available()
+    vgc.load()
+    return torch.device("cuda:0")
+
+
+def _inputs(dev, B, P, H, V, dtype, seed=0, masked=0.2):
+    import torch
+    gen = torch.Generator(device=dev).manual_seed(seed + 7 * B + 11 * P + 13 * H + V)
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    rand = lambda *s: torch.rand(s, generator=gen, device=dev)
+    W = (torch.randn(V, H, generator=gen, device=dev) / H ** 0.5).to(t)
+    target = (V * rand(B, P)).long().clamp_(max=V - 1)
+    X = (torch.randn(B, P, H, generator=gen, device=dev) + 12 * rand(B, P, 1) * W[target].float()).to(t)
+    target[rand(B, P) < masked] = -1
+    target[0, 0] = V - 1
+    return X, W, target
+
+
+def _calls(X, W, target, weight, want_dx=True, want_s=True):
+    """Both calls; every output and the workspace lie before guards that have to stay."""
+    import torch
+    from paper_1802_06058_amd import vgc
+    B, P, H = X.shape
+    V, N, dev = W.shape[0], B * P, X.device
+    code = vgc.BF16 if X.dtype == torch.bfloat16 else vgc.F32
+    guarded = lambda n, t=torch.float32: torch.full((n + 64,), 7.0, dtype=t, device=dev)
+    loss, lse, dX, s, g = guarded(N), guarded(N), guarded(N * H, X.dtype), guarded(V * H), guarded(V * H)
+    n1, n2 = vgc.softmax_loss_workspace_bytes(code, N, H, V), vgc.softmax_loss_backward_workspace_bytes(code, B, P, H, V)
+    ws = torch.full((max(n1, n2) + 64,), 0xFF, dtype=torch.uint8, device=dev)
+    vgc.softmax_loss(X, W, target, loss, lse, ws[:n1])
+    assert (ws[n1:] == 0xFF).all()
+    ws.fill_(0xFF)
+    vgc.softmax_loss_backward(X, W, target, lse, weight, 1.0 / B, dX[:N * H].view(B, P, H) if want_dx else None, s if want_s else None,
+                              g if want_s else None, ws[:n2])
+    for t, n in ((loss, N), (lse, N), (dX, N * H), (s, V * H), (g, V * H)):
+        assert (t[n:] == 7).all()
+    assert (ws[n2:] == 0xFF).all()
+    return loss[:N], lse[:N], dX[:N * H].view(B, P, H), s[:V * H].view(V, H), g[:V * H].view(V, H)
+
+
+@pytest.mark.parametrize("B,P,H,V", [(4, 100, 512, 8000), (2, 20, 129, 3001), (9, 33, 65, 2500), (3, 7, 264, 900), (64, 1, 512, 3001), (20, 1, 1001, 9000), (256, 1, 40, 1001), (4, 1024, 64, 200001),
+                                     (4, 300, 1500, 30000)])
+@pytest.mark.parametrize("sums", [False, True])
+def test_dx_is_rounded_once(dev, B, P, H, V, sums):
+    """bfloat16: rows that miss their classes by anything, so that the target's entry of D is what dX mostly consists of.  Besides the rounding of
+    dX itself, whose size is that of the exact dX's rounding (to 1 % in the root mean square over thousands of entries), every other
+    entry of D may be off by 2^-9 of itself, each by its own: in the root mean square at most 2^-9 sqrt(sum of (D W)^2); 2e-5 covers the float32
+    sums and exponentials.  (With the target's entry rounded too: 1.1 to 1.3 times the rounding.)"""
+    import torch
+    X, W, target = _inputs(dev, B, P, H, V, "bf16", seed=5)
+    weight = torch.full((B, P), 1.0 / P, device=dev)
+    _, lse, dX, _, _ = _calls(X, W, target, weight, want_s=sums)
+    w = W.double()
+    wt, want, others = w.t().contiguous(), [], 0.0
+    for z in range(0, B, B if P == 1 else 1):
+        n = B if P == 1 else 1
+        x, t, l = X[z:z + n].double().reshape(-1, H), target[z:z + n].reshape(-1), lse.double().view(B, P)[z:z + n].reshape(-1, 1)
+        D = torch.where((t >= 0)[:, None], weight[z:z + n].double().reshape(-1, 1), 0.0) * (x @ wt - l).exp_()
+        p = D.scatter(1, t.clamp(min=0)[:, None], 0.0)
+        others += float((p.square() @ w.square()).sum())
+        D = torch.where((t >= 0)[:, None], D.scatter_add(1, t.clamp(min=0)[:, None], -weight[z:z + n].double().reshape(-1, 1)), 0.0)
+        want.append(D @ w)
+    want = torch.cat(want)
+    size, got = want.norm(), dX.double().reshape(-1, H)
+    rounding = (want.to(torch.bfloat16).double() - want).norm() / size
+    assert float((got - want).norm() / size) <= float(1.01 * rounding + 2.0 ** -9 * others ** 0.5 / size) + 2e-5
