@@ -406,7 +406,9 @@ int vgc_unpack_apply(const uint32_t* const* words, const uint64_t* n_words,
  * [R, ceil(C / 32)].  Aligned to their elements.  C at most 2^31 - 1.  Errors: NULL, SIZE, DTYPE, ALIGN.
  *
  * vgc_sqgrad_act8 is vgc_sqgrad with X given in this form (codes [B, P, J], exps [B, P, ceil(J / 32)]) and D in dtype: the sums are
- * those of the decoded values.  The FC form rounds no square to 16 bits: with VGC_BF16 D both squares are multiplied exactly.
+ * those of the decoded values.  The FC form rounds no square to 16 bits: with VGC_BF16 D both squares are multiplied exactly (one below
+ * 2^-118 loses digits), and where a square alone leaves float32's range, or an infinity or a NaN is among them, an output is what
+ * float32 arithmetic makes of its samples' gradients x d and their squares.
  * workspace (required): DEVICE, 16-byte aligned, vgc_sqgrad_act8_workspace_bytes() bytes.  J at most 4194240. */
 int vgc_act8_encode(int dtype, const void* x, uint64_t R, uint32_t C, int8_t* codes, uint8_t* exps, void* stream);
 int vgc_act8_decode(int dtype, const int8_t* codes, const uint8_t* exps, uint64_t R, uint32_t C, void* out, void* stream);

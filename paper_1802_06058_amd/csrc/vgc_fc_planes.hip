@@ -5,7 +5,8 @@
 // 16 bits, in two.  The products of the planes are exact, so g and s carry float32 sums' errors and, for squares of values that
 // have 16 bits themselves, 2^-17; a product of squares takes four bfloat16 instructions, a quarter of the time of the float32 ones
 // that squares in float32 need.  What is left is what the outputs take to be written, 8 bytes of each element, while N rows are
-// read: 64 x (25088, 4096), g and s: 252 us by float32 instructions -> 160.  (A value whose square lies below 2^-118 loses digits of it.)
+// read: 64 x (25088, 4096), g and s: 252 us by float32 instructions -> 160.  A value whose square lies below 2^-118 loses digits of it; where
+// one leaves float32's range at the other end, the outputs that it reaches are formed again from the values.
 #include "vgc_gemm.h"
 #include "vgc_rows.h"
 
@@ -60,6 +61,23 @@ __global__ __launch_bounds__(256) void k_square_planes_act8(const int8_t* __rest
     store_square_planes<1>(dst + row * Kp + k, (uint64_t)R * Kp, f);
 }
 
+// An output that is not finite, from its samples' values: a square that leaves float32's range does so in planes (infinity, 0), and a plane's zero times
+// infinity is NaN, whatever the sample's gradient is.  Taken as x d and (x d)^2 in float, each output is what its samples make it.
+template <int PA>
+__device__ __forceinline__ void form_again(const Matrix& A, const Matrix& B, uint32_t m, uint32_t n, float c, float* g_out, float* s_out) {
+    float g = 0.f, s = 0.f;
+    for (uint32_t z = 0; z < A.rows && s == s; ++z) {        // (a NaN in s is one in g)
+        float x = 0.f;
+#pragma unroll
+        for (int q = PA - 1; q >= 0; --q) x += __uint_as_float((uint32_t)A.base[q * A.plane + (uint64_t)z * A.ld + m] << 16);
+        const float p = x * __uint_as_float((uint32_t)B.base[(uint64_t)z * B.ld + n] << 16);
+        g += p;
+        s = __builtin_fmaf(p, p, s);
+    }
+    if (g_out && !__builtin_isfinite(*g_out)) *g_out = c * (s == s ? g : s);
+    if (!__builtin_isfinite(*s_out)) *s_out = c * c * s;
+}
+
 typedef TileShape<128, 128, 64, 64, 32, 2, 2, 2> SquareTile;
 template <int PA> using ValueTile = TileShape<128, 128, 64, 64, 32, 2, PA, 1>;
 
@@ -76,7 +94,14 @@ __global__ __launch_bounds__(SquareTile::NW * 64, 2) void k_fc_planes(Matrix A, 
     const TilePlace at = in_bands(xcd_contiguous(blockIdx.x, gridDim.x), tiles_m, tiles_n);
     const uint32_t m0 = at.m * Tile::BM, n0 = at.n * Tile::BN, lane = threadIdx.x & 63u, half = lane >> 5;
     const uint32_t wm = m0 + Tile::wave_m(), wn = n0 + Tile::wave_n();
+    float again = 0.f;                                       // NaN: a sum of this lane's is not finite (each looked at as it is stored: 158 -> 167 us)
     auto store = [&](const f16v (&acc)[Tile::MT][Tile::NT], float scale, float* out) {
+#pragma unroll
+        for (int n = 0; n < Tile::NT; ++n)
+#pragma unroll
+            for (int m = 0; m < Tile::MT; ++m)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) again = __builtin_fmaf(acc[m][n][i], 0.f, again);
 #pragma unroll
         for (int n = 0; n < Tile::NT; ++n) {
             const uint32_t col = wn + n * 32u + (lane & 31u);
@@ -102,6 +127,13 @@ __global__ __launch_bounds__(SquareTile::NW * 64, 2) void k_fc_planes(Matrix A, 
     const Matrix A2 = {A.base + PA * A.plane, A.rows, A.ld, A.plane}, B2 = {B.base + B.plane, B.rows, B.ld, B.plane};
     ColumnTile<Tile>::run(acc, sh, A2, B2, m0, n0, 0u, A.rows);
     store(acc, c * c, s_out);
+    if (__builtin_expect(again == 0.f, 1)) return;
+    for (uint32_t e = 0; e < (uint32_t)(Tile::NT * Tile::MT * 16); ++e) {
+        const uint32_t i = e & 15u, t = e >> 4, col = wn + t / Tile::MT * 32u + (lane & 31u), row = wm + t % Tile::MT * 32u + 8u * (i >> 2) + 4u * half + (i & 3u);
+        if (col >= C || row >= M) continue;
+        float *gp = g_out ? g_out + (size_t)row * C + col : nullptr, *sp = s_out + (size_t)row * C + col;
+        if (!__builtin_isfinite(*sp) || (gp && !__builtin_isfinite(*gp))) form_again<PA>(A, B, row, col, c, gp, sp);
+    }
 }
 
 // Bytes of an operand's planes: `own` of the value and two of its square.
