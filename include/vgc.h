@@ -403,7 +403,8 @@ int vgc_unpack_apply(const uint32_t* const* words, const uint64_t* n_words,
  * count as that, so that every value is finite.  The value is a bfloat16 exactly.  A block of zeros gets exp = 120; one that holds an infinity or a NaN gets exp = 255 and decodes to NaN throughout.
  *
  * x, out: DEVICE, R rows of C elements, dtype VGC_F32 or VGC_BF16; codes: DEVICE int8 [R, C]; exps: DEVICE uint8
- * [R, ceil(C / 32)].  Aligned to their elements.  C at most 2^31 - 1.  Errors: NULL, SIZE, DTYPE, ALIGN.
+ * [R, ceil(C / 32)].  Aligned to their elements.  C at most 2^31 - 1; R rows at most 2^34 - 2^10 pieces, of which a row has one if C <= 8, else
+ * 4 ceil(C / 32).  Errors: NULL, SIZE, DTYPE, ALIGN.
  *
  * vgc_sqgrad_act8 is vgc_sqgrad with X given in this form (codes [B, P, J], exps [B, P, ceil(J / 32)]) and D in dtype: the sums are
  * those of the decoded values.  The FC form rounds no square to 16 bits: with VGC_BF16 D both squares are multiplied exactly (one below

@@ -85,8 +85,9 @@ static uint32_t pieces_per_row(uint32_t C) { return C <= 8 ? 1u : (C + kAct8Bloc
 
 static int act8_grid(uint64_t R, uint32_t C, const char* what, uint32_t* per_row, uint32_t* groups) {
     *per_row = pieces_per_row(C);
-    const uint64_t n = (R * *per_row + kPiecesPerGroup - 1) / kPiecesPerGroup;
-    if (R > (1ull << 40) || n > 0x7FFFFFFFull) { set_error("%s: %llu rows of %u elements exceed the launch limit", what, (unsigned long long)R, C); return VGC_ERR_SIZE; }
+    const uint64_t most = 0xFFFFFFFFull / 256u;              // workgroups of a launch, which has fewer than 2^32 threads
+    const uint64_t n = R > most * kPiecesPerGroup ? most + 1u : (R * *per_row + kPiecesPerGroup - 1) / kPiecesPerGroup;
+    if (n > most) { set_error("%s: %llu rows of %u elements exceed the launch limit", what, (unsigned long long)R, C); return VGC_ERR_SIZE; }
     *groups = (uint32_t)n;
     return VGC_OK;
 }
