@@ -798,8 +798,9 @@ typedef TileShape<128, 256, 64, 64, 64, 2, 2, 1> Sums;       // bfloat16: g and 
 typedef TileShape<128, 128, 64, 32, 64, 2, 3, 1> SumsOfFew;  // of few positions
 
 static uint32_t up8(uint32_t x) { return (x + 7u) / 8u * 8u; }
-static uint32_t tiles(uint32_t a, uint32_t ta, uint32_t b, uint32_t tb) { return (a + ta - 1) / ta * ((b + tb - 1) / tb); }
-template <typename Shape> static uint32_t tiles(uint32_t m, uint32_t n) { return tiles(m, Shape::BM, n, Shape::BN); }
+// (2^24 classes by 2^20 rows are 2^36 tiles of 16 x 16)
+static uint64_t tiles(uint32_t a, uint32_t ta, uint32_t b, uint32_t tb) { return (uint64_t)((a + ta - 1) / ta) * ((b + tb - 1) / tb); }
+template <typename Shape> static uint64_t tiles(uint32_t m, uint32_t n) { return tiles(m, Shape::BM, n, Shape::BN); }
 
 // The kernel that forms the logits.  Forward times (us, both launches) that the rule goes by:
 //   16 x 16 or 32 x 32 results a workgroup while there are no more workgroups than compute units, so that k is what is shared out: 64
@@ -954,7 +955,7 @@ static BackwardPlan backward_plan(int dtype, uint32_t B, uint32_t P, uint32_t H,
     // large tiles where there is work for them (16000 classes, 2048 x 2048: 265 us and 277 by small ones, 512 x 4096: 160 and 158, 256 x 512:
     // 51 and 39; 4000 classes, 4096 x 4096: 257 and 287)
     L.dx_large = dtype == VGC_BF16 && L.Lq > 128u && (uint64_t)L.Lq * H * V >= 50000000000u;
-    const uint32_t n = dtype == VGC_F32 ? tiles<Cut>(L.Lq, H) : L.dx_large ? tiles<Large>(L.Lq, H) : tiles<Small>(L.Lq, H);
+    const uint64_t n = dtype == VGC_F32 ? tiles<Cut>(L.Lq, H) : L.dx_large ? tiles<Large>(L.Lq, H) : tiles<Small>(L.Lq, H);
     L.splits = 1;
     while (n * L.splits < (dtype == VGC_F32 || L.dx_large ? 256u : 512u) && L.piece / (L.splits * 2u) >= 256u && L.splits < 64u) L.splits *= 2u;
     size_t off = 0;
