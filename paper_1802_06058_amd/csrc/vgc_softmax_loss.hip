@@ -874,7 +874,8 @@ static ForwardPlan forward_plan(int dtype, uint32_t N, uint32_t H, uint32_t V) {
     L.tile = logits_tile(dtype, V, N);
     L.rows = rows_plan(dtype, H, L.tile, false);
     const uint64_t row = 2ull * L.rows.planes * L.rows.Kp;
-    L.piece = L.rows.in_place ? V : piece_of(V, row, 256ull << 20);
+    // a launch has fewer than 2^32 threads: 2^36 logits at a time, of which a thread has 32 or more (the thin kernels, one, few altogether)
+    L.piece = (uint32_t)std::min<uint64_t>(L.rows.in_place ? V : piece_of(V, row, 256ull << 20), (1ull << 36) / N / 256u * 256u);
     L.blocks = (V + logits_block(L.tile) - 1) / logits_block(L.tile);
     size_t off = 0;
     L.x = off; if (!L.rows.in_place) off = align_up(off + N * row, 256);
