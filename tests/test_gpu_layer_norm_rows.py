@@ -1,5 +1,6 @@
-"""Layer norm's forward pass over many rows, against 64 bits.  Tolerances as in test_gpu_layer_norm.py: fewer than 128 roundings of 2^-24 of the
-magnitudes summed in a row's sums, a handful for the rest, and half a unit of a bfloat16 output."""
+"""Layer norm's forward pass over many rows that are not kept: other kernels than the kept form's from 520 channels on, so against 64 bits
+by itself.  Tolerances as in test_gpu_layer_norm.py: fewer than 128 roundings of 2^-24 of the magnitudes summed in a row's sums, a handful
+for the rest, and half a unit of a bfloat16 output."""
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -30,6 +31,22 @@ def _check(x, gamma, beta, eps, y, mean, rstd, depth=128):
     assert ((mean.double() - m[:, 0]).abs() <= (err_m + U * m.abs())[:, 0]).all()
     assert ((rstd.double() - r[:, 0]).abs() <= err_r[:, 0]).all()
     assert ((y.double() - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("R,C", [(16384, 513), (16400, 520), (16387, 1001), (20000, 1024), (16391, 2500), (16390, 4096)])
+def test_many_rows_that_are_not_kept(dev, R, C, dtype):
+    import torch
+    from paper_1802_06058_amd import vgc
+    gen = torch.Generator(device=dev).manual_seed(R + C)
+    randn = lambda *s: torch.randn(s, generator=gen, device=dev)
+    x = (randn(R, C) * randn(R, 1).exp() + 3 * randn(R, 1)).to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    gamma, beta = 1 + 0.2 * randn(C), randn(C)
+    y = torch.full((R * C + 32,), 7.0, dtype=x.dtype, device=dev)
+    mean, rstd = torch.full((R + 8,), 7.0, device=dev), torch.full((R + 8,), 7.0, device=dev)
+    vgc.layer_norm(x, gamma, beta, 1e-5, y[:R * C].view(R, C), mean, rstd)
+    _check(x, gamma, beta, 1e-5, y[:R * C].view(R, C), mean[:R], rstd[:R])
+    assert (y[R * C:] == 7).all() and (mean[R:] == 7).all() and (rstd[R:] == 7).all()
 
 
 @pytest.mark.parametrize("kept", [False, True])
