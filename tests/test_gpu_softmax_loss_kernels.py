@@ -52,6 +52,82 @@ def _calls(X, W, target, weight, want_dx=True, want_s=True):
     return loss[:N], lse[:N], dX[:N * H].view(B, P, H), s[:V * H].view(V, H), g[:V * H].view(V, H)
 
 
+def _check(X, W, target, weight, got, sums=True):
+    """Every entry, a sample at a time (samples of one position: all of them)."""
+    import torch
+    B, P, H = X.shape
+    V, bf16 = W.shape[0], X.dtype == torch.bfloat16
+    loss, lse, dX, s, g = got
+    w, c = W.double(), 1.0 / B
+    aw, wt = w.abs(), w.t().contiguous()
+    awt = aw.t().contiguous()
+    zero = torch.zeros(V, H, dtype=torch.float64, device=X.device) if sums else None
+    gw, sw, eg, es = (zero.clone() for _ in range(4)) if sums else [None] * 4
+    lse = lse.double().view(B, P)
+    for z0 in range(0, B, B if P == 1 else 1):
+        z1 = B if P == 1 else z0 + 1
+        x, t, l = X[z0:z1].double().reshape(-1, H), target[z0:z1].reshape(-1), lse[z0:z1].reshape(-1, 1)
+        z, ez = x @ wt, (H + 8) * E * (x.abs() @ awt)
+        wl = torch.logsumexp(z, 1)
+        el = ez.amax(1) + 16 * E * (1 + wl.abs()) + (V // 16 + 64) * E
+        assert ((l[:, 0] - wl).abs() <= el).all()
+        at = t.clamp(min=0)[:, None]
+        want = torch.where(t < 0, 0.0, wl - z.gather(1, at)[:, 0])
+        tol = torch.where(t < 0, 0.0, el + ez.gather(1, at)[:, 0] + 4 * E * (wl.abs() + el))
+        assert ((loss.double().view(B, P)[z0:z1].reshape(-1) - want).abs() <= tol).all()
+        asked = (t >= 0)[:, None]
+        wz = torch.where(asked, torch.ones_like(l) if weight is None else weight[z0:z1].double().reshape(-1, 1), 0.0)
+        p = (z - l).exp()
+        eD = wz.abs() * (p * (ez + 4 * E * (1 + z.abs() + l.abs())) + 2 * E)
+        D = wz * p.scatter_add(1, at, torch.full_like(l, -1.0))
+        aD = D.abs()
+        dXw = D @ w
+        edx = (eD + (2.0 ** -8 if bf16 else 4 * E) * aD) @ aw + (V + 8) * E * (aD @ aw) + (2.0 ** -8 if bf16 else E) * dXw.abs()
+        assert ((dX[z0:z1].double().reshape(-1, H) - dXw).abs() <= edx).all()
+        if not sums:
+            continue
+        x = torch.where(asked, x, 0.0)
+        e = eD + ((2.0 ** -17 if bf16 else 4 * E) + (P + 8) * E) * aD
+        if P == 1:
+            gw += D.t().contiguous() @ x
+            sw += D.square().t().contiguous() @ x.square()
+            eg += e.t().contiguous() @ x.abs() + (B + 8) * E * (aD.t().contiguous() @ x.abs())
+            es += (2 * aD * e + e * e).t().contiguous() @ x.square() + (B + 8) * E * sw
+        else:
+            G, eG = D.t().contiguous() @ x, e.t().contiguous() @ x.abs()
+            gw += G
+            sw += G * G
+            eg += eG + (B + 8) * E * G.abs()
+            es += 2 * G.abs() * eG + eG * eG + (B + 8) * E * G * G
+    if sums:
+        assert ((g.double() - c * gw).abs() <= c * eg).all()
+        assert ((s.double() - c * c * sw).abs() <= c * c * es).all()
+
+
+def _dx_splits(B, P, H, V):
+    """The number of parts of dX's sum that the workspace has room for, from its size: what tells the two tilings of a bfloat16 dX apart."""
+    from paper_1802_06058_amd import vgc
+    up = lambda x, m: -(-x // m) * m
+    N, Lq, Kp = B * P, B * up(P, 16), up(H, 8)
+    planes = 3 if N <= 512 or N * V * H <= 9e9 else 2
+    most = (2 << 30) // (2 * Kp + 2 * planes * Lq) // 256 * 256
+    piece = min(up(-(-V // -(-V // most)), 256), V)
+    rows = 0 if H % 8 == 0 else 2 * Kp
+    parts = up(N * rows, 256) + up(2 * H * Lq, 256) + up(piece * rows, 256) + up(2 * piece * planes * Lq, 256)
+    left = vgc.softmax_loss_backward_workspace_bytes(vgc.BF16, B, P, H, V) - parts
+    assert 0 <= left % (4 * N * H) < 4 * (B + N) + 4096, "the workspace is laid out differently"
+    return left // (4 * N * H), -(-V // piece)
+
+
+@pytest.mark.parametrize("B,P,H,V,splits,pieces", [(4, 300, 1500, 30000, 16, 1), (4, 1024, 64, 200001, 16, 2)])
+def test_large_tiles_of_the_input_gradient_in_parts(dev, B, P, H, V, splits, pieces):
+    """256 x 256 tiles of dX, with remainders in both directions, its sum over the classes in parts (30 and 16 tiles: 16 parts make 256
+    workgroups or the most there are; by 128 x 128 tiles there would be 8 parts of the first), and added to from piece to piece."""
+    assert _dx_splits(B, P, H, V) == (splits, pieces)
+    X, W, target = _inputs(dev, B, P, H, V, "bf16")
+    _check(X, W, target, None, _calls(X, W, target, None))
+
+
 @pytest.mark.parametrize("B,P,H,V", [(4, 100, 512, 8000), (2, 20, 129, 3001), (9, 33, 65, 2500), (3, 7, 264, 900), (64, 1, 512, 3001), (20, 1, 1001, 9000), (256, 1, 40, 1001), (4, 1024, 64, 200001),
                                      (4, 300, 1500, 30000)])
 @pytest.mark.parametrize("sums", [False, True])
