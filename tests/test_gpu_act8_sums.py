@@ -1,4 +1,5 @@
-"""The FC statistic of rows kept in 8 bits from bfloat16 planes: sums that are not finite or whose squares leave float32's range on the way."""
+"""The FC statistic of rows kept in 8 bits from bfloat16 planes: outputs beyond the caches, and sums that are not finite or whose squares leave
+float32's range on the way."""
 import numpy as np
 import pytest
 
@@ -28,6 +29,21 @@ def _call(dev, q, e, D):
     vgc.sqgrad_act8(vgc.FC, torch.from_numpy(q).to(dev), torch.from_numpy(e).to(dev), D, 1.0 / B, only, None, ws)
     assert torch.equal(only.view(torch.int32), s.view(torch.int32))
     return g[:J * C].view(J, C), s[:J * C].view(J, C)
+
+
+def test_sums_beyond_the_caches(dev):
+    """More than 256 MiB of g and s, by 1e-5 of the magnitudes summed (24 samples: as many roundings or truncations of 2^-23)."""
+    import torch
+    B, J, C = 24, 8209, 4133
+    rng = np.random.default_rng(0)
+    q, e = O.act8_encode(np.maximum(rng.standard_normal((B, J)), 0).astype(np.float32))
+    D = torch.from_numpy((1e-3 * rng.standard_normal((B, C))).astype(np.float32)).to(dev).to(torch.bfloat16)
+    g, s = _call(dev, q, e, D)
+    x, d = torch.from_numpy(O.act8_decode(q, e)).to(dev), D.double()
+    xt = x.t().contiguous()
+    assert ((g.double() - xt @ d / B).abs() <= 1e-5 * (xt.abs() @ d.abs()) / B).all()
+    want = xt.square() @ d.square() / B ** 2
+    assert ((s.double() - want).abs() <= 1e-5 * want).all()
 
 
 @pytest.mark.parametrize("B,J,C", [(5, 70, 40), (40, 300, 200), (70, 133, 135)])

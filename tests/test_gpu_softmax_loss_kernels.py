@@ -104,6 +104,21 @@ def _check(X, W, target, weight, got, sums=True):
         assert ((s.double() - c * c * sw).abs() <= c * c * es).all()
 
 
+def _tiles(V, N, bm, bn):
+    return -(-V // bm) * (-(-N // bn))
+
+
+@pytest.mark.parametrize("B,P,H,V", [(100, 1, 24, 60003), (100, 1, 9, 60003), (2, 160, 40, 20500), (2, 150, 17, 20501)])
+def test_small_tiles_of_the_logits(dev, B, P, H, V):
+    """128 x 128 tiles: bfloat16, more than 64 rows, enough of these tiles, and no more than 128 rows or too few of the large ones."""
+    import torch
+    for n in (B * P, B * (P if P == 1 else -(-P // 16) * 16)):
+        assert n > 64 and _tiles(V, n, 128, 128) >= 320 and (n <= 128 or _tiles(V, n, 256, 256) < 192)
+    X, W, target = _inputs(dev, B, P, H, V, "bf16")
+    weight = torch.full((B, P), 1.0 / P, device=dev)
+    _check(X, W, target, weight, _calls(X, W, target, weight))
+
+
 def _dx_splits(B, P, H, V):
     """The number of parts of dX's sum that the workspace has room for, from its size: what tells the two tilings of a bfloat16 dX apart."""
     from paper_1802_06058_amd import vgc
@@ -126,6 +141,19 @@ def test_large_tiles_of_the_input_gradient_in_parts(dev, B, P, H, V, splits, pie
     assert _dx_splits(B, P, H, V) == (splits, pieces)
     X, W, target = _inputs(dev, B, P, H, V, "bf16")
     _check(X, W, target, None, _calls(X, W, target, None))
+
+
+@pytest.mark.parametrize("dtype,B,P,H,V", [("bf16", 3, 40, 515, 60001), ("bf16", 5, 130, 515, 60001), ("bf16", 20, 1, 701, 50001), ("f32", 3, 40, 515, 60001)])
+def test_sums_beyond_the_caches(dev, dtype, B, P, H, V):
+    """g and s of more than 192 MiB (samples of one position: 256) are stored past the caches: from three planes of D, from two, by the FC
+    form, and from float32 planes."""
+    import torch
+    assert V * H * 8 > (256 << 20 if P == 1 else 192 << 20)
+    if dtype == "bf16" and P > 1:
+        assert (B * P > 512 and B * P * V * H > 9e9) == (B == 5)
+    X, W, target = _inputs(dev, B, P, H, V, dtype)
+    weight = torch.rand(B, P, device=dev)
+    _check(X, W, target, weight, _calls(X, W, target, weight))
 
 
 @pytest.mark.parametrize("B,P,H,V", [(4, 100, 512, 8000), (2, 20, 129, 3001), (9, 33, 65, 2500), (3, 7, 264, 900), (64, 1, 512, 3001), (20, 1, 1001, 9000), (256, 1, 40, 1001), (4, 1024, 64, 200001),
