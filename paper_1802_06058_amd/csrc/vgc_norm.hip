@@ -479,8 +479,9 @@ __global__ __launch_bounds__(1024) void k_layer_norm_sums(const float* __restric
 }
 
 // ---- launches ---------------------------------------------------------------------------------------------------------------
-// A team: the fewest lanes (8, 16, 32, 64) that hold a row with a piece each, 64 with two pieces, or a workgroup (`group`) of as many
-// waves as it takes with two pieces a lane (with one: `single`).  held: rows of up to 8192 elements.
+// A team: the fewest lanes (8, 16, 32, 64) that hold a row with a piece each, 64 with two pieces (forward only: backward, a lane has one up to
+// 4096 elements), or a workgroup (`group`) of as many waves as it takes with two pieces a lane (with one: `single`).  held: rows of up to
+// 8192 elements.
 struct Team { uint32_t lanes; bool group, single, held; };
 static Team team_of(uint32_t C, bool single) {
     const uint32_t pieces = (C + 7) / 8, each = single ? 64u : 128u;
@@ -576,7 +577,6 @@ int launch_layer_norm_backward(int dtype, const void* dy, const void* x, const f
         if (!t.held) hipLaunchKernelGGL((k_layer_norm_backward_long<T, KEPT>), grid, block, 0, stream, A); \
         else if (t.group && t.single) VGC_LAUNCH(T, KEPT, 1, 0); \
         else if (t.group) VGC_LAUNCH(T, KEPT, 2, 0); \
-        else if (!t.single) VGC_LAUNCH(T, KEPT, 2, 64); \
         else if (t.lanes == 64u) VGC_LAUNCH(T, KEPT, 1, 64); \
         else if (t.lanes == 32u) VGC_LAUNCH(T, KEPT, 1, 32); \
         else if (t.lanes == 16u) VGC_LAUNCH(T, KEPT, 1, 16); \

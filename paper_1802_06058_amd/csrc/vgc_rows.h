@@ -52,7 +52,7 @@ __device__ __forceinline__ void clip8(Raw8<float>& r, int n) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) r.f[i] = i < n ? r.f[i] : 0.f;
 }
-// Whether eight elements from any place of this row lie inside the rows' array.
+// Whether eight elements from a place of this row may reach past the rows' array: not where at least eight rows follow.
 __device__ __forceinline__ bool rows_at_end(uint64_t row, uint64_t R) { return row + 8u >= R; }
 __device__ __forceinline__ void widen8(const Raw8<uint16_t>& r, float (&f)[8]) {
 #pragma unroll
