@@ -456,8 +456,11 @@ int vgc_layer_norm_backward(int dtype, const void* dy, const void* x, const floa
  * piece of the classes: two GiB, and 256 classes at least.
  * Sums are float32.  VGC_BF16: D, relative to the largest weight of its sample's rows, is rounded to bfloat16 for dX, but for the target's
  * entry, which counts in float32, and kept in 16 significant bits for g and s, all of them up to 512 rows or N V H = 9e9 (weights below
- * 2^-110 of that largest one lose digits).  VGC_F32: products of the operands' 8-bit pieces as in vgc_sqgrad's conv form.  Errors: NULL, SIZE (a zero dimension, N = B P (P rounded up to 32 if it
- * is not 1) or H beyond 2^20, V beyond 2^24), DTYPE, ALIGN, PARAM. */
+ * 2^-110 of that largest one lose digits, and with P = 1 entries of D below 2^-59 in s).  VGC_F32: products of the operands' 8-bit pieces as
+ * in vgc_sqgrad's conv form.
+ * An infinity or a NaN in a row of X that is asked for reaches that row's loss, lse and dX and the sums, in its weight its dX and the sums,
+ * in W any result: as a NaN also where the formulas give an infinity.  It reaches nothing else.
+ * Errors: NULL, SIZE (a zero dimension, N = B P (P rounded up to 32 if it is not 1) or H beyond 2^20, V beyond 2^24), DTYPE, ALIGN, PARAM. */
 size_t vgc_softmax_loss_workspace_bytes(int dtype, uint32_t N, uint32_t H, uint32_t V);
 int vgc_softmax_loss(int dtype, const void* X, const void* W, const int64_t* target, uint32_t N, uint32_t H, uint32_t V, float* loss,
                      float* lse, void* workspace, size_t workspace_bytes, void* stream);

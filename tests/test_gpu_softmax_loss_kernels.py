@@ -182,3 +182,28 @@ def test_dx_is_rounded_once(dev, B, P, H, V, sums):
     size, got = want.norm(), dX.double().reshape(-1, H)
     rounding = (want.to(torch.bfloat16).double() - want).norm() / size
     assert float((got - want).norm() / size) <= float(1.01 * rounding + 2.0 ** -9 * others ** 0.5 / size) + 2e-5
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,P,H,V", [(20, 1, 72, 50), (70, 1, 72, 3000), (3, 7, 33, 40), (4, 100, 64, 6000), (300, 1, 520, 9000)])
+@pytest.mark.parametrize("where", ["x", "weight"])
+@pytest.mark.parametrize("value", [float("inf"), float("nan")])
+def test_values_that_are_not_finite_stay_with_their_row(dev, where, value, B, P, H, V, dtype):
+    """In a row that is asked for they reach its own results (a weight: not its loss) and the sums; the other rows keep their bits, and where
+    the value is a weight, which the rounding of its sample's other rows goes by, stay finite."""
+    import torch
+    X, W, target = _inputs(dev, B, P, H, V, dtype, masked=0.0)
+    weight = torch.rand(B, P, device=dev) + 0.5
+    clean = _calls(X, W, target, weight)
+    z, p = B // 2, P // 2
+    (X if where == "x" else weight.unsqueeze(-1))[z, p, 0] = value
+    loss, lse, dX, s, g = _calls(X, W, target, weight)
+    hit = torch.zeros(B, P, dtype=torch.bool, device=dev)
+    hit[z, p] = True
+    for a, b in ((loss, clean[0]), (lse, clean[1])):
+        a, b = a.view(B, P), b.view(B, P)
+        assert torch.equal(a[~hit], b[~hit]) and (torch.equal(a, b) if where == "weight" else not torch.isfinite(a[hit]).any())
+    assert not torch.isfinite(dX[hit]).any() and torch.isfinite(dX[~hit]).all()
+    others = ~hit if where == "x" else ~hit & (torch.arange(B, device=dev) != z)[:, None]
+    assert torch.equal(dX[others], clean[2][others])
+    assert not torch.isfinite(s).any() and not torch.isfinite(g).any()
