@@ -16,8 +16,8 @@
 // dX, which is rounded to bfloat16 itself; what that left of the target's entry, which all other classes' entries add up to, is added to dX in float
 // (128 rows of 1024, 8192 classes, without: dX 2.04e-3 off, so 1.66e-3, which its own rounding alone is); for g and s, which are float32, a second plane holds the rest, 16 significant bits in all, and
 // of few positions or small products a third what that leaves.  (A third plane for the target's entries alone was tried: k_loss_sums has no
-// registers for it.)  float32 inputs: every operand is cut exactly into three planes of 8 bits and a product is formed from the six pairs
-// of planes that reach 2^-24 of it; few rows are multiplied as floats instead.
+// registers for it.)  float32 inputs: every operand is cut exactly into three planes of 8 bits, rounded, and a product is formed from the six
+// pairs of planes that reach 2^-24 of it; few rows are multiplied as floats instead.
 #include <algorithm>
 
 #include "vgc_gemm.h"
@@ -28,46 +28,34 @@ namespace vgc {
 typedef float f4v __attribute__((ext_vector_type(4)));
 
 // ---- operands -------------------------------------------------------------------------------------------------------------
-// A float cut into three bfloat16 planes, largest first, by truncation: 8 + 8 + 8 bits, exact (but for bits below the smallest
-// subnormal).
-struct Cut3 { uint32_t p[3]; };                              // each the upper half of a float's bits
-__device__ __forceinline__ Cut3 cut3(float x) {
-    Cut3 c;
-    c.p[0] = __float_as_uint(x) >> 16;
-    const bool finite = (__float_as_uint(x) & 0x7F800000u) != 0x7F800000u;
-    if (!finite && (__float_as_uint(x) & 0x7FFFFFu)) c.p[0] |= 0x40u;        // (a NaN keeps being one without its low bits)
-    const float r1 = finite ? x - __uint_as_float(c.p[0] << 16) : 0.f;
-    c.p[1] = __float_as_uint(r1) >> 16;
-    const float r2 = r1 - __uint_as_float(c.p[1] << 16);
-    c.p[2] = __float_as_uint(r2) >> 16;
-    return c;
-}
-// The next plane of two entries of D, the first in the low half, taken out of them: float32 inputs the next 8 bits of the cut; bfloat16
-// ones the rounding of what is left (two planes: within 2^-18 of D; three: all of it).
+// The next plane of two floats, the first in the low half, taken out of them: rounded to the nearest bfloat16, so that what is left is
+// exact and of either sign.  Three planes of a float32 are all of it (8 bits each, but for bits below the smallest subnormal); planes that were
+// cut off instead would leave products too small, all of them, by what the pairs of planes that are not formed hold (logits of 16
+// 7e-7 too small).  bfloat16 inputs: two planes are within 2^-18 of an entry of D, three are all of it.
+// Of a float32, what would be rounded up to infinity is cut off, and an infinity or a NaN leaves nothing.
 template <bool kF32> __device__ __forceinline__ uint32_t next_plane(float& d0, float& d1) {
+    uint32_t x = two_bf16(d0, d1);
     if (kF32) {
-        const Cut3 a = cut3(d0), b = cut3(d1);
-        d0 = __uint_as_float(a.p[1] << 16) + __uint_as_float(a.p[2] << 16);
-        d1 = __uint_as_float(b.p[1] << 16) + __uint_as_float(b.p[2] << 16);
-        return a.p[0] | b.p[0] << 16;
+        const bool finite0 = __builtin_isfinite(d0), finite1 = __builtin_isfinite(d1);
+        if (finite0 && (x & 0x7FFFu) == 0x7F80u) x -= 1u;
+        if (finite1 && (x & 0x7FFF0000u) == 0x7F800000u) x -= 0x10000u;
+        d0 = finite0 ? d0 - __uint_as_float(x << 16) : 0.f;
+        d1 = finite1 ? d1 - __uint_as_float(x & 0xFFFF0000u) : 0.f;
+        return x;
     }
-    const uint32_t x = two_bf16(d0, d1);
     d0 -= __uint_as_float(x << 16);
     d1 -= __uint_as_float(x & 0xFFFF0000u);
     return x;
 }
 
-// Eight values as the planes of an operand, 16 bytes each.
-template <typename T> __device__ __forceinline__ void store_planes(uint16_t* out, uint64_t plane, const float (&f)[8]) {
+// Eight values (used up) as the planes of an operand, 16 bytes each.
+template <typename T> __device__ __forceinline__ void store_planes(uint16_t* out, uint64_t plane, float (&f)[8]) {
     if (sizeof(T) == 2) { store8(out, f, 8); return; }
-    Cut3 c[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) c[e] = cut3(f[e]);
 #pragma unroll
     for (int q = 0; q < 3; ++q) {
         any_u4 v;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = c[2 * e].p[q] | c[2 * e + 1].p[q] << 16;
+        for (int e = 0; e < 4; ++e) v[e] = next_plane<true>(f[2 * e], f[2 * e + 1]);
         *reinterpret_cast<any_u4*>(out + q * plane) = v;
     }
 }
@@ -325,15 +313,11 @@ __device__ __forceinline__ void store_by_classes(f16v (&acc)[MT][NT], uint8_t* t
 
 // Products far below the sum that a matrix instruction adds them to come out too small rather than rounded: with the six products of
 // planes that float32 operands bring for every 16 k, sums shrink as they grow (bfloat16 operands, whose products are of one
-// size, show none of it).  Taken out of the instructions' reach every 128 k, a sum is rounded as float sums are.
-template <typename Shape, bool kOn> struct InParts {
-    __device__ __forceinline__ void after(f16v (&)[Shape::MT][Shape::NT], uint32_t, int) {}
-    __device__ __forceinline__ void end(f16v (&)[Shape::MT][Shape::NT]) {}
-};
-template <typename Shape> struct InParts<Shape, true> {
+// size, show none of it).  Taken out of the instructions' reach every kPart k, a sum is rounded as float sums are.  0: left there.
+template <typename Shape, uint32_t kPart> struct InParts {
     f16v total[Shape::MT][Shape::NT] = {};
     __device__ __forceinline__ void after(f16v (&acc)[Shape::MT][Shape::NT], uint32_t step, int ks) {
-        if (ks != Shape::KS - 1 || (step + 1u) * Shape::BK % 128u != 0u) return;
+        if (ks != Shape::KS - 1 || (step + 1u) * Shape::BK % kPart != 0u) return;
 #pragma unroll
         for (int m = 0; m < Shape::MT; ++m)
 #pragma unroll
@@ -345,6 +329,10 @@ template <typename Shape> struct InParts<Shape, true> {
 #pragma unroll
             for (int n = 0; n < Shape::NT; ++n) acc[m][n] += total[m][n];
     }
+};
+template <typename Shape> struct InParts<Shape, 0u> {
+    __device__ __forceinline__ void after(f16v (&)[Shape::MT][Shape::NT], uint32_t, int) {}
+    __device__ __forceinline__ void end(f16v (&)[Shape::MT][Shape::NT]) {}
 };
 
 // 65536 classes x 2048 k, 4096 bfloat16 rows: forward 0.88-1.0 ms, 1.1-1.25 PFLOP/s, by the clock that the card keeps under the load
@@ -359,8 +347,9 @@ __global__ __launch_bounds__(Shape::NW * 64, 2) void k_logits(LossArgs A) {
     f16v acc[Shape::MT][Shape::NT] = {};
     // the tile's rows of X lie between those of its first and of its last position
     const uint32_t z0 = n0 / A.at.Pp, first = min(z0 * A.at.P + min(n0 - z0 * A.at.Pp, A.at.P), A.N);
-    // float32: in parts of 128 k (600 rows of 4096 channels, logits of 14: lse 1.2e-4 too small, so 1e-6 off)
-    InParts<Shape, Shape::PB == 3> parts;
+    // float32: in parts of 32 k (600 rows of 4096 channels, logits of 14: lse 1.2e-4 too small in one part; 2048 rows of 120, logits of 16: 2.0e-6
+    // off in parts of 128, so 0.9e-6; of 2048: 1.2e-6 and 1.9e-6, where float sums are 9.8e-6)
+    InParts<Shape, Shape::PB == 3 ? 32u : 0u> parts;
     RowTile<Shape>::run(acc, sh, A.w, A.x, m0, first, Shape::BN, [&](uint32_t n) {
         const uint32_t row = A.at.row(n0 + n);
         return row == 0xFFFFFFFFu ? row : row - first;
@@ -545,7 +534,7 @@ __global__ __launch_bounds__(Shape::NW * 64, 2) void k_loss_dx(Matrix Dt, Matrix
     const uint32_t k0 = (uint32_t)((uint64_t)split * steps / splits) * Shape::BK;
     const uint32_t k1 = min((uint32_t)((uint64_t)(split + 1u) * steps / splits) * Shape::BK, Dt.rows);
     f16v acc[Shape::MT][Shape::NT] = {};
-    InParts<Shape, Shape::PB == 3> parts;
+    InParts<Shape, Shape::PB == 3 ? 32u : 0u> parts;
     ColumnTile<Shape>::run(acc, sh, Dt, W, m0, n0, k0, k1, [&](uint32_t step, int ks) { parts.after(acc, step, ks); });
     parts.end(acc);
     const uint32_t lane = threadIdx.x & 63u, half = lane >> 5, wm = m0 + Shape::wave_m(), wn = n0 + Shape::wave_n();
@@ -739,7 +728,7 @@ __global__ __launch_bounds__(Shape::NW * 64, 2) void k_loss_sums(Matrix Dt, Matr
     const uint32_t V = Dt.rows, H = Xt.rows, tiles_n = (H + Shape::BN - 1) / Shape::BN;
     const uint32_t id = xcd_contiguous(blockIdx.x, gridDim.x), m0 = id / tiles_n * Shape::BM, n0 = id % tiles_n * Shape::BN;
     f16v acc[Shape::MT][Shape::NT] = {}, g[Shape::MT][Shape::NT] = {}, s[Shape::MT][Shape::NT] = {};
-    InParts<Shape, Shape::PB == 3> parts;
+    InParts<Shape, Shape::PB == 3 ? 32u : 0u> parts;
     constexpr bool kScaled = Shape::PB == 1;                 // (bfloat16; float32 planes hold D as it is)
     uint32_t left = Pp, z = 0;
     float scale = kScaled ? scales.at(0) : 1.f;
