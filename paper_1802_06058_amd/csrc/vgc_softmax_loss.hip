@@ -349,7 +349,9 @@ __global__ __launch_bounds__(Shape::NW * 64, 2) void k_logits(LossArgs A) {
     const uint32_t z0 = n0 / A.at.Pp, first = min(z0 * A.at.P + min(n0 - z0 * A.at.Pp, A.at.P), A.N);
     // float32: in parts of 32 k (600 rows of 4096 channels, logits of 14: lse 1.2e-4 too small in one part; 2048 rows of 120, logits of 16: 2.0e-6
     // off in parts of 128, so 0.9e-6; of 2048: 1.2e-6 and 1.9e-6, where float sums are 9.8e-6)
-    InParts<Shape, Shape::PB == 3 ? 32u : 0u> parts;
+    // bfloat16, few rows, whose logits' errors no sum averages: of 128 (10 rows of 1703, 21092 classes, logits of 16: lse 4.1e-6 off, so 1.3e-6;
+    // the larger tiles have no registers for it: 3.6e-6, where float sums are 8e-6 off)
+    InParts<Shape, Shape::PB == 3 ? 32u : Shape::MT * Shape::NT <= 2 ? 128u : 0u> parts;
     RowTile<Shape>::run(acc, sh, A.w, A.x, m0, first, Shape::BN, [&](uint32_t n) {
         const uint32_t row = A.at.row(n0 + n);
         return row == 0xFFFFFFFFu ? row : row - first;

@@ -228,3 +228,20 @@ def test_logits_of_floats_are_not_too_small(dev, N, H, V):
     off = lse.double() - want
     assert abs(float(off.mean())) <= 3.7e-7
     assert float(off.square().mean().sqrt()) <= 2.8e-7 * (H / 32 + 9) ** 0.5
+
+
+@pytest.mark.parametrize("N,H,V", [(10, 1703, 21092), (60, 2048, 8000), (128, 2048, 20000)])
+def test_logits_of_few_rows(dev, N, H, V):
+    """bfloat16, logits of 16 in a row: in the root mean square lse is off by H / 128 roundings, each half a step of its sum over sqrt 3 (2^-20.8 above
+    16, half of it below), and a few more of logsumexp.  (16 k at a time, as the instructions add them, there are eight times as many: 1.3 to 2 times this bound.)"""
+    import torch
+    from paper_1802_06058_amd import vgc
+    gen = torch.Generator(device=dev).manual_seed(N)
+    W = (torch.randn(V, H, generator=gen, device=dev) / H ** 0.5).to(torch.bfloat16)
+    t = torch.randint(0, V, (N,), generator=gen, device=dev)
+    X = (torch.randn(N, H, generator=gen, device=dev) + 16 * W[t].float()).to(torch.bfloat16)
+    want = torch.logsumexp(X.double() @ W.double().t().contiguous(), 1)
+    loss, lse = torch.empty(N, device=dev), torch.empty(N, device=dev)
+    ws = torch.empty(vgc.softmax_loss_workspace_bytes(vgc.BF16, N, H, V), dtype=torch.uint8, device=dev)
+    vgc.softmax_loss(X, W, t, loss, lse, ws)
+    assert float((lse.double() - want).square().mean().sqrt()) <= 2.0 ** -20.9 * (H / 128 + 2) ** 0.5
