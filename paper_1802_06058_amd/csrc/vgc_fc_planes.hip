@@ -1,10 +1,10 @@
 // The FC form of the statistic from bfloat16 planes:  g = c A^T B,  s = c^2 (A.A)^T (B.B)  for rows [N, M] and [N, C] of which a row
-// is a sample.  For operands of 16 significant bits or fewer: bfloat16 values, kept 8-bit values, and D of the softmax loss.
+// is a sample.  For bfloat16 values and kept 8-bit values, and for D of the softmax loss, which is float32, on one side of them.
 //
-// An operand enters as planes that add up to it and to its square: a value in one plane (exact) or two (16 bits), its square, 14 or
-// 16 bits, in two.  The products of the planes are exact, so g and s carry float32 sums' errors and, for squares of values that
-// have 16 bits themselves, 2^-17; a product of squares takes four bfloat16 instructions, a quarter of the time of the float32 ones
-// that squares in float32 need.  What is left is what the outputs take to be written, 8 bytes of each element, while N rows are
+// An operand enters as planes that add up to it and to its square: a bfloat16 in one plane and its square, 14 or 16 bits, in two; a float32
+// in three, and its square, rounded to 24 bits, in three.  The products of the planes are exact, so g and s carry float32 sums' errors (the
+// squares' third plane meets the other side's first only: 2^-25 of a product is left out); a product of squares takes four bfloat16
+// instructions, or five, a quarter of the time of the float32 ones that squares in float32 need.  What is left is what the outputs take to be written, 8 bytes of each element, while N rows are
 // read: 64 x (25088, 4096), g and s: 252 us by float32 instructions -> 160.  A value whose square lies below 2^-118 loses digits of it; where
 // one leaves float32's range at the other end, the outputs that it reaches are formed again from the values.
 #include "vgc_gemm.h"
@@ -17,20 +17,25 @@ __device__ __forceinline__ float rest_of(float x) {
     const float hi = __uint_as_float(two_bf16(x, 0.f) << 16);
     return __builtin_isfinite(hi) ? x - hi : 0.f;
 }
-// Planes of eight values: kOwn of the value (1: it is a bfloat16; 2), then two of its square.
+constexpr int square_planes(int own) { return own == 1 ? 2 : 3; }
+// Planes of eight values: kOwn of the value (1: it is a bfloat16; 3), then two or three of its square.
 template <int kOwn>
 __device__ __forceinline__ void store_square_planes(uint16_t* out, uint64_t plane, const float (&f)[8]) {
-    float lo[8], sq[8], sq_lo[8];
+    float rest[8], sq[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        sq[e] = f[e] * f[e];
-        lo[e] = rest_of(f[e]);
-        sq_lo[e] = rest_of(sq[e]);
+    for (int e = 0; e < 8; ++e) { rest[e] = f[e]; sq[e] = f[e] * f[e]; }
+#pragma unroll
+    for (int q = 0; q < kOwn; ++q) {
+        store8(out + q * plane, rest, 8);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) rest[e] = rest_of(rest[e]);
     }
-    store8(out, f, 8);
-    if (kOwn == 2) store8(out + plane, lo, 8);
-    store8(out + kOwn * plane, sq, 8);
-    store8(out + (kOwn + 1) * plane, sq_lo, 8);
+#pragma unroll
+    for (int q = 0; q < square_planes(kOwn); ++q) {
+        store8(out + (kOwn + q) * plane, sq, 8);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sq[e] = rest_of(sq[e]);
+    }
 }
 
 // Rows of T [R, K], padded with zeros to Kp, a multiple of 8; rows with a negative target (if given) as zeros.
@@ -79,16 +84,17 @@ __device__ __forceinline__ void form_again(const Matrix& A, const Matrix& B, uin
 }
 
 typedef TileShape<128, 128, 64, 64, 32, 2, 2, 2> SquareTile;
+typedef TileShape<128, 128, 64, 64, 32, 2, 1, 1> RestTile;
 template <int PA> using ValueTile = TileShape<128, 128, 64, 64, 32, 2, PA, 1>;
 
-// A: PA planes of the m side, then its squares' two; B: one plane of the n side, then its squares' two.
+// A: PA planes of the m side, then its squares'; B: one plane of the n side, then its squares' two.
 // kPast: outputs beyond what the caches hold are stored past them (64 x (25088, 4096), 822 MB: 184 us into them, 160 past them;
 // 128 x (4096, 1000), 33 MB: 20 and 24).
 template <int PA, bool kPast>
 __global__ __launch_bounds__(SquareTile::NW * 64, 2) void k_fc_planes(Matrix A, Matrix B, uint32_t M, uint32_t C, float c, float* __restrict__ g_out,
                                                                       float* __restrict__ s_out) {
     typedef SquareTile Tile;
-    static_assert(ValueTile<PA>::kLds <= Tile::kLds, "one array for both products");
+    static_assert(ValueTile<PA>::kLds <= Tile::kLds, "one array for all products");
     __shared__ __attribute__((aligned(1024))) uint8_t sh[Tile::kLds];
     const uint32_t tiles_n = (C + Tile::BN - 1) / Tile::BN, tiles_m = (M + Tile::BM - 1) / Tile::BM;
     const TilePlace at = in_bands(xcd_contiguous(blockIdx.x, gridDim.x), tiles_m, tiles_n);
@@ -125,6 +131,10 @@ __global__ __launch_bounds__(SquareTile::NW * 64, 2) void k_fc_planes(Matrix A, 
     }
     f16v acc[Tile::MT][Tile::NT] = {};
     const Matrix A2 = {A.base + PA * A.plane, A.rows, A.ld, A.plane}, B2 = {B.base + B.plane, B.rows, B.ld, B.plane};
+    if constexpr (square_planes(PA) == 3) {                  // (five pairs in one pass have more planes than two workgroups' LDS holds)
+        const Matrix A3 = {A2.base + 2 * A.plane, A.rows, A.ld, A.plane};
+        ColumnTile<RestTile>::run(acc, sh, A3, B2, m0, n0, 0u, A.rows);
+    }
     ColumnTile<Tile>::run(acc, sh, A2, B2, m0, n0, 0u, A.rows);
     store(acc, c * c, s_out);
     if (__builtin_expect(again == 0.f, 1)) return;
@@ -136,8 +146,8 @@ __global__ __launch_bounds__(SquareTile::NW * 64, 2) void k_fc_planes(Matrix A, 
     }
 }
 
-// Bytes of an operand's planes: `own` of the value and two of its square.
-size_t fc_planes_bytes(uint32_t own, uint32_t N, uint32_t K) { return align_up((size_t)(own + 2) * N * ((K + 7u) / 8u * 8u) * 2, 256); }
+// Bytes of an operand's planes: `own` of the value and those of its square.
+size_t fc_planes_bytes(uint32_t own, uint32_t N, uint32_t K) { return align_up((size_t)(own + square_planes((int)own)) * N * ((K + 7u) / 8u * 8u) * 2, 256); }
 // (a workgroup addresses a plane's rows with 32-bit offsets)
 bool fc_planes_supported(uint32_t N, uint32_t M, uint32_t C) { return (uint64_t)(N + 64) * (M + 128ull) * 2 < 0x7FFFFFFFull && (uint64_t)(N + 64) * (C + 128ull) * 2 < 0x7FFFFFFFull; }
 
@@ -146,11 +156,11 @@ int launch_square_planes_act8(const int8_t* codes, const uint8_t* exps, uint32_t
     hipLaunchKernelGGL(k_square_planes_act8, planes_grid(R, K), dim3(256), 0, stream, codes, exps, R, K, (K + 7u) / 8u * 8u, (uint16_t*)dst);
     return hip_check(hipGetLastError(), "launch k_square_planes_act8");
 }
-// bfloat16 rows give one plane of the value, float rows two.
+// bfloat16 rows give one plane of the value, float rows three.
 int launch_square_planes(int dtype, const void* src, const int64_t* target, uint32_t R, uint32_t K, void* dst, hipStream_t stream) {
     const uint32_t Kp = (K + 7u) / 8u * 8u;
     if (dtype == VGC_BF16) hipLaunchKernelGGL((k_square_planes<uint16_t, 1>), planes_grid(R, K), dim3(256), 0, stream, (const uint16_t*)src, target, R, K, Kp, (uint16_t*)dst);
-    else hipLaunchKernelGGL((k_square_planes<float, 2>), planes_grid(R, K), dim3(256), 0, stream, (const float*)src, target, R, K, Kp, (uint16_t*)dst);
+    else hipLaunchKernelGGL((k_square_planes<float, 3>), planes_grid(R, K), dim3(256), 0, stream, (const float*)src, target, R, K, Kp, (uint16_t*)dst);
     return hip_check(hipGetLastError(), "launch k_square_planes");
 }
 // a: planes of [N, M] with `own` planes of the value; b: planes of [N, C] with one.
@@ -161,7 +171,7 @@ int launch_fc_planes(const void* a, uint32_t own, const void* b, uint32_t N, uin
     const bool past = (uint64_t)M * C * (g_out ? 8u : 4u) > (256u << 20);
 #define VGC_LAUNCH(OWN, PAST) hipLaunchKernelGGL((k_fc_planes<OWN, PAST>), grid, dim3(SquareTile::NW * 64), 0, stream, A, B, M, C, c, g_out, s_out)
     if (own == 1) { if (past) VGC_LAUNCH(1, true); else VGC_LAUNCH(1, false); }
-    else { if (past) VGC_LAUNCH(2, true); else VGC_LAUNCH(2, false); }
+    else { if (past) VGC_LAUNCH(3, true); else VGC_LAUNCH(3, false); }
 #undef VGC_LAUNCH
     return hip_check(hipGetLastError(), "launch k_fc_planes");
 }

@@ -15,7 +15,7 @@
 // Precision.  bfloat16 inputs: products are exact, sums float32.  D, relative to its sample's largest weight, is rounded to bfloat16 for
 // dX, which is rounded to bfloat16 itself; what that left of the target's entry, which all other classes' entries add up to, is added to dX in float
 // (128 rows of 1024, 8192 classes, without: dX 2.04e-3 off, so 1.66e-3, which its own rounding alone is); for g and s, which are float32, a second plane holds the rest, 16 significant bits in all, and
-// of few positions or small products a third what that leaves.  (A third plane for the target's entries alone was tried: k_loss_sums has no
+// of few positions or small products a third what that leaves; samples of one position have D in float.  (A third plane for the target's entries alone was tried: k_loss_sums has no
 // registers for it.)  float32 inputs: every operand is cut exactly into three planes of 8 bits, rounded, and a product is formed from the six
 // pairs of planes that reach 2^-24 of it; few rows are multiplied as floats instead.
 #include <algorithm>
@@ -937,12 +937,14 @@ static BackwardPlan backward_plan(int dtype, uint32_t B, uint32_t P, uint32_t H,
     // 4 x 128: 229 and 271; 4 x 256: 343 and 462; where the product is small three cost nothing: 15 x 127 x 192, 3958 classes 104 and 97, 4 x 512 x
     // 1024, 4000 classes 133 and 137, but 2 x 1024 x 1000, 8000 classes 195 and 235, 16 x 128 x 256, 30000 classes 272 and 355
     L.planes = dtype == VGC_F32 ? 3u : P == 1 ? 1u : N <= 512u || (uint64_t)N * V * H <= 9000000000u ? 3u : 2u;
-    // samples of one position: the FC form, from planes where the outputs are what it takes (us of the whole call by planes and by floats, 4 M
-    // outputs: 47.0 and 47.6), directly where it is small (200000 outputs: 19 and by floats 21, 500000: 36 and 30), else from floats
+    // samples of one position: the FC form, from planes where many rows or outputs are what it takes (us of the whole call by planes and by floats:
+    // 64 x 1024, 4200 classes 57.0 and 52.8; 64 x 2048, 4000 58.9 and 66.7; 20 x 512, 9000 43.3 and 36.9; 16 x 1024, 32000 119 and 101; 32 x 4096,
+    // 20000 222 and 232; 128 x 2048, 50001 442 and 684), directly where it is small (200000 outputs: 19 and by floats 21, 500000: 36 and 30), else
+    // from floats
     L.sum_thin = P == 1 && N <= 256u && (uint64_t)V * H <= (256u << 10);
-    L.sum_planes = P == 1 && dtype == VGC_BF16 && N >= 16u && (uint64_t)V * H >= (4u << 20) && fc_planes_supported(N, 256, H);
+    L.sum_planes = P == 1 && dtype == VGC_BF16 && N >= 32u && (uint64_t)V * H >= (6u << 20) && fc_planes_supported(N, 256, H);
     const uint64_t row = 2ull * L.rows.planes * L.rows.Kp, dt = L.dx_thin ? 0 : 2ull * L.planes * L.Lq;
-    const uint64_t d32 = P == 1 ? (L.sum_planes ? 12ull : 4ull) * N : 0;
+    const uint64_t d32 = P == 1 ? (L.sum_planes ? 16ull : 4ull) * N : 0;
     L.piece = L.dx_thin ? V : piece_of(V, row + dt + d32, 2048ull << 20);
     // large tiles where there is work for them (16000 classes, 2048 x 2048: 265 us and 277 by small ones, 512 x 4096: 160 and 158, 256 x 512:
     // 51 and 39; 4000 classes, 4096 x 4096: 257 and 287)
@@ -956,7 +958,7 @@ static BackwardPlan backward_plan(int dtype, uint32_t B, uint32_t P, uint32_t H,
     L.w = off; if (!L.rows.in_place) off = align_up(off + L.piece * row, 256);
     L.d = off; if (!L.dx_thin) off = align_up(off + 2 * (size_t)L.piece * L.planes * L.Lq, 256);
     L.d32 = off; if (P == 1) off = align_up(off + 4 * (size_t)N * L.piece, 256);
-    L.d2 = off; if (L.sum_planes) off += fc_planes_bytes(2, N, L.piece);
+    L.d2 = off; if (L.sum_planes) off += fc_planes_bytes(3, N, L.piece);
     L.out = off; if (!L.dx_thin) off += (size_t)L.splits * N * H * sizeof(float);
     off = align_up(off, 16);
     L.scales = off; if (dtype == VGC_BF16 && P > 1) off += (size_t)B * sizeof(float);
@@ -1051,7 +1053,7 @@ int launch_softmax_loss_backward(int dtype, const void* X, const void* W, const 
             if ((rc = hip_check(hipGetLastError(), "launch k_loss_sums")) != VGC_OK) return rc;
         } else if (s_out && L.sum_planes) {
             if ((rc = launch_square_planes(VGC_F32, A.d32, nullptr, N, A.V, ws + L.d2, stream)) != VGC_OK) return rc;
-            if ((rc = launch_fc_planes(ws + L.d2, 2, xt, N, A.V, H, c, g, s, stream)) != VGC_OK) return rc;
+            if ((rc = launch_fc_planes(ws + L.d2, 3, xt, N, A.V, H, c, g, s, stream)) != VGC_OK) return rc;
         } else if (s_out && L.sum_thin) {
             const dim3 grid(tiles(H, 64u, A.V, 4u));
             if (dtype == VGC_F32) hipLaunchKernelGGL(k_loss_sums_thin<float>, grid, dim3(1024), 0, stream, A.d32, (const float*)X, target, N, A.V, H, c, g, s);

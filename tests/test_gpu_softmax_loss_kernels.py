@@ -143,12 +143,13 @@ def test_large_tiles_of_the_input_gradient_in_parts(dev, B, P, H, V, splits, pie
     _check(X, W, target, None, _calls(X, W, target, None))
 
 
-@pytest.mark.parametrize("dtype,B,P,H,V", [("bf16", 3, 40, 515, 60001), ("bf16", 5, 130, 515, 60001), ("bf16", 20, 1, 701, 50001), ("f32", 3, 40, 515, 60001)])
+@pytest.mark.parametrize("dtype,B,P,H,V", [("bf16", 3, 40, 515, 60001), ("bf16", 5, 130, 515, 60001), ("bf16", 20, 1, 701, 50001), ("f32", 3, 40, 515, 60001), ("bf16", 33, 1, 701, 50001),
+                                            ("bf16", 70, 1, 72, 90001)])
 def test_sums_beyond_the_caches(dev, dtype, B, P, H, V):
     """g and s of more than 192 MiB (samples of one position: 256) are stored past the caches: from three planes of D, from two, by the FC
-    form, and from float32 planes."""
+    form from planes (33 samples, and 70 with sums that the caches hold) and from floats, and from float32 planes."""
     import torch
-    assert V * H * 8 > (256 << 20 if P == 1 else 192 << 20)
+    assert V * H * 8 > (256 << 20 if P == 1 else 192 << 20) or H == 72
     if dtype == "bf16" and P > 1:
         assert (B * P > 512 and B * P * V * H > 9e9) == (B == 5)
     X, W, target = _inputs(dev, B, P, H, V, dtype)
@@ -245,3 +246,27 @@ def test_logits_of_few_rows(dev, N, H, V):
     ws = torch.empty(vgc.softmax_loss_workspace_bytes(vgc.BF16, N, H, V), dtype=torch.uint8, device=dev)
     vgc.softmax_loss(X, W, t, loss, lse, ws)
     assert float((lse.double() - want).square().mean().sqrt()) <= 2.0 ** -20.9 * (H / 128 + 2) ** 0.5
+
+
+def _s_off(dev, B, P, H, V, dtype="bf16"):
+    """How far s is off in the root mean square, for rows that lean to their classes by anything and samples that weight their positions alike."""
+    import torch
+    X, W, target = _inputs(dev, B, P, H, V, dtype, seed=9)
+    weight = torch.full((B, P), 1.0 / P, device=dev)
+    _, lse, _, s, _ = _calls(X, W, target, weight)
+    w, want = W.double().t().contiguous(), torch.zeros(V, H, dtype=torch.float64, device=dev)
+    for z in range(B):
+        x, t = X[z].double(), target[z]
+        D = (x @ w - lse.double().view(B, P)[z][:, None]).exp_()
+        D = D.scatter_add_(1, t.clamp(min=0)[:, None], torch.full((P, 1), -1.0, dtype=torch.float64, device=dev)) * torch.where(t >= 0, weight[z].double(), 0.0)[:, None]
+        want += (D.t().contiguous() @ torch.where((t >= 0)[:, None], x, 0.0)).square()
+    return float((s.double() * B * B - want).norm() / want.norm())
+
+
+@pytest.mark.parametrize("B,H,V", [(33, 192, 40001), (64, 105, 60505), (40, 704, 14413), (128, 512, 20011)])
+def test_sums_of_samples_of_one_position_keep_all_digits(dev, B, H, V):
+    """bfloat16, outputs large enough for the FC form from planes.  D is a float32 there: its target entry, p - 1, is off by p (1 - p) times the logit's
+    error, 1.5e-6 at most, of either sign and in the rows between missed and certain; the products, their sum and the scale round half a dozen
+    times at 2^-24 at most.  1e-6 covers both.  (D and its square in 16 bits: 1.3e-6 to 2.0e-6.)"""
+    assert B >= 32 and V * H >= 6 << 20
+    assert _s_off(dev, B, 1, H, V) <= 1e-6
