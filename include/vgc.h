@@ -455,7 +455,7 @@ int vgc_layer_norm_backward(int dtype, const void* dy, const void* x, const floa
  * workspace: DEVICE, 16-byte aligned, of the bytes that the function beside it gives; the backward pass's is bounded by X and by a
  * piece of the classes: two GiB, and 256 classes at least.
  * Sums are float32.  VGC_BF16: D, relative to the largest weight of its sample's rows, is rounded to bfloat16 for dX, but for the target's
- * entry, which counts in float32, and kept in 16 significant bits for g and s, all of them up to 512 rows or N V H = 9e9 and where P is 1
+ * entry, which counts in float32, and kept in 16 significant bits for g and s, all of them where P is below 512 or N V H at most 9e9
  * (weights below 2^-110 of that largest one lose digits, and with P = 1 entries of D below 2^-59 in s).  VGC_F32: products of the operands' 8-bit pieces as
  * in vgc_sqgrad's conv form.
  * An infinity or a NaN in a row of X that is asked for reaches that row's loss, lse and dX and the sums, in its weight its dX and the sums,

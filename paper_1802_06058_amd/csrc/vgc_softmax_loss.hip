@@ -15,7 +15,7 @@
 // Precision.  bfloat16 inputs: products are exact, sums float32.  D, relative to its sample's largest weight, is rounded to bfloat16 for
 // dX, which is rounded to bfloat16 itself; what that left of the target's entry, which all other classes' entries add up to, is added to dX in float
 // (128 rows of 1024, 8192 classes, without: dX 2.04e-3 off, so 1.66e-3, which its own rounding alone is); for g and s, which are float32, a second plane holds the rest, 16 significant bits in all, and
-// of few positions or small products a third what that leaves; samples of one position have D in float.  (A third plane for the target's entries alone was tried: k_loss_sums has no
+// for samples of few positions or small products a third what that leaves; samples of one position have D in float.  (A third plane for the target's entries alone was tried: k_loss_sums has no
 // registers for it.)  float32 inputs: every operand is cut exactly into three planes of 8 bits, rounded, and a product is formed from the six
 // pairs of planes that reach 2^-24 of it; few rows are multiplied as floats instead.
 #include <algorithm>
@@ -786,7 +786,7 @@ typedef TileShape<256, 128, 64, 64, 32, 2, 3, 3> Cut;        // float32: the log
 typedef TileShape<128, 128, 64, 32, 32, 2, 3, 3> CutSums;    // float32: g and s (registers for four accumulators; with 64 x 64 a wave they
 //   spilled: 4 x 512 positions of 1024, 4000 classes, the backward pass 404 us, so 301; 10 x 297 of 3755, 1191 classes, 799 and 727)
 typedef TileShape<128, 256, 64, 64, 64, 2, 2, 1> Sums;       // bfloat16: g and s
-typedef TileShape<128, 128, 64, 32, 64, 2, 3, 1> SumsOfFew;  // of few positions
+typedef TileShape<128, 128, 64, 32, 64, 2, 3, 1> SumsOfFew;  // from all bits of D
 
 static uint32_t up8(uint32_t x) { return (x + 7u) / 8u * 8u; }
 // (2^24 classes by 2^20 rows are 2^36 tiles of 16 x 16)
@@ -931,12 +931,13 @@ static BackwardPlan backward_plan(int dtype, uint32_t B, uint32_t P, uint32_t H,
     const uint64_t work = (uint64_t)N * V * H;
     L.dx_thin = P == 1 && (uint64_t)N * V <= (64u << 20) && (dtype == VGC_F32 ? work <= 2000000000u : V <= 1024u && work <= (256u << 20));
     L.rows = rows_plan(dtype, H, L.tile, !L.dx_thin);
-    // bfloat16: D of few positions, and of small products, in three planes, all its bits, as few positions do not average what two leave out: s off by, two and
-    // three, 2 x 34 positions, 34861 classes 3.2e-6 and 3.4e-7, 11 x 36, 85 classes 2.3e-6 and 2.4e-7, (two) 7 x 853, 5181 classes 1.1e-6.
-    // us of the call: 2 x 38 x 776, 44209 classes 227 and 160; 40 x 2048, 60000 classes 305 and 368; 4 x 64 x 1024, 32000 classes 171 and 195;
-    // 4 x 128: 229 and 271; 4 x 256: 343 and 462; where the product is small three cost nothing: 15 x 127 x 192, 3958 classes 104 and 97, 4 x 512 x
-    // 1024, 4000 classes 133 and 137, but 2 x 1024 x 1000, 8000 classes 195 and 235, 16 x 128 x 256, 30000 classes 272 and 355
-    L.planes = dtype == VGC_F32 ? 3u : P == 1 ? 1u : N <= 512u || (uint64_t)N * V * H <= 9000000000u ? 3u : 2u;
+    // bfloat16: D of samples of few positions, and of small products, in three planes, all its bits, as few positions do not average what two leave
+    // out: s off by, in float32 products, two planes and three, 16 x 64 x 512, 40000 classes 9.4e-7, 2.4e-6 and below 1e-6, 4 x 256 1.4e-6, 2.2e-6 and
+    // below 1e-6; but 2 x 512 1.9e-6 and (two) 2.0e-6, 4 x 1024 1.3e-6 and 1.5e-6, where two are what float32 products are.
+    // us of the call, two and three: 2 x 38 x 776, 44209 classes 227 and 160; 40 x 2048, 60000 classes 305 and 368; 4 x 64 x 1024, 32000 classes 171 and
+    // 195; 4 x 256: 345 and 466; 16 x 256: 1152 and 1553; 16 x 128 x 256, 30000 classes 278 and 355; where the product is small three cost nothing: 15 x
+    // 127 x 192, 3958 classes 104 and 97, 4 x 512 x 1024, 4000 classes 133 and 137, but 2 x 1024 x 1000, 8000 classes 195 and 235
+    L.planes = dtype == VGC_F32 ? 3u : P == 1 ? 1u : P < 512u || (uint64_t)N * V * H <= 9000000000u ? 3u : 2u;
     // samples of one position: the FC form, from planes where many rows or outputs are what it takes (us of the whole call by planes and by floats:
     // 64 x 1024, 4200 classes 57.0 and 52.8; 64 x 2048, 4000 58.9 and 66.7; 20 x 512, 9000 43.3 and 36.9; 16 x 1024, 32000 119 and 101; 32 x 4096,
     // 20000 222 and 232; 128 x 2048, 50001 442 and 684), directly where it is small (200000 outputs: 19 and by floats 21, 500000: 36 and 30), else
