@@ -51,7 +51,7 @@ __device__ __forceinline__ void keep_act8(const float (&f)[8], uint32_t C, uint3
 // A team takes rows team, team + teams, ..: its part of gamma and beta stays in registers, and the next row is on its way while the
 // present one is reduced and stored.  Teams: kL lanes each, or (kL = 0) the workgroup.  (A row a workgroup, gamma and beta read for each:
 // 16384 x 4096 bfloat16 68.5 us; so 52.6.)
-// 16384 x 4096 bfloat16: 50 us, 5.4 TB/s of x and y; kept in 8 bits too and decoded again by vgc_act8_decode 107, 4.3 TB/s.  128 x 1000
+// 16384 x 4096 bfloat16: 50 us, 5.4 TB/s of x and y; kept in 8 bits too and decoded again by vgc_act8_decode 107, 5.0 TB/s.  128 x 1000
 // float32: 8 us a call, which is the call's own time.
 template <typename T, int kNV, int kL, bool kKeep>
 __global__ __launch_bounds__(kL == 0 ? 512 : 256) void k_layer_norm(const T* __restrict__ x, uint32_t R, uint32_t C, uint32_t teams, const float* __restrict__ gamma,
@@ -117,7 +117,8 @@ __global__ __launch_bounds__(kL == 0 ? 512 : 256) void k_layer_norm(const T* __r
     }
 }
 
-// Rows beyond what a team holds: a workgroup a row, read three times (the last two from the cache).
+// Rows beyond what a team holds: a workgroup a row, read three times (the last two from the cache).  16384 x 12288 bfloat16: 219 us, 3.7 TB/s of x
+// and y, bound by the three passes following each other.
 template <typename T, bool kKeep>
 __global__ __launch_bounds__(1024) void k_layer_norm_long(const T* __restrict__ x, uint32_t C, const float* __restrict__ gamma,
                                                           const float* __restrict__ beta, float eps, T* __restrict__ y,
@@ -356,7 +357,8 @@ __global__ __launch_bounds__(kL == 0 ? 512 : 256) void k_layer_norm_backward(Nor
 }
 
 // Rows beyond what the largest workgroup holds: a workgroup per part of a sample, as above, that reads its rows twice (the
-// second time from the cache) and keeps its column sums where they end up, in its own planes of the workspace.
+// second time from the cache) and keeps its column sums where they end up, in its own planes of the workspace.  16 x 1024 x 12288 bfloat16 from
+// x: 804 us, 1.5 TB/s of dy, x and dx: the column sums are read and written for every row.
 template <typename T, bool kKept>
 __global__ __launch_bounds__(1024) void k_layer_norm_backward_long(NormArgs A) {
     __shared__ float sh[2][kMaxWaves][2];
@@ -508,7 +510,7 @@ int launch_layer_norm(int dtype, const void* x, uint64_t R, uint32_t C, const fl
     if (R > 0x7FFFFFFFull) { set_error("vgc_layer_norm: %llu rows exceed the launch limit", (unsigned long long)R); return VGC_ERR_SIZE; }
     // Sixteen waves a compute unit, which is what the loads in flight need, in whole workgroups a compute unit.  Many rows that are not
     // kept: one piece a lane (us; bfloat16, two pieces and one: 16384 x 4096 52.6 and 49.9, 60000 x 2048 94.5 and 91.4, but 4096 x 4096 13.5
-    // and 14.9, 16384 x 4096 kept 107.3 and 108.5).
+    // and 14.9, 16384 x 4096 kept 107.3 and 108.5; between 4096 and 16384 rows not measured).
     const uint32_t rows = (uint32_t)R;
     const Team t = team_of(C, !codes && rows >= 16384u && C <= 4096u);
     const uint32_t each = t.group ? 1u : 256u / t.lanes, want = 256u * (t.group ? std::max(1u, 16u / (t.lanes / 64u)) : 4u);

@@ -13,11 +13,12 @@
 // the loop of vgc_gemm.h.
 //
 // Precision.  bfloat16 inputs: products are exact, sums float32.  D, relative to its sample's largest weight, is rounded to bfloat16 for
-// dX, which is rounded to bfloat16 itself; what that left of the target's entry, which all other classes' entries add up to, is added to dX in float
-// (128 rows of 1024, 8192 classes, without: dX 2.04e-3 off, so 1.66e-3, which its own rounding alone is); for g and s, which are float32, a second plane holds the rest, 16 significant bits in all, and
-// for samples of few positions or small products a third what that leaves; samples of one position have D in float.  (A third plane for the target's entries alone was tried: k_loss_sums has no
-// registers for it.)  float32 inputs: every operand is cut exactly into three planes of 8 bits, rounded, and a product is formed from the six
-// pairs of planes that reach 2^-24 of it; few rows are multiplied as floats instead.
+// dX, which is rounded to bfloat16 itself; what that left of the target's entry, which all other classes' entries add up to, is added
+// to dX in float (128 rows of 1024, 8192 classes, without: dX 2.04e-3 off, so 1.66e-3, which its own rounding alone is).  For g and s, which
+// are float32, a second plane holds the rest, 16 significant bits in all, and for samples of few positions or small products a third what
+// that leaves; samples of one position have D in float.  (A third plane for the target's entries alone was tried: k_loss_sums has no
+// registers for it.)  float32 inputs: every operand is cut exactly into three planes of 8 bits, rounded, and a product is formed from the
+// six pairs of planes that reach 2^-24 of it; few rows are multiplied as floats instead.
 #include <algorithm>
 
 #include "vgc_gemm.h"
