@@ -66,26 +66,62 @@ __global__ __launch_bounds__(256) void k_square_planes_act8(const int8_t* __rest
     store_square_planes<1>(dst + row * Kp + k, (uint64_t)R * Kp, f);
 }
 
-// An output that is not finite, from its samples' values: a square that leaves float32's range does so in planes (infinity, 0), and a plane's zero times
-// infinity is NaN, whatever the sample's gradient is.  Taken as x d and (x d)^2 in float, each output is what its samples make it.
-template <int PA>
-__device__ __forceinline__ void form_again(const Matrix& A, const Matrix& B, uint32_t m, uint32_t n, float c, float* g_out, float* s_out) {
-    float g = 0.f, s = 0.f;
-    for (uint32_t z = 0; z < A.rows && s == s; ++z) {        // (a NaN in s is one in g)
-        float x = 0.f;
-#pragma unroll
-        for (int q = PA - 1; q >= 0; --q) x += __uint_as_float((uint32_t)A.base[q * A.plane + (uint64_t)z * A.ld + m] << 16);
-        const float p = x * __uint_as_float((uint32_t)B.base[(uint64_t)z * B.ld + n] << 16);
-        g += p;
-        s = __builtin_fmaf(p, p, s);
-    }
-    if (g_out && !__builtin_isfinite(*g_out)) *g_out = c * (s == s ? g : s);
-    if (!__builtin_isfinite(*s_out)) *s_out = c * c * s;
-}
-
 typedef TileShape<128, 128, 64, 64, 32, 2, 2, 2> SquareTile;
 typedef TileShape<128, 128, 64, 64, 32, 2, 1, 1> RestTile;
 template <int PA> using ValueTile = TileShape<128, 128, 64, 64, 32, 2, PA, 1>;
+
+// The outputs of a wave that are not finite, from their samples' values: a square that leaves float32's range does so in planes (infinity, 0), and
+// a plane's zero times infinity is NaN, whatever the sample's gradient is.  Taken as x d and (x d)^2 in float, each output is what its samples
+// make it.  A lane loads a row's and a column's value of a sample; its 64 products take theirs from the other lanes.  (64 x (25088, 4096)
+// with an infinity in every column: 1.9 ms; an output at a time, four loads for each of its samples, 9.9.  Where nothing but NaN is left, it ends.)
+template <int PA>
+__device__ __forceinline__ void form_again(const Matrix& A, const Matrix& B, uint32_t wm, uint32_t wn, uint32_t M, uint32_t C, float c, float* __restrict__ g_out,
+                                           float* __restrict__ s_out) {
+    typedef SquareTile Tile;
+    static_assert(Tile::WM == 64 && Tile::WN == 64, "a lane for each row and column");
+    const uint32_t lane = threadIdx.x & 63u, half = lane >> 5;
+    const uint16_t *a = A.base + min(wm + lane, M - 1u), *b = B.base + min(wn + lane, C - 1u);
+    f16v g[Tile::MT][Tile::NT] = {}, s[Tile::MT][Tile::NT] = {};
+    for (uint32_t z = 0; z < A.rows; ++z) {
+        float x = 0.f, d[Tile::NT];
+#pragma unroll
+        for (int q = PA - 1; q >= 0; --q) x += __uint_as_float((uint32_t)a[q * A.plane + (uint64_t)z * A.ld] << 16);
+        const float y = __uint_as_float((uint32_t)b[(uint64_t)z * B.ld] << 16);
+#pragma unroll
+        for (int n = 0; n < Tile::NT; ++n) d[n] = __shfl(y, n * 32 + (lane & 31u));
+        bool nothing = true;                                 // (a NaN in s is one in g)
+#pragma unroll
+        for (int m = 0; m < Tile::MT; ++m)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float r = __shfl(x, m * 32 + 8 * (i >> 2) + 4 * half + (i & 3));
+#pragma unroll
+                for (int n = 0; n < Tile::NT; ++n) {
+                    const float p = r * d[n];
+                    g[m][n][i] += p;
+                    s[m][n][i] = __builtin_fmaf(p, p, s[m][n][i]);
+                    nothing &= s[m][n][i] != s[m][n][i];
+                }
+            }
+        if (__all(nothing)) break;
+    }
+#pragma unroll
+    for (int n = 0; n < Tile::NT; ++n) {
+        const uint32_t col = wn + n * 32u + (lane & 31u);
+        if (col >= C) continue;
+#pragma unroll
+        for (int m = 0; m < Tile::MT; ++m)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const uint32_t row = wm + m * 32u + 8u * (i >> 2) + 4u * half + (i & 3);
+                if (row >= M) continue;
+                float *gp = g_out ? g_out + (size_t)row * C + col : nullptr, *sp = s_out + (size_t)row * C + col;
+                const float sum = s[m][n][i];
+                if (gp && !__builtin_isfinite(*gp)) *gp = c * (sum == sum ? g[m][n][i] : sum);
+                if (!__builtin_isfinite(*sp)) *sp = c * c * sum;
+            }
+    }
+}
 
 // A: PA planes of the m side, then its squares'; B: one plane of the n side, then its squares' two.
 // kPast: outputs beyond what the caches hold are stored past them (64 x (25088, 4096), 822 MB: 184 us into them, 160 past them;
@@ -137,13 +173,7 @@ __global__ __launch_bounds__(SquareTile::NW * 64, 2) void k_fc_planes(Matrix A, 
     }
     ColumnTile<Tile>::run(acc, sh, A2, B2, m0, n0, 0u, A.rows);
     store(acc, c * c, s_out);
-    if (__builtin_expect(again == 0.f, 1)) return;
-    for (uint32_t e = 0; e < (uint32_t)(Tile::NT * Tile::MT * 16); ++e) {
-        const uint32_t i = e & 15u, t = e >> 4, col = wn + t / Tile::MT * 32u + (lane & 31u), row = wm + t % Tile::MT * 32u + 8u * (i >> 2) + 4u * half + (i & 3u);
-        if (col >= C || row >= M) continue;
-        float *gp = g_out ? g_out + (size_t)row * C + col : nullptr, *sp = s_out + (size_t)row * C + col;
-        if (!__builtin_isfinite(*sp) || (gp && !__builtin_isfinite(*gp))) form_again<PA>(A, B, row, col, c, gp, sp);
-    }
+    if (__any(!(again == 0.f))) form_again<PA>(A, B, wm, wn, M, C, c, g_out, s_out);
 }
 
 // Bytes of an operand's planes: `own` of the value and those of its square.
