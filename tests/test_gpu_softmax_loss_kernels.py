@@ -186,7 +186,7 @@ def test_dx_is_rounded_once(dev, B, P, H, V, sums):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("B,P,H,V", [(20, 1, 72, 50), (70, 1, 72, 3000), (3, 7, 33, 40), (4, 100, 64, 6000), (300, 1, 520, 9000)])
+@pytest.mark.parametrize("B,P,H,V", [(20, 1, 72, 50), (70, 1, 72, 3000), (3, 7, 33, 40), (4, 100, 64, 6000), (300, 1, 520, 9000), (67, 1, 520, 13001)])
 @pytest.mark.parametrize("where", ["x", "weight"])
 @pytest.mark.parametrize("value", [float("inf"), float("nan")])
 def test_values_that_are_not_finite_stay_with_their_row(dev, where, value, B, P, H, V, dtype):
