@@ -469,6 +469,68 @@ int vgc_softmax_loss_backward(int dtype, const void* X, const void* W, const int
                               uint32_t B, uint32_t P, uint32_t H, uint32_t V, float c, void* dX, float* g_out, float* s_out,
                               void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- linear layer, dropout, group norm ------------------------------------------------------------
+ * The parts of a residual block between the weights whose sums the calls above form.  Activations, by number (in float32):
+ *     relu max(z, 0);   gelu z Phi(z) with Phi the normal distribution function;   silu z / (1 + e^-z)
+ *
+ * vgc_dropout:  y = residual + (dropped ? 0 : x 65536 / (65536 - t)),  t = round(65536 p), on R rows of C elements.  An element is dropped if its 16-bit
+ * number is below t.  The numbers are the words of Philox with four words and ten rounds (Salmon et al., SC 2011) under the key rng[0], low
+ * halves first, of the counter (column / 8, row, low half of rng[1], high half of rng[1]): eight columns a counter.  They depend on nothing else, so the mask is
+ * drawn again where it is needed and never stored: the backward pass is the same call on the output's gradient (without residual).
+ * rng: DEVICE uint64[2], a key and the number of the call (another for every dropout of a step and every step), read when the kernel runs: a recorded
+ * graph draws a new mask where they have changed.  NULL only where t = 0.  residual: NULL, or like x.  y may be x or residual.
+ * x, residual, y: DEVICE [R, C], dtype VGC_F32 or VGC_BF16, aligned to their elements; R, C at most 2^31 - 1.  A dropped infinity or NaN is 0.
+ * Errors: NULL, SIZE (a zero dimension or a larger one), DTYPE, ALIGN, PARAM (p outside [0, 1] or a NaN).
+ *
+ * vgc_linear:  z = X W + bias,  y = residual + drop(act(z)) with dropout as above on the rows of y, one rounding at the end.
+ * X [N, K], W [K, C] (the layout in which vgc_sqgrad gives its sums), residual, z, y [N, C]: DEVICE, dtype; bias: DEVICE float [C] or NULL; residual, z: or NULL.
+ * z is what the backward pass of an activation needs.  y may be residual; else no output overlaps an input.
+ *
+ * vgc_linear_backward, rows being P positions of B samples, from the output's gradient dy [B, P, C] (of each sample's own loss):
+ *     dz = drop(dy) act'(z),  dX = add + dz W^T,   H_z = sum_p dz[z, p]:  the gradient of the bias by sample;
+ *     g_bias = c sum_z H_z,  s_bias = c^2 sum_z H_z . H_z  (Alg. 1; c as for vgc_sqgrad);  the sums of W are vgc_sqgrad's of X and dz.
+ * z: what the forward call wrote (NULL for VGC_ACT_NONE; for relu any array with its signs will do, such as y without dropout and residual);
+ * rng as the forward call found it.  dz: DEVICE [B, P, C] in dtype, may be dy or z; dX: DEVICE [B, P, K] in dtype, or NULL; add: NULL, or like dX, and may be it;
+ * s_bias: DEVICE float [C] or NULL; g_bias: the same (NULL if s_bias is).  The bias's sums are those of dz before it is rounded.
+ * VGC_BF16: dX is formed from dz in bfloat16, for products N K C of at most 2^31 in two such pieces, 16 bits.  VGC_F32: products of the operands' 8-bit pieces as
+ * in vgc_sqgrad's conv form.
+ *
+ * X, W, dz: 16-byte aligned, the others to their elements.  workspace: DEVICE, 16-byte aligned, of the bytes that the function beside it gives (NULL
+ * if that is 0).  No result depends on scheduling.
+ * An infinity or a NaN in a row of X, residual, dy or z reaches that row, in W or bias any result; as a NaN also where the formulas give an infinity.
+ * Errors: NULL, SIZE (a zero dimension, N = B P, K or C beyond 2^20, K C beyond 2^30, N K or N C beyond 2^34), DTYPE, ALIGN, PARAM (act unknown, p as above, c
+ * not finite).
+ *
+ * vgc_group_norm on x [B, P, C] (channels last, P = height x width), G groups of w = C / G consecutive channels.  Of a sample's M = P w elements of a group:
+ *     mean = sum x / M,  rstd = 1 / sqrt(sum (x - mean)^2 / M + eps),  xhat = (x - mean) rstd,  y = act(gamma xhat + beta)
+ * Unlike a norm over the batch it leaves every sample a gradient of its own, which the method's sums are made of (Section 4.1).
+ * Backward:  e = dy act'(gamma xhat + beta),  d = e gamma,  dx = rstd (d - sum d / M - xhat sum (d xhat) / M);  G_z = sum_p e xhat,  H_z = sum_p e by channel:
+ *     g_gamma = c sum_z G_z,  s_gamma = c^2 sum_z G_z . G_z,  g_beta and s_beta likewise from H_z.
+ * x, y, dy, dx: DEVICE [B, P, C] in dtype, an output overlapping no input; gamma, beta: DEVICE float [C]; mean, rstd: DEVICE float [B, G]; the four
+ * sums: DEVICE float [C], g_gamma and g_beta or NULL.  Pointers are aligned to their elements; workspace as above.
+ * An infinity or a NaN gives NaN in that sample's group and in its channels' sums, nowhere else.
+ * Errors: NULL, SIZE (a zero dimension, G not dividing C, B P beyond 2^31 - 1, C beyond 2^20), DTYPE, ALIGN, PARAM (act unknown, eps negative or not finite, c not
+ * finite). */
+enum { VGC_ACT_NONE = 0, VGC_ACT_RELU = 1, VGC_ACT_GELU = 2, VGC_ACT_SILU = 3 };
+
+int vgc_dropout(int dtype, const void* x, const void* residual, uint64_t R, uint32_t C, float p, const uint64_t* rng, void* y, void* stream);
+
+size_t vgc_linear_workspace_bytes(int dtype, uint32_t N, uint32_t K, uint32_t C);
+int vgc_linear(int dtype, const void* X, const void* W, const float* bias, int act, float p, const uint64_t* rng, const void* residual, uint32_t N,
+               uint32_t K, uint32_t C, void* z, void* y, void* workspace, size_t workspace_bytes, void* stream);
+size_t vgc_linear_backward_workspace_bytes(int dtype, uint32_t B, uint32_t P, uint32_t K, uint32_t C);
+int vgc_linear_backward(int dtype, const void* dy, const void* z, const void* W, int act, float p, const uint64_t* rng, const void* add, uint32_t B,
+                        uint32_t P, uint32_t K, uint32_t C, float c, void* dz, void* dX, float* g_bias, float* s_bias, void* workspace,
+                        size_t workspace_bytes, void* stream);
+
+size_t vgc_group_norm_workspace_bytes(int dtype, uint32_t B, uint32_t P, uint32_t C, uint32_t G);
+int vgc_group_norm(int dtype, const void* x, uint32_t B, uint32_t P, uint32_t C, uint32_t G, const float* gamma, const float* beta, float eps, int act,
+                   void* y, float* mean, float* rstd, void* workspace, size_t workspace_bytes, void* stream);
+size_t vgc_group_norm_backward_workspace_bytes(int dtype, uint32_t B, uint32_t P, uint32_t C, uint32_t G);
+int vgc_group_norm_backward(int dtype, const void* dy, const void* x, const float* mean, const float* rstd, const float* gamma, const float* beta, int act,
+                            uint32_t B, uint32_t P, uint32_t C, uint32_t G, float c, void* dx, float* g_gamma, float* s_gamma, float* g_beta,
+                            float* s_beta, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -5,6 +5,7 @@
 #include <cstring>
 #include <mutex>
 
+#include "vgc_epilogue.h"
 #include "vgc_internal.h"
 
 namespace vgc {
@@ -876,6 +877,149 @@ int vgc_softmax_loss_backward(int dtype, const void* X, const void* W, const int
     if (!std::isfinite(c)) { set_error("vgc_softmax_loss_backward: c is not finite"); return VGC_ERR_PARAM; }
     if ((rc = workspace_check("vgc_softmax_loss_backward", workspace, workspace_bytes, softmax_loss_backward_workspace_bytes(dtype, B, P, H, V))) != VGC_OK) return rc;
     return launch_softmax_loss_backward(dtype, X, W, target, lse, weight, B, P, H, V, c, dX, g_out, s_out, workspace, static_cast<hipStream_t>(stream));
+}
+
+// ---- linear layer, dropout, group norm ----------------------------------------------------------------------------------------
+static int type_check(const char* what, int dtype) {
+    if (dtype != VGC_F32 && dtype != VGC_BF16) { set_error("%s: unknown dtype %d", what, dtype); return VGC_ERR_DTYPE; }
+    return VGC_OK;
+}
+static int act_check(const char* what, int act) {
+    if (act < VGC_ACT_NONE || act > VGC_ACT_SILU) { set_error("%s: unknown activation %d", what, act); return VGC_ERR_PARAM; }
+    return VGC_OK;
+}
+static int dropout_check(const char* what, float p, const uint64_t* rng) {
+    if (!(p >= 0.0f && p <= 1.0f)) { set_error("%s: p must be in [0, 1] (got %g)", what, p); return VGC_ERR_PARAM; }
+    if (dropout_of(p, rng).t != 0u && !rng) { set_error("%s: rng is required where elements are dropped", what); return VGC_ERR_NULL; }
+    if (!aligned(rng, 8)) { set_error("%s: rng must be aligned to its elements", what); return VGC_ERR_ALIGN; }
+    return VGC_OK;
+}
+
+int vgc_dropout(int dtype, const void* x, const void* residual, uint64_t R, uint32_t C, float p, const uint64_t* rng, void* y, void* stream) {
+    int rc = type_check("vgc_dropout", dtype);
+    if (rc != VGC_OK) return rc;
+    if (!x || !y) { set_error("vgc_dropout: x and y are required"); return VGC_ERR_NULL; }
+    if (R == 0 || C == 0) { set_error("vgc_dropout: zero dimension"); return VGC_ERR_SIZE; }
+    if (R > 0x7FFFFFFFu || C > 0x7FFFFFFFu) { set_error("vgc_dropout: %llu rows of %u elements", (unsigned long long)R, C); return VGC_ERR_SIZE; }
+    const size_t e = element_bytes(dtype);
+    if (!aligned(x, e) || !aligned(residual, e) || !aligned(y, e)) { set_error("vgc_dropout: pointers must be aligned to their elements"); return VGC_ERR_ALIGN; }
+    if ((rc = dropout_check("vgc_dropout", p, rng)) != VGC_OK) return rc;
+    return launch_dropout(dtype, x, residual, (uint32_t)R, C, dropout_of(p, rng), y, static_cast<hipStream_t>(stream));
+}
+
+static int linear_shape(const char* what, int dtype, uint32_t B, uint32_t P, uint32_t K, uint32_t C) {
+    const int rc = type_check(what, dtype);
+    if (rc != VGC_OK) return rc;
+    if (B == 0 || P == 0 || K == 0 || C == 0) { set_error("%s: zero dimension", what); return VGC_ERR_SIZE; }
+    const uint64_t N = (uint64_t)B * P;
+    if (N > (1u << 20) || K > (1u << 20) || C > (1u << 20)) { set_error("%s: %llu rows, %u to %u columns exceed 2^20", what, (unsigned long long)N, K, C); return VGC_ERR_SIZE; }
+    if ((uint64_t)K * C > (1u << 30)) { set_error("%s: a weight of %u x %u exceeds 2^30", what, K, C); return VGC_ERR_SIZE; }
+    if (N * K > (1ull << 34) || N * C > (1ull << 34)) { set_error("%s: %llu rows of %u and %u columns exceed 2^34", what, (unsigned long long)N, K, C); return VGC_ERR_SIZE; }
+    return VGC_OK;
+}
+
+size_t vgc_linear_workspace_bytes(int dtype, uint32_t N, uint32_t K, uint32_t C) {
+    return linear_shape("vgc_linear", dtype, N, 1, K, C) == VGC_OK ? linear_workspace_bytes(dtype, N, K, C) : 0;
+}
+
+int vgc_linear(int dtype, const void* X, const void* W, const float* bias, int act, float p, const uint64_t* rng, const void* residual, uint32_t N,
+               uint32_t K, uint32_t C, void* z, void* y, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!X || !W || !y) { set_error("vgc_linear: X, W and y are required"); return VGC_ERR_NULL; }
+    int rc = linear_shape("vgc_linear", dtype, N, 1, K, C);
+    if (rc != VGC_OK) return rc;
+    const size_t e = element_bytes(dtype);
+    if (!aligned(X, 16) || !aligned(W, 16) || !aligned(bias, 4) || !aligned(residual, e) || !aligned(z, e) || !aligned(y, e)) {
+        set_error("vgc_linear: X and W must be 16-byte aligned, the others to their elements");
+        return VGC_ERR_ALIGN;
+    }
+    if ((rc = act_check("vgc_linear", act)) != VGC_OK || (rc = dropout_check("vgc_linear", p, rng)) != VGC_OK) return rc;
+    if ((rc = workspace_check("vgc_linear", workspace, workspace_bytes, linear_workspace_bytes(dtype, N, K, C))) != VGC_OK) return rc;
+    LinearCall L = {};
+    L.dtype = dtype; L.act = act; L.X = X; L.W = W; L.residual = residual; L.bias = bias; L.p = p; L.rng = rng;
+    L.B = N; L.P = 1; L.K = K; L.C = C; L.z = z; L.y = y;
+    return launch_linear(L, workspace, static_cast<hipStream_t>(stream));
+}
+
+size_t vgc_linear_backward_workspace_bytes(int dtype, uint32_t B, uint32_t P, uint32_t K, uint32_t C) {
+    return linear_shape("vgc_linear_backward", dtype, B, P, K, C) == VGC_OK ? linear_backward_workspace_bytes(dtype, B, P, K, C) : 0;
+}
+
+int vgc_linear_backward(int dtype, const void* dy, const void* z, const void* W, int act, float p, const uint64_t* rng, const void* add, uint32_t B,
+                        uint32_t P, uint32_t K, uint32_t C, float c, void* dz, void* dX, float* g_bias, float* s_bias, void* workspace,
+                        size_t workspace_bytes, void* stream) {
+    if (!dy || !dz || (dX && !W)) { set_error("vgc_linear_backward: dy and dz are required, and W for dX"); return VGC_ERR_NULL; }
+    if ((g_bias && !s_bias) || (add && !dX)) { set_error("vgc_linear_backward: g_bias goes with s_bias, and add with dX"); return VGC_ERR_NULL; }
+    int rc = linear_shape("vgc_linear_backward", dtype, B, P, K, C);
+    if (rc != VGC_OK) return rc;
+    if ((rc = act_check("vgc_linear_backward", act)) != VGC_OK) return rc;
+    if (act != VGC_ACT_NONE && !z) { set_error("vgc_linear_backward: z is required with an activation"); return VGC_ERR_NULL; }
+    const size_t e = element_bytes(dtype);
+    if (!aligned(W, 16) || !aligned(dz, 16) || !aligned(dy, e) || !aligned(z, e) || !aligned(add, e) || !aligned(dX, e) || !aligned(g_bias, 4) || !aligned(s_bias, 4)) {
+        set_error("vgc_linear_backward: W and dz must be 16-byte aligned, the others to their elements");
+        return VGC_ERR_ALIGN;
+    }
+    if ((rc = dropout_check("vgc_linear_backward", p, rng)) != VGC_OK) return rc;
+    if (!std::isfinite(c)) { set_error("vgc_linear_backward: c is not finite"); return VGC_ERR_PARAM; }
+    if ((rc = workspace_check("vgc_linear_backward", workspace, workspace_bytes, linear_backward_workspace_bytes(dtype, B, P, K, C))) != VGC_OK) return rc;
+    LinearCall L = {};
+    L.dtype = dtype; L.act = act; L.W = W; L.residual = add; L.dy = dy; L.z_in = z; L.p = p; L.c = c; L.rng = rng;
+    L.B = B; L.P = P; L.K = K; L.C = C; L.dz = dz; L.dX = dX; L.g_bias = g_bias; L.s_bias = s_bias;
+    return launch_linear_backward(L, workspace, static_cast<hipStream_t>(stream));
+}
+
+static int group_norm_shape(const char* what, int dtype, uint32_t B, uint32_t P, uint32_t C, uint32_t G) {
+    const int rc = type_check(what, dtype);
+    if (rc != VGC_OK) return rc;
+    if (B == 0 || P == 0 || C == 0 || G == 0) { set_error("%s: zero dimension", what); return VGC_ERR_SIZE; }
+    if ((uint64_t)B * P > 0x7FFFFFFFull || C > (1u << 20)) { set_error("%s: %u x %u positions of %u channels", what, B, P, C); return VGC_ERR_SIZE; }
+    if (C % G != 0) { set_error("%s: %u channels are not %u groups of one size", what, C, G); return VGC_ERR_SIZE; }
+    return VGC_OK;
+}
+
+size_t vgc_group_norm_workspace_bytes(int dtype, uint32_t B, uint32_t P, uint32_t C, uint32_t G) {
+    return group_norm_shape("vgc_group_norm", dtype, B, P, C, G) == VGC_OK ? group_norm_workspace_bytes(dtype, B, P, C, G) : 0;
+}
+
+int vgc_group_norm(int dtype, const void* x, uint32_t B, uint32_t P, uint32_t C, uint32_t G, const float* gamma, const float* beta, float eps, int act,
+                   void* y, float* mean, float* rstd, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!x || !gamma || !beta || !y || !mean || !rstd) { set_error("vgc_group_norm: x, gamma, beta, y, mean and rstd are required"); return VGC_ERR_NULL; }
+    int rc = group_norm_shape("vgc_group_norm", dtype, B, P, C, G);
+    if (rc != VGC_OK) return rc;
+    const size_t e = element_bytes(dtype);
+    if (!aligned(x, e) || !aligned(y, e) || !aligned(gamma, 4) || !aligned(beta, 4) || !aligned(mean, 4) || !aligned(rstd, 4)) {
+        set_error("vgc_group_norm: pointers must be aligned to their elements");
+        return VGC_ERR_ALIGN;
+    }
+    if ((rc = act_check("vgc_group_norm", act)) != VGC_OK) return rc;
+    if (!std::isfinite(eps) || eps < 0.0f) { set_error("vgc_group_norm: eps must be finite and not negative (got %g)", eps); return VGC_ERR_PARAM; }
+    if ((rc = workspace_check("vgc_group_norm", workspace, workspace_bytes, group_norm_workspace_bytes(dtype, B, P, C, G))) != VGC_OK) return rc;
+    return launch_group_norm(dtype, x, B, P, C, G, gamma, beta, eps, act, y, mean, rstd, workspace, static_cast<hipStream_t>(stream));
+}
+
+size_t vgc_group_norm_backward_workspace_bytes(int dtype, uint32_t B, uint32_t P, uint32_t C, uint32_t G) {
+    return group_norm_shape("vgc_group_norm_backward", dtype, B, P, C, G) == VGC_OK ? group_norm_backward_workspace_bytes(dtype, B, P, C, G) : 0;
+}
+
+int vgc_group_norm_backward(int dtype, const void* dy, const void* x, const float* mean, const float* rstd, const float* gamma, const float* beta, int act,
+                            uint32_t B, uint32_t P, uint32_t C, uint32_t G, float c, void* dx, float* g_gamma, float* s_gamma, float* g_beta,
+                            float* s_beta, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!dy || !x || !mean || !rstd || !gamma || !beta || !dx || !s_gamma || !s_beta) {
+        set_error("vgc_group_norm_backward: dy, x, mean, rstd, gamma, beta, dx, s_gamma and s_beta are required");
+        return VGC_ERR_NULL;
+    }
+    int rc = group_norm_shape("vgc_group_norm_backward", dtype, B, P, C, G);
+    if (rc != VGC_OK) return rc;
+    const size_t e = element_bytes(dtype);
+    if (!aligned(dy, e) || !aligned(x, e) || !aligned(dx, e) || !aligned(mean, 4) || !aligned(rstd, 4) || !aligned(gamma, 4) || !aligned(beta, 4) ||
+        !aligned(g_gamma, 4) || !aligned(s_gamma, 4) || !aligned(g_beta, 4) || !aligned(s_beta, 4)) {
+        set_error("vgc_group_norm_backward: pointers must be aligned to their elements");
+        return VGC_ERR_ALIGN;
+    }
+    if ((rc = act_check("vgc_group_norm_backward", act)) != VGC_OK) return rc;
+    if (!std::isfinite(c)) { set_error("vgc_group_norm_backward: c is not finite"); return VGC_ERR_PARAM; }
+    if ((rc = workspace_check("vgc_group_norm_backward", workspace, workspace_bytes, group_norm_backward_workspace_bytes(dtype, B, P, C, G))) != VGC_OK) return rc;
+    return launch_group_norm_backward(dtype, dy, x, mean, rstd, gamma, beta, act, B, P, C, G, c, dx, g_gamma, s_gamma, g_beta, s_beta, workspace,
+                                      static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

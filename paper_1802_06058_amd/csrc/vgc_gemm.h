@@ -1,5 +1,5 @@
 // Matrix products C[m, n] = sum_k a[m, k] b[n, k] with bfloat16 operands and float32 accumulators, for operands whose k lies
-// contiguous (RowTile) and for operands whose m and n do (ColumnTile).
+// contiguous (RowTile), for operands whose m and n do (ColumnTile) and for one of each (MixedTile).
 //
 // A workgroup owns a BM x BN tile of C, a wave a WM x WN part of it in 32 x 32 tiles of v_mfma_f32_32x32x16_bf16.  Steps of BK k
 // travel from global memory straight into a ring of S stages in LDS (buffer loads with the LDS modifier: lane l of a wave-wide
@@ -21,6 +21,7 @@ namespace vgc {
 typedef __bf16 bf8v __attribute__((ext_vector_type(8)));
 typedef short s4v __attribute__((ext_vector_type(4)));
 typedef short s8v __attribute__((ext_vector_type(8)));
+typedef float f4v __attribute__((ext_vector_type(4)));
 typedef float f16v __attribute__((ext_vector_type(16)));
 typedef int i4v __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s4v* lds_s4v_ptr;
@@ -75,6 +76,7 @@ __device__ __forceinline__ TilePlace in_bands(uint32_t id, uint32_t tiles_m, uin
 // The pairs of planes of a product, smallest first.
 template <int PA, int PB> struct Pairs;
 template <> struct Pairs<1, 1> { static constexpr int n = 1, a[1] = {0}, b[1] = {0}; };
+template <> struct Pairs<1, 2> { static constexpr int n = 2, a[2] = {0, 0}, b[2] = {1, 0}; };
 template <> struct Pairs<2, 1> { static constexpr int n = 2, a[2] = {1, 0}, b[2] = {0, 0}; };
 template <> struct Pairs<3, 1> { static constexpr int n = 3, a[3] = {2, 1, 0}, b[3] = {0, 0, 0}; };
 template <> struct Pairs<2, 2> { static constexpr int n = 4, a[4] = {1, 1, 0, 0}, b[4] = {1, 0, 1, 0}; };
@@ -278,6 +280,87 @@ template <typename Shape> struct ColumnTile : Shape {
         auto fb = [&](uint32_t stage, int q, int ks, int t) { return read(sh + stage + q * Shape::kPlaneB + fB[t] + ks * 16 * BN * 2, 4 * BN * 2); };
         Shape::loop(acc, sh, steps, issue, fa, fb, after);
     }
+};
+
+// m contiguous in a, whose rows are k, and k contiguous in b, whose rows are n: a's stages lie and are read as ColumnTile's, b's as RowTile's.
+template <typename Shape> struct MixedTile : Shape {
+    using Shape::BM; using Shape::BN; using Shape::BK; using Shape::NW; using Shape::PA; using Shape::PB;
+    typedef RowTile<Shape> Rows;
+    static_assert(BM >= 128, "four units a row");
+
+    // acc += a[k, m0 ..] b[n0 .., k] over k < K (a multiple of 8, or beyond it zeros in a's rows and in b).  Columns past a row's end of a read its
+    // successor's, or zeros; rows past b's end are zeros.
+    template <typename After>
+    static __device__ __forceinline__ void run(f16v (&acc)[Shape::MT][Shape::NT], uint8_t* sh, const Matrix& A, const Matrix& B, uint32_t m0,
+                                               uint32_t n0, uint32_t K, After after) {
+        const uint32_t lane = threadIdx.x & 63u, wave = Shape::wave();
+        const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)sh) + wave * 1024u;
+        i4v ra[PA], rb[PB];
+#pragma unroll
+        for (int q = 0; q < PA; ++q) ra[q] = rows_rsrc(A, q, 0, K);
+#pragma unroll
+        for (int q = 0; q < PB; ++q) rb[q] = rows_rsrc(B, q, n0, BN);
+        constexpr uint32_t nprA = BM / 8, rpiA = 64 / nprA;
+        static_assert((NW * rpiA) % 4 == 0 && (NW * Rows::kRowsPerLoad) % 32 == 0, "the exchanges are the same in every load of a lane");
+        const uint32_t arow = wave * rpiA + lane / nprA, ap = lane % nprA, apiece = (((ap >> 2) ^ (arow & 3u)) << 2) | (ap & 3u);
+        const uint32_t offA = (arow * A.ld + m0 + apiece * 8u) * 2u, stepA = NW * rpiA * A.ld * 2u, rowsA = BK * A.ld * 2u;
+        const uint32_t brow = wave * Rows::kRowsPerLoad + lane / Rows::kPieces, kl = ((lane % Rows::kPieces) ^ Rows::mask(brow)) * 8u;
+        const uint32_t offB = (brow * B.ld + kl) * 2u, stepB = NW * Rows::kRowsPerLoad * B.ld * 2u;
+        const uint32_t steps = (K + BK - 1) / BK;
+        auto issue = [&](uint32_t stage, uint32_t step, int i) {
+            if (i < PA * Shape::kPerA) {
+                const int q = i / Shape::kPerA, j = i % Shape::kPerA;
+                piece_to_lds(lds0 + stage + q * Shape::kPlaneA + j * NW * 1024u, (offA + j * stepA + step * rowsA) | (step < steps ? 0u : 0xFFFFFFFFu), ra[q]);
+            } else {
+                const int q = (i - PA * Shape::kPerA) / Shape::kPerB, j = (i - PA * Shape::kPerA) % Shape::kPerB;
+                const uint32_t k = step * BK;
+                piece_to_lds(lds0 + stage + PA * Shape::kPlaneA + q * Shape::kPlaneB + j * NW * 1024u,
+                             (offB + j * stepB + k * 2u) | (k + kl < K ? 0u : 0xFFFFFFFFu), rb[q]);
+            }
+        };
+        const uint32_t r = lane & 15u, mhalf = (lane >> 4) & 1u, frow = (lane >> 5) * 8u + (r >> 2);
+        uint32_t fA[Shape::MT], place[Shape::KS];
+#pragma unroll
+        for (int t = 0; t < Shape::MT; ++t) fA[t] = frow * (BM * 2u) + (((Shape::wave_m() / 32u + t) ^ (frow & 3u)) * 64u) + mhalf * 32u + (r & 3u) * 8u;
+        const uint32_t rB = (Shape::wave_n() + (lane & 31u)) * Rows::kRowBytes;
+#pragma unroll
+        for (int ks = 0; ks < Shape::KS; ++ks) place[ks] = ((ks * 2u + (lane >> 5)) ^ Rows::mask(lane & 31u)) * 16u;
+        auto fa = [&](uint32_t stage, int q, int ks, int t) {
+            const uint8_t* p = sh + stage + q * Shape::kPlaneA + fA[t] + ks * 16 * BM * 2;
+            const s4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v_ptr)(p));
+            const s4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v_ptr)(p + 4 * BM * 2));
+            const s8v v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            return __builtin_bit_cast(bf8v, v);
+        };
+        auto fb = [&](uint32_t stage, int q, int ks, int t) {
+            return *reinterpret_cast<const bf8v*>(sh + stage + PA * Shape::kPlaneA + q * Shape::kPlaneB + rB + place[ks] + t * 32u * Rows::kRowBytes);
+        };
+        Shape::loop(acc, sh, steps, issue, fa, fb, after);
+    }
+};
+
+// Products far below the sum that a matrix instruction adds them to come out too small rather than rounded: with the six products of
+// planes that float32 operands bring for every 16 k, sums shrink as they grow (bfloat16 operands, whose products are of one
+// size, show none of it).  Taken out of the instructions' reach every kPart k, a sum is rounded as float sums are.  0: left there.
+template <typename Shape, uint32_t kPart> struct InParts {
+    f16v total[Shape::MT][Shape::NT] = {};
+    __device__ __forceinline__ void after(f16v (&acc)[Shape::MT][Shape::NT], uint32_t step, int ks) {
+        if (ks != Shape::KS - 1 || (step + 1u) * Shape::BK % kPart != 0u) return;
+#pragma unroll
+        for (int m = 0; m < Shape::MT; ++m)
+#pragma unroll
+            for (int n = 0; n < Shape::NT; ++n) { total[m][n] += acc[m][n]; acc[m][n] = f16v{}; }
+    }
+    __device__ __forceinline__ void end(f16v (&acc)[Shape::MT][Shape::NT]) {
+#pragma unroll
+        for (int m = 0; m < Shape::MT; ++m)
+#pragma unroll
+            for (int n = 0; n < Shape::NT; ++n) acc[m][n] += total[m][n];
+    }
+};
+template <typename Shape> struct InParts<Shape, 0u> {
+    __device__ __forceinline__ void after(f16v (&)[Shape::MT][Shape::NT], uint32_t, int) {}
+    __device__ __forceinline__ void end(f16v (&)[Shape::MT][Shape::NT]) {}
 };
 
 }  // namespace vgc

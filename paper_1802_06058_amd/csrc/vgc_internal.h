@@ -329,8 +329,43 @@ size_t layer_norm_backward_workspace_bytes(uint32_t B, uint32_t P, uint32_t C);
 int launch_layer_norm_backward(int dtype, const void* dy, const void* x, const float* mean, const int8_t* codes, const uint8_t* exps,
                                const float* rstd, const float* gamma, uint32_t B, uint32_t P, uint32_t C, float c, void* dx, float* g_gamma,
                                float* s_gamma, float* g_beta, float* s_beta, void* workspace, hipStream_t stream);
+// g and s over the samples of `vecs` (1 or 2) vectors from the column sums that workgroups left: partial[sample][part][vector][C], or of whole
+// samples partial[group][vector][g, s][C]
+int launch_column_sums(const float* partial, uint32_t vecs, uint32_t groups, uint32_t B, uint32_t parts, uint32_t C, bool whole, float c, float* g0, float* s0,
+                       float* g1, float* s1, hipStream_t stream);
+
+// Dropout (vgc_dropout.hip)
+struct Dropout;
+int launch_dropout(int dtype, const void* x, const void* residual, uint32_t R, uint32_t C, const Dropout& D, void* y, hipStream_t stream);
+
+// Group norm (vgc_group_norm.hip)
+size_t group_norm_workspace_bytes(int dtype, uint32_t B, uint32_t P, uint32_t C, uint32_t G);
+int launch_group_norm(int dtype, const void* x, uint32_t B, uint32_t P, uint32_t C, uint32_t G, const float* gamma, const float* beta, float eps, int act,
+                      void* y, float* mean, float* rstd, void* workspace, hipStream_t stream);
+size_t group_norm_backward_workspace_bytes(int dtype, uint32_t B, uint32_t P, uint32_t C, uint32_t G);
+int launch_group_norm_backward(int dtype, const void* dy, const void* x, const float* mean, const float* rstd, const float* gamma, const float* beta,
+                               int act, uint32_t B, uint32_t P, uint32_t C, uint32_t G, float c, void* dx, float* g_gamma, float* s_gamma, float* g_beta,
+                               float* s_beta, void* workspace, hipStream_t stream);
+
+// Linear layer (vgc_linear.hip)
+struct LinearCall {           // the arguments of vgc_linear and vgc_linear_backward, as there
+    int dtype, act;
+    const void *X, *W, *residual, *dy, *z_in;
+    const float* bias;
+    float p, c;
+    const uint64_t* rng;
+    uint32_t B, P, K, C;      // N = B P rows
+    void *z, *y, *dz, *dX;
+    float *g_bias, *s_bias;
+};
+size_t linear_workspace_bytes(int dtype, uint32_t N, uint32_t K, uint32_t C);
+int launch_linear(const LinearCall& L, void* workspace, hipStream_t stream);
+size_t linear_backward_workspace_bytes(int dtype, uint32_t B, uint32_t P, uint32_t K, uint32_t C);
+int launch_linear_backward(const LinearCall& L, void* workspace, hipStream_t stream);
 
 // Softmax cross entropy of a linear layer (vgc_softmax_loss.hip)
+// R rows of K elements as bfloat16 planes (one of bfloat16 rows, three of float32), rows padded with zeros to a multiple of 8, planes R rows apart
+int launch_plane_rows(int dtype, const void* src, uint32_t R, uint32_t K, uint16_t* dst, hipStream_t stream);
 size_t softmax_loss_workspace_bytes(int dtype, uint32_t N, uint32_t H, uint32_t V);
 int launch_softmax_loss(int dtype, const void* X, const void* W, const int64_t* target, uint32_t N, uint32_t H, uint32_t V, float* loss, float* lse,
                         void* workspace, hipStream_t stream);

@@ -409,10 +409,11 @@ __global__ __launch_bounds__(1024) void k_layer_norm_backward_long(NormArgs A) {
 
 // Adds the teams' partial sums in a fixed order: a workgroup takes 64 columns of one of the two vectors (blockIdx.y: gamma, beta),
 // four a lane, and its 64 groups of 16 lanes share the partial sums between them.
+//   vecs: vectors a group of partial sums holds, one after another.
 //   whole samples: planes g, s, summed over the workgroups that left them.
 //   parts: the parts of a sample are added before the square.  Groups take samples of their own if there are 64 or more; below,
 //   several groups share a sample's parts.
-__global__ __launch_bounds__(1024) void k_layer_norm_sums(const float* __restrict__ partial, uint32_t groups, uint32_t B, uint32_t parts, uint32_t C,
+__global__ __launch_bounds__(1024) void k_layer_norm_sums(const float* __restrict__ partial, uint32_t vecs, uint32_t groups, uint32_t B, uint32_t parts, uint32_t C,
                                                           int whole, float c, float* __restrict__ g_gamma, float* __restrict__ s_gamma,
                                                           float* __restrict__ g_beta, float* __restrict__ s_beta) {
     constexpr uint32_t kGroups = 64;
@@ -430,12 +431,12 @@ __global__ __launch_bounds__(1024) void k_layer_norm_sums(const float* __restric
     uint32_t share = 1;                                      // groups a sample's parts are spread over
     if (whole) {
         const float* at = partial + (size_t)(2u * vec) * C + col;
-        const size_t step = 4 * (size_t)C;
+        const size_t step = 2 * (size_t)vecs * C;
 #pragma unroll 4
         for (uint32_t t = group; t < groups; t += kGroups) { g += load(at + t * step); s += load(at + t * step + C); }
     } else {
         const float* at = partial + (size_t)vec * C + col;
-        const size_t step = 2 * (size_t)C;
+        const size_t step = (size_t)vecs * C;
         while (B * share * 2u <= kGroups) share *= 2u;
         const uint32_t sub = group % share;
         for (uint32_t z = group / share; z < B; z += kGroups / share) {
@@ -589,8 +590,12 @@ int launch_layer_norm_backward(int dtype, const void* dy, const void* x, const f
 #undef VGC_LAUNCH
     int rc = hip_check(hipGetLastError(), "launch k_layer_norm_backward");
     if (rc != VGC_OK) return rc;
-    hipLaunchKernelGGL(k_layer_norm_sums, dim3((C + 63) / 64, 2), dim3(1024), 0, stream, (const float*)workspace, L.groups, B, L.parts, C, (int)L.whole,
-                       c, g_gamma, s_gamma, g_beta, s_beta);
+    return launch_column_sums((const float*)workspace, 2, L.groups, B, L.parts, C, L.whole, c, g_gamma, s_gamma, g_beta, s_beta, stream);
+}
+
+int launch_column_sums(const float* partial, uint32_t vecs, uint32_t groups, uint32_t B, uint32_t parts, uint32_t C, bool whole, float c, float* g0, float* s0,
+                       float* g1, float* s1, hipStream_t stream) {
+    hipLaunchKernelGGL(k_layer_norm_sums, dim3((C + 63) / 64, vecs), dim3(1024), 0, stream, partial, vecs, groups, B, parts, C, (int)whole, c, g0, s0, g1, s1);
     return hip_check(hipGetLastError(), "launch k_layer_norm_sums");
 }
 

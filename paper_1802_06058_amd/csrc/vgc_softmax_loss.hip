@@ -22,45 +22,11 @@
 #include <algorithm>
 
 #include "vgc_gemm.h"
-#include "vgc_rows.h"
+#include "vgc_planes.h"
 
 namespace vgc {
 
-typedef float f4v __attribute__((ext_vector_type(4)));
-
 // ---- operands -------------------------------------------------------------------------------------------------------------
-// The next plane of two floats, the first in the low half, taken out of them: rounded to the nearest bfloat16, so that what is left is
-// exact and of either sign.  Three planes of a float32 are all of it (8 bits each, but for bits below the smallest subnormal); planes that were
-// cut off instead would leave products too small, all of them, by what the pairs of planes that are not formed hold (logits of 16
-// 7e-7 too small).  bfloat16 inputs: two planes are within 2^-18 of an entry of D, three are all of it.
-// Of a float32, what would be rounded up to infinity is cut off, and an infinity or a NaN leaves nothing.
-template <bool kF32> __device__ __forceinline__ uint32_t next_plane(float& d0, float& d1) {
-    uint32_t x = two_bf16(d0, d1);
-    if (kF32) {
-        const bool finite0 = __builtin_isfinite(d0), finite1 = __builtin_isfinite(d1);
-        if (finite0 && (x & 0x7FFFu) == 0x7F80u) x -= 1u;
-        if (finite1 && (x & 0x7FFF0000u) == 0x7F800000u) x -= 0x10000u;
-        d0 = finite0 ? d0 - __uint_as_float(x << 16) : 0.f;
-        d1 = finite1 ? d1 - __uint_as_float(x & 0xFFFF0000u) : 0.f;
-        return x;
-    }
-    d0 -= __uint_as_float(x << 16);
-    d1 -= __uint_as_float(x & 0xFFFF0000u);
-    return x;
-}
-
-// Eight values (used up) as the planes of an operand, 16 bytes each.
-template <typename T> __device__ __forceinline__ void store_planes(uint16_t* out, uint64_t plane, float (&f)[8]) {
-    if (sizeof(T) == 2) { store8(out, f, 8); return; }
-#pragma unroll
-    for (int q = 0; q < 3; ++q) {
-        any_u4 v;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = next_plane<true>(f[2 * e], f[2 * e + 1]);
-        *reinterpret_cast<any_u4*>(out + q * plane) = v;
-    }
-}
-
 // Rows as they are, padded with zeros to whole pieces of 8.
 template <typename T>
 __global__ __launch_bounds__(256) void k_planes_rows(const T* __restrict__ src, uint32_t R, uint32_t K, uint32_t Kp, uint16_t* __restrict__ dst) {
@@ -311,30 +277,6 @@ __device__ __forceinline__ void store_by_classes(f16v (&acc)[MT][NT], uint8_t* t
         __builtin_amdgcn_wave_barrier();
     }
 }
-
-// Products far below the sum that a matrix instruction adds them to come out too small rather than rounded: with the six products of
-// planes that float32 operands bring for every 16 k, sums shrink as they grow (bfloat16 operands, whose products are of one
-// size, show none of it).  Taken out of the instructions' reach every kPart k, a sum is rounded as float sums are.  0: left there.
-template <typename Shape, uint32_t kPart> struct InParts {
-    f16v total[Shape::MT][Shape::NT] = {};
-    __device__ __forceinline__ void after(f16v (&acc)[Shape::MT][Shape::NT], uint32_t step, int ks) {
-        if (ks != Shape::KS - 1 || (step + 1u) * Shape::BK % kPart != 0u) return;
-#pragma unroll
-        for (int m = 0; m < Shape::MT; ++m)
-#pragma unroll
-            for (int n = 0; n < Shape::NT; ++n) { total[m][n] += acc[m][n]; acc[m][n] = f16v{}; }
-    }
-    __device__ __forceinline__ void end(f16v (&acc)[Shape::MT][Shape::NT]) {
-#pragma unroll
-        for (int m = 0; m < Shape::MT; ++m)
-#pragma unroll
-            for (int n = 0; n < Shape::NT; ++n) acc[m][n] += total[m][n];
-    }
-};
-template <typename Shape> struct InParts<Shape, 0u> {
-    __device__ __forceinline__ void after(f16v (&)[Shape::MT][Shape::NT], uint32_t, int) {}
-    __device__ __forceinline__ void end(f16v (&)[Shape::MT][Shape::NT]) {}
-};
 
 // 65536 classes x 2048 k, 4096 bfloat16 rows: forward 0.88-1.0 ms, 1.1-1.25 PFLOP/s, by the clock that the card keeps under the load
 // (1.73-1.78 GHz; with zeros for inputs 0.73), LDS free of conflicts; as D, 65521 classes, 1.13-1.27 ms, with two planes, 1.07 GB, to be stored
@@ -833,7 +775,7 @@ static int launch_logits(LogitsTile t, int dtype, const ThinArgs& R, const LossA
     return hip_check(hipGetLastError(), "launch k_logits");
 }
 
-static int launch_rows(int dtype, const void* src, uint32_t R, uint32_t K, uint16_t* dst, hipStream_t stream) {
+int launch_plane_rows(int dtype, const void* src, uint32_t R, uint32_t K, uint16_t* dst, hipStream_t stream) {
     const uint32_t Kp = up8(K);
     const dim3 grid((uint32_t)(((uint64_t)R * (Kp / 8u) + 255u) / 256u));
     if (dtype == VGC_BF16) hipLaunchKernelGGL(k_planes_rows<uint16_t>, grid, dim3(256), 0, stream, (const uint16_t*)src, R, K, Kp, dst);
@@ -898,13 +840,13 @@ int launch_softmax_loss(int dtype, const void* X, const void* W, const int64_t* 
     A.partial = reinterpret_cast<float2*>(ws + L.partial);
     A.picked = reinterpret_cast<float*>(ws + L.picked);
     uint16_t *xs = reinterpret_cast<uint16_t*>(ws + L.x), *wp = reinterpret_cast<uint16_t*>(ws + L.w);
-    if (!L.rows.in_place && (rc = launch_rows(dtype, X, N, H, xs, stream)) != VGC_OK) return rc;
+    if (!L.rows.in_place && (rc = launch_plane_rows(dtype, X, N, H, xs, stream)) != VGC_OK) return rc;
     A.x = matrix_of(L.rows, X, xs, N, H);
     for (uint32_t v0 = 0; v0 < V; v0 += L.piece) {
         A.v0 = v0;
         A.V = std::min(L.piece, V - v0);
         const char* rows = static_cast<const char*>(W) + (size_t)v0 * H * size;
-        if (!L.rows.in_place && (rc = launch_rows(dtype, rows, A.V, H, wp, stream)) != VGC_OK) return rc;
+        if (!L.rows.in_place && (rc = launch_plane_rows(dtype, rows, A.V, H, wp, stream)) != VGC_OK) return rc;
         A.w = matrix_of(L.rows, rows, wp, A.V, H);
         A.block0 = v0 / logits_block(L.tile);
         if ((rc = launch_logits<true>(L.tile, dtype, ThinArgs{A.w.base, A.x.base, A.w.ld, A.x.ld}, A, stream)) != VGC_OK) return rc;
@@ -997,7 +939,7 @@ int launch_softmax_loss_backward(int dtype, const void* X, const void* W, const 
     A.planes = dtype == VGC_F32 || by_position ? L.planes : 1u;
     if (P == 1 && (s_out || L.dx_thin)) A.d32 = (float*)(ws + L.d32);
     if (dtype == VGC_BF16 && dX && !L.dx_thin) A.rest = (float*)(ws + L.rest);
-    if (!L.rows.in_place && (rc = launch_rows(dtype, X, N, H, xs, stream)) != VGC_OK) return rc;
+    if (!L.rows.in_place && (rc = launch_plane_rows(dtype, X, N, H, xs, stream)) != VGC_OK) return rc;
     A.x = matrix_of(L.rows, X, xs, N, H);
     if (by_position) {
         const dim3 grid((L.Lq + 63u) / 64u, (H + 63u) / 64u);
@@ -1017,7 +959,7 @@ int launch_softmax_loss_backward(int dtype, const void* X, const void* W, const 
         A.V = std::min(L.piece, V - v0);
         A.plane = (uint64_t)A.V * L.Lq;
         const char* rows = static_cast<const char*>(W) + (size_t)v0 * H * size;
-        if (!L.rows.in_place && (rc = launch_rows(dtype, rows, A.V, H, wp, stream)) != VGC_OK) return rc;
+        if (!L.rows.in_place && (rc = launch_plane_rows(dtype, rows, A.V, H, wp, stream)) != VGC_OK) return rc;
         A.w = matrix_of(L.rows, rows, wp, A.V, H);
         ThinArgs R = {A.w.base, A.x.base, A.w.ld, A.x.ld};
         if (dtype == VGC_F32) R = ThinArgs{rows, X, H, H};   // (as floats, also where the planes are there for dX)

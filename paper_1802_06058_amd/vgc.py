@@ -53,6 +53,7 @@ class Conv2dLayer(C.Structure):
 
 
 MOMENTUM_SGD, ADAM = 0, 1
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2, 3
 
 HDR_DTYPE = np.dtype([("exp_field", "<u4"), ("count", "<u4"), ("word_offset", "<u8")])
 
@@ -117,6 +118,19 @@ EXPORTS = {
     "vgc_softmax_loss_backward_workspace_bytes": (C.c_size_t, [C.c_int] + [C.c_uint32] * 4),
     "vgc_softmax_loss_backward": (C.c_int, [C.c_int] + [C.c_void_p] * 5 + [C.c_uint32] * 4 + [C.c_float] + [C.c_void_p] * 4 +
                                   [C.c_size_t, C.c_void_p]),
+    "vgc_dropout": (C.c_int, [C.c_int, C.c_void_p, C.c_void_p, C.c_uint64, C.c_uint32, C.c_float] + [C.c_void_p] * 3),
+    "vgc_linear_workspace_bytes": (C.c_size_t, [C.c_int] + [C.c_uint32] * 3),
+    "vgc_linear": (C.c_int, [C.c_int] + [C.c_void_p] * 3 + [C.c_int, C.c_float] + [C.c_void_p] * 2 + [C.c_uint32] * 3 + [C.c_void_p] * 3 +
+                   [C.c_size_t, C.c_void_p]),
+    "vgc_linear_backward_workspace_bytes": (C.c_size_t, [C.c_int] + [C.c_uint32] * 4),
+    "vgc_linear_backward": (C.c_int, [C.c_int] + [C.c_void_p] * 3 + [C.c_int, C.c_float] + [C.c_void_p] * 2 + [C.c_uint32] * 4 + [C.c_float] +
+                            [C.c_void_p] * 5 + [C.c_size_t, C.c_void_p]),
+    "vgc_group_norm_workspace_bytes": (C.c_size_t, [C.c_int] + [C.c_uint32] * 4),
+    "vgc_group_norm": (C.c_int, [C.c_int, C.c_void_p] + [C.c_uint32] * 4 + [C.c_void_p] * 2 + [C.c_float, C.c_int] + [C.c_void_p] * 4 +
+                       [C.c_size_t, C.c_void_p]),
+    "vgc_group_norm_backward_workspace_bytes": (C.c_size_t, [C.c_int] + [C.c_uint32] * 4),
+    "vgc_group_norm_backward": (C.c_int, [C.c_int] + [C.c_void_p] * 6 + [C.c_int] + [C.c_uint32] * 4 + [C.c_float] + [C.c_void_p] * 6 +
+                                [C.c_size_t, C.c_void_p]),
 }
 
 _lib = None
@@ -711,3 +725,107 @@ def softmax_loss_backward(X, W, target, lse, weight, c, dX, s_out, g_out=None, w
                (dX, R * H, X.dtype, "dX"), (s_out, V * H, f32, "s_out"), (g_out, V * H, f32, "g_out"), (workspace, nbytes, torch.uint8, "workspace")))
     _check(load().vgc_softmax_loss_backward(dtype, _ptr(X), _ptr(W), _ptr(target), _ptr(lse), _ptr(weight), B, P, H, V, float(c), _ptr(dX),
                                             _ptr(g_out), _ptr(s_out), _ptr(workspace), has, _stream()))
+
+
+def dropout(x, p, rng, y, residual=None):
+    """vgc_dropout on the rows of x [..., C] into y (which may be x or residual): every element is dropped with probability p, the others are
+    multiplied by 1 / (1 - p), and residual, if given, is added.  rng: int64 tensor of two elements, a key and the number of the call, read when the
+    kernel runs.  The backward pass is the same call on the gradient of y."""
+    R, Cc, dtype = _rows(x, "x")
+    _need_all(((x, 0, x.dtype, "x"), (residual, R * Cc, x.dtype, "residual"), (rng, 2, torch.int64, "rng"), (y, R * Cc, x.dtype, "y")))
+    _check(load().vgc_dropout(dtype, _ptr(x), _ptr(residual), R, Cc, float(p), _ptr(rng), _ptr(y), _stream()))
+
+
+def linear_workspace_bytes(dtype, N, K, Cc):
+    return int(load().vgc_linear_workspace_bytes(dtype, N, K, Cc))
+
+
+def _linear_shape(rows, W, what):
+    """(rows, columns, dtype code) of a contiguous tensor of rows beside W, which may be None."""
+    R, n, dtype = _rows(rows, what)
+    if W is not None and (W.dim() != 2 or W.dtype != rows.dtype or not W.is_contiguous()):
+        raise VgcError(f"W {tuple(W.shape)} {W.dtype} is not a contiguous [K, C] in the type of {what}, {rows.dtype}")
+    return R, n, dtype
+
+
+def linear(X, W, y, bias=None, act=ACT_NONE, z=None, residual=None, p=0.0, rng=None, workspace=None):
+    """vgc_linear: y = residual + drop(act(X W + bias)) for the rows of X [..., K] and W [K, C].  y, z and residual [..., C] like X; bias float32
+    [C]; p and rng as for dropout().  z, if given, receives X W + bias for the backward pass; y may be residual.
+    workspace: uint8 tensor of linear_workspace_bytes() bytes."""
+    R, K, dtype = _linear_shape(X, W, "X")
+    if W.shape[0] != K:
+        raise VgcError(f"W {tuple(W.shape)} does not take rows of {K} elements")
+    Cc = W.shape[1]
+    nbytes = linear_workspace_bytes(dtype, R, K, Cc)
+    has = _need_workspace(workspace, nbytes)
+    _need_all(((X, 0, X.dtype, "X"), (W, 0, X.dtype, "W"), (bias, Cc, torch.float32, "bias"), (residual, R * Cc, X.dtype, "residual"),
+               (z, R * Cc, X.dtype, "z"), (y, R * Cc, X.dtype, "y"), (rng, 2, torch.int64, "rng"), (workspace, nbytes, torch.uint8, "workspace")))
+    _check(load().vgc_linear(dtype, _ptr(X), _ptr(W), _ptr(bias), act, float(p), _ptr(rng), _ptr(residual), R, K, Cc, _ptr(z), _ptr(y),
+                             _ptr(workspace), has, _stream()))
+
+
+def linear_backward_workspace_bytes(dtype, B, P, K, Cc):
+    return int(load().vgc_linear_backward_workspace_bytes(dtype, B, P, K, Cc))
+
+
+def linear_backward(dy, z, W, act, c, dz, dX=None, s_bias=None, g_bias=None, add=None, p=0.0, rng=None, workspace=None):
+    """vgc_linear_backward for dy [B, P, C] and W [K, C]: dz like dy (the D of sqgrad for W, with X), dX [B, P, K] = add + dz W^T, and the two sums
+    over the samples for the bias, float32 [C].  z: what linear() wrote (None without an activation); p and rng as it had them.
+    workspace: uint8 tensor of linear_backward_workspace_bytes() bytes."""
+    if dy.dim() != 3:
+        raise VgcError(f"dy: need [B, P, C], got {tuple(dy.shape)}")
+    R, Cc, dtype = _linear_shape(dy, W, "dy")
+    if W is None or W.shape[1] != Cc:
+        raise VgcError(f"W {None if W is None else tuple(W.shape)} does not give rows of {Cc} elements")
+    B, P, K = dy.shape[0], dy.shape[1], W.shape[0]
+    f32 = torch.float32
+    nbytes = linear_backward_workspace_bytes(dtype, B, P, K, Cc)
+    has = _need_workspace(workspace, nbytes)
+    _need_all(((dy, 0, dy.dtype, "dy"), (z, R * Cc, dy.dtype, "z"), (W, 0, dy.dtype, "W"), (add, R * K, dy.dtype, "add"), (dz, R * Cc, dy.dtype, "dz"),
+               (dX, R * K, dy.dtype, "dX"), (s_bias, Cc, f32, "s_bias"), (g_bias, Cc, f32, "g_bias"), (rng, 2, torch.int64, "rng"),
+               (workspace, nbytes, torch.uint8, "workspace")))
+    _check(load().vgc_linear_backward(dtype, _ptr(dy), _ptr(z), _ptr(W), act, float(p), _ptr(rng), _ptr(add), B, P, K, Cc, float(c), _ptr(dz), _ptr(dX),
+                                      _ptr(g_bias), _ptr(s_bias), _ptr(workspace), has, _stream()))
+
+
+def _group_norm_shape(x, what, mean):
+    """(B, P, C, G, dtype code): x [B, ..., C] channels last, mean [B, G]."""
+    R, Cc, dtype = _rows(x, what)
+    if x.dim() < 3 or mean.dim() != 2 or mean.shape[0] != x.shape[0]:
+        raise VgcError(f"{what} {tuple(x.shape)} and mean {tuple(mean.shape)}: need [B, positions.., C] and [B, groups]")
+    return x.shape[0], R // x.shape[0] if x.shape[0] else 0, Cc, mean.shape[1], dtype
+
+
+def group_norm_workspace_bytes(dtype, B, P, Cc, G):
+    return int(load().vgc_group_norm_workspace_bytes(dtype, B, P, Cc, G))
+
+
+def group_norm(x, gamma, beta, eps, act, y, mean, rstd, workspace=None):
+    """vgc_group_norm of x [B, positions.., C], channels last: y = act(gamma xhat + beta) like x; gamma, beta float32 [C]; mean and rstd float32 [B, G],
+    whose shape says how many groups there are.  workspace: uint8 tensor of group_norm_workspace_bytes() bytes."""
+    B, P, Cc, G, dtype = _group_norm_shape(x, "x", mean)
+    f32, n = torch.float32, x.numel()
+    nbytes = group_norm_workspace_bytes(dtype, B, P, Cc, G)
+    has = _need_workspace(workspace, nbytes)
+    _need_all(((x, 0, x.dtype, "x"), (gamma, Cc, f32, "gamma"), (beta, Cc, f32, "beta"), (y, n, x.dtype, "y"), (mean, B * G, f32, "mean"),
+               (rstd, B * G, f32, "rstd"), (workspace, nbytes, torch.uint8, "workspace")))
+    _check(load().vgc_group_norm(dtype, _ptr(x), B, P, Cc, G, _ptr(gamma), _ptr(beta), float(eps), act, _ptr(y), _ptr(mean), _ptr(rstd),
+                                 _ptr(workspace), has, _stream()))
+
+
+def group_norm_backward_workspace_bytes(dtype, B, P, Cc, G):
+    return int(load().vgc_group_norm_backward_workspace_bytes(dtype, B, P, Cc, G))
+
+
+def group_norm_backward(dy, x, mean, rstd, gamma, beta, act, c, dx, s_gamma, s_beta, g_gamma=None, g_beta=None, workspace=None):
+    """vgc_group_norm_backward for dy [B, positions.., C]: dx, and the two sums over the samples for gamma and beta.  x, mean, rstd, gamma, beta and
+    act as group_norm() had and gave them.  workspace: uint8 tensor of group_norm_backward_workspace_bytes() bytes."""
+    B, P, Cc, G, dtype = _group_norm_shape(dy, "dy", mean)
+    f32, n = torch.float32, dy.numel()
+    nbytes = group_norm_backward_workspace_bytes(dtype, B, P, Cc, G)
+    has = _need_workspace(workspace, nbytes)
+    _need_all(((dy, 0, dy.dtype, "dy"), (x, n, dy.dtype, "x"), (mean, B * G, f32, "mean"), (rstd, B * G, f32, "rstd"), (gamma, Cc, f32, "gamma"),
+               (beta, Cc, f32, "beta"), (dx, n, dy.dtype, "dx"), (s_gamma, Cc, f32, "s_gamma"), (s_beta, Cc, f32, "s_beta"),
+               (g_gamma, Cc, f32, "g_gamma"), (g_beta, Cc, f32, "g_beta"), (workspace, nbytes, torch.uint8, "workspace")))
+    _check(load().vgc_group_norm_backward(dtype, _ptr(dy), _ptr(x), _ptr(mean), _ptr(rstd), _ptr(gamma), _ptr(beta), act, B, P, Cc, G, float(c),
+                                          _ptr(dx), _ptr(g_gamma), _ptr(s_gamma), _ptr(g_beta), _ptr(s_beta), _ptr(workspace), has, _stream()))

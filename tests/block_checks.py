@@ -1,0 +1,61 @@
+"""What the tests of the linear layer, dropout and group norm share.
+
+Roundings: U = 2^-24 is half a unit of float32, half of one of bfloat16 is 2^-8 relative to the value."""
+import numpy as np
+
+U = 2.0 ** -24
+ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+
+
+def device():
+    import torch
+    from paper_1802_06058_amd import vgc
+    assert torch.cuda.is_available()
+    vgc.load()
+    return torch.device("cuda:0")
+
+
+def dtype_of(name):
+    import torch
+    return torch.bfloat16 if name == "bf16" else torch.float32
+
+
+def half_unit(name):
+    return 2.0 ** -8 if name == "bf16" else U
+
+
+def to(a, name, dev):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(a, np.float32)).to(dtype_of(name)).to(dev)
+
+
+def back(t):
+    return t.double().cpu().numpy()
+
+
+def act_error(z, value):
+    """Of an activation's value (or slope, given as its size) at z in float32: Phi's polynomial is within 6 U, the exponential of z^2 / 2 or of z within
+    z^2 + 2 |z| units for its argument's roundings, and some ten roundings follow; values too small for a float are lost."""
+    return np.abs(value) * (24 + 2 * z * z + 4 * np.abs(z)) * U + 1e-37
+
+
+def rng_state(dev, key=0x123456789ABCDEF, call=(7 << 32) + 5):
+    import torch
+    return torch.tensor([key, call], dtype=torch.int64, device=dev)
+
+
+def guarded(n, dtype, dev, fill=7.0):
+    """A tensor of n elements with 32 more behind it that nobody may touch."""
+    import torch
+    whole = torch.full((n + 32,), fill, dtype=dtype, device=dev)
+    return whole[:n], whole[n:]
+
+
+def untouched(*guards):
+    return all(bool((g == 7).all()) for g in guards)
+
+
+def workspace(nbytes, dev):
+    """Working memory whose contents are NaN in any type."""
+    import torch
+    return torch.full((nbytes,), 255, dtype=torch.uint8, device=dev) if nbytes else None
