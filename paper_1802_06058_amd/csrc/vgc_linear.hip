@@ -28,7 +28,20 @@ struct Finish {
     uint32_t N, M;
     int act;
     Dropout drop;
+    bool past;                // results are stored past the caches
 };
+typedef uint32_t whole_u4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ void store8_past(uint16_t* p, const float (&f)[8]) {
+    whole_u4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = two_bf16(f[2 * i], f[2 * i + 1]);
+    __builtin_nontemporal_store(v, reinterpret_cast<whole_u4*>(p));
+}
+__device__ __forceinline__ void store8_past(float* p, const float (&f)[8]) {
+    const f4v a = {f[0], f[1], f[2], f[3]}, b = {f[4], f[5], f[6], f[7]};
+    __builtin_nontemporal_store(a, reinterpret_cast<f4v*>(p));
+    __builtin_nontemporal_store(b, reinterpret_cast<f4v*>(p + 4));
+}
 template <typename T>
 __device__ __forceinline__ void finish(const Finish& F, const DropoutKey& key, uint32_t row, uint32_t col, int n, const float (&bias)[8], float (&f)[8]) {
     const size_t at = (size_t)row * F.M + col;
@@ -36,7 +49,7 @@ __device__ __forceinline__ void finish(const Finish& F, const DropoutKey& key, u
     if (F.residual) r = load8(static_cast<const T*>(F.residual) + at, n);
 #pragma unroll
     for (int k = 0; k < 8; ++k) f[k] += bias[k];
-    if (F.z) store8(static_cast<T*>(F.z) + at, f, n);
+    if (F.z) { if (F.past) store8_past(static_cast<T*>(F.z) + at, f); else store8(static_cast<T*>(F.z) + at, f, n); }
     apply_act(F.act, f);
     apply_dropout(F.drop, key, row, col / 8u, f);
     if (F.residual) {
@@ -45,7 +58,8 @@ __device__ __forceinline__ void finish(const Finish& F, const DropoutKey& key, u
 #pragma unroll
         for (int k = 0; k < 8; ++k) f[k] += g[k];
     }
-    store8(static_cast<T*>(F.y) + at, f, n);
+    if (F.past) store8_past(static_cast<T*>(F.y) + at, f);
+    else store8(static_cast<T*>(F.y) + at, f, n);
 }
 __device__ __forceinline__ void bias_of(const Finish& F, uint32_t col, float (&bias)[8]) {
     const int n = (int)F.M - (int)col;
@@ -125,23 +139,213 @@ __global__ __launch_bounds__(Shape::NW * 64, Shape::kLds > 80 * 1024 && Shape::N
 
 // Adds the parts of k in their order, eight elements of a row a lane.
 template <typename T>
-__global__ __launch_bounds__(256) void k_linear_join(LinearArgs A) {
-    const uint32_t per_row = (A.F.M + 7u) / 8u;
+__global__ __launch_bounds__(256) void k_linear_join(Finish F, uint32_t splits, const float* __restrict__ parts) {
+    const uint32_t per_row = (F.M + 7u) / 8u;
     const uint64_t i = (uint64_t)blockIdx.x * 256u + threadIdx.x;
-    if (i >= (uint64_t)A.F.N * per_row) return;
+    if (i >= (uint64_t)F.N * per_row) return;
     const uint32_t row = (uint32_t)(i / per_row), col = (uint32_t)(i - (uint64_t)row * per_row) * 8u;
-    const int n = (int)min(A.F.M - col, 8u);
-    const float* from = A.parts + (size_t)row * A.F.M + col;
-    const size_t plane = (size_t)A.F.N * A.F.M;
+    const int n = (int)min(F.M - col, 8u);
+    const float* from = parts + (size_t)row * F.M + col;
+    const size_t plane = (size_t)F.N * F.M;
     float f[8] = {}, g[8], bias[8];
-    bias_of(A.F, col, bias);
+    bias_of(F, col, bias);
 #pragma unroll 4
-    for (uint32_t s = 0; s < A.splits; ++s) {
+    for (uint32_t s = 0; s < splits; ++s) {
         widen8(load8(from + s * plane, n), g);
 #pragma unroll
         for (int k = 0; k < 8; ++k) f[k] += g[k];
     }
-    finish<T>(A.F, dropout_key(A.F.drop), row, col, n, bias, f);
+    finish<T>(F, dropout_key(F.drop), row, col, n, bias, f);
+}
+
+// ---- few rows ---------------------------------------------------------------------------------------------------------------
+// A workgroup of 16 waves owns 16 kV columns by 16 NT rows of the output and its waves share k, both operands straight from memory into registers.
+// The instruction wants k by lane group and a row (of a) or column (of b) by lane; which k and which column a place stands for is free:
+//   forward   a lane asks for kV consecutive columns of W in each of its k's rows, so that a wave's load takes whole 16 kV columns of four rows; column j
+//             of the lanes is an instruction's operand (bfloat16: eight k's pairs put together by byte permutes)
+//   backward  a lane asks for 16 bytes of a row of W, instruction j taking rows 16 j + lane % 16
+// Rows are read at any alignment, so nothing is laid out before.  Requests have no branches, which would make a wave wait for what it asked for before: past an edge
+// a place is moved back to the last one inside, of k with the elements that others count dropped from b's, of columns and rows with results that others have too.  The waves' sums meet in LDS, four lanes add an output piece's sixteen and one finishes it.
+// float32 is multiplied as floats.
+constexpr uint32_t kThinWaves = 16;
+template <typename T> struct ThinArgs {
+    const T *a, *b, *rest;    // W; the rows of X or dz, and (backward, bfloat16) what rounding left of dz
+    uint32_t K, splits;
+    float* parts;             // [split][N][M] where k is shared out over workgroups too
+    Finish F;
+};
+template <int kBytes> struct AnyBytes;
+template <> struct AnyBytes<4> { typedef uint32_t type __attribute__((aligned(2))); };
+template <> struct AnyBytes<8> { typedef any_u2 type; };
+template <> struct AnyBytes<16> { typedef any_u4 type; };
+
+// kV columns of a row.
+template <typename T, int kV> struct Columns {
+    static constexpr int kWords = kV * (int)sizeof(T) / 4;
+    uint32_t w[kWords];
+    __device__ __forceinline__ void load(const T* p) {
+        const typename AnyBytes<kWords * 4>::type v = *reinterpret_cast<const typename AnyBytes<kWords * 4>::type*>(p);
+        if constexpr (kWords == 1) w[0] = v;
+        else
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) w[i] = v[i];
+    }
+};
+template <typename T> struct ThinRow;                        // a lane's k of a row, 16 bytes; drop: the first so many do not count
+template <> struct ThinRow<uint16_t> {
+    static constexpr uint32_t kK = 8;
+    any_u4 r;
+    __device__ __forceinline__ void load(const uint16_t* p) { r = *reinterpret_cast<const any_u4*>(p); }
+    __device__ __forceinline__ void drop(int n) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] &= n <= 2 * i ? 0xFFFFFFFFu : n == 2 * i + 1 ? 0xFFFF0000u : 0u;
+    }
+    __device__ __forceinline__ bf8v operand() const { return __builtin_bit_cast(bf8v, r); }
+};
+template <> struct ThinRow<float> {
+    static constexpr uint32_t kK = 4;
+    any_f4 r;
+    __device__ __forceinline__ void load(const float* p) { r = *reinterpret_cast<const any_f4*>(p); }
+    __device__ __forceinline__ void drop(int n) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = i >= n ? r[i] : 0.f;
+    }
+};
+
+template <typename T, bool kMixed, int kV, int NT, bool kRest>
+__global__ __launch_bounds__(kThinWaves * 64) void k_linear_thin(ThinArgs<T> A) {
+    typedef ThinRow<T> Row;
+    constexpr uint32_t kK = Row::kK, kStep = 4 * kK, kM = 16 * kV, kN = 16 * NT, kPitch = kM + 4;
+    constexpr int kRegs = kMixed ? (int)kK * Columns<T, kV < 2 && sizeof(T) == 2 ? 2 : kV>::kWords : kV * 4;   // of a step's a
+    constexpr int kAhead = kRegs + 4 * NT * (kRest ? 2 : 1) <= 16 ? 4 : 2;
+    __shared__ float sh[kThinWaves][kN][kPitch];
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15u, kl = (lane >> 4) * kK;
+    const uint32_t tiles_n = (A.F.N + kN - 1) / kN, tiles = gridDim.x / A.splits, id = xcd_contiguous(blockIdx.x, gridDim.x);
+    const uint32_t split = id / tiles, tile = id - split * tiles, m0 = tile / tiles_n * kM, n0 = tile % tiles_n * kN, M = A.F.M, K = A.K, steps = (K + kStep - 1) / kStep;
+    const uint32_t begin = (uint32_t)((uint64_t)split * steps / A.splits) * kStep, end = min((uint32_t)((uint64_t)(split + 1u) * steps / A.splits) * kStep, K);
+    struct Step {
+        Columns<T, kV> c[kMixed ? kK : 1];
+        Row w[kMixed ? 1 : kV], x[NT], rest[kRest ? NT : 1];
+    };
+    const T *b[NT], *rest[NT], *a[kMixed ? 1 : kV];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const size_t at = (size_t)min(n0 + t * 16u + l16, A.F.N - 1u) * K;
+        b[t] = A.b + at;
+        if constexpr (kRest) rest[t] = A.rest + at;
+    }
+    if constexpr (kMixed) {
+        a[0] = A.a + min(m0 + l16 * kV, M - (uint32_t)kV);
+    } else {
+#pragma unroll
+        for (int j = 0; j < kV; ++j) a[j] = A.a + (size_t)min(m0 + j * 16u + l16, M - 1u) * K;
+    }
+    auto request = [&](uint32_t k0) -> Step {
+        Step S;
+        const uint32_t k = min(k0 + kl, K - kK);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            S.x[t].load(b[t] + k);
+            if constexpr (kRest) S.rest[t].load(rest[t] + k);
+        }
+        if constexpr (kMixed) {
+#pragma unroll
+            for (uint32_t t = 0; t < kK; ++t) S.c[t].load(a[0] + (size_t)(k + t) * M);
+        } else {
+#pragma unroll
+            for (int j = 0; j < kV; ++j) S.w[j].load(a[j] + k);
+        }
+        return S;
+    };
+    f4v acc[kV][NT] = {};
+    auto multiply = [&](Step& S, uint32_t k0) {
+        if (k0 + kStep > K) {
+            const int moved = (int)(k0 + kl) - (int)(K - kK);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                S.x[t].drop(moved);
+                if constexpr (kRest) S.rest[t].drop(moved);
+            }
+        }
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int j = 0; j < kV; ++j) {
+                bf8v a;
+                if constexpr (kMixed) {
+                    uint32_t v[4];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+                        v[u] = __builtin_amdgcn_perm(S.c[2 * u + 1].w[j / 2], S.c[2 * u].w[j / 2], j % 2 ? 0x07060302u : 0x05040100u);
+                    const any_u4 q = {v[0], v[1], v[2], v[3]};
+                    a = __builtin_bit_cast(bf8v, q);
+                } else {
+                    a = S.w[j].operand();
+                }
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    if constexpr (kRest) acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, S.rest[t].operand(), acc[j][t], 0, 0, 0);
+                    acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, S.x[t].operand(), acc[j][t], 0, 0, 0);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int j = 0; j < kV; ++j)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        float a;
+                        if constexpr (kMixed) a = __uint_as_float(S.c[e].w[j]);
+                        else a = S.w[j].r[e];
+                        acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, S.x[t].r[e], acc[j][t], 0, 0, 0);
+                    }
+        }
+    };
+    constexpr uint32_t kTurn = kThinWaves * kStep;
+    Step S[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+        if (begin + wave * kStep + i * kTurn < end) S[i] = request(begin + wave * kStep + i * kTurn);
+    for (uint32_t k = begin + wave * kStep; k < end; k += kAhead * kTurn)
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (k + i * kTurn >= end) break;
+            multiply(S[i], k + i * kTurn);
+            if (k + (kAhead + i) * kTurn < end) S[i] = request(k + (kAhead + i) * kTurn);
+        }
+    // result r of a lane: row lane % 16 of the output's; column 4 (lane / 16) + r of instruction j
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int j = 0; j < kV; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const uint32_t q = (lane >> 4) * 4u + r, c = kMixed ? min(m0 + q * kV, M - (uint32_t)kV) + j - m0 : j * 16u + q;
+                if (!kMixed || c < kM) sh[wave][t * 16 + l16][c] = acc[j][t][r];       // (a column before the workgroup's first is another's)
+            }
+    __syncthreads();
+    constexpr uint32_t kPieces = kM / 8;
+    const uint32_t piece = tid / 4u % kPieces, r = tid / 4u / kPieces, row = n0 + r, c0 = m0 + piece * 8u;
+    if (r >= kN) return;
+    float f[8] = {};
+#pragma unroll
+    for (uint32_t w = 0; w < kThinWaves / 4u; ++w) {
+        const float* p = sh[(tid & 3u) * (kThinWaves / 4u) + w][r] + piece * 8u;
+        const any_f4 lo = *reinterpret_cast<const any_f4*>(p), hi = *reinterpret_cast<const any_f4*>(p + 4);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) { f[k] += lo[k]; f[4 + k] += hi[k]; }
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {                            // over four lanes
+        f[k] += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(f[k]), 0xB1, 0xF, 0xF, false));
+        f[k] += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(f[k]), 0x4E, 0xF, 0xF, false));
+    }
+    const int n = (int)M - (int)c0;
+    if ((tid & 3u) != 0u || row >= A.F.N || n <= 0) return;
+    if (A.splits > 1u) { store8(A.parts + ((size_t)split * A.F.N + row) * M + c0, f, n); return; }
+    float bias[8];
+    bias_of(A.F, c0, bias);
+    finish<T>(A.F, dropout_key(A.F.drop), row, c0, n, bias, f);
 }
 
 // ---- dz and the sums of the bias --------------------------------------------------------------------------------------------
@@ -151,6 +355,7 @@ __global__ __launch_bounds__(256) void k_linear_join(LinearArgs A) {
 struct SlopeArgs {
     const void *dy, *z;       // z: NULL without an activation
     void* dz;
+    void* rest;               // like dz: what rounding left of it, or NULL
     uint16_t* planes;         // dz as operand rows of ldp where the product cannot read it as it lies, or NULL
     uint32_t ldp, count;      // planes: 1 .. 3
     float* partial;           // or NULL
@@ -219,6 +424,16 @@ __global__ __launch_bounds__(256) void k_linear_slope(SlopeArgs A) {
                 for (int k = 0; k < 8; ++k) { g[k] += h[k]; s[k] = __builtin_fmaf(h[k], h[k], s[k]); h[k] = 0.f; }
             }
             if (n > 0) store8(static_cast<T*>(A.dz) + (size_t)r * A.C + c0, d, n);
+            if (A.rest && n > 0) {
+                float left[8];
+#pragma unroll
+                for (int k = 0; k < 8; k += 2) {
+                    const uint32_t x = two_bf16(d[k], d[k + 1]);
+                    left[k] = d[k] - __uint_as_float(x << 16);
+                    left[k + 1] = d[k + 1] - __uint_as_float(x & 0xFFFF0000u);
+                }
+                store8(static_cast<T*>(A.rest) + (size_t)r * A.C + c0, left, n);
+            }
             if (A.planes && n > 0) {
                 const size_t plane = (size_t)N * A.ldp;
                 for (uint32_t q = 0; q < A.count; ++q) {
@@ -249,25 +464,74 @@ __global__ __launch_bounds__(256) void k_linear_slope(SlopeArgs A) {
 // ---- launches -----------------------------------------------------------------------------------------------------------------
 //               BM   BN   WM  WN BK S PA PB
 typedef TileShape<256, 256, 128, 64, 64, 2, 1, 1> Large;     // bfloat16
-typedef TileShape<128, 128, 64, 64, 64, 2, 1, 1> Small;
-typedef TileShape<128, 128, 64, 64, 64, 2, 1, 2> Small2;     // dX from two planes of dz
+typedef TileShape<128, 128, 64, 64, 64, 2, 1, 1> Small;      // two workgroups a compute unit
+typedef TileShape<128, 128, 64, 32, 64, 4, 1, 1> Deep;       // one: what two would hide of each other's waits, four stages and two waves a SIMD have to
+typedef TileShape<128, 128, 64, 32, 64, 3, 1, 2> Small2;     // dX from two planes of dz
 typedef TileShape<256, 128, 64, 64, 32, 2, 3, 3> Cut;        // float32
 
 static uint32_t up8(uint32_t x) { return (x + 7u) / 8u * 8u; }
 static uint64_t tiles(uint32_t a, uint32_t ta, uint32_t b, uint32_t tb) { return (uint64_t)((a + ta - 1) / ta) * ((b + tb - 1) / tb); }
 
-enum class Tile { kLarge, kSmall, kSmall2, kCut };
+enum class Tile { kLarge, kSmall, kSmall2, kCut, kThin, kDeep };
+// Few rows, or little work (us of a forward call, thin and by tiles: bfloat16, 256 x 2048 x 2048: 11.5 and 15.9, 1024 x 1024 x 1024: 14.6 and 14.6, 512 x 2048 x 2048:
+// 21.4 and 20.4, 64 x 4096 x 4096: 19.3 and 17.2, 16 x 4096 x 4096: 12.9 and 15.2; float32, 1024 x 1024 x 1024: 35.0 and 37.0, 2048 x 512 x 2048: 64.6 and 54.9, but
+// 128 x 4096 x 4096: 61.5 and 71.1).
+static bool is_thin(int dtype, uint32_t N, uint32_t M, uint32_t K) {
+    if (K < (dtype == VGC_F32 ? 4u : 8u) || M < 4u) return false;       // (what a place past an edge is moved back by)
+    const uint64_t work = (uint64_t)N * M * K;
+    return N <= 16u || work < (1ull << 30) || (dtype == VGC_F32 && N <= 128u && work <= (1ull << 31));
+}
 // How a product [N, M] over K is formed.
-struct ProductPlan { Tile tile; uint32_t splits; size_t parts; };
+struct ProductPlan { Tile tile; uint32_t splits, v, t; size_t parts; };    // thin: kV and NT
 static ProductPlan product_plan(int dtype, uint32_t N, uint32_t M, uint32_t K, uint32_t planes_b) {
-    ProductPlan L;
-    L.tile = dtype == VGC_F32 ? Tile::kCut : planes_b == 2u ? Tile::kSmall2 : tiles(M, 256, N, 256) >= 192u ? Tile::kLarge : Tile::kSmall;
-    const uint64_t n = L.tile == Tile::kLarge ? tiles(M, 256, N, 256) : L.tile == Tile::kCut ? tiles(M, 256, N, 128) : tiles(M, 128, N, 128);
-    const uint32_t want = L.tile == Tile::kSmall ? 512u : 256u;
+    ProductPlan L = {};
     L.splits = 1;
-    while (n * L.splits < want && K / (L.splits * 2u) >= 256u && L.splits < 32u) L.splits *= 2u;
+    if (is_thin(dtype, N, M, K)) {
+        L.tile = Tile::kThin;
+        // The largest part of the output that still gives every compute unit a workgroup (float32, 64 x 2048 x 2048: 32 columns by 16 rows 12.2, by 32 19.7;
+        // 256 x 1024 x 1024: 64 by 16 10.5, 32 by 32 11.7).  Rows of W of 128 bytes a workgroup at least while there are several steps of k: a compute unit takes some 31 GB/s
+        // of whole lines, and of halves no more, so a long k is shared out over workgroups (1 x 4096 x 4096 bfloat16, 64 columns: one 20.0, two 15.3, four
+        // 11.6, eight 14.1; 8192 x 2048: one 35.5, four 15.1, eight 12.6; but 2048 x 2048: one 8.7, two 11.5).
+        const struct { uint32_t v, t; } shapes[] = {{4, 2}, {4, 1}, {2, 2}, {2, 1}, {1, 1}};
+        const uint32_t least = dtype == VGC_F32 ? 1u : 2u, line = dtype == VGC_F32 ? 2u : 4u;
+        const bool deep = K > 2048u && N <= 64u;
+        for (const auto& q : shapes) {
+            if (q.v < least || (deep && q.v < line) || (q.t == 2u && N <= 16u)) continue;
+            L.v = q.v;
+            L.t = q.t;
+            if (tiles(M, 16u * q.v, N, 16u * q.t) >= 256u) break;
+        }
+        if (deep) {
+            const uint64_t n = tiles(M, 16u * L.v, N, 16u * L.t);
+            L.splits = (uint32_t)std::min<uint64_t>((256u + n - 1u) / n, K / 1024u);
+            L.parts = L.splits > 1u ? (size_t)L.splits * N * M * sizeof(float) : 0;
+        }
+        return L;
+    }
+    // bfloat16 (us): 16384 x 2048 x 8192 by large tiles 460, small 566; 4096 x 4096 x 4096 116 and 148; 4096 x 1024 x 1024 27 and 16, 2048 x 2048 x 2048 50 and 31.
+    // Small ones of which a compute unit has one: 2048 x 2048 x 2048 31.0, deep 24.0; 4096 x 4096 x 1024 57.9 and 42.9; two: 8192 x 1024 x 1024 26.7 and 30.6.
+    const uint64_t large = tiles(M, 256, N, 256), small = tiles(M, 128, N, 128);
+    L.tile = dtype == VGC_F32 ? Tile::kCut : planes_b == 2u ? Tile::kSmall2 : large >= 192u ? Tile::kLarge : small > 256u ? Tile::kSmall : Tile::kDeep;
+    const uint64_t n = L.tile == Tile::kLarge ? large : L.tile == Tile::kCut ? tiles(M, 256, N, 128) : small;
+    // A long k in parts where that gives idle compute units work: a second kernel and the parts' way through memory have to be paid by it (us, in one, two, four, eight
+    // parts by small tiles: 128 x 4096 x 4096 57, 35, 23.8, 21.1; 512 x 4096 x 4096 deep 39.5 whole, small in four 37.2, but 512 x 2048 x 2048 17.4 and 21.8; float32
+    // 2048 x 2048 x 2048 129 and 114).
+    const uint32_t least = dtype == VGC_F32 ? 256u : 512u;
+    if (dtype == VGC_F32 || K > 2048u)
+        while (n * L.splits <= 128u && K / (L.splits * 2u) >= least && L.splits < 32u) L.splits *= 2u;
     L.parts = L.splits > 1u ? (size_t)L.splits * N * M * sizeof(float) : 0;
     return L;
+}
+
+// Results of whole aligned pieces, too large to be found in the caches again.
+static bool past(int dtype, uint32_t N, uint32_t M, const void* z, const void* y) {
+    return M % 8u == 0u && (((uintptr_t)z | (uintptr_t)y) & 15u) == 0u && (uint64_t)N * M * (dtype == VGC_F32 ? 4u : 2u) * (z ? 2u : 1u) > (192ull << 20);
+}
+template <typename T>
+static int launch_join(const Finish& F, uint32_t splits, float* parts, hipStream_t stream) {
+    const uint64_t pieces = (uint64_t)F.N * ((F.M + 7u) / 8u);
+    hipLaunchKernelGGL(k_linear_join<T>, dim3((uint32_t)((pieces + 255u) / 256u)), dim3(256), 0, stream, F, splits, parts);
+    return hip_check(hipGetLastError(), "launch k_linear_join");
 }
 
 template <typename T, bool kMixed>
@@ -278,13 +542,29 @@ static int launch_product(const ProductPlan& L, LinearArgs A, hipStream_t stream
     if constexpr (sizeof(T) == 4) VGC_LAUNCH(Cut);
     else if (L.tile == Tile::kLarge) VGC_LAUNCH(Large);
     else if (L.tile == Tile::kSmall) VGC_LAUNCH(Small);
+    else if (L.tile == Tile::kDeep) VGC_LAUNCH(Deep);
     else if constexpr (!kMixed) VGC_LAUNCH(Small2);
 #undef VGC_LAUNCH
     int rc = hip_check(hipGetLastError(), "launch k_linear");
-    if (rc != VGC_OK || L.splits == 1u) return rc;
-    const uint64_t pieces = (uint64_t)A.F.N * ((A.F.M + 7u) / 8u);
-    hipLaunchKernelGGL(k_linear_join<T>, dim3((uint32_t)((pieces + 255u) / 256u)), dim3(256), 0, stream, A);
-    return hip_check(hipGetLastError(), "launch k_linear_join");
+    return rc != VGC_OK || L.splits == 1u ? rc : launch_join<T>(A.F, L.splits, A.parts, stream);
+}
+
+template <typename T, bool kMixed, bool kRest>
+static int launch_thin(const ProductPlan& L, ThinArgs<T> A, float* parts, hipStream_t stream) {
+    A.splits = L.splits;
+    A.parts = parts;
+#define VGC_LAUNCH(V, NT) hipLaunchKernelGGL((k_linear_thin<T, kMixed, V, NT, kRest>), dim3(tiles(A.F.M, 16 * V, A.F.N, 16 * NT) * L.splits), dim3(kThinWaves * 64), 0, stream, A)
+    if (L.t == 1u) {
+        if (L.v == 4u) VGC_LAUNCH(4, 1);
+        else if (L.v == 2u) VGC_LAUNCH(2, 1);
+        else if constexpr (sizeof(T) == 4) VGC_LAUNCH(1, 1);
+    } else {
+        if (L.v == 4u) VGC_LAUNCH(4, 2);
+        else VGC_LAUNCH(2, 2);
+    }
+#undef VGC_LAUNCH
+    const int rc = hip_check(hipGetLastError(), "launch k_linear_thin");
+    return rc != VGC_OK || L.splits == 1u ? rc : launch_join<T>(A.F, L.splits, parts, stream);
 }
 
 struct LinearPlan { ProductPlan product; bool x_there, w_there; uint32_t Kp, Cp; size_t x, w, parts, total; };
@@ -293,8 +573,9 @@ static LinearPlan linear_plan(int dtype, uint32_t N, uint32_t K, uint32_t C) {
     L.product = product_plan(dtype, N, C, K, 1);
     L.Kp = up8(K);
     L.Cp = up8(C);
-    L.x_there = dtype == VGC_BF16 && K % 8u == 0u;
-    L.w_there = dtype == VGC_BF16 && C % 8u == 0u;
+    const bool thin = L.product.tile == Tile::kThin;
+    L.x_there = thin || (dtype == VGC_BF16 && K % 8u == 0u);
+    L.w_there = thin || (dtype == VGC_BF16 && C % 8u == 0u);
     const size_t planes = dtype == VGC_F32 ? 3 : 1;
     size_t off = 0;
     L.x = off; if (!L.x_there) off = align_up(off + 2 * planes * N * L.Kp, 256);
@@ -310,7 +591,12 @@ int launch_linear(const LinearCall& q, void* workspace, hipStream_t stream) {
     const LinearPlan L = linear_plan(q.dtype, N, q.K, q.C);
     char* ws = static_cast<char*>(workspace);
     uint16_t *x = (uint16_t*)(ws + L.x), *w = (uint16_t*)(ws + L.w);
+    const Finish F = {q.bias, q.residual, q.z, q.y, N, q.C, q.act, dropout_of(q.p, q.rng), past(q.dtype, N, q.C, q.z, q.y)};
     int rc;
+    if (L.product.tile == Tile::kThin) {
+        if (q.dtype == VGC_F32) return launch_thin<float, true, false>(L.product, ThinArgs<float>{(const float*)q.W, (const float*)q.X, nullptr, q.K, 1, nullptr, F}, (float*)(ws + L.parts), stream);
+        return launch_thin<uint16_t, true, false>(L.product, ThinArgs<uint16_t>{(const uint16_t*)q.W, (const uint16_t*)q.X, nullptr, q.K, 1, nullptr, F}, (float*)(ws + L.parts), stream);
+    }
     if (!L.x_there && (rc = launch_plane_rows(q.dtype, q.X, N, q.K, x, stream)) != VGC_OK) return rc;
     if (!L.w_there && (rc = launch_plane_rows(q.dtype, q.W, q.K, q.C, w, stream)) != VGC_OK) return rc;
     LinearArgs A = {};
@@ -318,11 +604,11 @@ int launch_linear(const LinearCall& q, void* workspace, hipStream_t stream) {
     A.a = L.w_there ? Matrix{(const uint16_t*)q.W, q.K, q.C, 0} : Matrix{w, q.K, L.Cp, (uint64_t)q.K * L.Cp};
     A.K = L.Kp;
     A.parts = (float*)(ws + L.parts);
-    A.F = Finish{q.bias, q.residual, q.z, q.y, N, q.C, q.act, dropout_of(q.p, q.rng)};
+    A.F = F;
     return q.dtype == VGC_F32 ? launch_product<float, true>(L.product, A, stream) : launch_product<uint16_t, true>(L.product, A, stream);
 }
 
-struct LinearBackwardPlan { ProductPlan product; bool w_there, dz_there, whole; uint32_t planes, Cp, lanes, blocks, samples_parts, groups; size_t w, dz, parts, partial, total; };
+struct LinearBackwardPlan { ProductPlan product; bool w_there, dz_there, rest, whole; uint32_t planes, Cp, lanes, blocks, samples_parts, groups; size_t w, dz, parts, partial, total; };
 static LinearBackwardPlan linear_backward_plan(int dtype, uint32_t B, uint32_t P, uint32_t K, uint32_t C) {
     LinearBackwardPlan L;
     const uint32_t N = B * P;
@@ -331,8 +617,10 @@ static LinearBackwardPlan linear_backward_plan(int dtype, uint32_t B, uint32_t P
     L.planes = dtype == VGC_F32 ? 3u : two ? 2u : 1u;
     L.product = product_plan(dtype, N, K, C, L.planes);
     L.Cp = up8(C);
-    L.w_there = dtype == VGC_BF16 && C % 8u == 0u;
-    L.dz_there = L.w_there && !two;
+    const bool thin = L.product.tile == Tile::kThin;
+    L.w_there = thin || (dtype == VGC_BF16 && C % 8u == 0u);
+    L.dz_there = thin || (L.w_there && !two);
+    L.rest = thin && two;
     const uint32_t pieces = (C + 7u) / 8u;
     L.lanes = power_of_two(std::min(pieces, 32u));
     L.blocks = (pieces + L.lanes - 1u) / L.lanes;
@@ -344,6 +632,7 @@ static LinearBackwardPlan linear_backward_plan(int dtype, uint32_t B, uint32_t P
     size_t off = 0;
     L.w = off; if (!L.w_there) off = align_up(off + 2 * (size_t)(dtype == VGC_F32 ? 3 : 1) * K * L.Cp, 256);
     L.dz = off; if (!L.dz_there) off = align_up(off + 2 * (size_t)L.planes * N * L.Cp, 256);
+    if (L.rest) off = align_up(off + 2 * (size_t)N * C, 256);    // (in dz's place)
     L.parts = off; off = align_up(off + L.product.parts, 256);
     L.partial = off; off += (size_t)L.groups * (L.whole ? 2u : 1u) * C * sizeof(float);
     L.total = off;
@@ -357,7 +646,7 @@ int launch_linear_backward(const LinearCall& q, void* workspace, hipStream_t str
     char* ws = static_cast<char*>(workspace);
     uint16_t *w = (uint16_t*)(ws + L.w), *planes = (uint16_t*)(ws + L.dz);
     const bool copy = q.dX && !L.dz_there;
-    SlopeArgs S = {q.dy, q.act == VGC_ACT_NONE ? nullptr : q.z_in, q.dz, copy ? planes : nullptr, L.Cp, L.planes, q.s_bias ? (float*)(ws + L.partial) : nullptr,
+    SlopeArgs S = {q.dy, q.act == VGC_ACT_NONE ? nullptr : q.z_in, q.dz, q.dX && L.rest ? planes : nullptr, copy ? planes : nullptr, L.Cp, L.planes, q.s_bias ? (float*)(ws + L.partial) : nullptr,
                    q.B, q.P, q.C, L.lanes, L.blocks, L.samples_parts, L.groups, L.whole, q.act, dropout_of(q.p, q.rng)};
     const dim3 grid(L.groups * L.blocks);
     if (q.dtype == VGC_F32) hipLaunchKernelGGL(k_linear_slope<float>, grid, dim3(256), 0, stream, S);
@@ -366,13 +655,20 @@ int launch_linear_backward(const LinearCall& q, void* workspace, hipStream_t str
     if (rc != VGC_OK) return rc;
     if (q.s_bias && (rc = launch_column_sums(S.partial, 1, L.groups, q.B, L.samples_parts, q.C, L.whole, q.c, q.g_bias, q.s_bias, nullptr, nullptr, stream)) != VGC_OK) return rc;
     if (!q.dX) return VGC_OK;
+    const Finish F = {nullptr, q.residual, nullptr, q.dX, N, q.K, VGC_ACT_NONE, Dropout{nullptr, 0u, 0.f}, past(q.dtype, N, q.K, nullptr, q.dX)};
+    if (L.product.tile == Tile::kThin) {
+        if (q.dtype == VGC_F32) return launch_thin<float, false, false>(L.product, ThinArgs<float>{(const float*)q.W, (const float*)q.dz, nullptr, q.C, 1, nullptr, F}, (float*)(ws + L.parts), stream);
+        const ThinArgs<uint16_t> T = {(const uint16_t*)q.W, (const uint16_t*)q.dz, planes, q.C, 1, nullptr, F};
+        float* parts = (float*)(ws + L.parts);
+        return L.rest ? launch_thin<uint16_t, false, true>(L.product, T, parts, stream) : launch_thin<uint16_t, false, false>(L.product, T, parts, stream);
+    }
     if (!L.w_there && (rc = launch_plane_rows(q.dtype, q.W, q.K, q.C, w, stream)) != VGC_OK) return rc;
     LinearArgs A = {};
     A.a = L.w_there ? Matrix{(const uint16_t*)q.W, q.K, q.C, 0} : Matrix{w, q.K, L.Cp, (uint64_t)q.K * L.Cp};
     A.b = L.dz_there ? Matrix{(const uint16_t*)q.dz, N, q.C, 0} : Matrix{planes, N, L.Cp, (uint64_t)N * L.Cp};
     A.K = L.Cp;
     A.parts = (float*)(ws + L.parts);
-    A.F = Finish{nullptr, q.residual, nullptr, q.dX, N, q.K, VGC_ACT_NONE, Dropout{nullptr, 0u, 0.f}};
+    A.F = F;
     return q.dtype == VGC_F32 ? launch_product<float, false>(L.product, A, stream) : launch_product<uint16_t, false>(L.product, A, stream);
 }
 

@@ -215,7 +215,8 @@ def test_values_that_are_not_finite_stay_in_their_rows(dev, dtype):
     for N, K, C in ((20, 100, 130), (300, 1000, 200)):
         _, X, W, b = _case(N, K, C, dtype, dev)
         X[3, K - 1], X[7, 0], X[N - 1, 5] = float("nan"), float("inf"), float("-inf")
-        ws = T.workspace(max(vgc.linear_workspace_bytes(vgc.F32, N, K, C), vgc.linear_backward_workspace_bytes(vgc.F32, N, 1, K, C)), dev)
+        code = vgc.F32 if dtype == "f32" else vgc.BF16
+        ws = T.workspace(max(vgc.linear_workspace_bytes(code, N, K, C), vgc.linear_backward_workspace_bytes(code, N, 1, K, C)), dev)
         y = torch.empty(N, C, dtype=X.dtype, device=dev)
         vgc.linear(X, W, y, b, vgc.ACT_SILU, workspace=ws)
         bad = ~torch.isfinite(y).all(1)
