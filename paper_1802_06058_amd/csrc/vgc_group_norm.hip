@@ -29,6 +29,7 @@ struct GroupNormArgs {
     float eps;
     uint32_t lanes, blocks, chunks, rows;                    // of a piece row; blocks of columns; chunks of a sample, positions each
     uint32_t groups, slabs;                                  // whole groups a workgroup takes, workgroups a sample
+    bool past;                // the result is stored past the caches
 };
 
 // gamma xhat + beta, rounded after each operation in both passes: relu's slope is decided by the sign that the forward pass saw, which with one
@@ -37,26 +38,70 @@ __device__ __forceinline__ float scaled(float xhat, float gamma, float beta) { r
 
 __device__ __forceinline__ uint32_t at_most(uint32_t a, uint32_t b) { return a < b ? a : b; }
 
-// Sums of chan over whole groups of w channels, a wave a group.  Ends with a barrier.
-template <typename Weight>
-__device__ __forceinline__ void sums_of_groups(const float* chan, uint32_t w, uint32_t groups, float* grp, Weight weight) {
+// Sums of two vectors of channels (or of one: b NULL) over whole groups of w, a wave a group: into ga and gb.  Ends with a barrier.
+template <bool kTwo, typename Weight>
+__device__ __forceinline__ void sums_of_groups(const float* a, const float* b, uint32_t w, uint32_t groups, float* ga, float* gb, Weight weight) {
     const uint32_t lane = threadIdx.x & 63u, waves = blockDim.x / 64u;
     for (uint32_t q = threadIdx.x >> 6; q < groups; q += waves) {
-        float sum = 0.f;
-        for (uint32_t c = lane; c < w; c += 64u) sum += weight(q * w + c) * chan[q * w + c];
-        sum = wave_sum(sum);
-        if (lane == 0) grp[q] = sum;
+        float s = 0.f, t = 0.f;
+        for (uint32_t c = lane; c < w; c += 64u) {
+            const float of = weight(q * w + c);
+            s = __builtin_fmaf(of, a[q * w + c], s);
+            if (kTwo) t = __builtin_fmaf(of, b[q * w + c], t);
+        }
+        s = wave_sum(s);
+        if (kTwo) t = wave_sum(t);
+        if (lane == 0) { ga[q] = s; if (kTwo) gb[q] = t; }
     }
     __syncthreads();
 }
 
 // ---- a sample's whole groups in one workgroup ---------------------------------------------------------------------------------
-// kNV rows of a team are held as they are in memory.
-constexpr uint32_t kMostThreads = 512, kMostSlab = 512;      // threads, channels
+// kNV rows of a team are held as they are in memory.  How a workgroup's groups lie in its lanes decides how a group's sum is formed: by channels, which may
+// belong to any group; a lane's eight channels of one group, then by lanes; or all lanes' of one.
+enum { kByChannel, kByLane, kOneGroup };
+constexpr uint32_t kMostThreads = 1024, kMostSlab = 512;     // threads, channels
 
-template <typename T, int kNV>
-__global__ __launch_bounds__(kMostThreads) void k_group_norm(GroupNormArgs A) {
-    __shared__ float sh[kMostThreads * 8], part[kMostThreads], chan[kMostSlab], grp[64];
+// The sum over the group that a lane's channels belong to, for each of them; `out` (by group) keeps it until the next but one barrier.
+template <int kMode> struct GroupSums {
+    float *sh, *part, *chan, *grp;
+    uint32_t lanes, w, groups;
+    __device__ __forceinline__ void of(const float (&v)[8]) const {
+        if constexpr (kMode == kByChannel) {
+            const float one[1][8] = {{v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]}};
+            channel_sums<1>(one, lanes, sh, part, chan);
+            sums_of_groups<false>(chan, nullptr, w, groups, grp, nullptr, [](uint32_t) { return 1.f; });
+            return;
+        }
+        const float sum = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+        const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, waves = blockDim.x / 64u;
+        if constexpr (kMode == kOneGroup) {
+            const float all = wave_sum(sum);
+            if (lane == 0) part[wave] = all;
+            __syncthreads();
+            float total = 0.f;
+            for (uint32_t i = 0; i < waves; ++i) total += part[i];
+            __syncthreads();
+            if (threadIdx.x == 0) grp[0] = total;
+            __syncthreads();
+        } else {
+            part[threadIdx.x] = sum;
+            __syncthreads();
+            const uint32_t each = w / 8u, entries = blockDim.x / lanes * each;         // lanes of a group in a team, in all
+            for (uint32_t q = wave; q < groups; q += waves) {
+                float s = 0.f;
+                for (uint32_t e = lane; e < entries; e += 64u) s += part[e / each * lanes + q * each + e % each];
+                s = wave_sum(s);
+                if (lane == 0) grp[q] = s;
+            }
+            __syncthreads();
+        }
+    }
+};
+
+template <typename T, int kNV, int kMode, int kThreads>
+__global__ __launch_bounds__(kThreads) void k_group_norm(GroupNormArgs A) {
+    __shared__ float sh[kMode == kByChannel ? kThreads * 8 : 1], part[kThreads], chan[kMode == kByChannel ? kMostSlab : 1], grp[64];
     const uint32_t b = blockIdx.x / A.slabs, slab = blockIdx.x - b * A.slabs, q0 = slab * A.groups, groups = min(A.groups, A.G - q0);
     const uint32_t lane = threadIdx.x % A.lanes, team = threadIdx.x / A.lanes, teams = blockDim.x / A.lanes;
     const uint32_t c0 = q0 * A.w, width = groups * A.w, own = lane * 8u;
@@ -69,14 +114,14 @@ __global__ __launch_bounds__(kMostThreads) void k_group_norm(GroupNormArgs A) {
         const uint32_t p = team + i * teams;
         raw[i] = load8(x + (uint64_t)p * A.C, p < A.P ? n : 0, rows_at_end((uint64_t)b * A.P + p, rows));
     }
-    uint32_t of[8];                                          // group of a channel
+    uint32_t of[kMode == kByChannel ? 8 : 1];                // group of a channel
 #pragma unroll
-    for (int k = 0; k < 8; ++k) of[k] = k < n ? (own + k) / A.w : 0u;
+    for (int k = 0; k < (kMode == kByChannel ? 8 : 1); ++k) of[k] = k < n && kMode != kOneGroup ? (own + k) / A.w : 0u;
     float ga[8], be[8];
     widen8(load8(A.gamma + c0 + own, n), ga);
     widen8(load8(A.beta + c0 + own, n), be);
     const float inv = 1.0f / ((float)A.P * (float)A.w);
-    auto one = [](uint32_t) { return 1.f; };
+    const GroupSums<kMode> sums = {sh, part, chan, grp, A.lanes, A.w, groups};
     float f[8], v[8] = {};
 #pragma unroll
     for (int i = 0; i < kNV; ++i) {
@@ -85,26 +130,28 @@ __global__ __launch_bounds__(kMostThreads) void k_group_norm(GroupNormArgs A) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] += f[k];
     }
-    channel_sums(v, A.lanes, sh, part, chan);
-    sums_of_groups(chan, A.w, groups, grp, one);
-    float mean[8], rstd[8];
+    sums.of(v);
+    constexpr int kM = kMode == kByChannel ? 8 : 1;
+    float mean[kM], rstd[kM];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) { mean[k] = grp[of[k]] * inv; v[k] = 0.f; }
+    for (int k = 0; k < kM; ++k) mean[k] = grp[of[k]] * inv;
     const float own_mean = threadIdx.x < groups ? grp[threadIdx.x] * inv : 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = 0.f;
 #pragma unroll
     for (int i = 0; i < kNV; ++i) {
         widen8(raw[i], f);
         if (team + i * teams < A.P)
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const float d = k < n ? f[k] - mean[k] : 0.f;
+                const float d = k < n ? f[k] - mean[kM == 8 ? k : 0] : 0.f;
                 v[k] = __builtin_fmaf(d, d, v[k]);
             }
     }
-    channel_sums(v, A.lanes, sh, part, chan);
-    sums_of_groups(chan, A.w, groups, grp, one);
+    if (kMode == kByLane) __syncthreads();                   // (the means have been read)
+    sums.of(v);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) rstd[k] = 1.0f / sqrtf(grp[of[k]] * inv + A.eps);
+    for (int k = 0; k < kM; ++k) rstd[k] = 1.0f / sqrtf(grp[of[k]] * inv + A.eps);
     if (threadIdx.x < groups) {
         A.mean_out[(uint64_t)b * A.G + q0 + threadIdx.x] = own_mean;
         A.rstd_out[(uint64_t)b * A.G + q0 + threadIdx.x] = 1.0f / sqrtf(grp[threadIdx.x] * inv + A.eps);
@@ -116,30 +163,34 @@ __global__ __launch_bounds__(kMostThreads) void k_group_norm(GroupNormArgs A) {
         if (p >= A.P || n <= 0) continue;
         widen8(raw[i], f);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) f[k] = scaled((f[k] - mean[k]) * rstd[k], ga[k], be[k]);
+        for (int k = 0; k < 8; ++k) f[k] = scaled((f[k] - mean[kM == 8 ? k : 0]) * rstd[kM == 8 ? k : 0], ga[k], be[k]);
         apply_act((int)A.act, f);
         store8(y + (uint64_t)p * A.C, f, n);
     }
 }
 
-// The groups' mean, rstd, gamma and beta for a lane's channels c0 .. (n of them).
-struct Channels { float mean[8], rstd[8], gamma[8], beta[8]; };
-__device__ __forceinline__ void channels_of(const GroupNormArgs& A, uint32_t b, uint32_t c0, int n, Channels& K) {
-    widen8(load8(A.gamma + c0, n), K.gamma);
-    widen8(load8(A.beta + c0, n), K.beta);
+// The groups' mean and rstd (kM = 1: one group's), gamma and beta for a lane's channels c0 .. (n of them).
+template <int kM> struct Channels {
+    float mean[kM], rstd[kM], gamma[8], beta[8];
+    __device__ __forceinline__ Channels(const GroupNormArgs& A, uint32_t b, uint32_t c0, int n) {
+        widen8(load8(A.gamma + c0, n), gamma);
+        widen8(load8(A.beta + c0, n), beta);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        K.mean[k] = K.rstd[k] = 0.f;
-        if (k >= n) continue;
-        const uint64_t at = (uint64_t)b * A.G + (c0 + k) / A.w;
-        K.mean[k] = A.mean[at];
-        K.rstd[k] = A.rstd[at];
+        for (int k = 0; k < kM; ++k) {
+            mean[k] = rstd[k] = 0.f;
+            if (k >= n) continue;
+            const uint64_t at = (uint64_t)b * A.G + (c0 + k) / A.w;
+            mean[k] = A.mean[at];
+            rstd[k] = A.rstd[at];
+        }
     }
-}
-// d becomes e = dy act'(gamma xhat + beta), x xhat.
-__device__ __forceinline__ void through_act(const GroupNormArgs& A, const Channels& K, float (&x)[8], float (&d)[8]) {
+    __device__ __forceinline__ float xhat(float x, int k) const { return (x - mean[kM == 8 ? k : 0]) * rstd[kM == 8 ? k : 0]; }
+};
+// x becomes xhat, d becomes e = dy act'(gamma xhat + beta).
+template <int kM>
+__device__ __forceinline__ void through_act(const GroupNormArgs& A, const Channels<kM>& K, float (&x)[8], float (&d)[8]) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) x[k] = (x[k] - K.mean[k]) * K.rstd[k];
+    for (int k = 0; k < 8; ++k) x[k] = K.xhat(x[k], k);
     if (A.act == VGC_ACT_NONE) return;
     float t[8];
 #pragma unroll
@@ -147,9 +198,9 @@ __device__ __forceinline__ void through_act(const GroupNormArgs& A, const Channe
     apply_slope((int)A.act, t, d);
 }
 
-template <typename T, int kNV>
-__global__ __launch_bounds__(kMostThreads) void k_group_norm_backward(GroupNormArgs A) {
-    __shared__ float sh[kMostThreads * 8], part[kMostThreads], chan[2][kMostSlab], grp[2][64];
+template <typename T, int kNV, int kThreads, int kM>
+__global__ __launch_bounds__(kThreads) void k_group_norm_backward(GroupNormArgs A) {
+    __shared__ float sh[2 * kThreads * 8], part[2 * kThreads], chan[2][kMostSlab], grp[2][64];
     const uint32_t b = blockIdx.x / A.slabs, slab = blockIdx.x - b * A.slabs, q0 = slab * A.groups, groups = min(A.groups, A.G - q0);
     const uint32_t lane = threadIdx.x % A.lanes, team = threadIdx.x / A.lanes, teams = blockDim.x / A.lanes;
     const uint32_t c0 = q0 * A.w, width = groups * A.w, own = lane * 8u;
@@ -163,9 +214,8 @@ __global__ __launch_bounds__(kMostThreads) void k_group_norm_backward(GroupNormA
         rx[i] = load8(static_cast<const T*>(A.x) + at + (uint64_t)p * A.C, m, rows_at_end((uint64_t)b * A.P + p, rows));
         rd[i] = load8(static_cast<const T*>(A.dy) + at + (uint64_t)p * A.C, m, rows_at_end((uint64_t)b * A.P + p, rows));
     }
-    Channels K;
-    channels_of(A, b, c0 + own, n, K);
-    float x[8], d[8], vg[8] = {}, vh[8] = {};
+    const Channels<kM> K(A, b, c0 + own, n);
+    float x[8], d[8], v[2][8] = {};
 #pragma unroll
     for (int i = 0; i < kNV; ++i) {
         if (team + i * teams >= A.P) continue;
@@ -175,22 +225,20 @@ __global__ __launch_bounds__(kMostThreads) void k_group_norm_backward(GroupNormA
         widen8(rd[i], d);
         through_act(A, K, x, d);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) { vg[k] = __builtin_fmaf(d[k], x[k], vg[k]); vh[k] += d[k]; }
+        for (int k = 0; k < 8; ++k) { v[0][k] = __builtin_fmaf(d[k], x[k], v[0][k]); v[1][k] += d[k]; }
     }
-    channel_sums(vg, A.lanes, sh, part, chan[0]);
-    channel_sums(vh, A.lanes, sh, part, chan[1]);
+    channel_sums<2>(v, A.lanes, sh, part, chan[0], chan[1]);
     const float* gamma = A.gamma + c0;
-    sums_of_groups(chan[1], A.w, groups, grp[0], [&](uint32_t c) { return gamma[c]; });
-    sums_of_groups(chan[0], A.w, groups, grp[1], [&](uint32_t c) { return gamma[c]; });
+    sums_of_groups<true>(chan[1], chan[0], A.w, groups, grp[0], grp[1], [&](uint32_t c) { return gamma[c]; });
     for (uint32_t c = threadIdx.x; c < 2u * width; c += blockDim.x) {
         const uint32_t v = c >= width, ch = c - v * width;
         A.sums[((uint64_t)b * 2u + v) * A.C + c0 + ch] = chan[v][ch];
     }
     if (n <= 0) return;
     const float inv = 1.0f / ((float)A.P * (float)A.w);
-    float m1[8], m2[8];
+    float m1[kM], m2[kM];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < kM; ++k) {
         const uint32_t q = k < n ? (own + k) / A.w : 0u;
         m1[k] = grp[0][q] * inv;
         m2[k] = grp[1][q] * inv;
@@ -203,7 +251,10 @@ __global__ __launch_bounds__(kMostThreads) void k_group_norm_backward(GroupNormA
         widen8(rd[i], d);
         through_act(A, K, x, d);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) d[k] = K.rstd[k] * __builtin_fmaf(-x[k], m2[k], __builtin_fmaf(d[k], K.gamma[k], -m1[k]));
+        for (int k = 0; k < 8; ++k) {
+            const int g = kM == 8 ? k : 0;
+            d[k] = K.rstd[g] * __builtin_fmaf(-x[k], m2[g], __builtin_fmaf(d[k], K.gamma[k], -m1[g]));
+        }
         store8(static_cast<T*>(A.out) + at + (uint64_t)p * A.C, d, n);
     }
 }
@@ -224,56 +275,49 @@ __device__ __forceinline__ Place place_of(const GroupNormArgs& A) {
     L.n = (int)A.C - (int)L.c0;
     return L;
 }
-// Mean and sum of squares about it, by channel.  A lane's sums are relative to the mean of its first kRows rows: what the sum of
+template <typename T> struct Stream { static constexpr int kRows = sizeof(T) == 2 ? 4 : 2; };
+template <typename T, bool kWhole, int kRows, int kArrays>
+__device__ __forceinline__ RowStream<T, kWhole, kRows, kArrays> rows_of(const GroupNormArgs& A, const Place& L, const void* a, const void* b) {
+    const uint64_t row0 = (uint64_t)L.b * A.P;
+    return RowStream<T, kWhole, kRows, kArrays>(static_cast<const T*>(a) + row0 * A.C, static_cast<const T*>(b) + (b ? row0 * A.C : 0u), A.C, L.c0, L.p0 + L.team, L.p1, L.teams,
+                                                (uint64_t)A.B * A.P - row0);
+}
+
+// Mean and sum of squares about it, by channel.  A lane's sums are relative to the mean of its first rows (kRows of them): what the sum of
 // squares then loses to the difference of that mean and its whole mean is at most the share of those rows, whatever the values.  Lanes are joined as
 // (count, mean, squares), so that a large mean costs no digits.
-constexpr int kRows = 4;
-template <typename T>
+template <typename T, bool kWhole>
 __global__ __launch_bounds__(256) void k_group_norm_moments(GroupNormArgs A) {
+    constexpr int kRows = Stream<T>::kRows;
     __shared__ float sm[2048], sq[2048], pm[256], pq[256];
     const Place L = place_of(A);
-    const uint64_t rows = (uint64_t)A.B * A.P;
-    const T* x = static_cast<const T*>(A.x) + (uint64_t)L.b * A.P * A.C + L.c0;
-    Raw8<T> raw[kRows];
-    auto request = [&](uint32_t p) {
-#pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            const uint32_t r = p + i * L.teams;
-            raw[i] = load8(x + (uint64_t)r * A.C, r < L.p1 ? L.n : 0, rows_at_end((uint64_t)L.b * A.P + r, rows));
-        }
-    };
+    auto X = rows_of<T, kWhole, kRows, 1>(A, L, A.x, nullptr);
     float base[8] = {}, s1[8] = {}, s2[8] = {}, f[8];
-    const uint32_t count = rows_of_team(L.p1 - L.p0, L.team, L.teams), first = at_most(count, kRows);
-    uint32_t p = L.p0 + L.team;
-    request(p);
+    const uint32_t count = rows_of_team(L.p1 - L.p0, L.team, L.teams);
+    const uint32_t first = at_most(count, kRows);
+    X.begin();
     if (first != 0u) {
         const float inv = 1.0f / (float)first;
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            widen8(raw[i], f);                               // (zeros past the chunk's end)
+        for (uint32_t i = 0; i < kRows; ++i) {
+            if (i >= first) continue;
+            widen8(kWhole ? X.set[0][0][i] : X.at(0, X.p + i * X.step), f);
 #pragma unroll
             for (int k = 0; k < 8; ++k) base[k] += f[k];
         }
 #pragma unroll
         for (int k = 0; k < 8; ++k) base[k] *= inv;
     }
-    for (; p < L.p1; p += kRows * L.teams) {
-        Raw8<T> now[kRows];
+    X.each([&](uint32_t, const Raw8<T> (&x)[1]) {
+        float f[8];
+        widen8(x[0], f);
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) now[i] = raw[i];
-        if (p + kRows * L.teams < L.p1) request(p + kRows * L.teams);
-#pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            if (p + i * L.teams >= L.p1) continue;
-            widen8(now[i], f);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const float d = f[k] - base[k];
-                s1[k] += d;
-                s2[k] = __builtin_fmaf(d, d, s2[k]);
-            }
+        for (int k = 0; k < 8; ++k) {
+            const float d = f[k] - base[k];
+            s1[k] += d;
+            s2[k] = __builtin_fmaf(d, d, s2[k]);
         }
-    }
+    });
     const float inv = count ? 1.0f / (float)count : 0.f;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
@@ -349,109 +393,68 @@ __global__ __launch_bounds__(256) void k_group_norm_join(GroupNormArgs A) {
     A.rstd_out[blockIdx.x] = (float)(1.0 / sqrt((var < 0. ? 0. : var) + (double)A.eps));   // (a NaN stays one)
 }
 
-template <typename T>
+template <typename T, bool kWhole, int kM>
 __global__ __launch_bounds__(256) void k_group_norm_apply(GroupNormArgs A) {
     const Place L = place_of(A);
-    if (L.n <= 0) return;
-    const uint64_t rows = (uint64_t)A.B * A.P, at = (uint64_t)L.b * A.P * A.C + L.c0;
-    const T* x = static_cast<const T*>(A.x) + at;
-    T* y = static_cast<T*>(A.out) + at;
-    Raw8<T> raw[kRows];
-    auto request = [&](uint32_t p) {
+    if (!kWhole && L.n <= 0) return;
+    auto X = rows_of<T, kWhole, Stream<T>::kRows, 1>(A, L, A.x, nullptr);
+    T* y = static_cast<T*>(A.out) + (uint64_t)L.b * A.P * A.C + L.c0;
+    X.begin();
+    const Channels<kM> K(A, L.b, L.c0, L.n);
+    X.each([&](uint32_t p, const Raw8<T> (&x)[1]) {
+        float f[8];
+        widen8(x[0], f);
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            const uint32_t r = p + i * L.teams;
-            raw[i] = load8(x + (uint64_t)r * A.C, r < L.p1 ? L.n : 0, rows_at_end((uint64_t)L.b * A.P + r, rows));
-        }
-    };
-    uint32_t p = L.p0 + L.team;
-    request(p);
-    Channels K;
-    channels_of(A, L.b, L.c0, L.n, K);
-    for (; p < L.p1; p += kRows * L.teams) {
-        Raw8<T> now[kRows];
-#pragma unroll
-        for (int i = 0; i < kRows; ++i) now[i] = raw[i];
-        if (p + kRows * L.teams < L.p1) request(p + kRows * L.teams);
-#pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            const uint32_t r = p + i * L.teams;
-            if (r >= L.p1) continue;
-            float f[8];
-            widen8(now[i], f);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) f[k] = scaled((f[k] - K.mean[k]) * K.rstd[k], K.gamma[k], K.beta[k]);
-            apply_act((int)A.act, f);
-            store8(y + (uint64_t)r * A.C, f, L.n);
-        }
-    }
+        for (int k = 0; k < 8; ++k) f[k] = scaled(K.xhat(f[k], k), K.gamma[k], K.beta[k]);
+        apply_act((int)A.act, f);
+        if (L.n > 0) store8_to(y + (uint64_t)p * A.C, f, L.n, A.past);
+    });
 }
 
 // kSums: G_z and H_z of the chunk; else dx.
-template <typename T, bool kSums>
+template <typename T, bool kWhole, int kM, bool kSums>
 __global__ __launch_bounds__(256) void k_group_norm_backward_rows(GroupNormArgs A) {
-    __shared__ float sh[kSums ? 2048 : 1], part[kSums ? 256 : 1], chan[kSums ? 256 : 1];
+    __shared__ float sh[kSums ? 4096 : 1], part[kSums ? 512 : 1], chan[2][kSums ? 256 : 1];
     const Place L = place_of(A);
-    if (!kSums && L.n <= 0) return;
-    const uint64_t rows = (uint64_t)A.B * A.P, at = (uint64_t)L.b * A.P * A.C + L.c0;
-    constexpr int kR = kRows / 2;
-    Raw8<T> rx[kR], rd[kR];
-    auto request = [&](uint32_t p) {
-#pragma unroll
-        for (int i = 0; i < kR; ++i) {
-            const uint32_t r = p + i * L.teams;
-            const bool at_end = rows_at_end((uint64_t)L.b * A.P + r, rows);
-            rx[i] = load8(static_cast<const T*>(A.x) + at + (uint64_t)r * A.C, r < L.p1 ? L.n : 0, at_end);
-            rd[i] = load8(static_cast<const T*>(A.dy) + at + (uint64_t)r * A.C, r < L.p1 ? L.n : 0, at_end);
-        }
-    };
-    uint32_t p = L.p0 + L.team;
-    request(p);
-    Channels K;
-    channels_of(A, L.b, L.c0, L.n, K);
-    float m1[8] = {}, m2[8] = {};
+    if (!kSums && !kWhole && L.n <= 0) return;
+    auto X = rows_of<T, kWhole, Stream<T>::kRows / 2, 2>(A, L, A.x, A.dy);
+    X.begin();
+    const Channels<kM> K(A, L.b, L.c0, L.n);
+    float m1[kM] = {}, m2[kM] = {};
     if (!kSums)
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
+        for (int k = 0; k < kM; ++k)
             if (k < L.n) {
                 const float* g = A.group_sums + ((uint64_t)L.b * A.G + (L.c0 + k) / A.w) * 2u;
                 m1[k] = g[0];
                 m2[k] = g[1];
             }
-    float vg[8] = {}, vh[8] = {};
-    for (; p < L.p1; p += kR * L.teams) {
-        Raw8<T> nx[kR], nd[kR];
+    float v[2][8] = {};
+    T* out = static_cast<T*>(A.out) + (uint64_t)L.b * A.P * A.C + L.c0;
+    X.each([&](uint32_t p, const Raw8<T> (&in)[2]) {
+        float x[8], d[8];
+        widen8(in[0], x);
+        widen8(in[1], d);
+        through_act(A, K, x, d);
+        if (kSums) {
 #pragma unroll
-        for (int i = 0; i < kR; ++i) { nx[i] = rx[i]; nd[i] = rd[i]; }
-        if (p + kR * L.teams < L.p1) request(p + kR * L.teams);
+            for (int k = 0; k < 8; ++k) { v[0][k] = __builtin_fmaf(d[k], x[k], v[0][k]); v[1][k] += d[k]; }
+        } else {
 #pragma unroll
-        for (int i = 0; i < kR; ++i) {
-            const uint32_t r = p + i * L.teams;
-            if (r >= L.p1) continue;
-            float x[8], d[8];
-            clip8(nx[i], L.n);
-            clip8(nd[i], L.n);
-            widen8(nx[i], x);
-            widen8(nd[i], d);
-            through_act(A, K, x, d);
-            if (kSums) {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) { vg[k] = __builtin_fmaf(d[k], x[k], vg[k]); vh[k] += d[k]; }
-            } else {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) d[k] = K.rstd[k] * __builtin_fmaf(-x[k], m2[k], __builtin_fmaf(d[k], K.gamma[k], -m1[k]));
-                store8(static_cast<T*>(A.out) + at + (uint64_t)r * A.C, d, L.n);
+            for (int k = 0; k < 8; ++k) {
+                const int g = kM == 8 ? k : 0;
+                d[k] = K.rstd[g] * __builtin_fmaf(-x[k], m2[g], __builtin_fmaf(d[k], K.gamma[k], -m1[g]));
             }
+            if (L.n > 0) store8_to(out + (uint64_t)p * A.C, d, L.n, A.past);
         }
-    }
+    });
     if (!kSums) return;
     const uint32_t first = L.c0 - (threadIdx.x % A.lanes) * 8u, c = first + threadIdx.x;
-    float* out = A.chunk_sums + ((uint64_t)L.b * A.chunks + L.chunk) * 2u * A.C;
-    channel_sums(vg, A.lanes, sh, part, chan);
-    if (threadIdx.x < A.lanes * 8u && c < A.C) out[c] = chan[threadIdx.x];
-    __syncthreads();
-    channel_sums(vh, A.lanes, sh, part, chan);
-    if (threadIdx.x < A.lanes * 8u && c < A.C) out[A.C + c] = chan[threadIdx.x];
+    float* sums = A.chunk_sums + ((uint64_t)L.b * A.chunks + L.chunk) * 2u * A.C;
+    channel_sums<2>(v, A.lanes, sh, part, chan[0], chan[1]);
+    if (threadIdx.x >= A.lanes * 8u || c >= A.C) return;
+    sums[c] = chan[0][threadIdx.x];
+    sums[A.C + c] = chan[1][threadIdx.x];
 }
 
 // G_z and H_z of a group's channels from their chunks, and the group's two sums.
@@ -493,40 +496,48 @@ __global__ __launch_bounds__(256) void k_group_norm_backward_join(GroupNormArgs 
 }
 
 // ---- launches -----------------------------------------------------------------------------------------------------------------
-// Held: whole groups of 64 channels and more a workgroup, so that a row of it is a cache line, of at most `most` rows a team.
+// Held: whole groups of a cache line's channels and more a workgroup (us; float32, 32 x 784 x 512 in 32 groups, lines of 32 channels 32.2, 64 39.1; bfloat16, 64 x 784 x 512, of 64 34.3, 32 46), with as many threads as leave a team few rows.  most: rows that a team can hold, with 512
+// threads and fewer and with 1024, whose lanes have 128 registers.
 struct GroupNormPlan {
     bool held;
     uint32_t lanes, threads, rows_of_team, groups, slabs;    // held
     uint32_t blocks, chunks, rows;                           // else
+    uint32_t samples;                                        // at a time
 };
-static GroupNormPlan group_norm_plan(uint32_t B, uint32_t P, uint32_t C, uint32_t G, uint32_t most) {
+constexpr uint32_t kGroups = 2048;
+constexpr uint64_t kSlice = 210ull << 20;
+static GroupNormPlan group_norm_plan(int dtype, bool backward, uint32_t B, uint32_t P, uint32_t C, uint32_t G) {
     GroupNormPlan L = {};
-    const uint32_t w = C / G;
-    L.groups = std::min(G, std::max(1u, (64u + w - 1u) / w));
+    const uint32_t w = C / G, line = dtype == VGC_F32 ? 32u : 64u;
+    L.groups = std::min(G, std::max(1u, (line + w - 1u) / w));
     L.slabs = (G + L.groups - 1u) / L.groups;
-    const uint32_t width = L.groups * w;
+    const uint32_t width = L.groups * w, wide = dtype == VGC_F32 ? 2u : 1u;
+    const uint32_t most = backward ? 8u / wide : 8u, most_1024 = backward ? (w % 8u == 0u ? 4u : 2u) / wide : 8u / wide, few = backward ? 4u / wide : 4u;
     if (width <= kMostSlab) {
         L.lanes = power_of_two((width + 7u) / 8u);
-        L.threads = 256u;
-        while (L.threads < kMostThreads && (uint64_t)P > (uint64_t)(L.threads / L.lanes) * std::min(most, 4u)) L.threads *= 2u;
-        const uint64_t teams = L.threads / L.lanes;
-        L.held = P <= teams * most;
-        L.rows_of_team = (uint32_t)((P + teams - 1u) / teams);
+        for (L.threads = 256u; L.threads < kMostThreads && P > (uint64_t)(L.threads / L.lanes) * few;) L.threads *= 2u;
+        if (L.threads == kMostThreads && P > (uint64_t)(L.threads / L.lanes) * most_1024) L.threads = 512u;
+        const uint32_t teams = L.threads / L.lanes;
+        L.rows_of_team = (P + teams - 1u) / teams;
+        L.held = L.rows_of_team <= (L.threads == kMostThreads ? most_1024 : most);
     }
-    if (L.held) return L;
+    if (L.held) { L.samples = std::min(B, std::max(1u, (1u << 22) / L.slabs)); return L; }
     const uint32_t pieces = (C + 7u) / 8u;
     L.lanes = power_of_two(std::min(pieces, 32u));
     L.threads = 256u;
     L.blocks = (pieces + L.lanes - 1u) / L.lanes;
     const uint32_t teams = 256u / L.lanes;
-    // eight workgroups a compute unit, of at least eight rows a team
-    const uint64_t want = std::max<uint64_t>(1, 2048u / std::max<uint64_t>(1, (uint64_t)B * L.blocks));
+    const uint64_t sample = (uint64_t)P * C * (dtype == VGC_F32 ? 4u : 2u) * (backward ? 2u : 1u), most_samples = std::max<uint64_t>(1, kSlice / sample);
+    const uint32_t times = (uint32_t)((B + most_samples - 1u) / most_samples);
+    L.samples = std::min((B + times - 1u) / times, std::max(1u, (1u << 22) / std::max(L.blocks, G)));
+    const uint64_t want = std::max<uint64_t>(1, kGroups / std::max<uint64_t>(1, (uint64_t)L.samples * L.blocks));
     L.chunks = (uint32_t)std::min<uint64_t>(want, (P + teams * 8u - 1u) / (teams * 8u));
-    L.rows = (P + L.chunks - 1u) / L.chunks;
+    const uint32_t batch = teams * (dtype == VGC_F32 ? 2u : 4u) * (backward ? 1u : 2u);      // (whole batches but for the sample's last)
+    L.rows = std::min(P, ((P + L.chunks - 1u) / L.chunks + batch / 2u) / batch * batch);
+    if (L.rows == 0u) L.rows = std::min(P, batch);
     L.chunks = (P + L.rows - 1u) / L.rows;
     return L;
 }
-static uint32_t most_rows(int dtype, bool backward) { return (dtype == VGC_F32 ? 8u : 16u) / (backward ? 2u : 1u); }
 
 struct GroupNormSpace { size_t chunk_sums, sums, group_sums, total; };
 static GroupNormSpace group_norm_space(const GroupNormPlan& L, uint32_t B, uint32_t C, uint32_t G, bool backward) {
@@ -539,20 +550,20 @@ static GroupNormSpace group_norm_space(const GroupNormPlan& L, uint32_t B, uint3
     return S;
 }
 size_t group_norm_workspace_bytes(int dtype, uint32_t B, uint32_t P, uint32_t C, uint32_t G) {
-    return group_norm_space(group_norm_plan(B, P, C, G, most_rows(dtype, false)), B, C, G, false).total;
+    return group_norm_space(group_norm_plan(dtype, false, B, P, C, G), B, C, G, false).total;
 }
 size_t group_norm_backward_workspace_bytes(int dtype, uint32_t B, uint32_t P, uint32_t C, uint32_t G) {
-    return group_norm_space(group_norm_plan(B, P, C, G, most_rows(dtype, true)), B, C, G, true).total;
+    return group_norm_space(group_norm_plan(dtype, true, B, P, C, G), B, C, G, true).total;
 }
 
-// Calls launch(args, samples) for ranges of samples, of `each` workgroups a sample at most, that a launch can hold.
+// Calls launch(args, samples) for the plan's samples at a time.
 template <typename Launch>
-static int by_samples(const GroupNormArgs& all, size_t size, uint64_t each, const GroupNormPlan& L, Launch launch) {
-    const uint32_t most = (uint32_t)std::max<uint64_t>(1, (1u << 22) / each);
-    for (uint32_t b = 0; b < all.B; b += std::min(most, all.B - b)) {
+static int by_samples(const GroupNormArgs& all, size_t size, const GroupNormPlan& L, Launch launch) {
+    const uint64_t sample = (uint64_t)all.P * all.C * size;
+    for (uint32_t b = 0; b < all.B; b += std::min(L.samples, all.B - b)) {
         GroupNormArgs A = all;
-        const size_t at = (size_t)b * A.P * A.C * size;
-        A.B = std::min(most, all.B - b);
+        const size_t at = (size_t)b * sample;
+        A.B = std::min(L.samples, all.B - b);
         A.x = (const char*)all.x + at;
         if (all.dy) A.dy = (const char*)all.dy + at;
         A.out = (char*)all.out + at;
@@ -572,62 +583,87 @@ static void place(GroupNormArgs& A, const GroupNormPlan& L) {
     A.lanes = L.lanes; A.blocks = L.blocks; A.chunks = L.chunks; A.rows = L.rows; A.groups = L.groups; A.slabs = L.slabs;
 }
 
+// Whether a lane's eight channels belong to one group wherever its piece lies.
+static bool by_lane(const GroupNormArgs& A) { return A.w % 8u == 0u; }
+
 template <typename T>
-static int launch_group_norm_of(GroupNormArgs& all, const GroupNormPlan& L, hipStream_t stream) {
+static int launch_group_norm_of(const GroupNormArgs& all, const GroupNormPlan& L, hipStream_t stream) {
     if (L.held)
-        return by_samples(all, sizeof(T), L.slabs, L, [&](const GroupNormArgs& A, uint32_t B) {
-#define VGC_LAUNCH(NV) hipLaunchKernelGGL((k_group_norm<T, NV>), dim3(B * L.slabs), dim3(L.threads), 0, stream, A)
-            if (L.rows_of_team <= 2u) VGC_LAUNCH(2);
-            else if (L.rows_of_team <= 4u) VGC_LAUNCH(4);
-            else if (L.rows_of_team <= 8u) VGC_LAUNCH(8);
-            else if constexpr (sizeof(T) == 2) VGC_LAUNCH(16);
+        return by_samples(all, sizeof(T), L, [&](const GroupNormArgs& A, uint32_t B) {
+#define VGC_LAUNCH(NV, THREADS) do { \
+            if (L.groups == 1u) hipLaunchKernelGGL((k_group_norm<T, NV, kOneGroup, THREADS>), dim3(B * L.slabs), dim3(L.threads), 0, stream, A); \
+            else if (by_lane(A)) hipLaunchKernelGGL((k_group_norm<T, NV, kByLane, THREADS>), dim3(B * L.slabs), dim3(L.threads), 0, stream, A); \
+            else hipLaunchKernelGGL((k_group_norm<T, NV, kByChannel, THREADS>), dim3(B * L.slabs), dim3(L.threads), 0, stream, A); } while (0)
+            if (L.rows_of_team <= 2u) VGC_LAUNCH(2, 1024);
+            else if (L.rows_of_team <= 4u) VGC_LAUNCH(4, 1024);
+            else if (sizeof(T) == 2 && L.threads == 1024u) VGC_LAUNCH(8, (sizeof(T) == 2 ? 1024 : 512));
+            else VGC_LAUNCH(8, 512);
 #undef VGC_LAUNCH
             return hip_check(hipGetLastError(), "launch k_group_norm");
         });
-    return by_samples(all, sizeof(T), std::max(L.blocks * L.chunks, all.G), L, [&](GroupNormArgs A, uint32_t B) {
+    return by_samples(all, sizeof(T), L, [&](GroupNormArgs A, uint32_t B) {
         const dim3 grid(B * L.blocks * L.chunks);
-        hipLaunchKernelGGL(k_group_norm_moments<T>, grid, dim3(256), 0, stream, A);
+        const bool whole = A.C % 8u == 0u;
+        if (whole) hipLaunchKernelGGL((k_group_norm_moments<T, true>), grid, dim3(256), 0, stream, A);
+        else hipLaunchKernelGGL((k_group_norm_moments<T, false>), grid, dim3(256), 0, stream, A);
         int rc = hip_check(hipGetLastError(), "launch k_group_norm_moments");
         if (rc != VGC_OK) return rc;
         hipLaunchKernelGGL(k_group_norm_join, dim3(B * A.G), dim3((uint64_t)L.chunks * A.w > 256u ? 256 : 64), 0, stream, A);
         if ((rc = hip_check(hipGetLastError(), "launch k_group_norm_join")) != VGC_OK) return rc;
         A.mean = A.mean_out;
         A.rstd = A.rstd_out;
-        hipLaunchKernelGGL(k_group_norm_apply<T>, grid, dim3(256), 0, stream, A);
+        if (by_lane(A)) hipLaunchKernelGGL((k_group_norm_apply<T, true, 1>), grid, dim3(256), 0, stream, A);
+        else if (whole) hipLaunchKernelGGL((k_group_norm_apply<T, true, 8>), grid, dim3(256), 0, stream, A);
+        else hipLaunchKernelGGL((k_group_norm_apply<T, false, 8>), grid, dim3(256), 0, stream, A);
         return hip_check(hipGetLastError(), "launch k_group_norm_apply");
     });
 }
 
 int launch_group_norm(int dtype, const void* x, uint32_t B, uint32_t P, uint32_t C, uint32_t G, const float* gamma, const float* beta, float eps, int act,
                       void* y, float* mean, float* rstd, void* workspace, hipStream_t stream) {
-    const GroupNormPlan L = group_norm_plan(B, P, C, G, most_rows(dtype, false));
+    const GroupNormPlan L = group_norm_plan(dtype, false, B, P, C, G);
     GroupNormArgs A = {};
     A.x = x; A.gamma = gamma; A.beta = beta; A.mean_out = mean; A.rstd_out = rstd; A.out = y;
     A.chunk_sums = static_cast<float*>(workspace);
     A.B = B; A.P = P; A.C = C; A.G = G; A.w = C / G; A.act = (uint32_t)act; A.eps = eps;
     place(A, L);
+    A.past = past_caches(y, C, (uint64_t)B * P * C * (dtype == VGC_F32 ? 4u : 2u) * 2u);
     return dtype == VGC_F32 ? launch_group_norm_of<float>(A, L, stream) : launch_group_norm_of<uint16_t>(A, L, stream);
 }
 
 template <typename T>
-static int launch_group_norm_backward_of(GroupNormArgs& all, const GroupNormPlan& L, hipStream_t stream) {
+static int launch_group_norm_backward_of(const GroupNormArgs& all, const GroupNormPlan& L, hipStream_t stream) {
     if (L.held)
-        return by_samples(all, sizeof(T), L.slabs, L, [&](const GroupNormArgs& A, uint32_t B) {
-#define VGC_LAUNCH(NV) hipLaunchKernelGGL((k_group_norm_backward<T, NV>), dim3(B * L.slabs), dim3(L.threads), 0, stream, A)
-            if (L.rows_of_team <= 2u) VGC_LAUNCH(2);
-            else if (L.rows_of_team <= 4u) VGC_LAUNCH(4);
-            else if constexpr (sizeof(T) == 2) VGC_LAUNCH(8);
+        return by_samples(all, sizeof(T), L, [&](const GroupNormArgs& A, uint32_t B) {
+            constexpr int kFew = sizeof(T) == 2 ? 4 : 2;
+#define VGC_LAUNCH(NV, THREADS, M) hipLaunchKernelGGL((k_group_norm_backward<T, NV, THREADS, M>), dim3(B * L.slabs), dim3(L.threads), 0, stream, A)
+#define VGC_ROWS(THREADS, M) do { if (L.rows_of_team <= kFew / 2) VGC_LAUNCH(kFew / 2, THREADS, M); else VGC_LAUNCH(kFew, THREADS, M); } while (0)
+            if (L.threads <= 512u) {
+                if (L.rows_of_team > (uint32_t)kFew) { if (by_lane(A)) VGC_LAUNCH(2 * kFew, 512, 1); else VGC_LAUNCH(2 * kFew, 512, 8); }
+                else if (by_lane(A)) VGC_ROWS(512, 1);
+                else VGC_ROWS(512, 8);
+            } else if (by_lane(A)) {
+                VGC_ROWS(1024, 1);
+            } else {
+                VGC_LAUNCH(kFew / 2, 1024, 8);
+            }
+#undef VGC_ROWS
 #undef VGC_LAUNCH
             return hip_check(hipGetLastError(), "launch k_group_norm_backward");
         });
-    return by_samples(all, sizeof(T), std::max(L.blocks * L.chunks, all.G), L, [&](const GroupNormArgs& A, uint32_t B) {
+    return by_samples(all, sizeof(T), L, [&](GroupNormArgs A, uint32_t B) {
         const dim3 grid(B * L.blocks * L.chunks);
-        hipLaunchKernelGGL((k_group_norm_backward_rows<T, true>), grid, dim3(256), 0, stream, A);
+#define VGC_LAUNCH(SUMS) do { \
+        if (by_lane(A)) hipLaunchKernelGGL((k_group_norm_backward_rows<T, true, 1, SUMS>), grid, dim3(256), 0, stream, A); \
+        else if (A.C % 8u == 0u) hipLaunchKernelGGL((k_group_norm_backward_rows<T, true, 8, SUMS>), grid, dim3(256), 0, stream, A); \
+        else hipLaunchKernelGGL((k_group_norm_backward_rows<T, false, 8, SUMS>), grid, dim3(256), 0, stream, A); } while (0)
+        VGC_LAUNCH(true);
         int rc = hip_check(hipGetLastError(), "launch k_group_norm_backward_rows");
         if (rc != VGC_OK) return rc;
         hipLaunchKernelGGL(k_group_norm_backward_join, dim3(B * A.G), dim3(256), 0, stream, A);
         if ((rc = hip_check(hipGetLastError(), "launch k_group_norm_backward_join")) != VGC_OK) return rc;
-        hipLaunchKernelGGL((k_group_norm_backward_rows<T, false>), grid, dim3(256), 0, stream, A);
+        VGC_LAUNCH(false);
+#undef VGC_LAUNCH
         return hip_check(hipGetLastError(), "launch k_group_norm_backward_rows");
     });
 }
@@ -635,7 +671,7 @@ static int launch_group_norm_backward_of(GroupNormArgs& all, const GroupNormPlan
 int launch_group_norm_backward(int dtype, const void* dy, const void* x, const float* mean, const float* rstd, const float* gamma, const float* beta,
                                int act, uint32_t B, uint32_t P, uint32_t C, uint32_t G, float c, void* dx, float* g_gamma, float* s_gamma, float* g_beta,
                                float* s_beta, void* workspace, hipStream_t stream) {
-    const GroupNormPlan L = group_norm_plan(B, P, C, G, most_rows(dtype, true));
+    const GroupNormPlan L = group_norm_plan(dtype, true, B, P, C, G);
     const GroupNormSpace S = group_norm_space(L, B, C, G, true);
     char* ws = static_cast<char*>(workspace);
     GroupNormArgs A = {};
@@ -645,6 +681,7 @@ int launch_group_norm_backward(int dtype, const void* dy, const void* x, const f
     if (!L.held) A.group_sums = (float*)(ws + S.group_sums);
     A.B = B; A.P = P; A.C = C; A.G = G; A.w = C / G; A.act = (uint32_t)act;
     place(A, L);
+    A.past = past_caches(dx, C, (uint64_t)B * P * C * (dtype == VGC_F32 ? 4u : 2u) * 3u);
     const int rc = dtype == VGC_F32 ? launch_group_norm_backward_of<float>(A, L, stream) : launch_group_norm_backward_of<uint16_t>(A, L, stream);
     if (rc != VGC_OK) return rc;
     return launch_column_sums(A.sums, 2, 0, B, 1, C, false, c, g_gamma, s_gamma, g_beta, s_beta, stream);

@@ -30,18 +30,6 @@ struct Finish {
     Dropout drop;
     bool past;                // results are stored past the caches
 };
-typedef uint32_t whole_u4 __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ void store8_past(uint16_t* p, const float (&f)[8]) {
-    whole_u4 v;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = two_bf16(f[2 * i], f[2 * i + 1]);
-    __builtin_nontemporal_store(v, reinterpret_cast<whole_u4*>(p));
-}
-__device__ __forceinline__ void store8_past(float* p, const float (&f)[8]) {
-    const f4v a = {f[0], f[1], f[2], f[3]}, b = {f[4], f[5], f[6], f[7]};
-    __builtin_nontemporal_store(a, reinterpret_cast<f4v*>(p));
-    __builtin_nontemporal_store(b, reinterpret_cast<f4v*>(p + 4));
-}
 template <typename T>
 __device__ __forceinline__ void finish(const Finish& F, const DropoutKey& key, uint32_t row, uint32_t col, int n, const float (&bias)[8], float (&f)[8]) {
     const size_t at = (size_t)row * F.M + col;
@@ -49,7 +37,7 @@ __device__ __forceinline__ void finish(const Finish& F, const DropoutKey& key, u
     if (F.residual) r = load8(static_cast<const T*>(F.residual) + at, n);
 #pragma unroll
     for (int k = 0; k < 8; ++k) f[k] += bias[k];
-    if (F.z) { if (F.past) store8_past(static_cast<T*>(F.z) + at, f); else store8(static_cast<T*>(F.z) + at, f, n); }
+    if (F.z) store8_to(static_cast<T*>(F.z) + at, f, n, F.past);
     apply_act(F.act, f);
     apply_dropout(F.drop, key, row, col / 8u, f);
     if (F.residual) {
@@ -58,8 +46,7 @@ __device__ __forceinline__ void finish(const Finish& F, const DropoutKey& key, u
 #pragma unroll
         for (int k = 0; k < 8; ++k) f[k] += g[k];
     }
-    if (F.past) store8_past(static_cast<T*>(F.y) + at, f);
-    else store8(static_cast<T*>(F.y) + at, f, n);
+    store8_to(static_cast<T*>(F.y) + at, f, n, F.past);
 }
 __device__ __forceinline__ void bias_of(const Finish& F, uint32_t col, float (&bias)[8]) {
     const int n = (int)F.M - (int)col;
@@ -364,10 +351,10 @@ struct SlopeArgs {
     int act;
     Dropout drop;
 };
-template <typename T>
+template <typename T, bool kWhole, bool kZ>
 __global__ __launch_bounds__(256) void k_linear_slope(SlopeArgs A) {
-    constexpr int kRows = 4;
-    __shared__ float sh[2048], part[256], chan[256];
+    constexpr int kRows = sizeof(T) == 2 ? 4 : 2;
+    __shared__ float sh[4096], part[512], chan[2][256];
     const uint32_t teams = 256u / A.lanes, team = threadIdx.x / A.lanes, block = blockIdx.x % A.blocks, group = blockIdx.x / A.blocks;
     const uint32_t c0 = (block * A.lanes + threadIdx.x % A.lanes) * 8u;
     const int n = (int)A.C - (int)c0;
@@ -385,35 +372,18 @@ __global__ __launch_bounds__(256) void k_linear_slope(SlopeArgs A) {
         step = teams;
     }
     const DropoutKey key = dropout_key(A.drop);
-    Raw8<T> rd[kRows], rz[kRows];
-    auto request = [&](uint32_t r0) {
-#pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            const uint32_t r = r0 + i * step;
-            const int m = r < end ? n : 0;
-            rd[i] = load8(static_cast<const T*>(A.dy) + (size_t)r * A.C + c0, m, rows_at_end(r, N));
-            if (A.z) rz[i] = load8(static_cast<const T*>(A.z) + (size_t)r * A.C + c0, m, rows_at_end(r, N));
-        }
-    };
     float h[8] = {}, g[8] = {}, s[8] = {};
     uint32_t left = A.P;
-    request(row);
-    for (; row < end; row += kRows * step) {
-        Raw8<T> nd[kRows], nz[kRows];
-#pragma unroll
-        for (int i = 0; i < kRows; ++i) { nd[i] = rd[i]; nz[i] = rz[i]; }
-        if (row + kRows * step < end) request(row + kRows * step);
-#pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            const uint32_t r = row + i * step;
-            if (r >= end) continue;
-            float d[8], z[8];
-            clip8(nd[i], n);
-            widen8(nd[i], d);
+    if (row < end) {
+        RowStream<T, kWhole, kRows, kZ ? 2 : 1> X(static_cast<const T*>(A.dy), static_cast<const T*>(A.z), A.C, c0, row, end, step, N);
+        X.begin();
+        X.each([&](uint32_t r, const Raw8<T> (&in)[kZ ? 2 : 1]) {
+            float d[8];
+            widen8(in[0], d);
             apply_dropout(A.drop, key, r, c0 / 8u, d);
-            if (A.z) {
-                clip8(nz[i], n);
-                widen8(nz[i], z);
+            if constexpr (kZ) {
+                float z[8];
+                widen8(in[1], z);
                 apply_slope(A.act, z, d);
             }
 #pragma unroll
@@ -423,18 +393,19 @@ __global__ __launch_bounds__(256) void k_linear_slope(SlopeArgs A) {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) { g[k] += h[k]; s[k] = __builtin_fmaf(h[k], h[k], s[k]); h[k] = 0.f; }
             }
-            if (n > 0) store8(static_cast<T*>(A.dz) + (size_t)r * A.C + c0, d, n);
-            if (A.rest && n > 0) {
-                float left[8];
+            if (n <= 0) return;
+            store8(static_cast<T*>(A.dz) + (size_t)r * A.C + c0, d, n);
+            if (A.rest) {
+                float left_of[8];
 #pragma unroll
                 for (int k = 0; k < 8; k += 2) {
                     const uint32_t x = two_bf16(d[k], d[k + 1]);
-                    left[k] = d[k] - __uint_as_float(x << 16);
-                    left[k + 1] = d[k + 1] - __uint_as_float(x & 0xFFFF0000u);
+                    left_of[k] = d[k] - __uint_as_float(x << 16);
+                    left_of[k + 1] = d[k + 1] - __uint_as_float(x & 0xFFFF0000u);
                 }
-                store8(static_cast<T*>(A.rest) + (size_t)r * A.C + c0, left, n);
+                store8(static_cast<T*>(A.rest) + (size_t)r * A.C + c0, left_of, n);
             }
-            if (A.planes && n > 0) {
+            if (A.planes) {
                 const size_t plane = (size_t)N * A.ldp;
                 for (uint32_t q = 0; q < A.count; ++q) {
                     any_u4 x;
@@ -443,27 +414,28 @@ __global__ __launch_bounds__(256) void k_linear_slope(SlopeArgs A) {
                     *reinterpret_cast<any_u4*>(A.planes + q * plane + (size_t)r * A.ldp + c0) = x;
                 }
             }
-        }
+        });
     }
     if (!A.partial) return;
     const uint32_t c = block * A.lanes * 8u + threadIdx.x;
     const bool mine = threadIdx.x < A.lanes * 8u && c < A.C;
     float* out = A.partial + (size_t)group * (A.whole ? 2u : 1u) * A.C + c;
     if (!A.whole) {
-        channel_sums(h, A.lanes, sh, part, chan);
-        if (mine) out[0] = chan[threadIdx.x];
+        const float v[1][8] = {{h[0], h[1], h[2], h[3], h[4], h[5], h[6], h[7]}};
+        channel_sums<1>(v, A.lanes, sh, part, chan[0]);
+        if (mine) out[0] = chan[0][threadIdx.x];
         return;
     }
-    channel_sums(g, A.lanes, sh, part, chan);
-    if (mine) out[0] = chan[threadIdx.x];
-    __syncthreads();
-    channel_sums(s, A.lanes, sh, part, chan);
-    if (mine) out[A.C] = chan[threadIdx.x];
+    const float v[2][8] = {{g[0], g[1], g[2], g[3], g[4], g[5], g[6], g[7]}, {s[0], s[1], s[2], s[3], s[4], s[5], s[6], s[7]}};
+    channel_sums<2>(v, A.lanes, sh, part, chan[0], chan[1]);
+    if (!mine) return;
+    out[0] = chan[0][threadIdx.x];
+    out[A.C] = chan[1][threadIdx.x];
 }
 
 // ---- launches -----------------------------------------------------------------------------------------------------------------
 //               BM   BN   WM  WN BK S PA PB
-typedef TileShape<256, 256, 128, 64, 64, 2, 1, 1> Large;     // bfloat16
+typedef TileShape<256, 256, 64, 128, 64, 2, 1, 1> Large;     // bfloat16 (with 128 x 64 a wave 16384 x 2048 x 8192 462 us, so 448; k in steps of 32 the same)
 typedef TileShape<128, 128, 64, 64, 64, 2, 1, 1> Small;      // two workgroups a compute unit
 typedef TileShape<128, 128, 64, 32, 64, 4, 1, 1> Deep;       // one: what two would hide of each other's waits, four stages and two waves a SIMD have to
 typedef TileShape<128, 128, 64, 32, 64, 3, 1, 2> Small2;     // dX from two planes of dz
@@ -508,7 +480,7 @@ static ProductPlan product_plan(int dtype, uint32_t N, uint32_t M, uint32_t K, u
         }
         return L;
     }
-    // bfloat16 (us): 16384 x 2048 x 8192 by large tiles 460, small 566; 4096 x 4096 x 4096 116 and 148; 4096 x 1024 x 1024 27 and 16, 2048 x 2048 x 2048 50 and 31.
+    // bfloat16 (us): 16384 x 2048 x 8192 by large tiles 448, small 566; 4096 x 4096 x 4096 113 and 148; 4096 x 1024 x 1024 27 and 16, 2048 x 2048 x 2048 50 and 31.
     // Small ones of which a compute unit has one: 2048 x 2048 x 2048 31.0, deep 24.0; 4096 x 4096 x 1024 57.9 and 42.9; two: 8192 x 1024 x 1024 26.7 and 30.6.
     const uint64_t large = tiles(M, 256, N, 256), small = tiles(M, 128, N, 128);
     L.tile = dtype == VGC_F32 ? Tile::kCut : planes_b == 2u ? Tile::kSmall2 : large >= 192u ? Tile::kLarge : small > 256u ? Tile::kSmall : Tile::kDeep;
@@ -523,9 +495,9 @@ static ProductPlan product_plan(int dtype, uint32_t N, uint32_t M, uint32_t K, u
     return L;
 }
 
-// Results of whole aligned pieces, too large to be found in the caches again.
-static bool past(int dtype, uint32_t N, uint32_t M, const void* z, const void* y) {
-    return M % 8u == 0u && (((uintptr_t)z | (uintptr_t)y) & 15u) == 0u && (uint64_t)N * M * (dtype == VGC_F32 ? 4u : 2u) * (z ? 2u : 1u) > (192ull << 20);
+static bool past(int dtype, uint32_t N, uint32_t M, uint32_t K, const void* z, const void* y) {
+    const uint64_t bytes = ((uint64_t)N * M * (z ? 2u : 1u) + (uint64_t)N * K + (uint64_t)K * M) * (dtype == VGC_F32 ? 4u : 2u);
+    return past_caches(y, M, bytes) && (!z || past_caches(z, M, bytes));
 }
 template <typename T>
 static int launch_join(const Finish& F, uint32_t splits, float* parts, hipStream_t stream) {
@@ -591,7 +563,7 @@ int launch_linear(const LinearCall& q, void* workspace, hipStream_t stream) {
     const LinearPlan L = linear_plan(q.dtype, N, q.K, q.C);
     char* ws = static_cast<char*>(workspace);
     uint16_t *x = (uint16_t*)(ws + L.x), *w = (uint16_t*)(ws + L.w);
-    const Finish F = {q.bias, q.residual, q.z, q.y, N, q.C, q.act, dropout_of(q.p, q.rng), past(q.dtype, N, q.C, q.z, q.y)};
+    const Finish F = {q.bias, q.residual, q.z, q.y, N, q.C, q.act, dropout_of(q.p, q.rng), past(q.dtype, N, q.C, q.K, q.z, q.y)};
     int rc;
     if (L.product.tile == Tile::kThin) {
         if (q.dtype == VGC_F32) return launch_thin<float, true, false>(L.product, ThinArgs<float>{(const float*)q.W, (const float*)q.X, nullptr, q.K, 1, nullptr, F}, (float*)(ws + L.parts), stream);
@@ -649,13 +621,16 @@ int launch_linear_backward(const LinearCall& q, void* workspace, hipStream_t str
     SlopeArgs S = {q.dy, q.act == VGC_ACT_NONE ? nullptr : q.z_in, q.dz, q.dX && L.rest ? planes : nullptr, copy ? planes : nullptr, L.Cp, L.planes, q.s_bias ? (float*)(ws + L.partial) : nullptr,
                    q.B, q.P, q.C, L.lanes, L.blocks, L.samples_parts, L.groups, L.whole, q.act, dropout_of(q.p, q.rng)};
     const dim3 grid(L.groups * L.blocks);
-    if (q.dtype == VGC_F32) hipLaunchKernelGGL(k_linear_slope<float>, grid, dim3(256), 0, stream, S);
-    else hipLaunchKernelGGL(k_linear_slope<uint16_t>, grid, dim3(256), 0, stream, S);
+#define VGC_LAUNCH(T, WHOLE) do { if (S.z) hipLaunchKernelGGL((k_linear_slope<T, WHOLE, true>), grid, dim3(256), 0, stream, S); \
+        else hipLaunchKernelGGL((k_linear_slope<T, WHOLE, false>), grid, dim3(256), 0, stream, S); } while (0)
+    if (q.dtype == VGC_F32) { if (q.C % 8u == 0u) VGC_LAUNCH(float, true); else VGC_LAUNCH(float, false); }
+    else { if (q.C % 8u == 0u) VGC_LAUNCH(uint16_t, true); else VGC_LAUNCH(uint16_t, false); }
+#undef VGC_LAUNCH
     int rc = hip_check(hipGetLastError(), "launch k_linear_slope");
     if (rc != VGC_OK) return rc;
     if (q.s_bias && (rc = launch_column_sums(S.partial, 1, L.groups, q.B, L.samples_parts, q.C, L.whole, q.c, q.g_bias, q.s_bias, nullptr, nullptr, stream)) != VGC_OK) return rc;
     if (!q.dX) return VGC_OK;
-    const Finish F = {nullptr, q.residual, nullptr, q.dX, N, q.K, VGC_ACT_NONE, Dropout{nullptr, 0u, 0.f}, past(q.dtype, N, q.K, nullptr, q.dX)};
+    const Finish F = {nullptr, q.residual, nullptr, q.dX, N, q.K, VGC_ACT_NONE, Dropout{nullptr, 0u, 0.f}, past(q.dtype, N, q.K, q.C, nullptr, q.dX)};
     if (L.product.tile == Tile::kThin) {
         if (q.dtype == VGC_F32) return launch_thin<float, false, false>(L.product, ThinArgs<float>{(const float*)q.W, (const float*)q.dz, nullptr, q.C, 1, nullptr, F}, (float*)(ws + L.parts), stream);
         const ThinArgs<uint16_t> T = {(const uint16_t*)q.W, (const uint16_t*)q.dz, planes, q.C, 1, nullptr, F};
