@@ -370,11 +370,12 @@ __device__ __forceinline__ double wave_sum_double(double x) {
 }
 
 // A group's moments from those of its channels and chunks; in 64 bits, so that mean^2 may be subtracted.
-__global__ __launch_bounds__(256) void k_group_norm_join(GroupNormArgs A) {
-    __shared__ double sh[2][4];
+__global__ __launch_bounds__(1024) void k_group_norm_join(GroupNormArgs A) {
+    __shared__ double sh[2][16];
     const uint32_t b = blockIdx.x / A.G, q = blockIdx.x - b * A.G, lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
     const float* in = A.chunk_sums + (uint64_t)b * A.chunks * 2u * A.C + q * A.w;
     double s1 = 0., s2 = 0.;
+#pragma unroll 4
     for (uint32_t e = threadIdx.x; e < A.chunks * A.w; e += blockDim.x) {
         const uint32_t chunk = e / A.w, c = e - chunk * A.w;
         const double m = (double)(min((chunk + 1u) * A.rows, A.P) - chunk * A.rows), mean = in[(uint64_t)chunk * 2u * A.C + c];
@@ -457,13 +458,14 @@ __global__ __launch_bounds__(256) void k_group_norm_backward_rows(GroupNormArgs 
     sums[A.C + c] = chan[1][threadIdx.x];
 }
 
-// G_z and H_z of a group's channels from their chunks, and the group's two sums.
-__global__ __launch_bounds__(256) void k_group_norm_backward_join(GroupNormArgs A) {
-    __shared__ float sh[2][256], total[2][4];
-    const uint32_t b = blockIdx.x / A.G, q = blockIdx.x - b * A.G;
+// G_z and H_z of a group's channels from their chunks, and the group's two sums.  Threads: up to 64 channels, the others share their chunks; a thread adds every
+// `subs`th in turn, then the channel's first its fellows' sums.
+__global__ __launch_bounds__(1024) void k_group_norm_backward_join(GroupNormArgs A) {
+    __shared__ float sh[2][1024], total[2][16];
+    const uint32_t b = blockIdx.x / A.G, q = blockIdx.x - b * A.G, threads = blockDim.x;
     uint32_t wp = 1;
-    while (wp < A.w && wp < 256u) wp *= 2u;
-    const uint32_t ch = threadIdx.x % wp, sub = threadIdx.x / wp, subs = 256u / wp;
+    while (wp < A.w && wp < 64u) wp *= 2u;
+    const uint32_t ch = threadIdx.x % wp, sub = threadIdx.x / wp, subs = threads / wp;
     float m1 = 0.f, m2 = 0.f;
     for (uint32_t c0 = 0; c0 < A.w; c0 += wp) {
         const uint32_t c = c0 + ch, col = q * A.w + c;
@@ -476,8 +478,18 @@ __global__ __launch_bounds__(256) void k_group_norm_backward_join(GroupNormArgs 
         sh[0][threadIdx.x] = g;
         sh[1][threadIdx.x] = h;
         __syncthreads();
+        for (uint32_t n = subs; n > 1u;) {                   // (subs: a power of two)
+            const uint32_t half = n / 2u;
+            if (sub < half) {
+                sh[0][threadIdx.x] += sh[0][threadIdx.x + half * wp];
+                sh[1][threadIdx.x] += sh[1][threadIdx.x + half * wp];
+            }
+            __syncthreads();
+            n = half;
+        }
         if (sub == 0u && c < A.w) {
-            for (uint32_t s = 1; s < subs; ++s) { g += sh[0][s * wp + ch]; h += sh[1][s * wp + ch]; }
+            g = sh[0][threadIdx.x];
+            h = sh[1][threadIdx.x];
             A.sums[(uint64_t)b * 2u * A.C + col] = g;
             A.sums[((uint64_t)b * 2u + 1u) * A.C + col] = h;
             const float gamma = A.gamma[col];
@@ -491,8 +503,9 @@ __global__ __launch_bounds__(256) void k_group_norm_backward_join(GroupNormArgs 
     if ((threadIdx.x & 63u) == 0u) { total[0][threadIdx.x >> 6] = m1; total[1][threadIdx.x >> 6] = m2; }
     __syncthreads();
     if (threadIdx.x >= 2u) return;
-    const float inv = 1.0f / ((float)A.P * (float)A.w);
-    A.group_sums[(uint64_t)blockIdx.x * 2u + threadIdx.x] = (total[threadIdx.x][0] + total[threadIdx.x][1] + total[threadIdx.x][2] + total[threadIdx.x][3]) * inv;
+    float sum = 0.f;
+    for (uint32_t v = 0; v < threads / 64u; ++v) sum += total[threadIdx.x][v];
+    A.group_sums[(uint64_t)blockIdx.x * 2u + threadIdx.x] = sum * (1.0f / ((float)A.P * (float)A.w));
 }
 
 // ---- launches -----------------------------------------------------------------------------------------------------------------
@@ -531,7 +544,7 @@ static GroupNormPlan group_norm_plan(int dtype, bool backward, uint32_t B, uint3
     const uint32_t times = (uint32_t)((B + most_samples - 1u) / most_samples);
     L.samples = std::min((B + times - 1u) / times, std::max(1u, (1u << 22) / std::max(L.blocks, G)));
     const uint64_t want = std::max<uint64_t>(1, kGroups / std::max<uint64_t>(1, (uint64_t)L.samples * L.blocks));
-    L.chunks = (uint32_t)std::min<uint64_t>(want, (P + teams * 8u - 1u) / (teams * 8u));
+    L.chunks = (uint32_t)std::min<uint64_t>(std::min<uint64_t>(want, 256u), (P + teams * 8u - 1u) / (teams * 8u));      // (256: of which a group's join has to read all)
     const uint32_t batch = teams * (dtype == VGC_F32 ? 2u : 4u) * (backward ? 1u : 2u);      // (whole batches but for the sample's last)
     L.rows = std::min(P, ((P + L.chunks - 1u) / L.chunks + batch / 2u) / batch * batch);
     if (L.rows == 0u) L.rows = std::min(P, batch);
@@ -583,6 +596,11 @@ static void place(GroupNormArgs& A, const GroupNormPlan& L) {
     A.lanes = L.lanes; A.blocks = L.blocks; A.chunks = L.chunks; A.rows = L.rows; A.groups = L.groups; A.slabs = L.slabs;
 }
 
+// Threads that join a group's chunks: four entries each.
+static uint32_t join_threads(const GroupNormPlan& L, uint32_t w) {
+    const uint64_t entries = (uint64_t)L.chunks * w;
+    return entries <= 256u ? 64u : entries <= 1024u ? 256u : 1024u;
+}
 // Whether a lane's eight channels belong to one group wherever its piece lies.
 static bool by_lane(const GroupNormArgs& A) { return A.w % 8u == 0u; }
 
@@ -608,7 +626,7 @@ static int launch_group_norm_of(const GroupNormArgs& all, const GroupNormPlan& L
         else hipLaunchKernelGGL((k_group_norm_moments<T, false>), grid, dim3(256), 0, stream, A);
         int rc = hip_check(hipGetLastError(), "launch k_group_norm_moments");
         if (rc != VGC_OK) return rc;
-        hipLaunchKernelGGL(k_group_norm_join, dim3(B * A.G), dim3((uint64_t)L.chunks * A.w > 256u ? 256 : 64), 0, stream, A);
+        hipLaunchKernelGGL(k_group_norm_join, dim3(B * A.G), dim3(join_threads(L, A.w)), 0, stream, A);
         if ((rc = hip_check(hipGetLastError(), "launch k_group_norm_join")) != VGC_OK) return rc;
         A.mean = A.mean_out;
         A.rstd = A.rstd_out;
@@ -660,7 +678,7 @@ static int launch_group_norm_backward_of(const GroupNormArgs& all, const GroupNo
         VGC_LAUNCH(true);
         int rc = hip_check(hipGetLastError(), "launch k_group_norm_backward_rows");
         if (rc != VGC_OK) return rc;
-        hipLaunchKernelGGL(k_group_norm_backward_join, dim3(B * A.G), dim3(256), 0, stream, A);
+        hipLaunchKernelGGL(k_group_norm_backward_join, dim3(B * A.G), dim3(join_threads(L, A.w)), 0, stream, A);
         if ((rc = hip_check(hipGetLastError(), "launch k_group_norm_backward_join")) != VGC_OK) return rc;
         VGC_LAUNCH(false);
 #undef VGC_LAUNCH

@@ -157,7 +157,7 @@ __global__ __launch_bounds__(256) void k_linear_join(Finish F, uint32_t splits, 
 constexpr uint32_t kThinWaves = 16;
 template <typename T> struct ThinArgs {
     const T *a, *b, *rest;    // W; the rows of X or dz, and (backward, bfloat16) what rounding left of dz
-    uint32_t K, splits;
+    uint32_t lda, ldb, K, splits;
     float* parts;             // [split][N][M] where k is shared out over workgroups too
     Finish F;
 };
@@ -217,7 +217,7 @@ __global__ __launch_bounds__(kThinWaves * 64) void k_linear_thin(ThinArgs<T> A) 
     const T *b[NT], *rest[NT], *a[kMixed ? 1 : kV];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-        const size_t at = (size_t)min(n0 + t * 16u + l16, A.F.N - 1u) * K;
+        const size_t at = (size_t)min(n0 + t * 16u + l16, A.F.N - 1u) * A.ldb;
         b[t] = A.b + at;
         if constexpr (kRest) rest[t] = A.rest + at;
     }
@@ -225,7 +225,7 @@ __global__ __launch_bounds__(kThinWaves * 64) void k_linear_thin(ThinArgs<T> A) 
         a[0] = A.a + min(m0 + l16 * kV, M - (uint32_t)kV);
     } else {
 #pragma unroll
-        for (int j = 0; j < kV; ++j) a[j] = A.a + (size_t)min(m0 + j * 16u + l16, M - 1u) * K;
+        for (int j = 0; j < kV; ++j) a[j] = A.a + (size_t)min(m0 + j * 16u + l16, M - 1u) * A.lda;
     }
     auto request = [&](uint32_t k0) -> Step {
         Step S;
@@ -237,7 +237,7 @@ __global__ __launch_bounds__(kThinWaves * 64) void k_linear_thin(ThinArgs<T> A) 
         }
         if constexpr (kMixed) {
 #pragma unroll
-            for (uint32_t t = 0; t < kK; ++t) S.c[t].load(a[0] + (size_t)(k + t) * M);
+            for (uint32_t t = 0; t < kK; ++t) S.c[t].load(a[0] + (size_t)(k + t) * A.lda);
         } else {
 #pragma unroll
             for (int j = 0; j < kV; ++j) S.w[j].load(a[j] + k);
@@ -445,52 +445,49 @@ static uint32_t up8(uint32_t x) { return (x + 7u) / 8u * 8u; }
 static uint64_t tiles(uint32_t a, uint32_t ta, uint32_t b, uint32_t tb) { return (uint64_t)((a + ta - 1) / ta) * ((b + tb - 1) / tb); }
 
 enum class Tile { kLarge, kSmall, kSmall2, kCut, kThin, kDeep };
-// Few rows, or little work (us of a forward call, thin and by tiles: bfloat16, 256 x 2048 x 2048: 11.5 and 15.9, 1024 x 1024 x 1024: 14.6 and 14.6, 512 x 2048 x 2048:
-// 21.4 and 20.4, 64 x 4096 x 4096: 19.3 and 17.2, 16 x 4096 x 4096: 12.9 and 15.2; float32, 1024 x 1024 x 1024: 35.0 and 37.0, 2048 x 512 x 2048: 64.6 and 54.9, but
-// 128 x 4096 x 4096: 61.5 and 71.1).
-static bool is_thin(int dtype, uint32_t N, uint32_t M, uint32_t K) {
-    if (K < (dtype == VGC_F32 ? 4u : 8u) || M < 4u) return false;       // (what a place past an edge is moved back by)
-    const uint64_t work = (uint64_t)N * M * K;
-    return N <= 16u || work < (1ull << 30) || (dtype == VGC_F32 && N <= 128u && work <= (1ull << 31));
-}
-// How a product [N, M] over K is formed.
+// How a product [N, M] over K is formed: the cheapest of its forms by what they take on this card, in us (the kernels, not the call).
+//   thin    workgroups in turn on 256 compute units, 3 us each and its operands' rows at 41 GB/s, where rows of x, of which a load takes 64 bytes, count twice.  (estimate and
+//           measured, bfloat16: 1 x 4096 x 4096 in 64 columns, four parts of k 13.8 and 11.6, whole 22 and 20; 256 x 2048 x 2048 15.8 and 11.5; 1024^3 19 and 14.6; float32: 1024^3 38 and 35,
+//           128 x 4096 x 4096 54 and 61, 2048 x 512 x 2048 75 and 65)
+//   tiles   in turn too: of 128 x 128 and 64 k bfloat16 0.55 us a step, from two planes of dz 0.9; of 256 x 128 and 32 k float32 2.6, after its operands were laid out.  (2048^3 20 and 24;
+//           512 x 4096 x 4096 in two parts 32 and 33; float32: 4096^3 758 and 663, 2048 x 512 x 2048 57 and 55)
+// A long k is shared out, in thin or by tiles, where that gives idle compute units work: the second kernel that adds the parts takes 6 us and their way through memory.
+// Rows of an odd number of bfloat16 are laid out at whole pieces first: a load at an odd element takes three times as long (129 x 1331 from 4513: 90 us, from 4512 27).
 struct ProductPlan { Tile tile; uint32_t splits, v, t; size_t parts; };    // thin: kV and NT
-static ProductPlan product_plan(int dtype, uint32_t N, uint32_t M, uint32_t K, uint32_t planes_b) {
-    ProductPlan L = {};
-    L.splits = 1;
-    if (is_thin(dtype, N, M, K)) {
-        L.tile = Tile::kThin;
-        // The largest part of the output that still gives every compute unit a workgroup (float32, 64 x 2048 x 2048: 32 columns by 16 rows 12.2, by 32 19.7;
-        // 256 x 1024 x 1024: 64 by 16 10.5, 32 by 32 11.7).  Rows of W of 128 bytes a workgroup at least while there are several steps of k: a compute unit takes some 31 GB/s
-        // of whole lines, and of halves no more, so a long k is shared out over workgroups (1 x 4096 x 4096 bfloat16, 64 columns: one 20.0, two 15.3, four
-        // 11.6, eight 14.1; 8192 x 2048: one 35.5, four 15.1, eight 12.6; but 2048 x 2048: one 8.7, two 11.5).
-        const struct { uint32_t v, t; } shapes[] = {{4, 2}, {4, 1}, {2, 2}, {2, 1}, {1, 1}};
-        const uint32_t least = dtype == VGC_F32 ? 1u : 2u, line = dtype == VGC_F32 ? 2u : 4u;
-        const bool deep = K > 2048u && N <= 64u;
-        for (const auto& q : shapes) {
-            if (q.v < least || (deep && q.v < line) || (q.t == 2u && N <= 16u)) continue;
-            L.v = q.v;
-            L.t = q.t;
-            if (tiles(M, 16u * q.v, N, 16u * q.t) >= 256u) break;
+static double rounds(uint64_t groups) { return (double)((groups + 255u) / 256u); }
+static double join_us(uint32_t splits, uint32_t N, uint32_t M) { return splits == 1u ? 0. : 6. + (double)splits * N * M * 4e-6 / 3.; }
+static double layout_us(double elements) { return 4. + elements * 2.5e-6; }
+static double thin_plan(int dtype, uint32_t N, uint32_t M, uint32_t K, uint32_t planes_b, ProductPlan& best) {
+    const bool f32 = dtype == VGC_F32;
+    const struct { uint32_t v, t; } shapes[] = {{4, 2}, {4, 1}, {2, 2}, {2, 1}, {1, 1}};
+    double least = 1e30;
+    for (const auto& q : shapes) {
+        if ((q.v < 2u && !f32) || (q.t == 2u && N <= 16u)) continue;
+        const uint64_t n = tiles(M, 16u * q.v, N, 16u * q.t);
+        for (uint32_t splits = 1; splits <= 16u && (splits == 1u || (K / splits >= 512u && n * splits <= 512u)); splits *= 2u) {
+            const double us = rounds(n * splits) * (3. + (double)K / splits * (q.v + 2u * q.t * (f32 ? 1u : planes_b)) * (f32 ? 64. : 32.) / 41e3) + join_us(splits, N, M);
+            if (us < least) { least = us; best = ProductPlan{Tile::kThin, splits, q.v, q.t, 0}; }
         }
-        if (deep) {
-            const uint64_t n = tiles(M, 16u * L.v, N, 16u * L.t);
-            L.splits = (uint32_t)std::min<uint64_t>((256u + n - 1u) / n, K / 1024u);
-            L.parts = L.splits > 1u ? (size_t)L.splits * N * M * sizeof(float) : 0;
-        }
-        return L;
     }
-    // bfloat16 (us): 16384 x 2048 x 8192 by large tiles 448, small 566; 4096 x 4096 x 4096 113 and 148; 4096 x 1024 x 1024 27 and 16, 2048 x 2048 x 2048 50 and 31.
-    // Small ones of which a compute unit has one: 2048 x 2048 x 2048 31.0, deep 24.0; 4096 x 4096 x 1024 57.9 and 42.9; two: 8192 x 1024 x 1024 26.7 and 30.6.
+    if (!f32 && K % 2u) least += layout_us((double)N * K * (planes_b == 2u ? 0. : 1.));
+    return least;
+}
+static ProductPlan product_plan(int dtype, uint32_t N, uint32_t M, uint32_t K, uint32_t planes_b, bool odd_w) {
+    const bool f32 = dtype == VGC_F32;
+    // Large tiles from 192 of them on, two small ones a compute unit, or one that is deep.  (us: 16384 x 2048 x 8192 by large tiles 448, small 566; 4096^3 113 and 148; 4096 x 1024 x 1024
+    // 27 and 16; 2048^3 small 31, deep 24; 4096 x 4096 x 1024 58 and 43; 8192 x 1024 x 1024 27 and 31)
     const uint64_t large = tiles(M, 256, N, 256), small = tiles(M, 128, N, 128);
-    L.tile = dtype == VGC_F32 ? Tile::kCut : planes_b == 2u ? Tile::kSmall2 : large >= 192u ? Tile::kLarge : small > 256u ? Tile::kSmall : Tile::kDeep;
-    const uint64_t n = L.tile == Tile::kLarge ? large : L.tile == Tile::kCut ? tiles(M, 256, N, 128) : small;
-    // A long k in parts where that gives idle compute units work: a second kernel and the parts' way through memory have to be paid by it (us, in one, two, four, eight
-    // parts by small tiles: 128 x 4096 x 4096 57, 35, 23.8, 21.1; 512 x 4096 x 4096 deep 39.5 whole, small in four 37.2, but 512 x 2048 x 2048 17.4 and 21.8; float32
-    // 2048 x 2048 x 2048 129 and 114).
-    const uint32_t least = dtype == VGC_F32 ? 256u : 512u;
-    if (dtype == VGC_F32 || K > 2048u)
-        while (n * L.splits <= 128u && K / (L.splits * 2u) >= least && L.splits < 32u) L.splits *= 2u;
+    ProductPlan L = {f32 ? Tile::kCut : planes_b == 2u ? Tile::kSmall2 : large >= 192u ? Tile::kLarge : small > 256u ? Tile::kSmall : Tile::kDeep, 1, 0, 0, 0}, thin;
+    const uint64_t n = L.tile == Tile::kLarge ? large : f32 ? tiles(M, 256, N, 128) : small;
+    const double steps = (K + (f32 ? 31u : 63u)) / (f32 ? 32u : 64u), step = f32 ? 2.6 : planes_b == 2u ? 0.9 : 0.55;
+    auto by_tiles = [&](uint32_t splits) { return rounds(n * splits) * (2.5 + step * steps / splits) + join_us(splits, N, M); };
+    for (uint32_t splits = 2; splits <= 32u && K / splits >= 256u && n * splits <= 256u; splits *= 2u)
+        if (by_tiles(splits) < by_tiles(L.splits)) L.splits = splits;
+    double us = by_tiles(L.splits) + (f32 || odd_w || M % 8u ? layout_us((double)K * M) : 0.) + (f32 || K % 8u ? layout_us((double)N * K) : 0.);
+    if (K >= (f32 ? 4u : 8u) && M >= 4u) {                   // (what a place past an edge is moved back by)
+        const double by_thin = thin_plan(dtype, N, M, K, planes_b, thin) + (!f32 && odd_w ? layout_us((double)K * M) : 0.);
+        if (by_thin < us) L = thin;
+    }
     L.parts = L.splits > 1u ? (size_t)L.splits * N * M * sizeof(float) : 0;
     return L;
 }
@@ -542,12 +539,12 @@ static int launch_thin(const ProductPlan& L, ThinArgs<T> A, float* parts, hipStr
 struct LinearPlan { ProductPlan product; bool x_there, w_there; uint32_t Kp, Cp; size_t x, w, parts, total; };
 static LinearPlan linear_plan(int dtype, uint32_t N, uint32_t K, uint32_t C) {
     LinearPlan L;
-    L.product = product_plan(dtype, N, C, K, 1);
+    L.product = product_plan(dtype, N, C, K, 1, C % 2u != 0u);
     L.Kp = up8(K);
     L.Cp = up8(C);
     const bool thin = L.product.tile == Tile::kThin;
-    L.x_there = thin || (dtype == VGC_BF16 && K % 8u == 0u);
-    L.w_there = thin || (dtype == VGC_BF16 && C % 8u == 0u);
+    L.x_there = (thin && dtype == VGC_F32) || (dtype == VGC_BF16 && K % (thin ? 2u : 8u) == 0u);
+    L.w_there = (thin && dtype == VGC_F32) || (dtype == VGC_BF16 && C % (thin ? 2u : 8u) == 0u);
     const size_t planes = dtype == VGC_F32 ? 3 : 1;
     size_t off = 0;
     L.x = off; if (!L.x_there) off = align_up(off + 2 * planes * N * L.Kp, 256);
@@ -565,17 +562,20 @@ int launch_linear(const LinearCall& q, void* workspace, hipStream_t stream) {
     uint16_t *x = (uint16_t*)(ws + L.x), *w = (uint16_t*)(ws + L.w);
     const Finish F = {q.bias, q.residual, q.z, q.y, N, q.C, q.act, dropout_of(q.p, q.rng), past(q.dtype, N, q.C, q.K, q.z, q.y)};
     int rc;
-    if (L.product.tile == Tile::kThin) {
-        if (q.dtype == VGC_F32) return launch_thin<float, true, false>(L.product, ThinArgs<float>{(const float*)q.W, (const float*)q.X, nullptr, q.K, 1, nullptr, F}, (float*)(ws + L.parts), stream);
-        return launch_thin<uint16_t, true, false>(L.product, ThinArgs<uint16_t>{(const uint16_t*)q.W, (const uint16_t*)q.X, nullptr, q.K, 1, nullptr, F}, (float*)(ws + L.parts), stream);
-    }
     if (!L.x_there && (rc = launch_plane_rows(q.dtype, q.X, N, q.K, x, stream)) != VGC_OK) return rc;
     if (!L.w_there && (rc = launch_plane_rows(q.dtype, q.W, q.K, q.C, w, stream)) != VGC_OK) return rc;
+    float* parts = (float*)(ws + L.parts);
+    if (L.product.tile == Tile::kThin) {
+        if (q.dtype == VGC_F32)
+            return launch_thin<float, true, false>(L.product, ThinArgs<float>{(const float*)q.W, (const float*)q.X, nullptr, q.C, q.K, q.K, 1, nullptr, F}, parts, stream);
+        const ThinArgs<uint16_t> T = {L.w_there ? (const uint16_t*)q.W : w, L.x_there ? (const uint16_t*)q.X : x, nullptr, L.w_there ? q.C : L.Cp, L.x_there ? q.K : L.Kp, q.K, 1, nullptr, F};
+        return launch_thin<uint16_t, true, false>(L.product, T, parts, stream);
+    }
     LinearArgs A = {};
     A.b = L.x_there ? Matrix{(const uint16_t*)q.X, N, q.K, 0} : Matrix{x, N, L.Kp, (uint64_t)N * L.Kp};
     A.a = L.w_there ? Matrix{(const uint16_t*)q.W, q.K, q.C, 0} : Matrix{w, q.K, L.Cp, (uint64_t)q.K * L.Cp};
     A.K = L.Kp;
-    A.parts = (float*)(ws + L.parts);
+    A.parts = parts;
     A.F = F;
     return q.dtype == VGC_F32 ? launch_product<float, true>(L.product, A, stream) : launch_product<uint16_t, true>(L.product, A, stream);
 }
@@ -587,20 +587,24 @@ static LinearBackwardPlan linear_backward_plan(int dtype, uint32_t B, uint32_t P
     // bfloat16: a small product reads dz in two planes, 16 bits: its few sums do not average what rounding left
     const bool two = dtype == VGC_BF16 && (uint64_t)N * K * C <= (1ull << 31);
     L.planes = dtype == VGC_F32 ? 3u : two ? 2u : 1u;
-    L.product = product_plan(dtype, N, K, C, L.planes);
+    L.product = product_plan(dtype, N, K, C, dtype == VGC_F32 ? 1u : L.planes, C % 2u != 0u);
     L.Cp = up8(C);
     const bool thin = L.product.tile == Tile::kThin;
-    L.w_there = thin || (dtype == VGC_BF16 && C % 8u == 0u);
-    L.dz_there = thin || (L.w_there && !two);
-    L.rest = thin && two;
+    L.w_there = (thin && dtype == VGC_F32) || (dtype == VGC_BF16 && C % (thin ? 2u : 8u) == 0u);
+    L.dz_there = L.w_there && (thin || !two);
+    L.rest = L.dz_there && two;
     const uint32_t pieces = (C + 7u) / 8u;
     L.lanes = power_of_two(std::min(pieces, 32u));
     L.blocks = (pieces + L.lanes - 1u) / L.lanes;
     const uint32_t teams = 256u / L.lanes;
-    const uint64_t want = std::max<uint64_t>(1, 2048u / L.blocks);
-    L.whole = P <= 32u;
-    L.samples_parts = L.whole ? 1u : (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(want / B, P / (teams * 4u)));
-    L.groups = L.whole ? (uint32_t)std::min<uint64_t>(want, (B + teams - 1u) / teams) : B * L.samples_parts;
+    // Samples whole or in parts, whichever leaves a team fewer rows in turn, counted over rounds of 1024 workgroups: a round takes some 3 us and 0.3 a row (16 samples of 32 x 512: whole, one
+    // team each, 16.7 us).
+    const uint64_t want = std::max<uint64_t>(1, 2048u / L.blocks), whole_groups = std::min<uint64_t>(want, (B + teams - 1u) / teams);
+    const uint64_t parts = std::max<uint64_t>(1, std::min<uint64_t>(want / B, P / (teams * 2u)));
+    auto us = [&](uint64_t groups, uint64_t rows) { return (double)((groups * L.blocks + 1023u) / 1024u) * (3. + 0.3 * (double)rows); };
+    L.whole = us(whole_groups, P * ((B + whole_groups * teams - 1u) / (whole_groups * teams))) <= us(B * parts, (P + parts * teams - 1u) / (parts * teams));
+    L.samples_parts = L.whole ? 1u : (uint32_t)parts;
+    L.groups = L.whole ? (uint32_t)whole_groups : B * L.samples_parts;
     size_t off = 0;
     L.w = off; if (!L.w_there) off = align_up(off + 2 * (size_t)(dtype == VGC_F32 ? 3 : 1) * K * L.Cp, 256);
     L.dz = off; if (!L.dz_there) off = align_up(off + 2 * (size_t)L.planes * N * L.Cp, 256);
@@ -631,18 +635,20 @@ int launch_linear_backward(const LinearCall& q, void* workspace, hipStream_t str
     if (q.s_bias && (rc = launch_column_sums(S.partial, 1, L.groups, q.B, L.samples_parts, q.C, L.whole, q.c, q.g_bias, q.s_bias, nullptr, nullptr, stream)) != VGC_OK) return rc;
     if (!q.dX) return VGC_OK;
     const Finish F = {nullptr, q.residual, nullptr, q.dX, N, q.K, VGC_ACT_NONE, Dropout{nullptr, 0u, 0.f}, past(q.dtype, N, q.K, q.C, nullptr, q.dX)};
-    if (L.product.tile == Tile::kThin) {
-        if (q.dtype == VGC_F32) return launch_thin<float, false, false>(L.product, ThinArgs<float>{(const float*)q.W, (const float*)q.dz, nullptr, q.C, 1, nullptr, F}, (float*)(ws + L.parts), stream);
-        const ThinArgs<uint16_t> T = {(const uint16_t*)q.W, (const uint16_t*)q.dz, planes, q.C, 1, nullptr, F};
-        float* parts = (float*)(ws + L.parts);
-        return L.rest ? launch_thin<uint16_t, false, true>(L.product, T, parts, stream) : launch_thin<uint16_t, false, false>(L.product, T, parts, stream);
-    }
     if (!L.w_there && (rc = launch_plane_rows(q.dtype, q.W, q.K, q.C, w, stream)) != VGC_OK) return rc;
+    float* parts = (float*)(ws + L.parts);
+    if (L.product.tile == Tile::kThin) {
+        if (q.dtype == VGC_F32)
+            return launch_thin<float, false, false>(L.product, ThinArgs<float>{(const float*)q.W, (const float*)q.dz, nullptr, q.C, q.C, q.C, 1, nullptr, F}, parts, stream);
+        const uint32_t ld = L.w_there ? q.C : L.Cp;
+        const ThinArgs<uint16_t> T = {L.w_there ? (const uint16_t*)q.W : w, L.dz_there ? (const uint16_t*)q.dz : planes, L.dz_there ? planes : planes + (size_t)N * L.Cp, ld, ld, q.C, 1, nullptr, F};
+        return L.planes == 2u ? launch_thin<uint16_t, false, true>(L.product, T, parts, stream) : launch_thin<uint16_t, false, false>(L.product, T, parts, stream);
+    }
     LinearArgs A = {};
     A.a = L.w_there ? Matrix{(const uint16_t*)q.W, q.K, q.C, 0} : Matrix{w, q.K, L.Cp, (uint64_t)q.K * L.Cp};
     A.b = L.dz_there ? Matrix{(const uint16_t*)q.dz, N, q.C, 0} : Matrix{planes, N, L.Cp, (uint64_t)N * L.Cp};
     A.K = L.Cp;
-    A.parts = (float*)(ws + L.parts);
+    A.parts = parts;
     A.F = F;
     return q.dtype == VGC_F32 ? launch_product<float, false>(L.product, A, stream) : launch_product<uint16_t, false>(L.product, A, stream);
 }

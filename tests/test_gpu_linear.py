@@ -57,7 +57,8 @@ def _forward(dev, N, K, C, act, dtype, keep=True, residual=True, p=0.25, bias=Tr
 
 
 SIZES = [(1, 1, 1), (1, 3, 2), (2, 8, 8), (1, 40, 1000), (1, 1000, 7), (1, 2048, 2048), (3, 1001, 33), (16, 512, 512), (17, 257, 130), (33, 64, 264), (64, 1000, 1000), (65, 784, 129),
-         (128, 784, 1000), (100, 5, 300), (129, 96, 128), (200, 4096, 64), (257, 72, 520), (300, 2048, 8), (1030, 256, 256), (700, 513, 261), (5, 8192, 24), (1, 16, 8192), (48, 4100, 96)]
+         (128, 784, 1000), (100, 5, 300), (129, 96, 128), (200, 4096, 64), (257, 72, 520), (300, 2048, 8), (1030, 256, 256), (700, 513, 261), (5, 8192, 24), (1, 16, 8192), (48, 4100, 96),
+         (1, 4096, 4096), (3, 6001, 515), (20, 5001, 1030), (2, 4099, 2050), (130, 4100, 520), (927, 64, 1032), (600, 24, 1416), (257, 2049, 264), (40, 7, 9)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -153,7 +154,8 @@ def _backward(dev, B, P, K, C, act, dtype, add=True, p=0.25, dx=True, sums=True)
 
 
 BACKWARD = [(1, 1, 1, 1), (1, 1, 2, 3), (2, 1, 8, 8), (1, 5, 33, 40), (3, 1, 1001, 130), (128, 1, 1000, 1000), (2, 33, 64, 264), (5, 13, 129, 784), (1, 300, 8, 2048), (300, 1, 2048, 9),
-            (4, 64, 520, 72), (2, 500, 256, 256), (600, 2, 96, 520), (3, 1000, 24, 100), (40, 32, 64, 33), (1, 2000, 16, 16), (2100, 1, 40, 520)]
+            (4, 64, 520, 72), (2, 500, 256, 256), (600, 2, 96, 520), (3, 1000, 24, 100), (40, 32, 64, 33), (1, 2000, 16, 16), (2100, 1, 40, 520),
+            (1, 1, 2048, 4096), (3, 6, 655, 7513), (129, 1, 131, 4513), (16, 32, 512, 512), (1, 40, 1000, 5000), (7, 3, 83, 2301), (2, 9, 9, 7)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
