@@ -328,15 +328,16 @@ __global__ __launch_bounds__(256) void k_group_norm_moments(GroupNormArgs A) {
     __syncthreads();
     // eight teams a thread, then the threads of a channel
     const uint32_t S = A.lanes * 8u, c = threadIdx.x % S, sub = threadIdx.x / S, subs = 256u / S, rows_here = L.p1 - L.p0;
+    const uint32_t each = rows_here / L.teams, more = rows_here - each * L.teams;             // rows of a team; teams with one more
     float total = 0.f, mean = 0.f, squares = 0.f;
     for (uint32_t t = 0; t < 8u; ++t) {
-        const float m = (float)rows_of_team(rows_here, sub * 8u + t, L.teams);
+        const float m = (float)(each + (sub * 8u + t < more ? 1u : 0u));
         total += m;
         mean = __builtin_fmaf(m, sm[(sub * 8u + t) * S + c], mean);
     }
     if (total > 0.f) mean /= total;
     for (uint32_t t = 0; t < 8u; ++t) {
-        const float m = (float)rows_of_team(rows_here, sub * 8u + t, L.teams), d = sm[(sub * 8u + t) * S + c] - mean;
+        const float m = (float)(each + (sub * 8u + t < more ? 1u : 0u)), d = sm[(sub * 8u + t) * S + c] - mean;
         if (m > 0.f) squares += __builtin_fmaf(m * d, d, sq[(sub * 8u + t) * S + c]);
     }
     if (subs > 1u) {
@@ -344,11 +345,7 @@ __global__ __launch_bounds__(256) void k_group_norm_moments(GroupNormArgs A) {
         pq[threadIdx.x] = squares;
         __syncthreads();
         if (threadIdx.x >= S) return;
-        auto rows_of_sub = [&](uint32_t q) {
-            uint32_t r = 0;
-            for (uint32_t t = 0; t < 8u; ++t) r += rows_of_team(rows_here, q * 8u + t, L.teams);
-            return (float)r;
-        };
+        auto rows_of_sub = [&](uint32_t q) { return (float)(each * 8u + (more > q * 8u ? min(more - q * 8u, 8u) : 0u)); };
         mean = squares = 0.f;
         for (uint32_t q = 0; q < subs; ++q) mean = __builtin_fmaf(rows_of_sub(q), pm[q * S + c], mean);
         mean /= (float)rows_here;
@@ -544,10 +541,10 @@ static GroupNormPlan group_norm_plan(int dtype, bool backward, uint32_t B, uint3
     const uint32_t times = (uint32_t)((B + most_samples - 1u) / most_samples);
     L.samples = std::min((B + times - 1u) / times, std::max(1u, (1u << 22) / std::max(L.blocks, G)));
     const uint64_t want = std::max<uint64_t>(1, kGroups / std::max<uint64_t>(1, (uint64_t)L.samples * L.blocks));
-    L.chunks = (uint32_t)std::min<uint64_t>(std::min<uint64_t>(want, 256u), (P + teams * 8u - 1u) / (teams * 8u));      // (256: of which a group's join has to read all)
+    L.chunks = (uint32_t)std::min<uint64_t>(std::min<uint64_t>(want, 256u), (P + teams * 2u - 1u) / (teams * 2u));      // (256: of which a group's join has to read all)
     const uint32_t batch = teams * (dtype == VGC_F32 ? 2u : 4u) * (backward ? 1u : 2u);      // (whole batches but for the sample's last)
-    L.rows = std::min(P, ((P + L.chunks - 1u) / L.chunks + batch / 2u) / batch * batch);
-    if (L.rows == 0u) L.rows = std::min(P, batch);
+    L.rows = (P + L.chunks - 1u) / L.chunks;
+    if (L.rows > 2u * batch) L.rows = (L.rows + batch / 2u) / batch * batch;
     L.chunks = (P + L.rows - 1u) / L.rows;
     return L;
 }

@@ -345,7 +345,9 @@ struct SlopeArgs {
     void* rest;               // like dz: what rounding left of it, or NULL
     uint16_t* planes;         // dz as operand rows of ldp where the product cannot read it as it lies, or NULL
     uint32_t ldp, count;      // planes: 1 .. 3
-    float* partial;           // or NULL
+    float* partial;           // or NULL (no sums); one group of whole samples leaves the sums themselves:
+    float *g_out, *s_out;     // (g_out or NULL)
+    float c;
     uint32_t B, P, C, lanes, blocks, parts, groups;
     bool whole;
     int act;
@@ -416,10 +418,10 @@ __global__ __launch_bounds__(256) void k_linear_slope(SlopeArgs A) {
             }
         });
     }
-    if (!A.partial) return;
+    if (!A.partial && !A.s_out) return;
     const uint32_t c = block * A.lanes * 8u + threadIdx.x;
     const bool mine = threadIdx.x < A.lanes * 8u && c < A.C;
-    float* out = A.partial + (size_t)group * (A.whole ? 2u : 1u) * A.C + c;
+    float* out = A.s_out ? nullptr : A.partial + (size_t)group * (A.whole ? 2u : 1u) * A.C + c;
     if (!A.whole) {
         const float v[1][8] = {{h[0], h[1], h[2], h[3], h[4], h[5], h[6], h[7]}};
         channel_sums<1>(v, A.lanes, sh, part, chan[0]);
@@ -429,6 +431,11 @@ __global__ __launch_bounds__(256) void k_linear_slope(SlopeArgs A) {
     const float v[2][8] = {{g[0], g[1], g[2], g[3], g[4], g[5], g[6], g[7]}, {s[0], s[1], s[2], s[3], s[4], s[5], s[6], s[7]}};
     channel_sums<2>(v, A.lanes, sh, part, chan[0], chan[1]);
     if (!mine) return;
+    if (A.s_out) {
+        if (A.g_out) A.g_out[c] = A.c * chan[0][threadIdx.x];
+        A.s_out[c] = A.c * A.c * chan[1][threadIdx.x];
+        return;
+    }
     out[0] = chan[0][threadIdx.x];
     out[A.C] = chan[1][threadIdx.x];
 }
@@ -580,7 +587,7 @@ int launch_linear(const LinearCall& q, void* workspace, hipStream_t stream) {
     return q.dtype == VGC_F32 ? launch_product<float, true>(L.product, A, stream) : launch_product<uint16_t, true>(L.product, A, stream);
 }
 
-struct LinearBackwardPlan { ProductPlan product; bool w_there, dz_there, rest, whole; uint32_t planes, Cp, lanes, blocks, samples_parts, groups; size_t w, dz, parts, partial, total; };
+struct LinearBackwardPlan { ProductPlan product; bool w_there, dz_there, rest, whole, direct; uint32_t planes, Cp, lanes, blocks, samples_parts, groups; size_t w, dz, parts, partial, total; };
 static LinearBackwardPlan linear_backward_plan(int dtype, uint32_t B, uint32_t P, uint32_t K, uint32_t C) {
     LinearBackwardPlan L;
     const uint32_t N = B * P;
@@ -598,19 +605,24 @@ static LinearBackwardPlan linear_backward_plan(int dtype, uint32_t B, uint32_t P
     L.blocks = (pieces + L.lanes - 1u) / L.lanes;
     const uint32_t teams = 256u / L.lanes;
     // Samples whole or in parts, whichever leaves a team fewer rows in turn, counted over rounds of 1024 workgroups: a round takes some 3 us and 0.3 a row (16 samples of 32 x 512: whole, one
-    // team each, 16.7 us).
+    // team each, 16.7 us, in parts 5.2).  The second kernel takes 4.5, without which one group of workgroups of 32 teams can do where it has few samples (128 x 1000 to 1000 float32, the
+    // whole call 17.1 -> 13.9).
+    auto us = [&](uint64_t groups, uint64_t rows) { return (double)((groups * L.blocks + 1023u) / 1024u) * (3. + 0.3 * (double)rows); };
     const uint64_t want = std::max<uint64_t>(1, 2048u / L.blocks), whole_groups = std::min<uint64_t>(want, (B + teams - 1u) / teams);
     const uint64_t parts = std::max<uint64_t>(1, std::min<uint64_t>(want / B, P / (teams * 2u)));
-    auto us = [&](uint64_t groups, uint64_t rows) { return (double)((groups * L.blocks + 1023u) / 1024u) * (3. + 0.3 * (double)rows); };
-    L.whole = us(whole_groups, P * ((B + whole_groups * teams - 1u) / (whole_groups * teams))) <= us(B * parts, (P + parts * teams - 1u) / (parts * teams));
+    const double whole_us = us(whole_groups, P * ((B + whole_groups * teams - 1u) / (whole_groups * teams))), parts_us = us(B * parts, (P + parts * teams - 1u) / (parts * teams));
+    L.whole = whole_us <= parts_us;
     L.samples_parts = L.whole ? 1u : (uint32_t)parts;
     L.groups = L.whole ? (uint32_t)whole_groups : B * L.samples_parts;
+    const uint32_t narrow = std::min(L.lanes, 8u), narrow_blocks = (pieces + narrow - 1u) / narrow;
+    L.direct = (double)((narrow_blocks + 1023u) / 1024u) * (3. + 0.3 * (double)P * (double)((B + 256u / narrow - 1u) / (256u / narrow))) <= std::min(whole_us, parts_us) + 4.5;
+    if (L.direct) { L.lanes = narrow; L.blocks = narrow_blocks; L.whole = true; L.samples_parts = L.groups = 1u; }
     size_t off = 0;
     L.w = off; if (!L.w_there) off = align_up(off + 2 * (size_t)(dtype == VGC_F32 ? 3 : 1) * K * L.Cp, 256);
     L.dz = off; if (!L.dz_there) off = align_up(off + 2 * (size_t)L.planes * N * L.Cp, 256);
     if (L.rest) off = align_up(off + 2 * (size_t)N * C, 256);    // (in dz's place)
     L.parts = off; off = align_up(off + L.product.parts, 256);
-    L.partial = off; off += (size_t)L.groups * (L.whole ? 2u : 1u) * C * sizeof(float);
+    L.partial = off; if (!L.direct) off += (size_t)L.groups * (L.whole ? 2u : 1u) * C * sizeof(float);
     L.total = off;
     return L;
 }
@@ -622,8 +634,8 @@ int launch_linear_backward(const LinearCall& q, void* workspace, hipStream_t str
     char* ws = static_cast<char*>(workspace);
     uint16_t *w = (uint16_t*)(ws + L.w), *planes = (uint16_t*)(ws + L.dz);
     const bool copy = q.dX && !L.dz_there;
-    SlopeArgs S = {q.dy, q.act == VGC_ACT_NONE ? nullptr : q.z_in, q.dz, q.dX && L.rest ? planes : nullptr, copy ? planes : nullptr, L.Cp, L.planes, q.s_bias ? (float*)(ws + L.partial) : nullptr,
-                   q.B, q.P, q.C, L.lanes, L.blocks, L.samples_parts, L.groups, L.whole, q.act, dropout_of(q.p, q.rng)};
+    SlopeArgs S = {q.dy, q.act == VGC_ACT_NONE ? nullptr : q.z_in, q.dz, q.dX && L.rest ? planes : nullptr, copy ? planes : nullptr, L.Cp, L.planes, q.s_bias && !L.direct ? (float*)(ws + L.partial) : nullptr,
+                   L.direct ? q.g_bias : nullptr, L.direct ? q.s_bias : nullptr, q.c, q.B, q.P, q.C, L.lanes, L.blocks, L.samples_parts, L.groups, L.whole, q.act, dropout_of(q.p, q.rng)};
     const dim3 grid(L.groups * L.blocks);
 #define VGC_LAUNCH(T, WHOLE) do { if (S.z) hipLaunchKernelGGL((k_linear_slope<T, WHOLE, true>), grid, dim3(256), 0, stream, S); \
         else hipLaunchKernelGGL((k_linear_slope<T, WHOLE, false>), grid, dim3(256), 0, stream, S); } while (0)
@@ -632,7 +644,7 @@ int launch_linear_backward(const LinearCall& q, void* workspace, hipStream_t str
 #undef VGC_LAUNCH
     int rc = hip_check(hipGetLastError(), "launch k_linear_slope");
     if (rc != VGC_OK) return rc;
-    if (q.s_bias && (rc = launch_column_sums(S.partial, 1, L.groups, q.B, L.samples_parts, q.C, L.whole, q.c, q.g_bias, q.s_bias, nullptr, nullptr, stream)) != VGC_OK) return rc;
+    if (q.s_bias && !L.direct && (rc = launch_column_sums(S.partial, 1, L.groups, q.B, L.samples_parts, q.C, L.whole, q.c, q.g_bias, q.s_bias, nullptr, nullptr, stream)) != VGC_OK) return rc;
     if (!q.dX) return VGC_OK;
     const Finish F = {nullptr, q.residual, nullptr, q.dX, N, q.K, VGC_ACT_NONE, Dropout{nullptr, 0u, 0.f}, past(q.dtype, N, q.K, q.C, nullptr, q.dX)};
     if (!L.w_there && (rc = launch_plane_rows(q.dtype, q.W, q.K, q.C, w, stream)) != VGC_OK) return rc;
