@@ -57,8 +57,11 @@ __device__ __forceinline__ void sums_of_groups(const float* a, const float* b, u
 }
 
 // ---- a sample's whole groups in one workgroup ---------------------------------------------------------------------------------
-// kNV rows of a team are held as they are in memory.  How a workgroup's groups lie in its lanes decides how a group's sum is formed: by channels, which may
-// belong to any group; a lane's eight channels of one group, then by lanes; or all lanes' of one.
+// kNV rows of a team are held as they are in memory.  A workgroup's reading, sums and writing follow each other, with one or two workgroups a
+// compute unit, which bounds them (32 x 49 x 2048 float32 in 32 groups 8.7 us a call, 64 x 784 x 512 bfloat16 34, both 3.0 TB/s of the 5.1 that a
+// copy reaches; as chunks 16.3 and 39.5.  Backward 32 x 196 x 1024 float32 27.5, as chunks 37).
+// How a workgroup's groups lie in its lanes decides how a group's sum is formed: by channels, which may belong to any group; a lane's eight
+// channels of one group, then by lanes; or all lanes' of one.
 enum { kByChannel, kByLane, kOneGroup };
 constexpr uint32_t kMostThreads = 1024, kMostSlab = 512;     // threads, channels
 
@@ -148,7 +151,6 @@ __global__ __launch_bounds__(kThreads) void k_group_norm(GroupNormArgs A) {
                 v[k] = __builtin_fmaf(d, d, v[k]);
             }
     }
-    if (kMode == kByLane) __syncthreads();                   // (the means have been read)
     sums.of(v);
 #pragma unroll
     for (int k = 0; k < kM; ++k) rstd[k] = 1.0f / sqrtf(grp[of[k]] * inv + A.eps);
@@ -260,7 +262,9 @@ __global__ __launch_bounds__(kThreads) void k_group_norm_backward(GroupNormArgs 
 }
 
 // ---- samples beyond that: sums by channel and chunk, then the result ------------------------------------------------------------
-// Workgroup (sample, block of columns, chunk of positions): teams take the chunk's rows in turn, kRows of them in flight.
+// Workgroup (sample, block of columns, chunk of positions): teams take the chunk's rows in turn, two sets of kRows of them in turn in flight.
+// Both passes are bound by memory (64 x 50176 x 64 bfloat16 with relu, 411 MB: 219 us, the moments at 4 TB/s, which is what reading alone reaches
+// on this card, the result from the last-level cache for what it keeps.  Backward, 32 x 3136 x 256 float32 with silu, 103 MB an array: 96 us).
 struct Place { uint32_t b, chunk, c0, team, teams, p0, p1; int n; };
 __device__ __forceinline__ Place place_of(const GroupNormArgs& A) {
     Place L;
@@ -366,7 +370,8 @@ __device__ __forceinline__ double wave_sum_double(double x) {
     return x;
 }
 
-// A group's moments from those of its channels and chunks; in 64 bits, so that mean^2 may be subtracted.
+// A group's moments from those of its channels and chunks; in 64 bits, so that mean^2 may be subtracted.  (With 64 threads for any number of
+// entries 2 x 47061 x 296 float32 waited 150 us for its two groups of many chunks.)
 __global__ __launch_bounds__(1024) void k_group_norm_join(GroupNormArgs A) {
     __shared__ double sh[2][16];
     const uint32_t b = blockIdx.x / A.G, q = blockIdx.x - b * A.G, lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
@@ -409,7 +414,7 @@ __global__ __launch_bounds__(256) void k_group_norm_apply(GroupNormArgs A) {
     });
 }
 
-// kSums: G_z and H_z of the chunk; else dx.
+// kSums: G_z and H_z of the chunk; else dx.  (The passes of 32 x 3136 x 256 float32: 45 and 41 us.)
 template <typename T, bool kWhole, int kM, bool kSums>
 __global__ __launch_bounds__(256) void k_group_norm_backward_rows(GroupNormArgs A) {
     __shared__ float sh[kSums ? 4096 : 1], part[kSums ? 512 : 1], chan[2][kSums ? 256 : 1];
@@ -506,8 +511,11 @@ __global__ __launch_bounds__(1024) void k_group_norm_backward_join(GroupNormArgs
 }
 
 // ---- launches -----------------------------------------------------------------------------------------------------------------
-// Held: whole groups of a cache line's channels and more a workgroup (us; float32, 32 x 784 x 512 in 32 groups, lines of 32 channels 32.2, 64 39.1; bfloat16, 64 x 784 x 512, of 64 34.3, 32 46), with as many threads as leave a team few rows.  most: rows that a team can hold, with 512
-// threads and fewer and with 1024, whose lanes have 128 registers.
+// Held: whole groups of a cache line's channels and more a workgroup (us; float32, 32 x 784 x 512 in 32 groups, lines of 32 channels 32.2, 64 39.1;
+// bfloat16, 64 x 784 x 512, of 64 34.3, 32 46), with as many threads as leave a team few rows.  most: rows that a team can hold, with 512 threads
+// and fewer and with 1024, whose lanes have 128 registers.
+// Else: workgroups to fill the compute units, and as many samples at a time as the last-level cache keeps of them between the two passes, that is
+// somewhat less than its 256 MB (us, 64 x 50176 x 64 bfloat16: 210 MB in 2048 workgroups 219, in 1024 232; 128 MB 255; all at once 246).
 struct GroupNormPlan {
     bool held;
     uint32_t lanes, threads, rows_of_team, groups, slabs;    // held
@@ -531,7 +539,7 @@ static GroupNormPlan group_norm_plan(int dtype, bool backward, uint32_t B, uint3
         L.rows_of_team = (P + teams - 1u) / teams;
         L.held = L.rows_of_team <= (L.threads == kMostThreads ? most_1024 : most);
     }
-    if (L.held) { L.samples = std::min(B, std::max(1u, (1u << 22) / L.slabs)); return L; }
+    if (L.held) { L.samples = std::min(B, std::max(1u, (1u << 20) / L.slabs)); return L; }      // (a launch has fewer than 2^32 threads)
     const uint32_t pieces = (C + 7u) / 8u;
     L.lanes = power_of_two(std::min(pieces, 32u));
     L.threads = 256u;
@@ -539,7 +547,7 @@ static GroupNormPlan group_norm_plan(int dtype, bool backward, uint32_t B, uint3
     const uint32_t teams = 256u / L.lanes;
     const uint64_t sample = (uint64_t)P * C * (dtype == VGC_F32 ? 4u : 2u) * (backward ? 2u : 1u), most_samples = std::max<uint64_t>(1, kSlice / sample);
     const uint32_t times = (uint32_t)((B + most_samples - 1u) / most_samples);
-    L.samples = std::min((B + times - 1u) / times, std::max(1u, (1u << 22) / std::max(L.blocks, G)));
+    L.samples = std::min((B + times - 1u) / times, std::max(1u, (1u << 20) / std::max(L.blocks, G)));
     const uint64_t want = std::max<uint64_t>(1, kGroups / std::max<uint64_t>(1, (uint64_t)L.samples * L.blocks));
     L.chunks = (uint32_t)std::min<uint64_t>(std::min<uint64_t>(want, 256u), (P + teams * 2u - 1u) / (teams * 2u));      // (256: of which a group's join has to read all)
     const uint32_t batch = teams * (dtype == VGC_F32 ? 2u : 4u) * (backward ? 1u : 2u);      // (whole batches but for the sample's last)

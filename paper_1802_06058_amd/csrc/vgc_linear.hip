@@ -8,8 +8,9 @@
 // finishes eight consecutive elements of a row: bias, activation, dropout and residual meet the sum while it is float32, and it is rounded once.
 // Where the output has few tiles, k is shared out, and a second kernel adds the parts in a fixed order and finishes them.
 //
-// Precision.  bfloat16: products are exact, sums float32; dz, which is stored in bfloat16 for the sums of W, is read so by dX's product.  float32: three planes of 8 bits an operand, rounded, six
-// products of them, taken out of the instructions' sums every 32 k.
+// Precision.  bfloat16: products are exact, sums float32.  dz is stored in bfloat16, as the D that W's sums are formed from, and dX's product reads it so: rounded at random it leaves dX, which is
+// rounded itself, 1.4 times as far off as its own rounding alone (2.3e-3 and 1.65e-3); small products, whose few sums may be further off than that, read 16 bits of it in two planes, which costs them nothing
+// beside the call.  float32: three planes of 8 bits an operand, rounded, six products of them, taken out of the instructions' sums every 32 k; few rows are multiplied as floats.
 #include <algorithm>
 
 #include "vgc_columns.h"
@@ -101,8 +102,12 @@ __device__ __forceinline__ void finish_tile(f16v (&acc)[MT][NT], float* turn, ui
     }
 }
 
+// Bound by the matrix instructions at the clock that the card keeps under them.  bfloat16, 16384 rows: 8192 to 2048 with dropout and residual 457 us, 1.20 PFLOP/s; 2048 to 8192 448, with gelu and z
+// kept 525-537, since nothing of another tile runs beside a workgroup's end, and gelu is some 26 issue slots an element; its backward product 430-440.  (Two workgroups of 256 x 128 a compute unit,
+// whose ends would overlap: 498 and 605 with results stored into the caches, 477 and 551 past them, against 510 and 568, 460 and 536 then; 128 x 128 a wave, four of them: 803.)  float32, 4096^3: 663 us,
+// 207 TFLOP/s.
 template <typename Shape, typename T, bool kMixed>
-__global__ __launch_bounds__(Shape::NW * 64, Shape::kLds > 80 * 1024 && Shape::NW == 4 ? 1 : 2) void k_linear(LinearArgs A) {
+__global__ __launch_bounds__(Shape::NW * 64, 2) void k_linear(LinearArgs A) {
     __shared__ __attribute__((aligned(1024))) uint8_t sh[Shape::kLds];
     static_assert(Shape::NW * kTurnBytes <= Shape::kLds, "room to turn");
     const uint32_t tiles_n = (A.F.N + Shape::BN - 1) / Shape::BN, tiles_m = (A.F.M + Shape::BM - 1) / Shape::BM;
@@ -124,7 +129,7 @@ __global__ __launch_bounds__(Shape::NW * 64, Shape::kLds > 80 * 1024 && Shape::N
     finish_tile<T>(acc, reinterpret_cast<float*>(sh + Shape::wave() * kTurnBytes), m0 + Shape::wave_m(), n0 + Shape::wave_n(), split, A);
 }
 
-// Adds the parts of k in their order, eight elements of a row a lane.
+// Adds the parts of k in their order, eight elements of a row a lane.  Four parts of one row of 4096: 3.5 us, a launch's own time.
 template <typename T>
 __global__ __launch_bounds__(256) void k_linear_join(Finish F, uint32_t splits, const float* __restrict__ parts) {
     const uint32_t per_row = (F.M + 7u) / 8u;
@@ -151,9 +156,11 @@ __global__ __launch_bounds__(256) void k_linear_join(Finish F, uint32_t splits, 
 //   forward   a lane asks for kV consecutive columns of W in each of its k's rows, so that a wave's load takes whole 16 kV columns of four rows; column j
 //             of the lanes is an instruction's operand (bfloat16: eight k's pairs put together by byte permutes)
 //   backward  a lane asks for 16 bytes of a row of W, instruction j taking rows 16 j + lane % 16
-// Rows are read at any alignment, so nothing is laid out before.  Requests have no branches, which would make a wave wait for what it asked for before: past an edge
-// a place is moved back to the last one inside, of k with the elements that others count dropped from b's, of columns and rows with results that others have too.  The waves' sums meet in LDS, four lanes add an output piece's sixteen and one finishes it.
+// Rows are read where they lie (but for odd numbers of bfloat16, see product_plan).  Requests have no branches, which would make a wave wait for what it asked for before: past an edge
+// a place is moved back to the last one inside, of k with the elements that others count dropped from b's, of columns and rows with results that others have too.
+// The waves' sums meet in LDS, four lanes add an output piece's sixteen and one finishes it.
 // float32 is multiplied as floats.
+// Bound by what a compute unit's loads bring, whole lines of 128 bytes at some 31-41 GB/s each: 1 x 4096 x 4096 bfloat16 8.7 us (four parts of k) and the join, 128 x 784 x 1000 float32 7.7.
 constexpr uint32_t kThinWaves = 16;
 template <typename T> struct ThinArgs {
     const T *a, *b, *rest;    // W; the rows of X or dz, and (backward, bfloat16) what rounding left of dz
@@ -338,7 +345,7 @@ __global__ __launch_bounds__(kThinWaves * 64) void k_linear_thin(ThinArgs<T> A) 
 // ---- dz and the sums of the bias --------------------------------------------------------------------------------------------
 // Workgroup (block of columns, group of rows): a team holds a row's pieces of the block, kRows of its rows in flight.  Samples of many
 // positions are cut into parts, which leave a column sum each; of few, a team takes whole ones and keeps both sums.  A second kernel adds them
-// in a fixed order.  Bound by memory: dy, z and dz once.
+// in a fixed order.  Bound by memory: dy, z and dz once; 16 x 1024 x 8192 bfloat16 with gelu 150-165 us, 4.9-5.4 TB/s.
 struct SlopeArgs {
     const void *dy, *z;       // z: NULL without an activation
     void* dz;
@@ -471,6 +478,7 @@ static double thin_plan(int dtype, uint32_t N, uint32_t M, uint32_t K, uint32_t 
     for (const auto& q : shapes) {
         if ((q.v < 2u && !f32) || (q.t == 2u && N <= 16u)) continue;
         const uint64_t n = tiles(M, 16u * q.v, N, 16u * q.t);
+        if (n > (1u << 20)) continue;                        // (a launch has fewer than 2^32 threads)
         for (uint32_t splits = 1; splits <= 16u && (splits == 1u || (K / splits >= 512u && n * splits <= 512u)); splits *= 2u) {
             const double us = rounds(n * splits) * (3. + (double)K / splits * (q.v + 2u * q.t * (f32 ? 1u : planes_b)) * (f32 ? 64. : 32.) / 41e3) + join_us(splits, N, M);
             if (us < least) { least = us; best = ProductPlan{Tile::kThin, splits, q.v, q.t, 0}; }

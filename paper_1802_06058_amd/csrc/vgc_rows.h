@@ -1,5 +1,5 @@
-// Rows of activations in pieces of eight elements, and the 8-bit form of a block of them: shared by the kernels of
-// vgc_act8.hip and vgc_norm.hip.
+// Rows of activations in pieces of eight elements, shared by the kernels that go through such rows, and the 8-bit form of a block of them, by
+// those of vgc_act8.hip and vgc_norm.hip.
 #ifndef VGC_ROWS_H
 #define VGC_ROWS_H
 

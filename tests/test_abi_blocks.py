@@ -24,11 +24,11 @@ def test_dropout():
 
 
 def test_linear():
-    need = vgc.linear_workspace_bytes(vgc.F32, 4, 24, 40)
-    assert need > 0
+    need = vgc.linear_workspace_bytes(vgc.F32, 4, 3, 40)              # (a k that is laid out in planes; 24 needs none)
+    assert need > 0 and vgc.linear_workspace_bytes(vgc.F32, 4, 24, 40) == 0
     for bad in [(2, 4, 24, 40), (0, 0, 24, 40), (0, 4, 0, 40), (0, 4, 24, 0), (0, (1 << 20) + 1, 24, 40), (0, 4, 1 << 20, 1 << 11), (0, 4, (1 << 20) + 8, 8), (0, 1 << 20, 8, 1 << 15)]:
         assert vgc.linear_workspace_bytes(*bad) == 0, bad
-    good = dict(dtype=0, X=P, W=P, bias=None, act=1, p=0.5, rng=P, residual=None, N=4, K=24, C=40, z=None, y=P, ws=P, nb=need, stream=None)
+    good = dict(dtype=0, X=P, W=P, bias=None, act=1, p=0.5, rng=P, residual=None, N=4, K=3, C=40, z=None, y=P, ws=P, nb=need, stream=None)
     _codes(good, [(dict(dtype=2), DTYPE), *[(dict([(k, None)]), NULL) for k in ("X", "W", "y", "rng", "ws")], *[(dict([(k, 0)]), SIZE) for k in ("N", "K", "C")],
                   (dict(N=(1 << 20) + 1), SIZE), (dict(K=1 << 15, C=(1 << 15) + 1), SIZE), (dict(X=P + 8), ALIGN), (dict(W=P + 4), ALIGN), (dict(bias=P + 2), ALIGN),
                   (dict(residual=P + 2), ALIGN), (dict(z=P + 1), ALIGN), (dict(y=P + 2), ALIGN), (dict(rng=P + 4), ALIGN), (dict(act=4), PARAM), (dict(act=-1), PARAM), (dict(p=1.5), PARAM),
@@ -83,7 +83,7 @@ def test_tensors_that_do_not_belong_together():
     with pytest.raises(vgc.VgcError, match="W "):
         vgc.linear(x, t(24, 8, dtype=torch.bfloat16), t(4, 8), workspace=ws)
     with pytest.raises(vgc.VgcError, match="workspace"):
-        vgc.linear(x, t(24, 8), t(4, 8))
+        vgc.linear(t(4, 3), t(3, 8), t(4, 8))                       # (3: laid out, which needs working memory)
     with pytest.raises(vgc.VgcError, match="bias"):
         vgc.linear(x, t(24, 8), t(4, 8), t(7), workspace=ws)
     with pytest.raises(vgc.VgcError, match="does not give"):

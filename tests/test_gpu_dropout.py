@@ -108,3 +108,20 @@ def test_a_recorded_call_draws_anew_when_its_state_changes(dev):
         assert torch.equal(y, want)
         seen.append(y.clone())
     assert torch.equal(seen[0], seen[2]) and not torch.equal(seen[0], seen[1])
+
+
+def test_tensors_of_another_device_than_the_current_one_are_refused(dev, monkeypatch):
+    """(Told from the device's number: there is one here.)"""
+    import torch
+    from paper_1802_06058_amd import vgc
+    x, y = torch.randn(4, 8, device=dev), torch.full((4, 8), 7.0, device=dev)
+    W, ws, f = torch.randn(8, 8, device=dev), torch.empty(1 << 20, dtype=torch.uint8, device=dev), torch.ones(8, device=dev)
+    mean = torch.ones(4, 2, device=dev)
+    v, o = x.view(4, 1, 8), y.view(4, 1, 8)
+    with monkeypatch.context() as m:
+        m.setattr(torch.cuda, "current_device", lambda: 1)
+        for call in (lambda: vgc.dropout(x, 0.5, T.rng_state(dev), y), lambda: vgc.linear(x, W, y, workspace=ws), lambda: vgc.linear_backward(v, None, W, 0, 1.0, o, workspace=ws),
+                     lambda: vgc.group_norm(v, f, f, 1e-5, 0, o, mean, mean, ws), lambda: vgc.group_norm_backward(v, v, mean, mean, f, f, 0, 1.0, o, f, f, workspace=ws)):
+            with pytest.raises(vgc.VgcError, match="current device"):
+                call()
+    assert (y == 7).all()
