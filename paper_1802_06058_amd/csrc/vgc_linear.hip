@@ -32,14 +32,18 @@ struct Finish {
     bool past;                // results are stored past the caches
 };
 template <typename T>
-__device__ __forceinline__ void finish(const Finish& F, const DropoutKey& key, uint32_t row, uint32_t col, int n, const float (&bias)[8], float (&f)[8]) {
-    const size_t at = (size_t)row * F.M + col;
+__device__ __forceinline__ Raw8<T> residual_of(const Finish& F, uint32_t row, uint32_t col, int n) {
     Raw8<T> r;
-    if (F.residual) r = load8(static_cast<const T*>(F.residual) + at, n);
+    if (F.residual) r = load8(static_cast<const T*>(F.residual) + (size_t)row * F.M + col, row < F.N ? n : 0);
+    return r;
+}
+template <typename T>
+__device__ __forceinline__ void finish(const Finish& F, const DropoutKey& key, uint32_t row, uint32_t col, int n, const float (&bias)[8], const Raw8<T>& r, float (&f)[8]) {
+    const size_t at = (size_t)row * F.M + col;
 #pragma unroll
     for (int k = 0; k < 8; ++k) f[k] += bias[k];
     if (F.z) store8_to(static_cast<T*>(F.z) + at, f, n, F.past);
-    apply_act(F.act, f);
+    apply_act<sizeof(T) == 2>(F.act, f);
     apply_dropout(F.drop, key, row, col / 8u, f);
     if (F.residual) {
         float g[8];
@@ -77,8 +81,16 @@ __device__ __forceinline__ void finish_tile(f16v (&acc)[MT][NT], float* turn, ui
         const int n = (int)A.F.M - (int)col;
         float bias[8];
         if (!A.parts) bias_of(A.F, col, bias);
+        Raw8<T> res[2][4];                                   // the residual's rows, asked for 32 rows ahead
+        auto ask = [&](int nt) {
+            if (A.parts) return;
+#pragma unroll
+            for (uint32_t q = 0; q < 4u; ++q) res[nt & 1][q] = residual_of<T>(A.F, n0 + nt * 32u + q * 8u + lane / 8u, col, n);
+        };
+        ask(0);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
+            if (nt + 1 < NT) ask(nt + 1);
 #pragma unroll
             for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -94,7 +106,7 @@ __device__ __forceinline__ void finish_tile(f16v (&acc)[MT][NT], float* turn, ui
                 float f[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
                 if (row >= A.F.N || n <= 0) continue;
                 if (A.parts) store8(A.parts + ((size_t)split * A.F.N + row) * A.F.M + col, f, n);
-                else finish<T>(A.F, key, row, col, n, bias, f);
+                else finish<T>(A.F, key, row, col, n, bias, res[nt & 1][q], f);
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
@@ -147,7 +159,7 @@ __global__ __launch_bounds__(256) void k_linear_join(Finish F, uint32_t splits, 
 #pragma unroll
         for (int k = 0; k < 8; ++k) f[k] += g[k];
     }
-    finish<T>(F, dropout_key(F.drop), row, col, n, bias, f);
+    finish<T>(F, dropout_key(F.drop), row, col, n, bias, residual_of<T>(F, row, col, n), f);
 }
 
 // ---- few rows ---------------------------------------------------------------------------------------------------------------
@@ -339,7 +351,7 @@ __global__ __launch_bounds__(kThinWaves * 64) void k_linear_thin(ThinArgs<T> A) 
     if (A.splits > 1u) { store8(A.parts + ((size_t)split * A.F.N + row) * M + c0, f, n); return; }
     float bias[8];
     bias_of(A.F, c0, bias);
-    finish<T>(A.F, dropout_key(A.F.drop), row, c0, n, bias, f);
+    finish<T>(A.F, dropout_key(A.F.drop), row, c0, n, bias, residual_of<T>(A.F, row, c0, n), f);
 }
 
 // ---- dz and the sums of the bias --------------------------------------------------------------------------------------------

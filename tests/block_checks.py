@@ -33,10 +33,11 @@ def back(t):
     return t.double().cpu().numpy()
 
 
-def act_error(z, value):
+def act_error(z, value, short=False):
     """Of an activation's value (or slope, given as its size) at z in float32: Phi's polynomial is within 6 U, the exponential of z^2 / 2 or of z within
-    z^2 + 2 |z| units for its argument's roundings, and some ten roundings follow; values too small for a float are lost."""
-    return np.abs(value) * (24 + 2 * z * z + 4 * np.abs(z)) * U + 1e-37
+    z^2 + 2 |z| units for its argument's roundings, and some ten roundings follow; values too small for a float are lost.  short: GELU for values that are
+    rounded to bfloat16 next, whose polynomial is within 3.2e-5 of Phi below zero (Phi of the opposite above zero is the smaller part)."""
+    return np.abs(value) * ((24 + 2 * z * z + 4 * np.abs(z)) * U + (3.2e-5 if short else 0)) + 1e-37
 
 
 def rng_state(dev, key=0x123456789ABCDEF, call=(7 << 32) + 5):
