@@ -251,3 +251,14 @@ def test_gelu_where_it_is_small_and_large(dev):
         want = O.act(z64, T.ACTS[act])
         tol = T.act_error(z64, want, act == "gelu")
         assert (np.abs(T.back(short) - want) <= tol + T.half_unit("bf16") * (np.abs(want) + tol)).all()
+
+
+@pytest.mark.parametrize("N,K,C", [(845, 427, 1829), (701, 301, 3001), (2045, 509, 2043), (520, 1210, 1100), (260, 1030, 2050), (1100, 1030, 515), (1024, 1024, 1024)])
+def test_float32_products_of_middle_size(dev, N, K, C):
+    """By halves and quarters of the large tiles, k whole and in parts."""
+    _forward(dev, N, K, C, "silu", "f32")
+
+
+@pytest.mark.parametrize("B,P,K,C", [(6, 100, 2401, 601), (4, 511, 509, 2045), (3, 500, 1500, 1500), (7, 100, 1500, 300), (1030, 1, 700, 1100)])
+def test_backward_of_float32_products_of_middle_size(dev, B, P, K, C):
+    _backward(dev, B, P, K, C, "gelu", "f32")
