@@ -114,10 +114,10 @@ __device__ __forceinline__ void finish_tile(f16v (&acc)[MT][NT], float* turn, ui
     }
 }
 
-// Bound by the matrix instructions at the clock that the card keeps under them.  bfloat16, 16384 rows: 8192 to 2048 with dropout and residual 457 us, 1.20 PFLOP/s; 2048 to 8192 448, with gelu and z
-// kept 525-537, since nothing of another tile runs beside a workgroup's end, and gelu is some 26 issue slots an element; its backward product 430-440.  (Two workgroups of 256 x 128 a compute unit,
-// whose ends would overlap: 498 and 605 with results stored into the caches, 477 and 551 past them, against 510 and 568, 460 and 536 then; 128 x 128 a wave, four of them: 803.)  float32, 4096^3: 663 us,
-// 207 TFLOP/s.
+// Bound by the matrix instructions at the clock that the power limit leaves: pipes two thirds busy at 1.7-1.8 GHz of 2.4.  bfloat16, 16384 rows, us from card to card: 8192 to 2048 418-430, with dropout
+// and residual 453-475 (1.16-1.21 PFLOP/s); 2048 to 8192 437-485, with gelu and z kept 509-557, since nothing of another tile runs beside a workgroup's end: z is 20 us of it, gelu 40; its backward product
+// 430-460.  (Two workgroups of 256 x 128 a compute unit, whose ends would overlap: 477 and 551 against 460 and 536 then; four waves of 128 x 128, two thirds of the reads from LDS but one wave a
+// SIMD: 485 and 574 against 450 and 527.)  float32, 4096^3: 636 us, 216 TFLOP/s.
 template <typename Shape, typename T, bool kMixed>
 __global__ __launch_bounds__(Shape::NW * 64, 2) void k_linear(LinearArgs A) {
     __shared__ __attribute__((aligned(1024))) uint8_t sh[Shape::kLds];
