@@ -464,6 +464,7 @@ __global__ __launch_bounds__(256) void k_linear_slope(SlopeArgs A) {
 typedef TileShape<256, 256, 64, 128, 64, 2, 1, 1> Large;     // bfloat16 (with 128 x 64 a wave 16384 x 2048 x 8192 462 us, so 448; k in steps of 32 the same)
 typedef TileShape<128, 128, 64, 64, 64, 2, 1, 1> Small;      // two workgroups a compute unit
 typedef TileShape<128, 128, 64, 32, 64, 4, 1, 1> Deep;       // one: what two would hide of each other's waits, four stages and two waves a SIMD have to
+typedef TileShape<128, 64, 64, 32, 64, 3, 1, 1> Narrow;      // where those leave compute units idle
 typedef TileShape<128, 128, 64, 32, 64, 3, 1, 2> Small2;     // dX from two planes of dz
 typedef TileShape<256, 128, 64, 64, 32, 2, 3, 3> Cut;        // float32: the largest that registers and LDS hold, and, where those leave compute units idle,
 typedef TileShape<128, 128, 64, 32, 32, 3, 3, 3> CutMid;     // halves
@@ -472,13 +473,13 @@ typedef TileShape<128, 64, 64, 32, 32, 4, 3, 3> CutSmall;    // and quarters of 
 static uint32_t up8(uint32_t x) { return (x + 7u) / 8u * 8u; }
 static uint64_t tiles(uint32_t a, uint32_t ta, uint32_t b, uint32_t tb) { return (uint64_t)((a + ta - 1) / ta) * ((b + tb - 1) / tb); }
 
-enum class Tile { kLarge, kSmall, kSmall2, kCut, kCutMid, kCutSmall, kThin, kDeep };
+enum class Tile { kLarge, kSmall, kSmall2, kCut, kCutMid, kCutSmall, kThin, kDeep, kNarrow };
 // How a product [N, M] over K is formed: the cheapest of its forms by what they take on this card, in us (the kernels, not the call).
 //   thin    workgroups in turn on 256 compute units, 3 us each and its operands' rows at 41 GB/s, where rows of x, of which a load takes 64 bytes, count twice.  (estimate and
 //           measured, bfloat16: 1 x 4096 x 4096 in 64 columns, four parts of k 13.8 and 11.6, whole 22 and 20; 256 x 2048 x 2048 15.8 and 11.5; 1024^3 19 and 14.6; float32: 1024^3 38 and 35,
 //           128 x 4096 x 4096 54 and 61, 2048 x 512 x 2048 75 and 65)
-//   tiles   in turn too: of 128 x 128 and 64 k bfloat16 0.55 us a step, from two planes of dz 0.9, and 2.5 before and after.  (2048^3 20 and 24;
-//           512 x 4096 x 4096 in two parts 32 and 33.)  float32, of 32 k, after its operands were laid out: 256 x 128 2.15 us a step, 128 x 128 1.05, 128 x 64 0.7.  (4096^3 645 and 636, 691 and 830 by
+//   tiles   in turn too: of 128 x 128 and 64 k bfloat16 0.55 us a step, from two planes of dz 0.9, of 128 x 64 0.4, and 2.5 before and after.  (2048^3 20 and 24, of
+//           128 x 64 31 and 29; 512 x 4096 x 4096 in two parts 32 and 33; 512 x 2048 x 2048 20 and 17.7, of 128 x 64 15.3 and 14.6.)  float32, of 32 k, after its operands were laid out: 256 x 128 2.15 us a step, 128 x 128 1.05, 128 x 64 0.7.  (4096^3 645 and 636, 691 and 830 by
 //           the smaller ones; 2048^3 119 and 136, 103 and 105, 128 and 124; 840 x 424 x 1832 44 and 40, 30 and 30, 25 and 28; in thin 33 and 35)
 // A long k is shared out, in thin or by tiles, where that gives idle compute units work: the second kernel that adds the parts takes 6 us and their way through memory.
 // Rows of an odd number of bfloat16 are laid out at whole pieces first: a load at an odd element takes three times as long (129 x 1331 from 4513: 90 us, from 4512 27).
@@ -494,7 +495,7 @@ static double thin_plan(int dtype, uint32_t N, uint32_t M, uint32_t K, uint32_t 
         if ((q.v < 2u && !f32) || (q.t == 2u && N <= 16u)) continue;
         const uint64_t n = tiles(M, 16u * q.v, N, 16u * q.t);
         if (n > (1u << 20)) continue;                        // (a launch has fewer than 2^32 threads)
-        for (uint32_t splits = 1; splits <= 16u && (splits == 1u || (K / splits >= 512u && n * splits <= 512u)); splits *= 2u) {
+        for (uint32_t splits = 1; splits <= 16u && (splits == 1u || (K / splits >= 512u && n * splits <= 2048u)); splits *= 2u) {
             const double us = rounds(n * splits) * (3. + (double)K / splits * (q.v + 2u * q.t * (f32 ? 1u : planes_b)) * (f32 ? 64. : 32.) / 41e3) + join_us(splits, N, M);
             if (us < least) { least = us; best = ProductPlan{Tile::kThin, splits, q.v, q.t, 0}; }
         }
@@ -510,7 +511,7 @@ static ProductPlan product_plan(int dtype, uint32_t N, uint32_t M, uint32_t K, u
     ProductPlan L, thin;
     double us = 1e30;
     auto by_tiles = [&](Tile tile, uint64_t n, uint32_t k, double start, double step) {
-        for (uint32_t splits = 1; splits <= 32u && (splits == 1u || (K / splits >= 256u && n * splits <= 256u)); splits *= 2u) {
+        for (uint32_t splits = 1; splits <= 32u && (splits == 1u || (K / splits >= 256u && n * splits <= 512u)); splits *= 2u) {
             const double t = rounds(n * splits) * (start + step * (double)((K + k - 1u) / k) / splits) + join_us(splits, N, M);
             if (t < us) { us = t; L = ProductPlan{tile, splits, 0, 0, 0}; }
         }
@@ -521,7 +522,10 @@ static ProductPlan product_plan(int dtype, uint32_t N, uint32_t M, uint32_t K, u
         by_tiles(Tile::kCutSmall, tiles(M, 128, N, 64), 32u, 4., 0.7);
     } else if (planes_b == 2u) by_tiles(Tile::kSmall2, small, 64u, 2.5, 0.9);
     else if (large >= 192u) by_tiles(Tile::kLarge, large, 64u, 2.5, 0.55);
-    else by_tiles(small > 256u ? Tile::kSmall : Tile::kDeep, small, 64u, 2.5, 0.55);
+    else {
+        by_tiles(small > 256u ? Tile::kSmall : Tile::kDeep, small, 64u, 2.5, 0.55);
+        by_tiles(Tile::kNarrow, tiles(M, 128, N, 64), 64u, 2.5, 0.4);
+    }
     us += (f32 || odd_w || M % 8u ? layout_us((double)K * M) : 0.) + (f32 || K % 8u ? layout_us((double)N * K) : 0.);
     if (K >= (f32 ? 4u : 8u) && M >= 4u) {                   // (what a place past an edge is moved back by)
         const double by_thin = thin_plan(dtype, N, M, K, planes_b, thin) + (!f32 && odd_w ? layout_us((double)K * M) : 0.);
@@ -555,6 +559,7 @@ static int launch_product(const ProductPlan& L, LinearArgs A, hipStream_t stream
     else if (L.tile == Tile::kLarge) VGC_LAUNCH(Large);
     else if (L.tile == Tile::kSmall) VGC_LAUNCH(Small);
     else if (L.tile == Tile::kDeep) VGC_LAUNCH(Deep);
+    else if (L.tile == Tile::kNarrow) VGC_LAUNCH(Narrow);
     else if constexpr (!kMixed) VGC_LAUNCH(Small2);
 #undef VGC_LAUNCH
     int rc = hip_check(hipGetLastError(), "launch k_linear");

@@ -262,3 +262,14 @@ def test_float32_products_of_middle_size(dev, N, K, C):
 @pytest.mark.parametrize("B,P,K,C", [(6, 100, 2401, 601), (4, 511, 509, 2045), (3, 500, 1500, 1500), (7, 100, 1500, 300), (1030, 1, 700, 1100)])
 def test_backward_of_float32_products_of_middle_size(dev, B, P, K, C):
     _backward(dev, B, P, K, C, "gelu", "f32")
+
+
+@pytest.mark.parametrize("N,K,C", [(500, 2056, 2000), (1001, 1031, 1096), (390, 2049, 2051), (1024, 4096, 1024)])
+def test_bfloat16_products_of_middle_size(dev, N, K, C):
+    """By narrow tiles, k whole and in parts."""
+    _forward(dev, N, K, C, "gelu", "bf16")
+
+
+@pytest.mark.parametrize("B,P,K,C", [(2, 512, 2048, 2048), (7, 100, 1700, 2001)])
+def test_backward_of_bfloat16_products_of_middle_size(dev, B, P, K, C):
+    _backward(dev, B, P, K, C, "silu", "bf16")
