@@ -365,7 +365,8 @@ int launch_linear_backward(const LinearCall& L, void* workspace, hipStream_t str
 
 // Softmax cross entropy of a linear layer (vgc_softmax_loss.hip)
 // R rows of K elements as bfloat16 planes (one of bfloat16 rows, three of float32), rows padded with zeros to a multiple of 8, planes R rows apart
-int launch_plane_rows(int dtype, const void* src, uint32_t R, uint32_t K, uint16_t* dst, hipStream_t stream);
+struct PlaneRows { const void* src; uint32_t R, K; uint16_t* dst; };
+int launch_plane_rows(int dtype, const PlaneRows& first, const PlaneRows& second, hipStream_t stream);      // (second: {} for none)
 size_t softmax_loss_workspace_bytes(int dtype, uint32_t N, uint32_t H, uint32_t V);
 int launch_softmax_loss(int dtype, const void* X, const void* W, const int64_t* target, uint32_t N, uint32_t H, uint32_t V, float* loss, float* lse,
                         void* workspace, hipStream_t stream);

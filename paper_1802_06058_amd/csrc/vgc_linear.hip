@@ -482,7 +482,7 @@ enum class Tile { kLarge, kSmall, kSmall2, kCut, kCutMid, kCutSmall, kThin, kDee
 //           128 x 64 31 and 29; 512 x 4096 x 4096 in two parts 32 and 33; 512 x 2048 x 2048 20 and 17.7, of 128 x 64 15.3 and 14.6.)  float32, of 32 k, after its operands were laid out: 256 x 128 2.15 us a step, 128 x 128 1.05, 128 x 64 0.7.  (4096^3 645 and 636, 691 and 830 by
 //           the smaller ones; 2048^3 119 and 136, 103 and 105, 128 and 124; 840 x 424 x 1832 44 and 40, 30 and 30, 25 and 28; in thin 33 and 35)
 // A long k is shared out, in thin or by tiles, where that gives idle compute units work: the second kernel that adds the parts takes 6 us and their way through memory.
-// Rows of an odd number of bfloat16 are laid out at whole pieces first: a load at an odd element takes three times as long (129 x 1331 from 4513: 90 us, from 4512 27).
+// Where both operands are laid out, one launch does it (840 x 424 x 1832 float32 27.6 -> 25.2 us).  Rows of an odd number of bfloat16 are laid out at whole pieces first: a load at an odd element takes three times as long (129 x 1331 from 4513: 90 us, from 4512 27).
 struct ProductPlan { Tile tile; uint32_t splits, v, t; size_t parts; };    // thin: kV and NT
 static double rounds(uint64_t groups) { return (double)((groups + 255u) / 256u); }
 static double join_us(uint32_t splits, uint32_t N, uint32_t M) { return splits == 1u ? 0. : 6. + (double)splits * N * M * 4e-6 / 3.; }
@@ -610,8 +610,9 @@ int launch_linear(const LinearCall& q, void* workspace, hipStream_t stream) {
     uint16_t *x = (uint16_t*)(ws + L.x), *w = (uint16_t*)(ws + L.w);
     const Finish F = {q.bias, q.residual, q.z, q.y, N, q.C, q.act, dropout_of(q.p, q.rng), past(q.dtype, N, q.C, q.K, q.z, q.y)};
     int rc;
-    if (!L.x_there && (rc = launch_plane_rows(q.dtype, q.X, N, q.K, x, stream)) != VGC_OK) return rc;
-    if (!L.w_there && (rc = launch_plane_rows(q.dtype, q.W, q.K, q.C, w, stream)) != VGC_OK) return rc;
+    const PlaneRows X = {q.X, N, q.K, x}, W = {q.W, q.K, q.C, w};
+    if (!L.x_there && (rc = launch_plane_rows(q.dtype, X, L.w_there ? PlaneRows{} : W, stream)) != VGC_OK) return rc;
+    if (L.x_there && !L.w_there && (rc = launch_plane_rows(q.dtype, W, {}, stream)) != VGC_OK) return rc;
     float* parts = (float*)(ws + L.parts);
     if (L.product.tile == Tile::kThin) {
         if (q.dtype == VGC_F32)
@@ -688,7 +689,7 @@ int launch_linear_backward(const LinearCall& q, void* workspace, hipStream_t str
     if (q.s_bias && !L.direct && (rc = launch_column_sums(S.partial, 1, L.groups, q.B, L.samples_parts, q.C, L.whole, q.c, q.g_bias, q.s_bias, nullptr, nullptr, stream)) != VGC_OK) return rc;
     if (!q.dX) return VGC_OK;
     const Finish F = {nullptr, q.residual, nullptr, q.dX, N, q.K, VGC_ACT_NONE, Dropout{nullptr, 0u, 0.f}, past(q.dtype, N, q.K, q.C, nullptr, q.dX)};
-    if (!L.w_there && (rc = launch_plane_rows(q.dtype, q.W, q.K, q.C, w, stream)) != VGC_OK) return rc;
+    if (!L.w_there && (rc = launch_plane_rows(q.dtype, {q.W, q.K, q.C, w}, {}, stream)) != VGC_OK) return rc;
     float* parts = (float*)(ws + L.parts);
     if (L.product.tile == Tile::kThin) {
         if (q.dtype == VGC_F32)

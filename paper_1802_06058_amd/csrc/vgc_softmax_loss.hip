@@ -27,17 +27,19 @@
 namespace vgc {
 
 // ---- operands -------------------------------------------------------------------------------------------------------------
-// Rows as they are, padded with zeros to whole pieces of 8.
+// Rows as they are, padded with zeros to whole pieces of 8; of one matrix or two, whose workgroups follow each other.
 template <typename T>
-__global__ __launch_bounds__(256) void k_planes_rows(const T* __restrict__ src, uint32_t R, uint32_t K, uint32_t Kp, uint16_t* __restrict__ dst) {
-    const uint32_t per_row = Kp / 8u;
-    const uint64_t i = (uint64_t)blockIdx.x * 256u + threadIdx.x;
-    if (i >= (uint64_t)R * per_row) return;
+__global__ __launch_bounds__(256) void k_planes_rows(PlaneRows first, PlaneRows second, uint32_t groups) {
+    const bool other = blockIdx.x >= groups;
+    const PlaneRows M = other ? second : first;
+    const uint32_t Kp = (M.K + 7u) / 8u * 8u, per_row = Kp / 8u;
+    const uint64_t i = (uint64_t)(blockIdx.x - (other ? groups : 0u)) * 256u + threadIdx.x;
+    if (i >= (uint64_t)M.R * per_row) return;
     const uint64_t row = i / per_row;
     const uint32_t k = (uint32_t)(i - row * per_row) * 8u;
     float f[8];
-    widen8(load8(src + row * K + k, (int)(K - k)), f);
-    store_planes<T>(dst + row * Kp + k, (uint64_t)R * Kp, f);
+    widen8(load8(static_cast<const T*>(M.src) + row * M.K + k, (int)(M.K - k)), f);
+    store_planes<T>(M.dst + row * Kp + k, (uint64_t)M.R * Kp, f);
 }
 
 // Positions: sample z's position p is number z Pp + p, P <= Pp; the numbers between are no positions.
@@ -775,11 +777,12 @@ static int launch_logits(LogitsTile t, int dtype, const ThinArgs& R, const LossA
     return hip_check(hipGetLastError(), "launch k_logits");
 }
 
-int launch_plane_rows(int dtype, const void* src, uint32_t R, uint32_t K, uint16_t* dst, hipStream_t stream) {
-    const uint32_t Kp = up8(K);
-    const dim3 grid((uint32_t)(((uint64_t)R * (Kp / 8u) + 255u) / 256u));
-    if (dtype == VGC_BF16) hipLaunchKernelGGL(k_planes_rows<uint16_t>, grid, dim3(256), 0, stream, (const uint16_t*)src, R, K, Kp, dst);
-    else hipLaunchKernelGGL(k_planes_rows<float>, grid, dim3(256), 0, stream, (const float*)src, R, K, Kp, dst);
+int launch_plane_rows(int dtype, const PlaneRows& first, const PlaneRows& second, hipStream_t stream) {
+    auto groups_of = [](const PlaneRows& M) { return (uint32_t)(((uint64_t)M.R * (up8(M.K) / 8u) + 255u) / 256u); };
+    const uint32_t groups = groups_of(first);
+    const dim3 grid(groups + groups_of(second));
+    if (dtype == VGC_BF16) hipLaunchKernelGGL(k_planes_rows<uint16_t>, grid, dim3(256), 0, stream, first, second, groups);
+    else hipLaunchKernelGGL(k_planes_rows<float>, grid, dim3(256), 0, stream, first, second, groups);
     return hip_check(hipGetLastError(), "launch k_planes_rows");
 }
 
@@ -840,13 +843,13 @@ int launch_softmax_loss(int dtype, const void* X, const void* W, const int64_t* 
     A.partial = reinterpret_cast<float2*>(ws + L.partial);
     A.picked = reinterpret_cast<float*>(ws + L.picked);
     uint16_t *xs = reinterpret_cast<uint16_t*>(ws + L.x), *wp = reinterpret_cast<uint16_t*>(ws + L.w);
-    if (!L.rows.in_place && (rc = launch_plane_rows(dtype, X, N, H, xs, stream)) != VGC_OK) return rc;
+    if (!L.rows.in_place && (rc = launch_plane_rows(dtype, {X, N, H, xs}, {}, stream)) != VGC_OK) return rc;
     A.x = matrix_of(L.rows, X, xs, N, H);
     for (uint32_t v0 = 0; v0 < V; v0 += L.piece) {
         A.v0 = v0;
         A.V = std::min(L.piece, V - v0);
         const char* rows = static_cast<const char*>(W) + (size_t)v0 * H * size;
-        if (!L.rows.in_place && (rc = launch_plane_rows(dtype, rows, A.V, H, wp, stream)) != VGC_OK) return rc;
+        if (!L.rows.in_place && (rc = launch_plane_rows(dtype, {rows, A.V, H, wp}, {}, stream)) != VGC_OK) return rc;
         A.w = matrix_of(L.rows, rows, wp, A.V, H);
         A.block0 = v0 / logits_block(L.tile);
         if ((rc = launch_logits<true>(L.tile, dtype, ThinArgs{A.w.base, A.x.base, A.w.ld, A.x.ld}, A, stream)) != VGC_OK) return rc;
@@ -939,7 +942,7 @@ int launch_softmax_loss_backward(int dtype, const void* X, const void* W, const 
     A.planes = dtype == VGC_F32 || by_position ? L.planes : 1u;
     if (P == 1 && (s_out || L.dx_thin)) A.d32 = (float*)(ws + L.d32);
     if (dtype == VGC_BF16 && dX && !L.dx_thin) A.rest = (float*)(ws + L.rest);
-    if (!L.rows.in_place && (rc = launch_plane_rows(dtype, X, N, H, xs, stream)) != VGC_OK) return rc;
+    if (!L.rows.in_place && (rc = launch_plane_rows(dtype, {X, N, H, xs}, {}, stream)) != VGC_OK) return rc;
     A.x = matrix_of(L.rows, X, xs, N, H);
     if (by_position) {
         const dim3 grid((L.Lq + 63u) / 64u, (H + 63u) / 64u);
@@ -959,7 +962,7 @@ int launch_softmax_loss_backward(int dtype, const void* X, const void* W, const 
         A.V = std::min(L.piece, V - v0);
         A.plane = (uint64_t)A.V * L.Lq;
         const char* rows = static_cast<const char*>(W) + (size_t)v0 * H * size;
-        if (!L.rows.in_place && (rc = launch_plane_rows(dtype, rows, A.V, H, wp, stream)) != VGC_OK) return rc;
+        if (!L.rows.in_place && (rc = launch_plane_rows(dtype, {rows, A.V, H, wp}, {}, stream)) != VGC_OK) return rc;
         A.w = matrix_of(L.rows, rows, wp, A.V, H);
         ThinArgs R = {A.w.base, A.x.base, A.w.ld, A.x.ld};
         if (dtype == VGC_F32) R = ThinArgs{rows, X, H, H};   // (as floats, also where the planes are there for dX)
