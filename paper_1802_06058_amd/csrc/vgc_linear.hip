@@ -119,7 +119,7 @@ __device__ __forceinline__ void finish_tile(f16v (&acc)[MT][NT], float* turn, ui
 // 430-460.  (Two workgroups of 256 x 128 a compute unit, whose ends would overlap: 477 and 551 against 460 and 536 then; four waves of 128 x 128, two thirds of the reads from LDS but one wave a
 // SIMD: 485 and 574 against 450 and 527.)  float32, 4096^3: 636 us, 216 TFLOP/s.
 template <typename Shape, typename T, bool kMixed>
-__global__ __launch_bounds__(Shape::NW * 64, 2) void k_linear(LinearArgs A) {
+__global__ __launch_bounds__(Shape::NW * 64, Shape::NW / 4 * (160 * 1024 / Shape::kLds)) void k_linear(LinearArgs A) {
     __shared__ __attribute__((aligned(1024))) uint8_t sh[Shape::kLds];
     static_assert(Shape::NW * kTurnBytes <= Shape::kLds, "room to turn");
     const uint32_t tiles_n = (A.F.N + Shape::BN - 1) / Shape::BN, tiles_m = (A.F.M + Shape::BM - 1) / Shape::BM;
@@ -475,14 +475,17 @@ static uint64_t tiles(uint32_t a, uint32_t ta, uint32_t b, uint32_t tb) { return
 
 enum class Tile { kLarge, kSmall, kSmall2, kCut, kCutMid, kCutSmall, kThin, kDeep, kNarrow };
 // How a product [N, M] over K is formed: the cheapest of its forms by what they take on this card, in us (the kernels, not the call).
-//   thin    workgroups in turn on 256 compute units, 3 us each and its operands' rows at 41 GB/s, where rows of x, of which a load takes 64 bytes, count twice.  (estimate and
-//           measured, bfloat16: 1 x 4096 x 4096 in 64 columns, four parts of k 13.8 and 11.6, whole 22 and 20; 256 x 2048 x 2048 15.8 and 11.5; 1024^3 19 and 14.6; float32: 1024^3 38 and 35,
-//           128 x 4096 x 4096 54 and 61, 2048 x 512 x 2048 75 and 65)
-//   tiles   in turn too: of 128 x 128 and 64 k bfloat16 0.55 us a step, from two planes of dz 0.9, of 128 x 64 0.4, and 2.5 before and after.  (2048^3 20 and 24, of
-//           128 x 64 31 and 29; 512 x 4096 x 4096 in two parts 32 and 33; 512 x 2048 x 2048 20 and 17.7, of 128 x 64 15.3 and 14.6.)  float32, of 32 k, after its operands were laid out: 256 x 128 2.15 us a step, 128 x 128 1.05, 128 x 64 0.7.  (4096^3 645 and 636, 691 and 830 by
-//           the smaller ones; 2048^3 119 and 136, 103 and 105, 128 and 124; 840 x 424 x 1832 44 and 40, 30 and 30, 25 and 28; in thin 33 and 35)
+//   thin    workgroups in turn on 256 compute units, 3 us each and its operands' rows at 41 GB/s, where rows of x, of which a load takes 64 bytes, count twice.
+//           (estimate and measured, bfloat16: 1 x 4096 x 4096 in 64 columns, four parts of k 13.8 and 11.6, whole 22 and 20; 256 x 2048 x 2048 15.8 and 11.5; float32:
+//           1000^3 31 and 35, 128 x 4096 x 4096 54 and 61, 2048 x 512 x 2048 75 and 65)
+//   tiles   in turn too, 2.5-4 us before and after a tile's steps.  bfloat16, of 64 k: 128 x 128 0.55 us a step, from two planes of dz 0.9, 128 x 64 0.4.  (2048^3 20 and
+//           24, of 128 x 64 31 and 29; 512 x 4096 x 4096 in two parts 32 and 33; 512 x 2048 x 2048 20 and 17.7, of 128 x 64 15.3 and 14.6.)  float32, of 32 k, after the
+//           operands were laid out: 256 x 128 2.15 us a step, 128 x 128 1.05, 128 x 64 0.7.  (4096^3 645 and 636, of the smaller ones 691 and 830; 2048^3 119 and 136, 103
+//           and 105, 128 and 124; 840 x 424 x 1832 44 and 40, 30 and 30, 25 and 28; in thin 33 and 35)
 // A long k is shared out, in thin or by tiles, where that gives idle compute units work: the second kernel that adds the parts takes 6 us and their way through memory.
-// Where both operands are laid out, one launch does it (840 x 424 x 1832 float32 27.6 -> 25.2 us).  Rows of an odd number of bfloat16 are laid out at whole pieces first: a load at an odd element takes three times as long (129 x 1331 from 4513: 90 us, from 4512 27).
+// (more workgroups than units, for a last round less empty: 8815 x 6464 x 64 float32 in four parts 130, whole 183.)
+// Where both operands are laid out, one launch does it (840 x 424 x 1832 float32 27.6 -> 25.2).  Rows of an odd number of bfloat16 are laid out at whole pieces first: a
+// load at an odd element takes three times as long (129 x 1331 from 4513: 90 us, from 4512 27).
 struct ProductPlan { Tile tile; uint32_t splits, v, t; size_t parts; };    // thin: kV and NT
 static double rounds(uint64_t groups) { return (double)((groups + 255u) / 256u); }
 static double join_us(uint32_t splits, uint32_t N, uint32_t M) { return splits == 1u ? 0. : 6. + (double)splits * N * M * 4e-6 / 3.; }
