@@ -727,10 +727,12 @@ def softmax_loss_backward(X, W, target, lse, weight, c, dX, s_out, g_out=None, w
                                             _ptr(g_out), _ptr(s_out), _ptr(workspace), has, _stream()))
 
 
-def _need_current(t, what):
-    """The calls below run on the current device's stream, so that is where their tensors have to be."""
-    if t.get_device() != torch.cuda.current_device():
-        raise VgcError(f"{what}: tensor is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+def _stream_of(t, what):
+    """The current stream, on which the calls below run: its device is where their tensors have to be."""
+    device = torch.cuda.current_device()
+    if t.get_device() != device:
+        raise VgcError(f"{what}: tensor is on {t.device}, the current device is cuda:{device}")
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
 def dropout(x, p, rng, y, residual=None):
@@ -739,8 +741,7 @@ def dropout(x, p, rng, y, residual=None):
     kernel runs.  The backward pass is the same call on the gradient of y."""
     R, Cc, dtype = _rows(x, "x")
     _need_all(((x, 0, x.dtype, "x"), (residual, R * Cc, x.dtype, "residual"), (rng, 2, torch.int64, "rng"), (y, R * Cc, x.dtype, "y")))
-    _need_current(x, "x")
-    _check(load().vgc_dropout(dtype, _ptr(x), _ptr(residual), R, Cc, float(p), _ptr(rng), _ptr(y), _stream()))
+    _check(load().vgc_dropout(dtype, _ptr(x), _ptr(residual), R, Cc, float(p), _ptr(rng), _ptr(y), _stream_of(x, "x")))
 
 
 def linear_workspace_bytes(dtype, N, K, Cc):
@@ -767,9 +768,8 @@ def linear(X, W, y, bias=None, act=ACT_NONE, z=None, residual=None, p=0.0, rng=N
     has = _need_workspace(workspace, nbytes)
     _need_all(((X, 0, X.dtype, "X"), (W, 0, X.dtype, "W"), (bias, Cc, torch.float32, "bias"), (residual, R * Cc, X.dtype, "residual"),
                (z, R * Cc, X.dtype, "z"), (y, R * Cc, X.dtype, "y"), (rng, 2, torch.int64, "rng"), (workspace, nbytes, torch.uint8, "workspace")))
-    _need_current(X, "X")
     _check(load().vgc_linear(dtype, _ptr(X), _ptr(W), _ptr(bias), act, float(p), _ptr(rng), _ptr(residual), R, K, Cc, _ptr(z), _ptr(y),
-                             _ptr(workspace), has, _stream()))
+                             _ptr(workspace), has, _stream_of(X, "X")))
 
 
 def linear_backward_workspace_bytes(dtype, B, P, K, Cc):
@@ -792,9 +792,8 @@ def linear_backward(dy, z, W, act, c, dz, dX=None, s_bias=None, g_bias=None, add
     _need_all(((dy, 0, dy.dtype, "dy"), (z, R * Cc, dy.dtype, "z"), (W, 0, dy.dtype, "W"), (add, R * K, dy.dtype, "add"), (dz, R * Cc, dy.dtype, "dz"),
                (dX, R * K, dy.dtype, "dX"), (s_bias, Cc, f32, "s_bias"), (g_bias, Cc, f32, "g_bias"), (rng, 2, torch.int64, "rng"),
                (workspace, nbytes, torch.uint8, "workspace")))
-    _need_current(dy, "dy")
     _check(load().vgc_linear_backward(dtype, _ptr(dy), _ptr(z), _ptr(W), act, float(p), _ptr(rng), _ptr(add), B, P, K, Cc, float(c), _ptr(dz), _ptr(dX),
-                                      _ptr(g_bias), _ptr(s_bias), _ptr(workspace), has, _stream()))
+                                      _ptr(g_bias), _ptr(s_bias), _ptr(workspace), has, _stream_of(dy, "dy")))
 
 
 def _group_norm_shape(x, what, mean):
@@ -818,9 +817,8 @@ def group_norm(x, gamma, beta, eps, act, y, mean, rstd, workspace=None):
     has = _need_workspace(workspace, nbytes)
     _need_all(((x, 0, x.dtype, "x"), (gamma, Cc, f32, "gamma"), (beta, Cc, f32, "beta"), (y, n, x.dtype, "y"), (mean, B * G, f32, "mean"),
                (rstd, B * G, f32, "rstd"), (workspace, nbytes, torch.uint8, "workspace")))
-    _need_current(x, "x")
     _check(load().vgc_group_norm(dtype, _ptr(x), B, P, Cc, G, _ptr(gamma), _ptr(beta), float(eps), act, _ptr(y), _ptr(mean), _ptr(rstd),
-                                 _ptr(workspace), has, _stream()))
+                                 _ptr(workspace), has, _stream_of(x, "x")))
 
 
 def group_norm_backward_workspace_bytes(dtype, B, P, Cc, G):
@@ -837,6 +835,5 @@ def group_norm_backward(dy, x, mean, rstd, gamma, beta, act, c, dx, s_gamma, s_b
     _need_all(((dy, 0, dy.dtype, "dy"), (x, n, dy.dtype, "x"), (mean, B * G, f32, "mean"), (rstd, B * G, f32, "rstd"), (gamma, Cc, f32, "gamma"),
                (beta, Cc, f32, "beta"), (dx, n, dy.dtype, "dx"), (s_gamma, Cc, f32, "s_gamma"), (s_beta, Cc, f32, "s_beta"),
                (g_gamma, Cc, f32, "g_gamma"), (g_beta, Cc, f32, "g_beta"), (workspace, nbytes, torch.uint8, "workspace")))
-    _need_current(dy, "dy")
     _check(load().vgc_group_norm_backward(dtype, _ptr(dy), _ptr(x), _ptr(mean), _ptr(rstd), _ptr(gamma), _ptr(beta), act, B, P, Cc, G, float(c),
-                                          _ptr(dx), _ptr(g_gamma), _ptr(s_gamma), _ptr(g_beta), _ptr(s_beta), _ptr(workspace), has, _stream()))
+                                          _ptr(dx), _ptr(g_gamma), _ptr(s_gamma), _ptr(g_beta), _ptr(s_beta), _ptr(workspace), has, _stream_of(dy, "dy")))
