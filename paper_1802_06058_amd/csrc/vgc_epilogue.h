@@ -14,22 +14,12 @@ namespace vgc {
 // Phi(-a) = e^(-a^2 / 2) E(a) for a >= 0, and E, which falls like 1 / a, is t times a polynomial in t = 1 / (1 + 0.35 a): of degree 8, its
 // coefficients fitted to E on 0 <= a <= 14 so that the largest relative error is least (3.3e-8; 3.3e-7 evaluated in float32).  Small values
 // of Phi so keep their digits, which 1 + erf does not, and the exponential serves the slope too.
-// kShort: of degree 4 in t = 1 / (1 + 0.375 a), within 3.2e-5, for a value that is rounded to bfloat16 next, whose half steps are 2^-9 to 2^-8 of it: four
-// issue slots of some 25 less, which show where matrix instructions wait for them (16384 x 2048 to 8192: with z kept, 523 us and 509).
+// One polynomial for both types: a shorter one within 3.2e-5 for values that are rounded to bfloat16 next took 14 us of 523 less (16384 x 2048 to 8192 with
+// z kept), but gave some of them the neighbour of the nearest bfloat16, 1.1e-4 off the nearest ones in the root mean square.
 struct Normal { float below, density; };                     // Phi(z), sqrt(2 pi) phi(z)
-template <bool kShort = false>
 __device__ __forceinline__ Normal normal_at(float z) {
-    const float a = fabsf(z), t = __builtin_amdgcn_rcpf(__builtin_fmaf(kShort ? 0.375f : 0.35f, a, 1.f));
+    const float a = fabsf(z), t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.35f, a, 1.f));
     const float e = __builtin_amdgcn_exp2f(z * z * -0.72134752f);          // (log2(e) / 2)
-    if constexpr (kShort) {
-        float p = -0.0906427652f;
-        p = __builtin_fmaf(p, t, 0.200281575f);
-        p = __builtin_fmaf(p, t, 0.0835641250f);
-        p = __builtin_fmaf(p, t, 0.157733962f);
-        p = __builtin_fmaf(p, t, 0.149061024f);
-        const float q = p * t * e;
-        return Normal{z > 0.f ? 1.f - q : q, e};
-    }
     float p = -0.0291574303f;
     p = __builtin_fmaf(p, t, 0.144028597f);
     p = __builtin_fmaf(p, t, -0.255833956f);
@@ -44,14 +34,13 @@ __device__ __forceinline__ Normal normal_at(float z) {
 }
 __device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.44269504f)); }
 
-template <bool kShort>
 __device__ __forceinline__ void apply_act(int act, float (&f)[8]) {        // (act is uniform)
     if (act == VGC_ACT_RELU) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) f[k] = f[k] < 0.f ? 0.f : f[k];
     } else if (act == VGC_ACT_GELU) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) f[k] *= normal_at<kShort>(f[k]).below;
+        for (int k = 0; k < 8; ++k) f[k] *= normal_at(f[k]).below;
     } else if (act == VGC_ACT_SILU) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) f[k] *= sigmoid(f[k]);

@@ -166,7 +166,7 @@ __global__ __launch_bounds__(kThreads) void k_group_norm(GroupNormArgs A) {
         widen8(raw[i], f);
 #pragma unroll
         for (int k = 0; k < 8; ++k) f[k] = scaled((f[k] - mean[kM == 8 ? k : 0]) * rstd[kM == 8 ? k : 0], ga[k], be[k]);
-        apply_act<false>((int)A.act, f);
+        apply_act((int)A.act, f);
         store8(y + (uint64_t)p * A.C, f, n);
     }
 }
@@ -409,7 +409,7 @@ __global__ __launch_bounds__(256) void k_group_norm_apply(GroupNormArgs A) {
         widen8(x[0], f);
 #pragma unroll
         for (int k = 0; k < 8; ++k) f[k] = scaled(K.xhat(f[k], k), K.gamma[k], K.beta[k]);
-        apply_act<false>((int)A.act, f);
+        apply_act((int)A.act, f);
         if (L.n > 0) store8_to(y + (uint64_t)p * A.C, f, L.n, A.past);
     });
 }

@@ -43,7 +43,7 @@ __device__ __forceinline__ void finish(const Finish& F, const DropoutKey& key, u
 #pragma unroll
     for (int k = 0; k < 8; ++k) f[k] += bias[k];
     if (F.z) store8_to(static_cast<T*>(F.z) + at, f, n, F.past);
-    apply_act<sizeof(T) == 2>(F.act, f);
+    apply_act(F.act, f);
     apply_dropout(F.drop, key, row, col / 8u, f);
     if (F.residual) {
         float g[8];
