@@ -57,6 +57,12 @@ ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2, 3
 
 HDR_DTYPE = np.dtype([("exp_field", "<u4"), ("count", "<u4"), ("word_offset", "<u8")])
 
+class U32:
+    """A tensor's size that the library takes as uint32.  C.c_uint32 would put any integer there modulo 2^32; here one that does not fit is no
+    argument (ctypes.ArgumentError).  It takes no longer than C.c_uint32."""
+    from_param = range(1 << 32).__getitem__
+
+
 EXPORTS = {
     # name: (restype, argtypes)
     "vgc_last_error": (C.c_char_p, []),
@@ -66,15 +72,15 @@ EXPORTS = {
     "vgc_scratch_bytes": (C.c_size_t, [C.c_void_p, C.c_uint32, C.c_uint64]),
     "vgc_scratch_bitmap_offset": (C.c_size_t, [C.c_void_p, C.c_uint32, C.c_uint64]),
     "vgc_plan_build": (C.c_int, [C.c_void_p, C.c_uint32, C.c_uint64, C.c_void_p, C.c_size_t]),
-    "vgc_sqgrad_workspace_bytes": (C.c_size_t, [C.c_int, C.c_int, C.c_uint32, C.c_uint32, C.c_uint32, C.c_uint32]),
-    "vgc_sqgrad": (C.c_int, [C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_uint32, C.c_uint32, C.c_uint32,
-                             C.c_uint32, C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
-    "vgc_sqgrad_noalloc": (C.c_int, [C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_uint32, C.c_uint32, C.c_uint32,
-                                     C.c_uint32, C.c_float, C.c_void_p, C.c_void_p, C.c_void_p]),
-    "vgc_sqgrad_conv2d_workspace_bytes": (C.c_size_t, [C.c_int] + [C.c_uint32] * 11),
-    "vgc_sqgrad_conv2d": (C.c_int, [C.c_int, C.c_void_p, C.c_void_p] + [C.c_uint32] * 11 +
+    "vgc_sqgrad_workspace_bytes": (C.c_size_t, [C.c_int, C.c_int, U32, U32, U32, U32]),
+    "vgc_sqgrad": (C.c_int, [C.c_int, C.c_int, C.c_void_p, C.c_void_p, U32, U32, U32,
+                             U32, C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "vgc_sqgrad_noalloc": (C.c_int, [C.c_int, C.c_int, C.c_void_p, C.c_void_p, U32, U32, U32,
+                                     U32, C.c_float, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "vgc_sqgrad_conv2d_workspace_bytes": (C.c_size_t, [C.c_int] + [U32] * 11),
+    "vgc_sqgrad_conv2d": (C.c_int, [C.c_int, C.c_void_p, C.c_void_p] + [U32] * 11 +
                           [C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
-    "vgc_sqgrad_conv2d_batch": (C.c_int, [C.c_void_p, C.c_uint32, C.c_void_p]),
+    "vgc_sqgrad_conv2d_batch": (C.c_int, [C.c_void_p, U32, C.c_void_p]),
     "vgc_accumulate_select": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p,
                                         C.c_uint32, C.c_void_p, C.c_float, C.c_float, C.c_void_p, C.c_void_p]),
     "vgc_accumulate_select_hybrid": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p,
@@ -83,10 +89,10 @@ EXPORTS = {
     "vgc_accumulate_select_range": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p,
                                               C.c_uint32, C.c_void_p, C.c_uint32, C.c_uint32, C.c_float, C.c_float,
                                               C.c_void_p, C.c_void_p]),
-    "vgc_sqgrad_accumulate_select_workspace_bytes": (C.c_size_t, [C.c_int, C.c_uint32, C.c_uint32, C.c_uint32]),
-    "vgc_sqgrad_accumulate_select": (C.c_int, [C.c_int, C.c_void_p, C.c_void_p, C.c_uint32, C.c_uint32, C.c_uint32, C.c_float,
-                                               C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p, C.c_uint32, C.c_void_p,
-                                               C.c_uint32, C.c_float, C.c_float, C.c_void_p, C.c_void_p, C.c_size_t,
+    "vgc_sqgrad_accumulate_select_workspace_bytes": (C.c_size_t, [C.c_int, U32, U32, U32]),
+    "vgc_sqgrad_accumulate_select": (C.c_int, [C.c_int, C.c_void_p, C.c_void_p, U32, U32, U32, C.c_float,
+                                               C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p, U32, C.c_void_p,
+                                               U32, C.c_float, C.c_float, C.c_void_p, C.c_void_p, C.c_size_t,
                                                C.c_void_p, C.c_void_p, C.c_void_p]),
     "vgc_pack": (C.c_int, [C.c_uint64, C.c_void_p, C.c_uint32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint64,
                            C.c_void_p, C.c_void_p, C.c_void_p]),
@@ -103,33 +109,33 @@ EXPORTS = {
     "vgc_unpack_apply": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint32, C.c_void_p, C.c_uint32,
                                    C.c_void_p, C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint64,
                                    C.c_void_p]),
-    "vgc_act8_encode": (C.c_int, [C.c_int, C.c_void_p, C.c_uint64, C.c_uint32, C.c_void_p, C.c_void_p, C.c_void_p]),
-    "vgc_act8_decode": (C.c_int, [C.c_int, C.c_void_p, C.c_void_p, C.c_uint64, C.c_uint32, C.c_void_p, C.c_void_p]),
-    "vgc_sqgrad_act8_workspace_bytes": (C.c_size_t, [C.c_int, C.c_int] + [C.c_uint32] * 4),
-    "vgc_sqgrad_act8": (C.c_int, [C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p] + [C.c_uint32] * 4 +
+    "vgc_act8_encode": (C.c_int, [C.c_int, C.c_void_p, C.c_uint64, U32, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "vgc_act8_decode": (C.c_int, [C.c_int, C.c_void_p, C.c_void_p, C.c_uint64, U32, C.c_void_p, C.c_void_p]),
+    "vgc_sqgrad_act8_workspace_bytes": (C.c_size_t, [C.c_int, C.c_int] + [U32] * 4),
+    "vgc_sqgrad_act8": (C.c_int, [C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p] + [U32] * 4 +
                         [C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
-    "vgc_layer_norm": (C.c_int, [C.c_int, C.c_void_p, C.c_uint64, C.c_uint32, C.c_void_p, C.c_void_p, C.c_float] + [C.c_void_p] * 6),
-    "vgc_layer_norm_backward_workspace_bytes": (C.c_size_t, [C.c_uint32] * 3),
-    "vgc_layer_norm_backward": (C.c_int, [C.c_int] + [C.c_void_p] * 7 + [C.c_uint32] * 3 + [C.c_float] + [C.c_void_p] * 6 +
+    "vgc_layer_norm": (C.c_int, [C.c_int, C.c_void_p, C.c_uint64, U32, C.c_void_p, C.c_void_p, C.c_float] + [C.c_void_p] * 6),
+    "vgc_layer_norm_backward_workspace_bytes": (C.c_size_t, [U32] * 3),
+    "vgc_layer_norm_backward": (C.c_int, [C.c_int] + [C.c_void_p] * 7 + [U32] * 3 + [C.c_float] + [C.c_void_p] * 6 +
                                 [C.c_size_t, C.c_void_p]),
-    "vgc_softmax_loss_workspace_bytes": (C.c_size_t, [C.c_int] + [C.c_uint32] * 3),
-    "vgc_softmax_loss": (C.c_int, [C.c_int, C.c_void_p, C.c_void_p, C.c_void_p] + [C.c_uint32] * 3 + [C.c_void_p] * 3 +
+    "vgc_softmax_loss_workspace_bytes": (C.c_size_t, [C.c_int] + [U32] * 3),
+    "vgc_softmax_loss": (C.c_int, [C.c_int, C.c_void_p, C.c_void_p, C.c_void_p] + [U32] * 3 + [C.c_void_p] * 3 +
                          [C.c_size_t, C.c_void_p]),
-    "vgc_softmax_loss_backward_workspace_bytes": (C.c_size_t, [C.c_int] + [C.c_uint32] * 4),
-    "vgc_softmax_loss_backward": (C.c_int, [C.c_int] + [C.c_void_p] * 5 + [C.c_uint32] * 4 + [C.c_float] + [C.c_void_p] * 4 +
+    "vgc_softmax_loss_backward_workspace_bytes": (C.c_size_t, [C.c_int] + [U32] * 4),
+    "vgc_softmax_loss_backward": (C.c_int, [C.c_int] + [C.c_void_p] * 5 + [U32] * 4 + [C.c_float] + [C.c_void_p] * 4 +
                                   [C.c_size_t, C.c_void_p]),
-    "vgc_dropout": (C.c_int, [C.c_int, C.c_void_p, C.c_void_p, C.c_uint64, C.c_uint32, C.c_float] + [C.c_void_p] * 3),
-    "vgc_linear_workspace_bytes": (C.c_size_t, [C.c_int] + [C.c_uint32] * 3),
-    "vgc_linear": (C.c_int, [C.c_int] + [C.c_void_p] * 3 + [C.c_int, C.c_float] + [C.c_void_p] * 2 + [C.c_uint32] * 3 + [C.c_void_p] * 3 +
+    "vgc_dropout": (C.c_int, [C.c_int, C.c_void_p, C.c_void_p, C.c_uint64, U32, C.c_float] + [C.c_void_p] * 3),
+    "vgc_linear_workspace_bytes": (C.c_size_t, [C.c_int] + [U32] * 3),
+    "vgc_linear": (C.c_int, [C.c_int] + [C.c_void_p] * 3 + [C.c_int, C.c_float] + [C.c_void_p] * 2 + [U32] * 3 + [C.c_void_p] * 3 +
                    [C.c_size_t, C.c_void_p]),
-    "vgc_linear_backward_workspace_bytes": (C.c_size_t, [C.c_int] + [C.c_uint32] * 4),
-    "vgc_linear_backward": (C.c_int, [C.c_int] + [C.c_void_p] * 3 + [C.c_int, C.c_float] + [C.c_void_p] * 2 + [C.c_uint32] * 4 + [C.c_float] +
+    "vgc_linear_backward_workspace_bytes": (C.c_size_t, [C.c_int] + [U32] * 4),
+    "vgc_linear_backward": (C.c_int, [C.c_int] + [C.c_void_p] * 3 + [C.c_int, C.c_float] + [C.c_void_p] * 2 + [U32] * 4 + [C.c_float] +
                             [C.c_void_p] * 5 + [C.c_size_t, C.c_void_p]),
-    "vgc_group_norm_workspace_bytes": (C.c_size_t, [C.c_int] + [C.c_uint32] * 4),
-    "vgc_group_norm": (C.c_int, [C.c_int, C.c_void_p] + [C.c_uint32] * 4 + [C.c_void_p] * 2 + [C.c_float, C.c_int] + [C.c_void_p] * 4 +
+    "vgc_group_norm_workspace_bytes": (C.c_size_t, [C.c_int] + [U32] * 4),
+    "vgc_group_norm": (C.c_int, [C.c_int, C.c_void_p] + [U32] * 4 + [C.c_void_p] * 2 + [C.c_float, C.c_int] + [C.c_void_p] * 4 +
                        [C.c_size_t, C.c_void_p]),
-    "vgc_group_norm_backward_workspace_bytes": (C.c_size_t, [C.c_int] + [C.c_uint32] * 4),
-    "vgc_group_norm_backward": (C.c_int, [C.c_int] + [C.c_void_p] * 6 + [C.c_int] + [C.c_uint32] * 4 + [C.c_float] + [C.c_void_p] * 6 +
+    "vgc_group_norm_backward_workspace_bytes": (C.c_size_t, [C.c_int] + [U32] * 4),
+    "vgc_group_norm_backward": (C.c_int, [C.c_int] + [C.c_void_p] * 6 + [C.c_int] + [U32] * 4 + [C.c_float] + [C.c_void_p] * 6 +
                                 [C.c_size_t, C.c_void_p]),
 }
 
@@ -735,16 +741,26 @@ def _stream_of(t, what):
     return torch._C._cuda_getCurrentRawStream(device)
 
 
+def _need_u32(what, *sizes):
+    for n in sizes:
+        if n >> 32:
+            raise VgcError(f"{what}: a size of {n} does not fit into 32 bits")
+
+
 def dropout(x, p, rng, y, residual=None):
     """vgc_dropout on the rows of x [..., C] into y (which may be x or residual): every element is dropped with probability p, the others are
     multiplied by 1 / (1 - p), and residual, if given, is added.  rng: int64 tensor of two elements, a key and the number of the call, read when the
     kernel runs.  The backward pass is the same call on the gradient of y."""
     R, Cc, dtype = _rows(x, "x")
+    if Cc >> 32:
+        _need_u32("x", Cc)
     _need_all(((x, 0, x.dtype, "x"), (residual, R * Cc, x.dtype, "residual"), (rng, 2, torch.int64, "rng"), (y, R * Cc, x.dtype, "y")))
     _check(load().vgc_dropout(dtype, _ptr(x), _ptr(residual), R, Cc, float(p), _ptr(rng), _ptr(y), _stream_of(x, "x")))
 
 
 def linear_workspace_bytes(dtype, N, K, Cc):
+    if (N | K | Cc) >> 32:
+        _need_u32("linear", N, K, Cc)
     return int(load().vgc_linear_workspace_bytes(dtype, N, K, Cc))
 
 
@@ -773,6 +789,8 @@ def linear(X, W, y, bias=None, act=ACT_NONE, z=None, residual=None, p=0.0, rng=N
 
 
 def linear_backward_workspace_bytes(dtype, B, P, K, Cc):
+    if (B | P | K | Cc) >> 32:
+        _need_u32("linear_backward", B, P, K, Cc)
     return int(load().vgc_linear_backward_workspace_bytes(dtype, B, P, K, Cc))
 
 
@@ -805,6 +823,8 @@ def _group_norm_shape(x, what, mean):
 
 
 def group_norm_workspace_bytes(dtype, B, P, Cc, G):
+    if (B | P | Cc | G) >> 32:
+        _need_u32("group_norm", B, P, Cc, G)
     return int(load().vgc_group_norm_workspace_bytes(dtype, B, P, Cc, G))
 
 
@@ -822,6 +842,8 @@ def group_norm(x, gamma, beta, eps, act, y, mean, rstd, workspace=None):
 
 
 def group_norm_backward_workspace_bytes(dtype, B, P, Cc, G):
+    if (B | P | Cc | G) >> 32:
+        _need_u32("group_norm_backward", B, P, Cc, G)
     return int(load().vgc_group_norm_backward_workspace_bytes(dtype, B, P, Cc, G))
 
 
