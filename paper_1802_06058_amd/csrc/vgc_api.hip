@@ -1022,4 +1022,11 @@ int vgc_group_norm_backward(int dtype, const void* dy, const void* x, const floa
                                       static_cast<hipStream_t>(stream));
 }
 
+// Not in vgc.h: which of its forms a call takes, for tests that have to reach them all.
+int vgc_form_group_norm(int dtype, int backward, uint32_t B, uint32_t P, uint32_t C, uint32_t G, uint32_t* form) {
+    const int rc = group_norm_shape("vgc_form_group_norm", dtype, B, P, C, G);
+    if (rc == VGC_OK) group_norm_form(dtype, backward != 0, B, P, C, G, form);
+    return rc;
+}
+
 }  // extern "C"

@@ -513,7 +513,8 @@ __global__ __launch_bounds__(1024) void k_group_norm_backward_join(GroupNormArgs
 // ---- launches -----------------------------------------------------------------------------------------------------------------
 // Held: whole groups of a cache line's channels and more a workgroup (us; float32, 32 x 784 x 512 in 32 groups, lines of 32 channels 32.2, 64 39.1;
 // bfloat16, 64 x 784 x 512, of 64 34.3, 32 46), with as many threads as leave a team few rows.  most: rows that a team can hold, with 512 threads
-// and fewer and with 1024, whose lanes have 128 registers.
+// and fewer and with 1024, whose lanes have 128 registers: backward half as many, and by channel, which takes more of them, none.  (Forward, 1024 threads hold whatever
+// 512 would.)
 // Else: workgroups to fill the compute units, and as many samples at a time as the last-level cache keeps of them between the two passes, that is
 // somewhat less than its 256 MB (us, 64 x 50176 x 64 bfloat16: 210 MB in 2048 workgroups 219, in 1024 232; 128 MB 255; all at once 246).
 struct GroupNormPlan {
@@ -530,11 +531,11 @@ static GroupNormPlan group_norm_plan(int dtype, bool backward, uint32_t B, uint3
     L.groups = std::min(G, std::max(1u, (line + w - 1u) / w));
     L.slabs = (G + L.groups - 1u) / L.groups;
     const uint32_t width = L.groups * w, wide = dtype == VGC_F32 ? 2u : 1u;
-    const uint32_t most = backward ? 8u / wide : 8u, most_1024 = backward ? (w % 8u == 0u ? 4u : 2u) / wide : 8u / wide, few = backward ? 4u / wide : 4u;
+    const uint32_t most = 8u / wide, most_1024 = backward ? (w % 8u == 0u ? 4u / wide : 0u) : most, few = backward ? 4u / wide : 4u;
     if (width <= kMostSlab) {
         L.lanes = power_of_two((width + 7u) / 8u);
         for (L.threads = 256u; L.threads < kMostThreads && P > (uint64_t)(L.threads / L.lanes) * few;) L.threads *= 2u;
-        if (L.threads == kMostThreads && P > (uint64_t)(L.threads / L.lanes) * most_1024) L.threads = 512u;
+        if (backward && L.threads == kMostThreads && P > (uint64_t)(L.threads / L.lanes) * most_1024) L.threads = 512u;
         const uint32_t teams = L.threads / L.lanes;
         L.rows_of_team = (P + teams - 1u) / teams;
         L.held = L.rows_of_team <= (L.threads == kMostThreads ? most_1024 : most);
@@ -555,6 +556,11 @@ static GroupNormPlan group_norm_plan(int dtype, bool backward, uint32_t B, uint3
     if (L.rows > 2u * batch) L.rows = (L.rows + batch / 2u) / batch * batch;
     L.chunks = (P + L.rows - 1u) / L.rows;
     return L;
+}
+
+void group_norm_form(int dtype, bool backward, uint32_t B, uint32_t P, uint32_t C, uint32_t G, uint32_t* form) {
+    const GroupNormPlan L = group_norm_plan(dtype, backward, B, P, C, G);
+    form[0] = L.held; form[1] = L.threads; form[2] = L.rows_of_team; form[3] = L.groups; form[4] = L.samples; form[5] = L.chunks;
 }
 
 struct GroupNormSpace { size_t chunk_sums, sums, group_sums, total; };
@@ -618,9 +624,8 @@ static int launch_group_norm_of(const GroupNormArgs& all, const GroupNormPlan& L
             else if (by_lane(A)) hipLaunchKernelGGL((k_group_norm<T, NV, kByLane, THREADS>), dim3(B * L.slabs), dim3(L.threads), 0, stream, A); \
             else hipLaunchKernelGGL((k_group_norm<T, NV, kByChannel, THREADS>), dim3(B * L.slabs), dim3(L.threads), 0, stream, A); } while (0)
             if (L.rows_of_team <= 2u) VGC_LAUNCH(2, 1024);
-            else if (L.rows_of_team <= 4u) VGC_LAUNCH(4, 1024);
-            else if (sizeof(T) == 2 && L.threads == 1024u) VGC_LAUNCH(8, (sizeof(T) == 2 ? 1024 : 512));
-            else VGC_LAUNCH(8, 512);
+            else if (sizeof(T) == 4 || L.rows_of_team <= 4u) VGC_LAUNCH(4, 1024);
+            else if constexpr (sizeof(T) == 2) VGC_LAUNCH(8, 1024);
 #undef VGC_LAUNCH
             return hip_check(hipGetLastError(), "launch k_group_norm");
         });
@@ -660,16 +665,11 @@ static int launch_group_norm_backward_of(const GroupNormArgs& all, const GroupNo
         return by_samples(all, sizeof(T), L, [&](const GroupNormArgs& A, uint32_t B) {
             constexpr int kFew = sizeof(T) == 2 ? 4 : 2;
 #define VGC_LAUNCH(NV, THREADS, M) hipLaunchKernelGGL((k_group_norm_backward<T, NV, THREADS, M>), dim3(B * L.slabs), dim3(L.threads), 0, stream, A)
-#define VGC_ROWS(THREADS, M) do { if (L.rows_of_team <= kFew / 2) VGC_LAUNCH(kFew / 2, THREADS, M); else VGC_LAUNCH(kFew, THREADS, M); } while (0)
-            if (L.threads <= 512u) {
-                if (L.rows_of_team > (uint32_t)kFew) { if (by_lane(A)) VGC_LAUNCH(2 * kFew, 512, 1); else VGC_LAUNCH(2 * kFew, 512, 8); }
-                else if (by_lane(A)) VGC_ROWS(512, 1);
-                else VGC_ROWS(512, 8);
-            } else if (by_lane(A)) {
-                VGC_ROWS(1024, 1);
-            } else {
-                VGC_LAUNCH(kFew / 2, 1024, 8);
-            }
+#define VGC_ROWS(M) do { if (L.rows_of_team <= kFew / 2) VGC_LAUNCH(kFew / 2, 512, M); else VGC_LAUNCH(kFew, 512, M); } while (0)
+            if (L.threads == kMostThreads) VGC_LAUNCH(kFew, 1024, 1);      // (by lane, of more than kFew / 2 rows a team)
+            else if (L.rows_of_team > (uint32_t)kFew) VGC_LAUNCH(2 * kFew, 512, 8);        // (by lane 1024 threads hold these)
+            else if (by_lane(A)) VGC_ROWS(1);
+            else VGC_ROWS(8);
 #undef VGC_ROWS
 #undef VGC_LAUNCH
             return hip_check(hipGetLastError(), "launch k_group_norm_backward");

@@ -347,6 +347,9 @@ int launch_group_norm_backward(int dtype, const void* dy, const void* x, const f
                                int act, uint32_t B, uint32_t P, uint32_t C, uint32_t G, float c, void* dx, float* g_gamma, float* s_gamma, float* g_beta,
                                float* s_beta, void* workspace, hipStream_t stream);
 
+// what a call takes, for tests: held, threads, rows of a team, groups of a workgroup, samples at a time, chunks
+void group_norm_form(int dtype, bool backward, uint32_t B, uint32_t P, uint32_t C, uint32_t G, uint32_t* form);
+
 // Linear layer (vgc_linear.hip)
 struct LinearCall {           // the arguments of vgc_linear and vgc_linear_backward, as there
     int dtype, act;

@@ -195,3 +195,54 @@ def test_images_repeat_bit_for_bit_and_side_by_side(dev, P):
     torch.cuda.synchronize()
     for r in results:
         assert all(torch.equal(a, b) for a, b in zip(first, r))
+
+
+# what SIZES leaves out of the forms that hold a sample (tests/test_group_norm_forms.py counts them)
+HELD = [(2, 500, 64, 1), (1, 300, 32, 2), (2, 800, 96, 12), (3, 400, 60, 12), (2, 250, 75, 3), (2, 200, 512, 4), (2, 790, 40, 8), (3, 200, 75, 3), (2, 130, 40, 1), (4, 110, 99, 9), (3, 60, 96, 12)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,P,C,G", HELD)
+def test_forms_that_hold_a_sample(dev, B, P, C, G, dtype):
+    _forward(dev, B, P, C, G, "gelu", dtype)
+    _backward(dev, B, P, C, G, "silu", dtype)
+
+
+def test_more_held_samples_than_a_launch_takes(dev):
+    """A slab a sample, 2^20 samples a launch: the second one's samples, statistics and sums lie behind the first one's."""
+    import ctypes
+    import torch
+    from paper_1802_06058_amd import vgc
+    B, P, C, G = (1 << 20) + 5, 2, 8, 2
+    for backward in (0, 1):
+        form = (ctypes.c_uint32 * 6)()
+        assert vgc.load().vgc_form_group_norm(vgc.BF16, backward, B, P, C, G, form) == 0 and form[0] == 1 and form[4] == 1 << 20
+    x = torch.randn(B, P, C, device=dev, generator=torch.Generator(device=dev).manual_seed(3)).to(torch.bfloat16)
+    dy = torch.randn(B, P, C, device=dev, generator=torch.Generator(device=dev).manual_seed(4)).to(torch.bfloat16)
+    gamma, beta = torch.linspace(0.5, 1.5, C, device=dev), torch.linspace(-0.5, 0.5, C, device=dev)
+    some = torch.tensor([0, 1, (1 << 20) - 1, 1 << 20, (1 << 20) + 1, B - 1], device=dev)
+
+    def run(x, dy, s_of_all=True):
+        n = x.shape[0]
+        y, dx, mean, rstd = torch.empty_like(x), torch.empty_like(x), torch.empty(n, G, device=dev), torch.empty(n, G, device=dev)
+        out = [torch.empty(C, device=dev) for _ in range(4)]
+        vgc.group_norm(x, gamma, beta, EPS, vgc.ACT_SILU, y, mean, rstd, T.workspace(vgc.group_norm_workspace_bytes(vgc.BF16, n, P, C, G), dev))
+        vgc.group_norm_backward(dy, x, mean, rstd, gamma, beta, vgc.ACT_SILU, 1.0, dx, *out, workspace=T.workspace(vgc.group_norm_backward_workspace_bytes(vgc.BF16, n, P, C, G), dev))
+        return (y, dx, mean, rstd), out
+
+    whole, sums = run(x, dy)
+    few, _ = run(x[some].contiguous(), dy[some].contiguous())
+    for a, b in zip(whole, few):                                     # (a sample's results do not depend on the others)
+        assert torch.equal(a[some], b)
+    # the sums over all samples, from their own gradients in 64 bits
+    v = x.double().view(B, P, G, C // G)
+    m, r = whole[2].double()[:, None, :, None], whole[3].double()[:, None, :, None]
+    xhat = ((v - m) * r).view(B, P, C)
+    t = xhat * gamma.double() + beta.double()
+    sig = torch.sigmoid(t)
+    e = dy.double() * (sig + t * sig * (1 - sig))
+    for S, g, s in (((e * xhat).sum(1), sums[2], sums[0]), (e.sum(1), sums[3], sums[1])):
+        n = 200 * U                                                  # roundings of a sample's terms (as in the other tests, with values of a few units)
+        eS = n * (e.abs() * (2 + xhat.abs())).sum(1)
+        assert ((g.double() - S.sum(0)).abs() <= (eS + (B / 64 + 64) * U * S.abs()).sum(0)).all()
+        assert ((s.double() - (S * S).sum(0)).abs() <= ((2 * S.abs() + eS) * eS + (B / 64 + 64) * U * S * S).sum(0)).all()
