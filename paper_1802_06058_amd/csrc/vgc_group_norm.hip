@@ -552,9 +552,10 @@ static GroupNormPlan group_norm_plan(int dtype, bool backward, uint32_t B, uint3
     const uint64_t want = std::max<uint64_t>(1, kGroups / std::max<uint64_t>(1, (uint64_t)L.samples * L.blocks));
     L.chunks = (uint32_t)std::min<uint64_t>(std::min<uint64_t>(want, 256u), (P + teams * 2u - 1u) / (teams * 2u));      // (256: of which a group's join has to read all)
     const uint32_t batch = teams * (dtype == VGC_F32 ? 2u : 4u) * (backward ? 1u : 2u);      // (whole batches but for the sample's last)
-    L.rows = (P + L.chunks - 1u) / L.chunks;
+    L.rows = (P - 1u) / L.chunks + 1u;
     if (L.rows > 2u * batch) L.rows = (L.rows + batch / 2u) / batch * batch;
-    L.chunks = (P + L.rows - 1u) / L.rows;
+    if ((P - 1u) / L.rows >= 256u) L.rows += batch;         // (rounded down)
+    L.chunks = (P - 1u) / L.rows + 1u;
     return L;
 }
 

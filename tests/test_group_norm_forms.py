@@ -56,3 +56,14 @@ def test_every_held_form_is_some_calls(name, backward):
         built[t].add((int(a), int(b), int(c)) if backward else (int(a), int(c), int(b)))
     for t, dtype in (("float", vgc.F32), ("unsigned short", vgc.BF16)):
         assert built[t] and built[t] == _held_forms(dtype, backward), (t, built[t] ^ _held_forms(dtype, backward))
+
+
+@pytest.mark.parametrize("dtype", [vgc.F32, vgc.BF16])
+@pytest.mark.parametrize("backward", [False, True])
+def test_a_sample_has_256_chunks_at_most(dtype, backward):
+    """What a group's join has to read, also after a chunk's rows were made whole batches."""
+    for B, P, C, G in [(4, 327266, 20, 4), (1, 2 ** 31 - 1, 1, 1), (3, 300007, 4800, 32), (2, 47061, 296, 2)]:
+        assert form(dtype, backward, B, P, C, G)["chunks"] <= 256, (B, P, C, G)
+    gen = random.Random(9)
+    for P, w, G in _sizes(100000, 5, 24):
+        assert form(dtype, backward, gen.randint(1, 4), P, w * G, G)["chunks"] <= 256, (P, w, G)
