@@ -490,7 +490,8 @@ int vgc_softmax_loss_backward(int dtype, const void* X, const void* W, const int
  *     dz = drop(dy) act'(z),  dX = add + dz W^T,   H_z = sum_p dz[z, p]:  the gradient of the bias by sample;
  *     g_bias = c sum_z H_z,  s_bias = c^2 sum_z H_z . H_z  (Alg. 1; c as for vgc_sqgrad);  the sums of W are vgc_sqgrad's of X and dz.
  * z: what the forward call wrote (NULL for VGC_ACT_NONE; for relu any array with its signs will do, such as y without dropout and residual);
- * rng as the forward call found it.  dz: DEVICE [B, P, C] in dtype, may be dy or z; dX: DEVICE [B, P, K] in dtype, or NULL; add: NULL, or like dX, and may be it;
+ * rng as the forward call found it.  dz: DEVICE [B, P, C] in dtype, may be dy or z; dX: DEVICE [B, P, K] in dtype, or NULL, without which W
+ * is not read and may be NULL; add: NULL, or like dX, and may be it;
  * s_bias: DEVICE float [C] or NULL; g_bias: the same (NULL if s_bias is).  The bias's sums are those of dz before it is rounded.
  * VGC_BF16: dX is formed from dz in bfloat16, for products N K C of at most 2^31 in two such pieces, 16 bits.  VGC_F32: products of the operands' 8-bit pieces as
  * in vgc_sqgrad's conv form.

@@ -796,14 +796,16 @@ def linear_backward_workspace_bytes(dtype, B, P, K, Cc):
 
 def linear_backward(dy, z, W, act, c, dz, dX=None, s_bias=None, g_bias=None, add=None, p=0.0, rng=None, workspace=None):
     """vgc_linear_backward for dy [B, P, C] and W [K, C]: dz like dy (the D of sqgrad for W, with X), dX [B, P, K] = add + dz W^T, and the two sums
-    over the samples for the bias, float32 [C].  z: what linear() wrote (None without an activation); p and rng as it had them.
-    workspace: uint8 tensor of linear_backward_workspace_bytes() bytes."""
+    over the samples for the bias, float32 [C].  z: what linear() wrote (None without an activation); p and rng as it had them.  W may be None where dX
+    is; K, for the workspace, is then 1.  workspace: uint8 tensor of linear_backward_workspace_bytes() bytes."""
     if dy.dim() != 3:
         raise VgcError(f"dy: need [B, P, C], got {tuple(dy.shape)}")
     R, Cc, dtype = _linear_shape(dy, W, "dy")
-    if W is None or W.shape[1] != Cc:
-        raise VgcError(f"W {None if W is None else tuple(W.shape)} does not give rows of {Cc} elements")
-    B, P, K = dy.shape[0], dy.shape[1], W.shape[0]
+    if W is None and dX is not None:
+        raise VgcError("dX needs W")
+    if W is not None and W.shape[1] != Cc:
+        raise VgcError(f"W {tuple(W.shape)} does not give rows of {Cc} elements")
+    B, P, K = dy.shape[0], dy.shape[1], 1 if W is None else W.shape[0]
     f32 = torch.float32
     nbytes = linear_backward_workspace_bytes(dtype, B, P, K, Cc)
     has = _need_workspace(workspace, nbytes)

@@ -96,3 +96,14 @@ def test_tensors_that_do_not_belong_together():
         vgc.group_norm(t(4, 3, 8), t(8), t(8), 1e-5, vgc.ACT_NONE, t(4, 3, 8), t(4, 2), t(4, 1), ws)
     with pytest.raises(vgc.VgcError, match="s_beta"):
         vgc.group_norm_backward(t(4, 3, 8), t(4, 3, 8), t(4, 2), t(4, 2), t(8), t(8), vgc.ACT_NONE, 1.0, t(4, 3, 8), t(8), t(7), workspace=ws)
+
+
+def test_a_backward_pass_without_the_weight():
+    """W is read for dX alone: without both the binding goes on (to the device check: these are host tensors), with dX it refuses."""
+    import torch
+    t = torch.zeros
+    ws = torch.empty(1 << 20, dtype=torch.uint8)
+    with pytest.raises(vgc.VgcError, match="GPU|device|cpu"):
+        vgc.linear_backward(t(2, 2, 8), None, None, vgc.ACT_NONE, 1.0, t(2, 2, 8), s_bias=t(8), workspace=ws)
+    with pytest.raises(vgc.VgcError, match="dX needs W"):
+        vgc.linear_backward(t(2, 2, 8), None, None, vgc.ACT_NONE, 1.0, t(2, 2, 8), t(2, 2, 24), workspace=ws)
