@@ -1,6 +1,6 @@
 """One worker's training step of a small token classifier, from its activations to the updated parameters, on the GPU:
 
-    h = x W1            a linear layer; its input x is kept in 8 bits       (act8_encode)
+    h = x W1            a linear layer; its input x is kept in 8 bits       (linear, act8_encode)
     y = layer norm(h)   the normalised rows are kept in 8 bits              (layer_norm)
     u = gelu(y Wa + ba) a residual feed-forward block, if asked for: its    (linear)
     y += drop(u Wb + bb)    dropout's mask is drawn again in the backward pass
@@ -61,7 +61,7 @@ class TokenStep:
         rows = lambda C, t=dtype: torch.empty(B, P, C, dtype=t, device=device)
         kept = lambda C: (rows(C, torch.int8), rows((C + 31) // 32, torch.uint8))
         self.kept_x, self.kept_h = kept(J), kept(H)
-        self.y, self.dy, self.dh = rows(H), rows(H), rows(H)
+        self.h, self.y, self.dy, self.dh = rows(H), rows(H), rows(H), rows(H)
         if F:
             self.za, self.u, self.du, self.out, self.dout, self.dzb = rows(F), rows(F), rows(F), rows(H), rows(H), rows(H)
             self.rng = torch.tensor([seed, 0], device=device)          # the dropout's key and the number of the step, which lives on the device too
@@ -69,7 +69,8 @@ class TokenStep:
         code = vgc.F32 if dtype == torch.float32 else vgc.BF16
         # the calls of a step follow each other on one stream: one workspace serves them all
         need = [vgc.softmax_loss_workspace_bytes(code, B * P, H, V), vgc.softmax_loss_backward_workspace_bytes(code, B, P, H, V),
-                vgc.layer_norm_backward_workspace_bytes(B, P, H), vgc.sqgrad_act8_workspace_bytes(vgc.CONV, code, B, P, J, H)]
+                vgc.layer_norm_backward_workspace_bytes(B, P, H), vgc.sqgrad_act8_workspace_bytes(vgc.CONV, code, B, P, J, H),
+                vgc.linear_workspace_bytes(code, B * P, J, H)]
         if F:
             for K, C in ((H, F), (F, H)):
                 need += [vgc.linear_workspace_bytes(code, B * P, K, C), vgc.linear_backward_workspace_bytes(code, B, P, K, C),
@@ -83,8 +84,8 @@ class TokenStep:
         weight = (1.0 / asked).expand(self.B, self.P).contiguous().float()     # a sequence's own loss: the mean over what it is asked for
         W1, W = self.p["W1"].to(self.dtype), self.p["W"].to(self.dtype)
         vgc.act8_encode(x, *self.kept_x)
-        h = torch.matmul(x.view(self.B * self.P, self.J), W1).view(self.B, self.P, self.H)
-        vgc.layer_norm(h, self.p["gamma"], self.p["beta"], 1e-5, self.y, self.mean, self.rstd, self.kept_h)
+        vgc.linear(x if x.data_ptr() % 16 == 0 else x.clone(), W1, self.h, workspace=ws)
+        vgc.layer_norm(self.h, self.p["gamma"], self.p["beta"], 1e-5, self.y, self.mean, self.rstd, self.kept_h)
         out, dout = (self.out, self.dout) if self.F else (self.y, self.dy)
         if self.F:
             Wa, Wb = self.p["Wa"].to(self.dtype), self.p["Wb"].to(self.dtype)
