@@ -37,7 +37,7 @@ class TokenStep:
         f32 = dict(dtype=torch.float32, device=device)
         shapes = dict(W1=(J, H), gamma=(H,), beta=(H,), W=(V, H))
         if F:
-            shapes.update(Wa=(H, F), ba=(F,), Wb=(F, H), bb=(H,))
+            shapes.update(Wa=(H, F), Wb=(F, H), ba=(F,), bb=(H,))        # (weights first: where they lie is then aligned for any F)
         sizes = [torch.Size(s).numel() for s in shapes.values()]
         groups = workloads.groups_from_sizes(sizes)
         self.plan = vgc.Plan(groups, device)
