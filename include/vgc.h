@@ -498,7 +498,8 @@ int vgc_softmax_loss_backward(int dtype, const void* X, const void* W, const int
  *
  * X, W, dz: 16-byte aligned, the others to their elements.  workspace: DEVICE, 16-byte aligned, of the bytes that the function beside it gives (NULL
  * if that is 0).  No result depends on scheduling.
- * An infinity or a NaN in a row of X, residual, dy or z reaches that row, in W or bias any result; as a NaN also where the formulas give an infinity.
+ * An infinity or a NaN in a row of X, residual, dy or z reaches that row, in W or bias any result; as a NaN also where the formulas give an infinity.  Not
+ * through dropout where it drops, nor through relu's slope, which is 0 at a NaN of z: dz is 0 there, and dX and the sums do not show it.
  * Errors: NULL, SIZE (a zero dimension, N = B P, K or C beyond 2^20, K C beyond 2^30, N K or N C beyond 2^34), DTYPE, ALIGN, PARAM (act unknown, p as above, c
  * not finite).
  *
@@ -509,7 +510,9 @@ int vgc_softmax_loss_backward(int dtype, const void* X, const void* W, const int
  *     g_gamma = c sum_z G_z,  s_gamma = c^2 sum_z G_z . G_z,  g_beta and s_beta likewise from H_z.
  * x, y, dy, dx: DEVICE [B, P, C] in dtype, an output overlapping no input; gamma, beta: DEVICE float [C]; mean, rstd: DEVICE float [B, G]; the four
  * sums: DEVICE float [C], g_gamma and g_beta or NULL.  Pointers are aligned to their elements; workspace as above.
- * An infinity or a NaN gives NaN in that sample's group and in its channels' sums, nowhere else.
+ * An infinity or a NaN of x: y, mean, rstd and dx of that sample's group are not finite, nor are the sums for gamma of the group's channels; those for beta
+ * depend on x through the slope alone, which is a NaN for gelu and silu and 0 for relu, so that without an activation or with relu they stay finite.  One of dy: dx of
+ * its group and the four sums of its channel are not finite, unless relu's slope is 0 for it.  Nothing else is reached.
  * Errors: NULL, SIZE (a zero dimension, G not dividing C, B P beyond 2^31 - 1, C beyond 2^20), DTYPE, ALIGN, PARAM (act unknown, eps negative or not finite, c not
  * finite). */
 enum { VGC_ACT_NONE = 0, VGC_ACT_RELU = 1, VGC_ACT_GELU = 2, VGC_ACT_SILU = 3 };
