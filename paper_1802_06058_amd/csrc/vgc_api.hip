@@ -1029,4 +1029,10 @@ int vgc_form_group_norm(int dtype, int backward, uint32_t B, uint32_t P, uint32_
     return rc;
 }
 
+int vgc_form_linear(int dtype, int backward, uint32_t B, uint32_t P, uint32_t K, uint32_t C, uint32_t* form) {
+    const int rc = linear_shape("vgc_form_linear", dtype, B, P, K, C);
+    if (rc == VGC_OK) linear_form(dtype, backward != 0, B, P, K, C, form);
+    return rc;
+}
+
 }  // extern "C"

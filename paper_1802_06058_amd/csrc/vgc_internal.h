@@ -365,6 +365,8 @@ size_t linear_workspace_bytes(int dtype, uint32_t N, uint32_t K, uint32_t C);
 int launch_linear(const LinearCall& L, void* workspace, hipStream_t stream);
 size_t linear_backward_workspace_bytes(int dtype, uint32_t B, uint32_t P, uint32_t K, uint32_t C);
 int launch_linear_backward(const LinearCall& L, void* workspace, hipStream_t stream);
+// what a call's product takes, for tests: tile, parts of k, and of the kernel for few rows its columns and rows; planes of dz
+void linear_form(int dtype, bool backward, uint32_t B, uint32_t P, uint32_t K, uint32_t C, uint32_t* form);
 
 // Softmax cross entropy of a linear layer (vgc_softmax_loss.hip)
 // R rows of K elements as bfloat16 planes (one of bfloat16 rows, three of float32), rows padded with zeros to a multiple of 8, planes R rows apart

@@ -710,4 +710,17 @@ int launch_linear_backward(const LinearCall& q, void* workspace, hipStream_t str
     return q.dtype == VGC_F32 ? launch_product<float, false>(L.product, A, stream) : launch_product<uint16_t, false>(L.product, A, stream);
 }
 
+void linear_form(int dtype, bool backward, uint32_t B, uint32_t P, uint32_t K, uint32_t C, uint32_t* form) {
+    ProductPlan L;
+    form[4] = 1u;
+    if (backward) {
+        const LinearBackwardPlan q = linear_backward_plan(dtype, B, P, K, C);
+        L = q.product;
+        form[4] = q.planes;
+    } else {
+        L = linear_plan(dtype, B * P, K, C).product;
+    }
+    form[0] = (uint32_t)L.tile; form[1] = L.splits; form[2] = L.v; form[3] = L.t;
+}
+
 }  // namespace vgc
