@@ -48,10 +48,11 @@ __device__ __forceinline__ void channel_sums(const float (&v)[kN][8], uint32_t l
     __syncthreads();
 }
 
-// A lane's pieces of the rows that its team takes: row `p` and every `step` on, below p1, of arrays of rows of C elements.  kWhole: rows are whole pieces (C % 8 == 0), and requests have
-// no branches, which would make a wave wait for what it asked for before: lanes past the last column take its piece again, rows past p1 are its last again, and neither counts.  Two sets of
-// kRows rows are asked for in turn, one while the other is used (in one set, whose places the next requests take, the compiler moves registers at the loop's end, for which it waits for all
-// of them).  Else rows come one by one, their ends element by element.
+// A lane's pieces of the rows that its team takes: row `p` and every `step` on, below p1, of arrays of rows of C elements.  kWhole: rows are whole pieces (C % 8
+// == 0), and requests have no branches, which would make a wave wait for what it asked for before: lanes past the last column take its piece again, rows past
+// p1 are its last again, and neither counts.  Two sets of kRows rows are asked for in turn, one while the other is used (in one set, whose places the next
+// requests take, the compiler moves registers at the loop's end, for which it waits for all of them).  Else rows come one by one, their ends element by
+// element.
 template <typename T, bool kWhole, int kRows, int kArrays> struct RowStream {
     const T* base[kArrays];
     uint64_t rows;            // of the arrays

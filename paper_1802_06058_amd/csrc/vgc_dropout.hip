@@ -9,7 +9,7 @@ namespace vgc {
 
 // A lane takes a piece of eight elements of a row; two sets of kPieces in turn, one asked for while the other is used.  kWhole: rows are whole
 // pieces, and requests have no branches (past the last piece it is asked for again).  A piece's numbers are one Philox block, ten rounds, under
-// which the loads lie.  16384 x 4096 bfloat16 with a residual: 79 us, 5.1 TB/s, as a copy; 128 x 1000 float32: 3.6 us, the launch.
+// which the loads lie.  16384 x 4096 bfloat16 with a residual: 81-82 us a call, 4.9 TB/s where a copy reaches 5.1; 128 x 1000 float32: 3.0 us, the launch.
 template <typename T, bool kWhole, bool kResidual>
 __global__ __launch_bounds__(256) void k_dropout(const T* x, const T* residual, uint32_t row0, uint32_t C, uint32_t per_row, uint32_t pieces, Dropout D, bool past, T* y) {
     constexpr int kPieces = sizeof(T) == 2 ? 4 : 2;

@@ -58,7 +58,7 @@ __device__ __forceinline__ void sums_of_groups(const float* a, const float* b, u
 
 // ---- a sample's whole groups in one workgroup ---------------------------------------------------------------------------------
 // kNV rows of a team are held as they are in memory.  A workgroup's reading, sums and writing follow each other, with one or two workgroups a
-// compute unit, which bounds them (32 x 49 x 2048 float32 in 32 groups 8.7 us a call, 64 x 784 x 512 bfloat16 34, both 3.0 TB/s of the 5.1 that a
+// compute unit, which bounds them (32 x 49 x 2048 float32 in 32 groups 8.5 us, 64 x 784 x 512 bfloat16 a call of 32-34, both 3.0-3.2 TB/s of the 5.1 that a
 // copy reaches; as chunks 16.3 and 39.5.  Backward 32 x 196 x 1024 float32 27.5, as chunks 37).
 // How a workgroup's groups lie in its lanes decides how a group's sum is formed: by channels, which may belong to any group; a lane's eight
 // channels of one group, then by lanes; or all lanes' of one.
@@ -263,8 +263,8 @@ __global__ __launch_bounds__(kThreads) void k_group_norm_backward(GroupNormArgs 
 
 // ---- samples beyond that: sums by channel and chunk, then the result ------------------------------------------------------------
 // Workgroup (sample, block of columns, chunk of positions): teams take the chunk's rows in turn, two sets of kRows of them in turn in flight.
-// Both passes are bound by memory (64 x 50176 x 64 bfloat16 with relu, 411 MB: 219 us, the moments at 4 TB/s, which is what reading alone reaches
-// on this card, the result from the last-level cache for what it keeps.  Backward, 32 x 3136 x 256 float32 with silu, 103 MB an array: 96 us).
+// Both passes are bound by memory (64 x 50176 x 64 bfloat16 with relu, 411 MB: 211 us in two halves of the samples, of each the moments 40, 5.1 TB/s, and the result
+// 65, 6.3 TB/s, from the last-level cache for what it keeps.  Backward, 32 x 3136 x 256 float32 with silu, 103 MB an array: 97 us).
 struct Place { uint32_t b, chunk, c0, team, teams, p0, p1; int n; };
 __device__ __forceinline__ Place place_of(const GroupNormArgs& A) {
     Place L;
@@ -414,7 +414,7 @@ __global__ __launch_bounds__(256) void k_group_norm_apply(GroupNormArgs A) {
     });
 }
 
-// kSums: G_z and H_z of the chunk; else dx.  (The passes of 32 x 3136 x 256 float32: 45 and 41 us.)
+// kSums: G_z and H_z of the chunk; else dx.  (32 x 3136 x 256 float32: the sums 39 us, 5.2 TB/s, dx 49.)
 template <typename T, bool kWhole, int kM, bool kSums>
 __global__ __launch_bounds__(256) void k_group_norm_backward_rows(GroupNormArgs A) {
     __shared__ float sh[kSums ? 4096 : 1], part[kSums ? 512 : 1], chan[2][kSums ? 256 : 1];

@@ -8,9 +8,11 @@
 // finishes eight consecutive elements of a row: bias, activation, dropout and residual meet the sum while it is float32, and it is rounded once.
 // Where the output has few tiles, k is shared out, and a second kernel adds the parts in a fixed order and finishes them.
 //
-// Precision.  bfloat16: products are exact, sums float32.  dz is stored in bfloat16, as the D that W's sums are formed from, and dX's product reads it so: rounded at random it leaves dX, which is
-// rounded itself, 1.4 times as far off as its own rounding alone (2.3e-3 and 1.65e-3); small products, whose few sums may be further off than that, read 16 bits of it in two planes, which costs them nothing
-// beside the call.  float32: three planes of 8 bits an operand, rounded, six products of them, taken out of the instructions' sums every 32 k; few rows are multiplied as floats.
+// Precision.  bfloat16: products are exact, sums float32.  dz is stored in bfloat16, as the D that W's sums are formed from, and dX's product reads it so:
+// rounded at random it leaves dX, which is rounded itself, 1.3 times as far off as its own rounding alone (2.13e-3 and 1.65e-3); two planes of it would take
+// twice the matrix instructions.  Products N K C of at most 2^31, whose few sums may be further off than that, read 16 bits of it in two planes, which costs
+// them nothing beside the call.  float32: three planes of 8 bits an operand, rounded, six products of them, taken out of the instructions' sums every 32 k (2e-7
+// off in the root mean square); few rows are multiplied as floats.
 #include <algorithm>
 
 #include "vgc_columns.h"
@@ -114,10 +116,11 @@ __device__ __forceinline__ void finish_tile(f16v (&acc)[MT][NT], float* turn, ui
     }
 }
 
-// Bound by the matrix instructions at the clock that the power limit leaves: pipes two thirds busy at 1.7-1.8 GHz of 2.4.  bfloat16, 16384 rows, us from card to card: 8192 to 2048 418-430, with dropout
-// and residual 453-475 (1.16-1.21 PFLOP/s); 2048 to 8192 437-485, with gelu and z kept 509-557, since nothing of another tile runs beside a workgroup's end: z is 20 us of it, gelu 40; its backward product
-// 430-460.  (Two workgroups of 256 x 128 a compute unit, whose ends would overlap: 477 and 551 against 460 and 536 then; four waves of 128 x 128, two thirds of the reads from LDS but one wave a
-// SIMD: 485 and 574 against 450 and 527.)  float32, 4096^3: 636 us, 216 TFLOP/s.
+// Bound by the matrix instructions at the clock that the power limit leaves: pipes two thirds busy at 1.6-1.8 GHz of 2.4.  bfloat16, 16384 rows, us from card to
+// card: 8192 to 2048 418-445, with dropout and residual 453-490 (1.12-1.21 PFLOP/s); 2048 to 8192 437-485, with gelu and z kept 523-574, since nothing of
+// another tile runs beside a workgroup's end: z is 20 us of it, gelu 54; its backward product 430-480.  (Two workgroups of 256 x 128 a compute unit, whose ends
+// would overlap: 477 and 551 against 460 and 536 then; four waves of 128 x 128, two thirds of the reads from LDS but one wave a SIMD: 485 and 574 against 450
+// and 527.)  float32, 4096^3 by 256 x 128: 636 us, 216 TFLOP/s; by its halves, which the estimates below prefer by 1 %, 691-731.
 template <typename Shape, typename T, bool kMixed>
 __global__ __launch_bounds__(Shape::NW * 64, Shape::NW / 4 * (160 * 1024 / Shape::kLds)) void k_linear(LinearArgs A) {
     __shared__ __attribute__((aligned(1024))) uint8_t sh[Shape::kLds];
@@ -168,11 +171,13 @@ __global__ __launch_bounds__(256) void k_linear_join(Finish F, uint32_t splits, 
 //   forward   a lane asks for kV consecutive columns of W in each of its k's rows, so that a wave's load takes whole 16 kV columns of four rows; column j
 //             of the lanes is an instruction's operand (bfloat16: eight k's pairs put together by byte permutes)
 //   backward  a lane asks for 16 bytes of a row of W, instruction j taking rows 16 j + lane % 16
-// Rows are read where they lie (but for odd numbers of bfloat16, see product_plan).  Requests have no branches, which would make a wave wait for what it asked for before: past an edge
-// a place is moved back to the last one inside, of k with the elements that others count dropped from b's, of columns and rows with results that others have too.
+// Rows are read where they lie (but for odd numbers of bfloat16, see product_plan).  Requests have no branches, which would make a wave wait for what it asked
+// for before: past an edge a place is moved back to the last one inside, of k with the elements that others count dropped from b's, of columns and rows with
+// results that others have too.
 // The waves' sums meet in LDS, four lanes add an output piece's sixteen and one finishes it.
 // float32 is multiplied as floats.
-// Bound by what a compute unit's loads bring, whole lines of 128 bytes at some 31-41 GB/s each: 1 x 4096 x 4096 bfloat16 8.7 us (four parts of k) and the join, 128 x 784 x 1000 float32 7.7.
+// Bound by what a compute unit's loads bring, whole lines of 128 bytes at some 31-41 GB/s each: 128 x 784 x 1000 float32 7.7 us; one row of bfloat16 by 4096 x
+// 4096, four parts of k, 8.7 and the join (the estimates below give that size to tiles).
 constexpr uint32_t kThinWaves = 16;
 template <typename T> struct ThinArgs {
     const T *a, *b, *rest;    // W; the rows of X or dz, and (backward, bfloat16) what rounding left of dz
@@ -476,16 +481,23 @@ static uint64_t tiles(uint32_t a, uint32_t ta, uint32_t b, uint32_t tb) { return
 enum class Tile { kLarge, kSmall, kSmall2, kCut, kCutMid, kCutSmall, kThin, kDeep, kNarrow };
 // How a product [N, M] over K is formed: the cheapest of its forms by what they take on this card, in us (the kernels, not the call).
 //   thin    workgroups in turn on 256 compute units, 3 us each and its operands' rows at 41 GB/s, where rows of x, of which a load takes 64 bytes, count twice.
-//           (estimate and measured, bfloat16: 1 x 4096 x 4096 in 64 columns, four parts of k 13.8 and 11.6, whole 22 and 20; 256 x 2048 x 2048 15.8 and 11.5; float32:
-//           1000^3 31 and 35, 128 x 4096 x 4096 54 and 61, 2048 x 512 x 2048 75 and 65)
-//   tiles   in turn too, 2.5-4 us before and after a tile's steps.  bfloat16, of 64 k: 128 x 128 0.55 us a step, from two planes of dz 0.9, 128 x 64 0.4.  (2048^3 20 and
-//           24, of 128 x 64 31 and 29; 512 x 4096 x 4096 in two parts 32 and 33; 512 x 2048 x 2048 20 and 17.7, of 128 x 64 15.3 and 14.6.)  float32, of 32 k, after the
-//           operands were laid out: 256 x 128 2.15 us a step, 128 x 128 1.05, 128 x 64 0.7.  (4096^3 645 and 636, of the smaller ones 691 and 830; 2048^3 119 and 136, 103
-//           and 105, 128 and 124; 840 x 424 x 1832 44 and 40, 30 and 30, 25 and 28; in thin 33 and 35)
-// A long k is shared out, in thin or by tiles, where that gives idle compute units work: the second kernel that adds the parts takes 6 us and their way through memory.
-// (more workgroups than units, for a last round less empty: 8815 x 6464 x 64 float32 in four parts 130, whole 183.)
-// Where both operands are laid out, one launch does it (840 x 424 x 1832 float32 27.6 -> 25.2).  Rows of an odd number of bfloat16 are laid out at whole pieces first: a
-// load at an odd element takes three times as long (129 x 1331 from 4513: 90 us, from 4512 27).
+//           (estimate and measured, bfloat16: 1 x 4096 x 4096 in 64 columns, four parts of k 13.8 and 11.6, whole 22 and 20; 256 x 2048 x 2048 15.8 and
+//           11.5; float32: 1000^3 31 and 35, 128 x 4096 x 4096 54 and 61, 2048 x 512 x 2048 75 and 65.  Rows that share their lines take less than
+//           that: one row by 4096 x 4096 goes to 128 x 64 tiles in eight parts, 11.7 by estimate, a call of 12.3-12.7)
+//   tiles   in turn too, 2.5-4 us before and after a tile's steps.  bfloat16, of 64 k: 128 x 128 0.55 us a step, from two planes of dz 0.9, 128 x 64 0.4.
+//           (2048^3 20 and 24, of 128 x 64 31 and 29; 512 x 4096 x 4096 in two parts 32 and 33; 512 x 2048 x 2048 20 and 17.7, of 128 x 64 15.3 and 14.6.)
+//           float32, of 32 k, after the operands were laid out: 256 x 128 2.15 us a step, 128 x 128 1.05, 128 x 64 0.7.  (4096^3 647 and 636, of the
+//           smaller ones 641 and 691, 841 and 830; 2048^3 119 and 136, 103 and 105, 128 and 124; 840 x 424 x 1832 44 and 40, 30 and 30, 25 and 28; in
+//           thin 33 and 35)
+//   large   256 x 256 tiles of bfloat16 stand beside thin alone, which takes their place where it is expected to be cheaper than 0.55 us a step.  They take 1.75,
+//           but thin takes twice its estimate where its workgroups are many: a bound for which both are right would need a better estimate of thin first.
+//           (with 1.75 and with 0.55: 9 x 2872 x 60896 72 and 85, 83009 x 9064 x 8 363 and 542; 48 x 131 x 128766 74 and 37, 1017955 x 2044 x 129
+//           5750 and 2410)
+// A long k is shared out, in thin or by tiles, where that gives idle compute units work: the second kernel that adds the parts takes 6 us and their way through
+// memory.  (more workgroups than units, for a last round less empty: 8815 x 6464 x 64 float32 in four parts 130, whole 183.)
+// Where both operands are laid out, one launch does it (840 x 424 x 1832 float32 27.6 -> 25.2).  Rows of an odd number of bfloat16 are laid out at whole pieces
+// first: a load at an odd element takes three times as long (129 x 1331 from 4513: 90 us, from 4512 27).  Tiles are charged for layouts as the forward pass has
+// them, W's by M and X's by K; backward it is K that decides for W too, and dz's planes are written by the pass before.
 struct ProductPlan { Tile tile; uint32_t splits, v, t; size_t parts; };    // thin: kV and NT
 static double rounds(uint64_t groups) { return (double)((groups + 255u) / 256u); }
 static double join_us(uint32_t splits, uint32_t N, uint32_t M) { return splits == 1u ? 0. : 6. + (double)splits * N * M * 4e-6 / 3.; }
@@ -508,8 +520,8 @@ static double thin_plan(int dtype, uint32_t N, uint32_t M, uint32_t K, uint32_t 
 }
 static ProductPlan product_plan(int dtype, uint32_t N, uint32_t M, uint32_t K, uint32_t planes_b, bool odd_w) {
     const bool f32 = dtype == VGC_F32;
-    // Large tiles from 192 of them on, two small ones a compute unit, or one that is deep.  (us: 16384 x 2048 x 8192 by large tiles 448, small 566; 4096^3 113 and 148; 4096 x 1024 x 1024
-    // 27 and 16; 2048^3 small 31, deep 24; 4096 x 4096 x 1024 58 and 43; 8192 x 1024 x 1024 27 and 31)
+    // Large tiles from 192 of them on, two small ones a compute unit, or one that is deep.  (us: 16384 x 2048 x 8192 by large tiles 448, small 566; 4096^3 113
+    // and 148; 4096 x 1024 x 1024 27 and 16; 2048^3 small 31, deep 24; 4096 x 4096 x 1024 58 and 43; 8192 x 1024 x 1024 27 and 31)
     const uint64_t large = tiles(M, 256, N, 256), small = tiles(M, 128, N, 128);
     ProductPlan L, thin;
     double us = 1e30;
@@ -649,9 +661,9 @@ static LinearBackwardPlan linear_backward_plan(int dtype, uint32_t B, uint32_t P
     L.lanes = power_of_two(std::min(pieces, 32u));
     L.blocks = (pieces + L.lanes - 1u) / L.lanes;
     const uint32_t teams = 256u / L.lanes;
-    // Samples whole or in parts, whichever leaves a team fewer rows in turn, counted over rounds of 1024 workgroups: a round takes some 3 us and 0.3 a row (16 samples of 32 x 512: whole, one
-    // team each, 16.7 us, in parts 5.2).  The second kernel takes 4.5, without which one group of workgroups of 32 teams can do where it has few samples (128 x 1000 to 1000 float32, the
-    // whole call 17.1 -> 13.9).
+    // Samples whole or in parts, whichever leaves a team fewer rows in turn, counted over rounds of 1024 workgroups: a round takes some 3 us and 0.3 a row (16
+    // samples of 32 x 512: whole, one team each, 16.7 us, in parts 5.2).  The second kernel takes 4.5, without which one group of workgroups of 32 teams can do
+    // where it has few samples (128 x 1000 to 1000 float32, the whole call 17.1 -> 13.9).
     auto us = [&](uint64_t groups, uint64_t rows) { return (double)((groups * L.blocks + 1023u) / 1024u) * (3. + 0.3 * (double)rows); };
     const uint64_t want = std::max<uint64_t>(1, 2048u / L.blocks), whole_groups = std::min<uint64_t>(want, (B + teams - 1u) / teams);
     const uint64_t parts = std::max<uint64_t>(1, std::min<uint64_t>(want / B, P / (teams * 2u)));

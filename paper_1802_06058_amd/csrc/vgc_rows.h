@@ -93,8 +93,8 @@ __device__ __forceinline__ void store8(float* p, const float (&f)[8], int n) {
             if (i < n) p[i] = f[i];
     }
 }
-// Results of whole aligned pieces are stored past the caches where what a call touches (bytes) is more than they hold: that leaves room for what is read (the linear layer's 16384 x 2048 x 8192
-// bfloat16 with z 512 -> 477 us).
+// Results of whole aligned pieces are stored past the caches where what a call touches (bytes) is more than they hold: that leaves room for what is read (the
+// linear layer's 16384 x 2048 x 8192 bfloat16 with z 512 -> 477 us).
 typedef uint32_t whole_u4 __attribute__((ext_vector_type(4)));
 typedef float whole_f4 __attribute__((ext_vector_type(4)));
 inline bool past_caches(const void* p, uint32_t row, uint64_t bytes) { return row % 8u == 0u && (reinterpret_cast<uintptr_t>(p) & 15u) == 0u && bytes > (256ull << 20); }
